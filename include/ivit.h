@@ -227,6 +227,171 @@ int ivit_action_combine(const float* x0_dev, const float* v0_dev, const float* v
                         const float* alpha_dev, const float* beta_dev, const float* b_dev,
                         int32_t batch, int32_t dim, float* xT_dev, void* stream);
 
+/* ------------------------------------------------------- language backbone
+ * The operators that a policy's language backbone needs around the encoder's tokens: its
+ * keys and values live in a cache of pages, its queries and keys are normalised per head
+ * and rotated by positions of one or several axes, and a step answers with one token or a
+ * tree of drafted tokens that is verified in one pass.  None needs a handle, allocates or
+ * synchronises; all work is enqueued on `stream`; arrays named *_dev are device memory of
+ * the current device.  Failures are described by ivit_last_error(NULL).
+ *
+ * A request's step: ivit_step_plan reserves pages for its new rows and gives their slots,
+ * positions and tree masks; per layer ivit_qk_norm_rope turns the projections into queries
+ * and keys (prompt rows go straight into the cache) and ivit_tree_attention lets the new
+ * rows attend over the cached tokens and over each other; after the verification
+ * ivit_kv_write puts the accepted rows of every layer into their slots.
+ *
+ * Slot s of a cache is token s % page_size of page s / page_size.  Rows of a call are the
+ * new tokens of all requests back to back (cu_rows[i] .. cu_rows[i + 1] are request i's). */
+#define IVIT_BF16 0
+#define IVIT_FP16 1
+
+/* Keys (and, in an array of its own with the same layout, values) of one layer: element d of
+ * head h of token t of page p is at p * page_stride + t * token_stride + h * head_stride + d.
+ * Supported: page_size a power of two up to 1024, n_pages * page_size < 2^31, head_dim a
+ * multiple of 8 up to 256, kv_heads up to 256, strides multiples of 8 elements, arrays
+ * 16-byte aligned. */
+typedef struct ivit_cache_layout {
+  int32_t n_pages, page_size, kv_heads, head_dim;
+  int32_t dtype;         /* IVIT_BF16 or IVIT_FP16: the cache's type and that of the rows */
+  int32_t reserved;      /* 0 */
+  int64_t page_stride, token_stride, head_stride;  /* in elements */
+} ivit_cache_layout;
+
+/* Limits: n_req up to 4096, max_rows and max_pages up to 262144, page_size as above,
+ * n_pages * page_size < 2^31, mask_words up to 32768. */
+typedef struct ivit_plan_config {
+  int32_t n_req;         /* requests of the step */
+  int32_t max_rows;      /* rows that the row arrays have room for */
+  int32_t max_pages;     /* columns of the block table */
+  int32_t page_size;
+  int32_t n_pages;       /* pages of the cache = places of the ring of free pages */
+  int32_t mask_words;    /* 32-bit words of a row's tree mask, 0: no mask */
+} ivit_plan_config;
+
+/* Pages, slots, positions and tree masks of a step, from the requests' lengths.
+ * In (int32): held_dev [n_req] tokens for which request i holds pages, base_dev [n_req]
+ * tokens that it has in the cache, new_dev [n_req] rows that it adds; parent_dev [max_rows]
+ * the row that a drafted row hangs on, counted from the request's first (-1, or anything
+ * that is not an earlier row of the request: a root), or NULL: the rows are a run;
+ * ring_dev [n_pages] the ids of the free pages, as a ring of which ring_in_dev[1] places
+ * from ring_in_dev[0] on are filled; table_dev [n_req][max_pages] the block table.
+ * A request needs pages for base + new tokens: what it lacks is taken from the ring's front
+ * and entered in the table, what it holds beyond is put behind the ring's end (a finished
+ * request has base = new = 0).  Pages that are returned are free from the next call on.
+ * Out: table_dev and ring_dev in place (so a repeated call with the same inputs gives the
+ * same result), ring_out_dev [2] (may not be ring_in_dev), cu_rows_dev [n_req + 1], and per
+ * row: req_dev the request, slot_dev the slot of token base + j for the request's row j,
+ * pos_dev base + depth in the tree (base + j without one), mask_dev [max_rows][mask_words]
+ * with bit k set for the row itself and its ancestors (rows past 32 * mask_words have no
+ * bit).  req_dev, pos_dev and mask_dev may be NULL.  Rows past the step's get -1, -1, 0, 0.
+ * The new held lengths are base + new.
+ * status_dev [1]: 0, or why the step was refused -- 1 too few free pages, 2 a request has
+ * more pages than the table, 4 more rows than max_rows, 8 a negative length or an invalid
+ * ring.  A refused step takes and returns no page, ring_out = ring_in, and every row is
+ * marked as past the step's (cu_rows 0). */
+int ivit_step_plan(const ivit_plan_config* cfg, const int32_t* held_dev, const int32_t* base_dev,
+                   const int32_t* new_dev, const int32_t* parent_dev, int32_t* ring_dev,
+                   const int32_t* ring_in_dev, int32_t* table_dev, int32_t* cu_rows_dev, int32_t* req_dev,
+                   int32_t* slot_dev, int32_t* pos_dev, uint32_t* mask_dev, int32_t* ring_out_dev,
+                   int32_t* status_dev, void* stream);
+
+/* Norm and rotation of heads of head_dim values (a multiple of 8, up to 256), the first
+ * rot_dim (a multiple of 8) of which are rotated; heads and kv_heads up to 256. */
+typedef struct ivit_rope_config {
+  int32_t heads, kv_heads, head_dim, rot_dim;
+  int32_t n_axes;        /* axes of a position (1: text; 3: time, height, width), up to 4 */
+  int32_t interleaved;   /* pairs (2f, 2f + 1) if 1, (f, f + rot_dim / 2) if 0 */
+  int32_t dtype;         /* IVIT_BF16 or IVIT_FP16 */
+  float eps;             /* of the norm, >= 0 */
+} ivit_rope_config;
+
+/* For every row and every head of q [n_rows][heads][head_dim] and k [n_rows][kv_heads][..]:
+ *   y = x / sqrt(mean(x^2) + eps) * weight       (weight [head_dim]; NULL: y = x)
+ *   (u, w) -> (u cos a - w sin a, w cos a + u sin a), a = pos[axis[f]][row] * freq[f]
+ * for the pairs f = 0 .. rot_dim / 2 - 1; values past rot_dim are not rotated.  freq fp32 and
+ * axis int32 (0 .. n_axes - 1; others count as 0) [rot_dim / 2]; pos int32, axis a of row r at
+ * a * pos_stride + r (pos_stride 0: all axes share one position), exact up to 2^24 either way.
+ * All arithmetic is fp32, rounded once.  The *_stride of a row array is the number of elements
+ * from one row to the next (a multiple of 8; heads are contiguous in a row), so that q, k and v
+ * can be parts of one projection's output.
+ * q_out; k_out (or NULL); and with `cache` also k and v into the slots slot_dev [n_rows] of
+ * k_cache_dev and v_cache_dev (slots outside the cache, as -1, are skipped; slots of a call
+ * are distinct).  Without `cache`, v and the cache arguments are NULL.  q_out may be q and
+ * k_out may be k.  Arrays 16-byte aligned (freq, axis, pos, slot 4). */
+int ivit_qk_norm_rope(const ivit_rope_config* cfg, int32_t n_rows, const void* q_dev, int64_t q_stride,
+                      const void* k_dev, int64_t k_stride, const void* v_dev, int64_t v_stride,
+                      const void* q_weight_dev, const void* k_weight_dev, const int32_t* pos_dev,
+                      int64_t pos_stride, const float* freq_dev, const int32_t* axis_dev, void* q_out_dev,
+                      int64_t q_out_stride, void* k_out_dev, int64_t k_out_stride,
+                      const ivit_cache_layout* cache, void* k_cache_dev, void* v_cache_dev,
+                      const int32_t* slot_dev, void* stream);
+
+/* Gradients of the above: from grad_q, grad_k (of q_out, k_out) and the inputs q, k to dq, dk
+ * (which may be grad_q, grad_k, or q, k, with the same strides) and, where
+ * there is a weight, dq_weight_dev, dk_weight_dev fp32 [head_dim] (or NULL), summed over rows
+ * and heads in an order that depends on the sizes alone.  workspace_dev: 16-byte aligned,
+ * ivit_qk_norm_rope_backward_workspace(cfg) bytes (0: cfg is invalid), of no meaning between
+ * calls; calls that overlap on the GPU need one each. */
+size_t ivit_qk_norm_rope_backward_workspace(const ivit_rope_config* cfg);
+int ivit_qk_norm_rope_backward(const ivit_rope_config* cfg, int32_t n_rows, const void* grad_q_dev,
+                               int64_t grad_q_stride, const void* grad_k_dev, int64_t grad_k_stride,
+                               const void* q_dev, int64_t q_stride, const void* k_dev, int64_t k_stride,
+                               const void* q_weight_dev, const void* k_weight_dev, const int32_t* pos_dev,
+                               int64_t pos_stride, const float* freq_dev, const int32_t* axis_dev,
+                               void* dq_dev, int64_t dq_stride, void* dk_dev, int64_t dk_stride,
+                               float* dq_weight_dev, float* dk_weight_dev, void* workspace_dev,
+                               void* stream);
+
+#define IVIT_MASK_CAUSAL 0     /* a row sees itself and the request's rows before it */
+#define IVIT_MASK_ALL 1        /* a row sees all of the request's rows */
+#define IVIT_MASK_TREE 2       /* a row sees the rows whose bits are set in its mask */
+
+/* Limits: n_req up to 4096, heads up to 256 and a multiple of the cache's kv_heads, max_new up
+ * to 65536, max_pages * page_size < 2^31, mask_words up to 32768. */
+typedef struct ivit_attention_config {
+  int32_t n_req;
+  int32_t heads;         /* query heads; head h reads key / value head h * kv_heads / heads */
+  int32_t max_pages;     /* columns of the block table */
+  int32_t max_new;       /* most new rows of a request (further ones are not computed) */
+  int32_t mask_mode;     /* IVIT_MASK_* */
+  int32_t mask_words;    /* IVIT_MASK_TREE: words of a mask row; rows past 32 * mask_words are unseen */
+  float scale;           /* of the scores, > 0 (usually 1 / sqrt(head_dim)) */
+} ivit_attention_config;
+
+/* New rows over the cached tokens and over each other.  For row r of request i and head h:
+ *   o = sum_j exp(scale q.k_j) v_j / sum_j exp(scale q.k_j),  lse = log sum_j exp(scale q.k_j)
+ * over the request's len_dev[i] cached tokens (all of which a row sees) and the new rows that
+ * the mask lets it see, whose keys and values are k_new, v_new [n_rows][kv_heads][head_dim]
+ * (not read from the cache, so that drafts need no slots before they are accepted).  A row that
+ * sees nothing gets o = 0, lse = -inf; keys whose scores are -inf take no part; what a row does
+ * not see does not reach it, NaN and infinities included.  Sums and the softmax are fp32;
+ * probabilities enter the product with V as 16-bit values.
+ * table_dev int32 [n_req][max_pages]; len_dev int32 [n_req] (more than the table holds counts as
+ * that much, pages outside the cache read as zeros); cu_rows_dev int32 [n_req + 1];
+ * mask_dev uint32 [n_rows][mask_words] for IVIT_MASK_TREE, else NULL; out [n_rows][heads]
+ * [head_dim], lse_dev fp32 [n_rows][heads] or NULL.  Row strides as in ivit_qk_norm_rope; rows
+ * that belong to no request are left as they are.  workspace_dev: 16-byte aligned,
+ * ivit_tree_attention_workspace(cfg, cache) bytes (0: invalid arguments), of no meaning between
+ * calls; calls that overlap on the GPU need one each. */
+size_t ivit_tree_attention_workspace(const ivit_attention_config* cfg, const ivit_cache_layout* cache);
+int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_cache_layout* cache, int32_t n_rows,
+                        const void* q_dev, int64_t q_stride, const void* k_new_dev, int64_t k_new_stride,
+                        const void* v_new_dev, int64_t v_new_stride, const void* k_cache_dev,
+                        const void* v_cache_dev, const int32_t* table_dev, const int32_t* len_dev,
+                        const int32_t* cu_rows_dev, const uint32_t* mask_dev, void* out_dev,
+                        int64_t out_stride, float* lse_dev, void* workspace_dev, void* stream);
+
+/* Row src_row_dev[i] of k and v ([n_layers][n_src][kv_heads][head_dim], row and layer strides in
+ * elements, multiples of 8) into slot slot_dev[i] of every layer's cache (k_cache_dev,
+ * v_cache_dev: layer l begins cache_layer_stride * l elements in), for i < n.  Entries whose row
+ * is outside [0, n_src) or whose slot is outside the cache are skipped; slots of a call are
+ * distinct. */
+int ivit_kv_write(const ivit_cache_layout* cache, int32_t n_layers, int32_t n, int32_t n_src, const void* k_dev,
+                  const void* v_dev, int64_t row_stride, int64_t layer_stride, const int32_t* src_row_dev,
+                  const int32_t* slot_dev, void* k_cache_dev, void* v_cache_dev, int64_t cache_layer_stride,
+                  void* stream);
+
 /* Message of the last failure on `h` (or of the last failed create if h is NULL). */
 const char* ivit_last_error(const ivit_handle* h);
 

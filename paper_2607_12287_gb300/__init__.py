@@ -29,7 +29,9 @@ EXPORTED = [
     "ivit_weights_size", "ivit_create", "ivit_encode_full", "ivit_encode_incremental",
     "ivit_get_changed", "ivit_get_cache", "ivit_reset", "ivit_timeline",
     "ivit_timeline_read", "ivit_device_status", "ivit_last_launch_count", "ivit_destroy",
-    "ivit_last_error", "ivit_select_noalloc", "ivit_action_combine",
+    "ivit_last_error", "ivit_select_noalloc", "ivit_action_combine", "ivit_step_plan",
+    "ivit_qk_norm_rope", "ivit_qk_norm_rope_backward_workspace", "ivit_qk_norm_rope_backward",
+    "ivit_tree_attention_workspace", "ivit_tree_attention", "ivit_kv_write",
 ]
 IVIT_NOALLOC_MAX_TOKENS = 65536
 
@@ -43,6 +45,29 @@ class IvitConfig(C.Structure):
         ("threshold", C.c_float), ("topk", C.c_int32), ("ref_mode", C.c_int32),
         ("score_source", C.c_int32), ("schedule", C.c_int32), ("mlp_tokens", C.c_int32),
     ]
+
+
+class IvitCacheLayout(C.Structure):
+    """Layout of a paged key (or value) cache of one layer; build it with ``make_cache_layout``."""
+    _fields_ = [
+        ("n_pages", C.c_int32), ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("dtype", C.c_int32), ("reserved", C.c_int32), ("page_stride", C.c_int64), ("token_stride", C.c_int64),
+        ("head_stride", C.c_int64),
+    ]
+
+
+class IvitPlanConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_req", "max_rows", "max_pages", "page_size", "n_pages", "mask_words")]
+
+
+class IvitRopeConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("heads", "kv_heads", "head_dim", "rot_dim", "n_axes", "interleaved", "dtype")]
+    _fields_.append(("eps", C.c_float))
+
+
+class IvitAttentionConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_req", "heads", "max_pages", "max_new", "mask_mode", "mask_words")]
+    _fields_.append(("scale", C.c_float))
 
 
 class IvitError(RuntimeError):
@@ -85,6 +110,17 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     L.ivit_action_combine.argtypes = [P, P, P, P, P, P, C.c_int32, C.c_int32, P, P]
     L.ivit_select_noalloc.argtypes = [P, P, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                       C.c_float, C.c_int32, P, P, P]
+    I32 = C.c_int32
+    L.ivit_step_plan.argtypes = [P] * 16
+    L.ivit_qk_norm_rope.argtypes = [P, I32, P, I64, P, I64, P, I64, P, P, P, I64, P, P, P, I64, P, I64, P, P, P, P, P]
+    L.ivit_qk_norm_rope_backward_workspace.restype = C.c_size_t
+    L.ivit_qk_norm_rope_backward_workspace.argtypes = [P]
+    L.ivit_qk_norm_rope_backward.argtypes = [P, I32, P, I64, P, I64, P, I64, P, I64, P, P, P, I64, P, P, P, I64, P, I64, P,
+                                             P, P, P]
+    L.ivit_tree_attention_workspace.restype = C.c_size_t
+    L.ivit_tree_attention_workspace.argtypes = [P, P]
+    L.ivit_tree_attention.argtypes = [P, P, I32, P, I64, P, I64, P, I64, P, P, P, P, P, P, P, I64, P, P, P]
+    L.ivit_kv_write.argtypes = [P, I32, I32, I32, P, P, I64, I64, P, P, P, P, I64, P]
     _lib = L
     return L
 
@@ -108,7 +144,7 @@ def _tensor_type():
     t = _dtypes.get("tensor")
     if t is None:
         import torch
-        for name in ("uint8", "int32", "float32", "bfloat16"):
+        for name in ("uint8", "int32", "float32", "bfloat16", "float16"):
             _dtypes[name] = getattr(torch, name)
         t = _dtypes["tensor"] = torch.Tensor
     return t
@@ -283,6 +319,245 @@ def ivit_action_combine(x0, v0, v7, alpha, beta, b, xT, stream=None) -> None:
     _require(beta, "beta", "float32", B)
     _check(load().ivit_action_combine(_ptr(x0), _ptr(v0), _ptr(v7), _ptr(alpha), _ptr(beta), _ptr(b), B, A,
                                       _ptr(xT), _stream(stream)), None)
+
+
+# ------------------------------------------------------- language backbone
+
+IVIT_BF16 = 0
+IVIT_FP16 = 1
+IVIT_MASK_CAUSAL = 0
+IVIT_MASK_ALL = 1
+IVIT_MASK_TREE = 2
+_DTYPES = {"bfloat16": IVIT_BF16, "float16": IVIT_FP16}
+_DTYPE_NAMES = {v: k for k, v in _DTYPES.items()}
+_MASKS = {"causal": IVIT_MASK_CAUSAL, "all": IVIT_MASK_ALL, "tree": IVIT_MASK_TREE}
+
+
+def _dtype_code(dtype) -> int:
+    name = str(dtype).replace("torch.", "")
+    if name not in _DTYPES:
+        raise TypeError(f"dtype {dtype}: bfloat16 or float16 is required")
+    return _DTYPES[name]
+
+
+def make_cache_layout(cache) -> IvitCacheLayout:
+    """Layout of a paged cache given as a tensor [pages, page_size, kv_heads, head_dim] (any strides with
+    contiguous heads, so a [pages, kv_heads, page_size, head_dim] array transposed will do)."""
+    if len(cache.shape) != 4:
+        raise ValueError(f"cache: shape {tuple(cache.shape)}, expected [pages, page_size, kv_heads, head_dim]")
+    st = cache.stride()
+    if st[3] != 1:
+        raise ValueError("cache: the values of a head are not contiguous")
+    lay = IvitCacheLayout(*cache.shape, _dtype_code(cache.dtype), 0, st[0], st[1], st[2])
+    lay.shape, lay.strides = tuple(cache.shape), tuple(st)
+    return lay
+
+
+def make_plan_config(n_req: int, max_rows: int, max_pages: int, page_size: int, n_pages: int,
+                     mask_words: int = 0) -> IvitPlanConfig:
+    return IvitPlanConfig(n_req, max_rows, max_pages, page_size, n_pages, mask_words)
+
+
+def make_rope_config(heads: int, kv_heads: int, head_dim: int, rot_dim: Optional[int] = None, n_axes: int = 1,
+                     interleaved: bool = False, eps: float = 1e-6, dtype="bfloat16") -> IvitRopeConfig:
+    return IvitRopeConfig(heads, kv_heads, head_dim, head_dim if rot_dim is None else rot_dim, n_axes,
+                          int(interleaved), _dtype_code(dtype), eps)
+
+
+def make_attention_config(n_req: int, heads: int, max_pages: int, max_new: int, mask="causal", mask_words: int = 0,
+                          scale: float = 1.0) -> IvitAttentionConfig:
+    """``mask``: "causal", "all" or "tree" (with ``mask_words`` 32-bit words a row)."""
+    return IvitAttentionConfig(n_req, heads, max_pages, max_new, _MASKS.get(mask, mask), mask_words, scale)
+
+
+def _rows(t, name: str, dtype: int, n_rows: int, heads: int, dim: int) -> int:
+    """The row stride of a tensor [rows, heads, dim] whose heads are contiguous in a row; rejects one that
+    the kernels would misread, as ``_require`` does."""
+    if isinstance(t, (int, np.ndarray)) or t is None:
+        raise TypeError(f"{name}: a CUDA tensor is required")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name}: tensor on {t.device}; a CUDA tensor is required")
+    _tensor_type()
+    if t.dtype is not _dtypes[_DTYPE_NAMES[dtype]]:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected torch.{_DTYPE_NAMES[dtype]}")
+    sh = t.shape
+    if len(sh) != 3 or sh[0] < n_rows or sh[1] != heads or sh[2] != dim:
+        raise ValueError(f"{name}: shape {tuple(sh)}, expected [{n_rows}, {heads}, {dim}]")
+    st = t.stride()
+    if st[2] != 1 or (heads > 1 and st[1] != dim):
+        raise ValueError(f"{name}: the heads of a row are not contiguous")
+    return st[0] if sh[0] > 1 else heads * dim
+
+
+def _row_count(t, name: str) -> int:
+    if t is None or isinstance(t, (int, np.ndarray)) or len(t.shape) != 3:
+        raise ValueError(f"{name}: a CUDA tensor [rows, heads, head_dim] is required")
+    return t.shape[0]
+
+
+def _cache(t, name: str, layout: IvitCacheLayout, layered: bool = False) -> None:
+    """Rejects a tensor that is not a cache of this layout (with a leading layer dimension if ``layered``)."""
+    if t is None or isinstance(t, (int, np.ndarray)):
+        raise TypeError(f"{name}: a CUDA tensor is required")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name}: tensor on {t.device}; a CUDA tensor is required")
+    _tensor_type()
+    if t.dtype is not _dtypes[_DTYPE_NAMES[layout.dtype]]:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected torch.{_DTYPE_NAMES[layout.dtype]}")
+    sh, st = (t.shape[1:], t.stride()[1:]) if layered else (t.shape, t.stride())
+    if tuple(sh) != layout.shape or tuple(st) != layout.strides:
+        raise ValueError(f"{name}: shape {tuple(sh)} and strides {tuple(st)} are not the layout's, {layout.shape} and "
+                         f"{layout.strides}")
+
+
+def ivit_step_plan(cfg: IvitPlanConfig, held, base, new, parent, ring, ring_in, table, cu_rows, req, slots, positions,
+                   mask, ring_out, status, stream=None) -> None:
+    """Pages, slots, positions and tree masks of a step (int32 tensors; parent, req, positions and mask may be
+    None): ``table`` [n_req, max_pages] and ``ring`` [n_pages] are updated, ``cu_rows`` [n_req + 1], the row arrays
+    [max_rows], ``mask`` [max_rows, mask_words], ``ring_out`` [2] and ``status`` [1] written."""
+    n, rows = cfg.n_req, cfg.max_rows
+    _require(held, "held", "int32", n)
+    _require(base, "base", "int32", n)
+    _require(new, "new", "int32", n)
+    _require(parent, "parent", "int32", rows)
+    _require(ring, "ring", "int32", cfg.n_pages)
+    _require(ring_in, "ring_in", "int32", 2)
+    _require(table, "table", "int32", n * cfg.max_pages)
+    _require(cu_rows, "cu_rows", "int32", n + 1)
+    _require(req, "req", "int32", rows)
+    _require(slots, "slots", "int32", rows)
+    _require(positions, "positions", "int32", rows)
+    _require(mask, "mask", "int32", rows * cfg.mask_words)
+    _require(ring_out, "ring_out", "int32", 2)
+    _require(status, "status", "int32", 1)
+    _check(load().ivit_step_plan(C.addressof(cfg), _ptr(held), _ptr(base), _ptr(new), _ptr(parent), _ptr(ring), _ptr(ring_in),
+                                 _ptr(table), _ptr(cu_rows), _ptr(req), _ptr(slots), _ptr(positions), _ptr(mask),
+                                 _ptr(ring_out), _ptr(status), _stream(stream)), None)
+
+
+def _rope_inputs(cfg: IvitRopeConfig, n: int, q_weight, k_weight, positions, freq, axis) -> int:
+    """Checks what the rotation and its gradient have in common; the stride of the position axes."""
+    _require(q_weight, "q_weight", _DTYPE_NAMES[cfg.dtype], cfg.head_dim)
+    _require(k_weight, "k_weight", _DTYPE_NAMES[cfg.dtype], cfg.head_dim)
+    _require(freq, "freq", "float32", cfg.rot_dim // 2)
+    _require(axis, "axis", "int32", cfg.rot_dim // 2)
+    if positions is None or isinstance(positions, (int, np.ndarray)) or len(positions.shape) > 2:
+        raise TypeError("positions: a CUDA tensor [rows] or [axes, rows] is required")
+    if len(positions.shape) == 1 or positions.shape[0] == 1:  # one position for all axes
+        _require(positions, "positions", "int32", n)
+        return 0
+    if positions.shape[0] < cfg.n_axes or positions.shape[1] < n:
+        raise ValueError(f"positions: shape {tuple(positions.shape)}, expected [{cfg.n_axes}, {n}]")
+    _require(positions, "positions", "int32", cfg.n_axes * n)
+    return positions.shape[1]
+
+
+def ivit_qk_norm_rope(cfg: IvitRopeConfig, q, k, v, q_weight, k_weight, positions, freq, axis, q_out, k_out=None,
+                      cache: Optional[IvitCacheLayout] = None, k_cache=None, v_cache=None, slots=None,
+                      stream=None) -> None:
+    """Norm (where there is a weight) and rotation of q [rows, heads, head_dim] and k [rows, kv_heads, head_dim]
+    into ``q_out``, ``k_out`` and, with ``cache``, of k and v into the ``slots`` of the paged caches.
+    ``positions``: int32 [rows] or [axes, rows]; ``freq``, ``axis``: of each pair."""
+    n = _row_count(q, "q")
+    dt, heads, kv, dim = cfg.dtype, cfg.heads, cfg.kv_heads, cfg.head_dim
+    qs = _rows(q, "q", dt, n, heads, dim)
+    ks = _rows(k, "k", dt, n, kv, dim)
+    qos = _rows(q_out, "q_out", dt, n, heads, dim)
+    kos = 0 if k_out is None else _rows(k_out, "k_out", dt, n, kv, dim)
+    vs, lay = 0, None
+    if cache is not None:
+        vs = _rows(v, "v", dt, n, kv, dim)
+        _cache(k_cache, "k_cache", cache)
+        _cache(v_cache, "v_cache", cache)
+        _require(slots, "slots", "int32", n)
+        lay = C.addressof(cache)
+    ps = _rope_inputs(cfg, n, q_weight, k_weight, positions, freq, axis)
+    _check(load().ivit_qk_norm_rope(C.addressof(cfg), n, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(q_weight), _ptr(k_weight),
+                                    _ptr(positions), ps, _ptr(freq), _ptr(axis), _ptr(q_out), qos, _ptr(k_out), kos, lay,
+                                    _ptr(k_cache), _ptr(v_cache), _ptr(slots), _stream(stream)), None)
+
+
+def ivit_qk_norm_rope_backward_workspace(cfg: IvitRopeConfig) -> int:
+    """Bytes of the workspace of ``ivit_qk_norm_rope_backward`` (0: the configuration is invalid)."""
+    return int(load().ivit_qk_norm_rope_backward_workspace(C.addressof(cfg)))
+
+
+def ivit_qk_norm_rope_backward(cfg: IvitRopeConfig, grad_q, grad_k, q, k, q_weight, k_weight, positions, freq, axis, dq, dk,
+                               dq_weight=None, dk_weight=None, workspace=None, stream=None) -> None:
+    """Gradients of ``ivit_qk_norm_rope``: ``dq``, ``dk`` and the weights' fp32
+    [head_dim] (or None)."""
+    n = _row_count(q, "q")
+    dt, heads, kv, dim = cfg.dtype, cfg.heads, cfg.kv_heads, cfg.head_dim
+    gqs = _rows(grad_q, "grad_q", dt, n, heads, dim)
+    gks = _rows(grad_k, "grad_k", dt, n, kv, dim)
+    qs = _rows(q, "q", dt, n, heads, dim)
+    ks = _rows(k, "k", dt, n, kv, dim)
+    dqs, dks = _rows(dq, "dq", dt, n, heads, dim), _rows(dk, "dk", dt, n, kv, dim)
+    _require(dq_weight, "dq_weight", "float32", dim)
+    _require(dk_weight, "dk_weight", "float32", dim)
+    ps = _rope_inputs(cfg, n, q_weight, k_weight, positions, freq, axis)
+    if dq_weight is not None or dk_weight is not None:
+        _require(workspace, "workspace", "uint8", ivit_qk_norm_rope_backward_workspace(cfg))
+    _check(load().ivit_qk_norm_rope_backward(C.addressof(cfg), n, _ptr(grad_q), gqs, _ptr(grad_k), gks, _ptr(q), qs, _ptr(k), ks,
+                                             _ptr(q_weight), _ptr(k_weight), _ptr(positions), ps, _ptr(freq), _ptr(axis),
+                                             _ptr(dq), dqs, _ptr(dk), dks, _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace),
+                                             _stream(stream)), None)
+
+
+def ivit_tree_attention_workspace(cfg: IvitAttentionConfig, cache: IvitCacheLayout) -> int:
+    """Bytes of the workspace of ``ivit_tree_attention`` (0: the arguments are invalid)."""
+    return int(load().ivit_tree_attention_workspace(C.addressof(cfg), C.addressof(cache)))
+
+
+def ivit_tree_attention(cfg: IvitAttentionConfig, cache: IvitCacheLayout, q, k_new, v_new, k_cache, v_cache, table, lengths,
+                        cu_rows, mask, out, lse=None, workspace=None, stream=None) -> None:
+    """Attention of the new rows q [rows, heads, head_dim] over the cached tokens of their requests and over the new
+    keys and values [rows, kv_heads, head_dim] that the mask lets them see; ``lse`` fp32 [rows, heads] or None."""
+    n = _row_count(q, "q")
+    dt, heads, kv, dim = cache.dtype, cfg.heads, cache.kv_heads, cache.head_dim
+    qs = _rows(q, "q", dt, n, heads, dim)
+    ks = _rows(k_new, "k_new", dt, n, kv, dim)
+    vs = _rows(v_new, "v_new", dt, n, kv, dim)
+    os_ = _rows(out, "out", dt, n, heads, dim)
+    _cache(k_cache, "k_cache", cache)
+    _cache(v_cache, "v_cache", cache)
+    _require(table, "table", "int32", cfg.n_req * cfg.max_pages)
+    _require(lengths, "lengths", "int32", cfg.n_req)
+    _require(cu_rows, "cu_rows", "int32", cfg.n_req + 1)
+    if cfg.mask_mode == IVIT_MASK_TREE:
+        _require(mask, "mask", "int32", n * cfg.mask_words)
+    _require(lse, "lse", "float32", n * heads)
+    _require(workspace, "workspace", "uint8", ivit_tree_attention_workspace(cfg, cache))
+    _check(load().ivit_tree_attention(C.addressof(cfg), C.addressof(cache), n, _ptr(q), qs, _ptr(k_new), ks, _ptr(v_new), vs,
+                                      _ptr(k_cache), _ptr(v_cache), _ptr(table), _ptr(lengths), _ptr(cu_rows), _ptr(mask),
+                                      _ptr(out), os_, _ptr(lse), _ptr(workspace), _stream(stream)), None)
+
+
+def ivit_kv_write(cache: IvitCacheLayout, k, v, rows, slots, k_cache, v_cache, stream=None) -> None:
+    """Rows ``rows`` (int32, -1: none) of k and v [layers, rows, kv_heads, head_dim] into the ``slots`` of the caches
+    [layers, pages, page_size, kv_heads, head_dim] of all layers."""
+    for t, name in ((k, "k"), (v, "v")):
+        if t is None or isinstance(t, (int, np.ndarray)) or len(t.shape) != 4:
+            raise ValueError(f"{name}: a CUDA tensor [layers, rows, kv_heads, head_dim] is required")
+    layers, n_src = k.shape[0], k.shape[1]
+    strides = []
+    for t, name in ((k, "k"), (v, "v")):
+        if t.shape[0] != layers or t.shape[1] != n_src:
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [{layers}, {n_src}, ...]")
+        row = _rows(t[0] if layers else t.flatten(0, 1), name, cache.dtype, n_src, cache.kv_heads, cache.head_dim)
+        strides.append((row, t.stride()[0] if layers > 1 else 0))
+    if strides[0] != strides[1]:
+        raise ValueError("v: strides other than k's")
+    _cache(k_cache, "k_cache", cache, layered=True)
+    _cache(v_cache, "v_cache", cache, layered=True)
+    if k_cache.shape[0] < layers or v_cache.shape[0] < layers or k_cache.stride()[0] != v_cache.stride()[0]:
+        raise ValueError("k_cache, v_cache: fewer layers than k and v, or of different strides")
+    n = rows.numel() if hasattr(rows, "numel") else 0
+    _require(rows, "rows", "int32", n)
+    _require(slots, "slots", "int32", n)
+    _check(load().ivit_kv_write(C.addressof(cache), layers, n, n_src, _ptr(k), _ptr(v), strides[0][0], strides[0][1],
+                                _ptr(rows), _ptr(slots), _ptr(k_cache), _ptr(v_cache), k_cache.stride()[0],
+                                _stream(stream)), None)
 
 
 # ------------------------------------------------------------ convenience

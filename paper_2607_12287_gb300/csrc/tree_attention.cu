@@ -1,0 +1,729 @@
+// New rows of every request over its cached tokens and over each other (ivit_tree_attention):
+//
+//   o = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q.k_j - m),  lse = m + log sum_j p_j
+//
+// over the keys j that a row sees: all cached ones, and the new rows that its mask names.
+//
+// Rows that share a key head (the new rows x the query heads of the group) form tiles of 16, 32 or
+// 64; a tile walks its keys -- the cached tokens and, behind them, the new rows -- 64 at a time.
+// All (request, key head, row tile, 64 keys) of the call, in this order, are cut into as many equal
+// runs as there are CTAs, two per SM, so that ragged lengths and few requests load the chip alike.
+// A run that holds a tile's keys only in part leaves its running maximum, sum and output (fp32) in
+// the workspace, and a second kernel joins the parts of a tile in the order of their keys.
+//
+// A CTA of four warps: 16-byte asynchronous copies fill a ring of K and V tiles in shared memory
+// (swizzled; the pages are looked up one tile ahead), mma.m16n8k16 multiplies.  Row groups of 16 are
+// split over the warps and, for 16 and 32 rows, the 64 keys too (KW warps with a running maximum,
+// sum and output each, which meet in shared memory at the end).  Probabilities enter the product
+// with V as two 16-bit terms (their fp32 value but for 16 of 24 bits and more) up to 32 rows, where
+// the bytes of the cache bound the kernel and the second product is free, and rounded to one
+// above; sums use their fp32 values.
+//
+// Bound: the cache's bytes for few rows per key head, mma.sync's rate for many.
+#include <algorithm>
+#include <type_traits>
+
+#include "attention.cuh"
+#include "backbone.cuh"
+
+namespace ivit {
+namespace {
+
+constexpr int THREADS = 128;
+constexpr int TK = 64;              // keys of a tile
+constexpr int MAX_REQ = 4096;
+constexpr int MAX_CTAS = 512;       // of the attention kernel: the workspace's parts
+// Probabilities are kept 2^SHIFT times too large, which keeps small fp16 ones normal.
+constexpr float SHIFT = 10.f;
+
+struct TreeArgs {
+  const void *q, *k_new, *v_new, *k_cache, *v_cache;
+  const int *table, *len, *cu;
+  const uint32_t* mask;
+  void* out;
+  float *lse, *parts;
+  int4* joins;                      // [CTAs] the tile that CTA c's run begins and others go on with: request (-1:
+                                    // none), key head, row tile, 2 * last CTA + whether it is c's second part
+  long long q_stride, k_new_stride, v_new_stride, out_stride;
+  PagedCache cache;
+  int n_req, n_rows, heads, group, max_pages, max_new, mask_mode, mask_words;
+  float scale_log2;                 // scale * log2(e)
+};
+
+template <typename T>
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma<bf16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  mma_bf16_16816(d, a[0], a[1], a[2], a[3], b0, b1);
+}
+template <>
+__device__ __forceinline__ void mma<half>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+
+// 16 bytes to shared memory, or zeros (nothing is read) if not `ok`.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// Rows and cached tokens of a request, within the bounds the host vouches for.
+struct Request {
+  int row0, n, len;
+};
+
+__device__ __forceinline__ Request request(const TreeArgs& a, int i) {
+  Request r;
+  const int lo = a.cu[i], hi = a.cu[i + 1], most = a.max_pages << a.cache.page_shift;
+  r.row0 = min(max(lo, 0), a.n_rows);
+  r.n = min(max(min(hi, a.n_rows) - r.row0, 0), a.max_new);
+  r.len = min(max(a.len[i], 0), most);
+  return r;
+}
+
+__device__ __forceinline__ int key_tiles(const Request& r) { return r.n > 0 ? (r.len + r.n + TK - 1) / TK : 0; }
+
+template <int M>
+__device__ __forceinline__ int row_tiles(const TreeArgs& a, const Request& r) {
+  return (r.n * a.group + M - 1) / M;
+}
+
+// A place in the order of units (request, key head, row tile, key tile).
+template <int M>
+struct Place {
+  Request r;
+  int req, head, rt, kt, nkt, nrt;
+
+  __device__ __forceinline__ void enter(const TreeArgs& a, int i) {  // the first unit of request i or later
+    for (req = i; req < a.n_req; ++req) {
+      r = request(a, req);
+      if (r.n > 0) break;
+    }
+    nkt = key_tiles(r);
+    nrt = row_tiles<M>(a, r);
+    head = rt = kt = 0;
+  }
+  __device__ __forceinline__ void next(const TreeArgs& a) {
+    if (++kt < nkt) return;
+    kt = 0;
+    if (++rt < nrt) return;
+    rt = 0;
+    if (++head < a.cache.heads) return;
+    enter(a, req + 1);
+  }
+};
+
+template <int DP, int RW>
+struct Cfg {
+  static constexpr int M = 16 * RW, KW = 4 / RW, WK = TK / KW;   // rows, warps along the keys, keys of a warp
+  static constexpr int ROW = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;  // bytes of a row in shared memory
+  static constexpr int TILE = TK * ROW;
+  static constexpr int STAGES = 3;
+  static constexpr int CTAS = DP <= 128 ? 2 : 1;                 // per SM
+  static constexpr int TERMS = RW < 4 ? 2 : 1;
+  static constexpr int MEET = DP + 4;                            // floats of a row where the warps meet
+  static constexpr int OFF_MEET = STAGES * 2 * TILE;
+  static constexpr int OFF_FLAGS = OFF_MEET + (KW > 1 ? M * (MEET + 2) * 4 : 0);
+  static constexpr int BYTES = OFF_FLAGS + STAGES * 8;
+  static constexpr int PART = M * (DP + 2);                      // floats of a part in the workspace
+  static_assert(MAX_REQ * 8 + 8 <= OFF_MEET, "the units before each request");
+};
+
+// Shared-memory address of 16-byte piece c of a row.
+template <int ROW>
+__device__ __forceinline__ uint32_t piece(uint32_t tile, int row, int c) {
+  return tile + row * ROW + ((c ^ (row & 7)) << 4);
+}
+
+// Which of the 64 keys from k0 on new row `node` of the request sees (bit j: key k0 + j).
+__device__ __forceinline__ uint64_t seen(const TreeArgs& a, const Request& r, int node, int k0) {
+  const auto low = [](int n) { return n >= 64 ? ~0ull : n > 0 ? (1ull << n) - 1 : 0ull; };
+  const int first = k0 - r.len;  // new row of bit 0 (negative: cached tokens up to there)
+  if (a.mask_mode == IVIT_MASK_CAUSAL) return low(node + 1 - first);
+  if (a.mask_mode == IVIT_MASK_ALL) return low(r.n - first);
+  const uint32_t* words = a.mask + static_cast<size_t>(r.row0 + node) * a.mask_words;
+  const auto word = [&](int w) { return static_cast<uint64_t>(w < a.mask_words ? words[w] : 0u); };
+  uint64_t bits;
+  if (first < 0) {
+    bits = ((word(0) | word(1) << 32) << -first) | low(-first);
+  } else {
+    const int w = first >> 5, s = first & 31;
+    bits = (word(w) | word(w + 1) << 32) >> s;
+    if (s) bits |= word(w + 2) << (64 - s);
+  }
+  return bits & low(r.n - first);
+}
+
+template <typename T, int DP, int RW>
+__global__ void __launch_bounds__(THREADS, Cfg<DP, RW>::CTAS) tree_attention_kernel(const TreeArgs a) {
+  using C = Cfg<DP, RW>;
+  constexpr int M = C::M, KW = C::KW, WK = C::WK, ROW = C::ROW, STAGES = C::STAGES;
+  constexpr int PIECES = DP / 8, COPIES = (TK * PIECES + THREADS - 1) / THREADS;
+  constexpr bool QREG = DP <= 128;   // queries in registers (else read again for every tile)
+  extern __shared__ __align__(128) uint8_t sm[];
+  const uint32_t sb = smem_u32(sm);
+  uint32_t* flags = reinterpret_cast<uint32_t*>(sm + C::OFF_FLAGS);  // [STAGES][2] keys whose values are not finite
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int rw = warp / KW, kw = warp % KW;  // row group and key group of the warp
+  const int pieces = a.cache.dim >> 3;
+  pdl_wait();
+  pdl_launch_dependents();
+
+  // units before each request, and this CTA's run [lo, hi)
+  __shared__ unsigned long long carry[THREADS / 32];
+  unsigned long long* before = reinterpret_cast<unsigned long long*>(sm);
+  unsigned long long total = 0;
+  for (int i0 = 0; i0 < a.n_req; i0 += THREADS) {
+    const int i = i0 + tid;
+    unsigned long long n = 0;
+    if (i < a.n_req) {
+      const Request r = request(a, i);
+      n = static_cast<unsigned long long>(key_tiles(r)) * row_tiles<M>(a, r) * a.cache.heads;
+    }
+    unsigned long long run = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned long long up = __shfl_up_sync(0xffffffffu, run, o);
+      if (lane >= o) run += up;
+    }
+    if (lane == 31) carry[warp] = run;
+    __syncthreads();
+    unsigned long long ahead = total;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+      if (w < warp) ahead += carry[w];
+      total += carry[w];
+    }
+    if (i < a.n_req) before[i] = ahead + run - n;
+    __syncthreads();
+  }
+  // (no more runs than units, so that no run is empty between two that share a tile)
+  const unsigned long long ctas = total < gridDim.x ? total : gridDim.x;
+  if (tid == 0) a.joins[blockIdx.x].x = -1;
+  if (blockIdx.x >= ctas) return;
+  const unsigned long long lo = total * blockIdx.x / ctas, hi = total * (blockIdx.x + 1) / ctas;
+  Place<M> load;
+  {
+    int i = 0, j = a.n_req - 1;  // last request with before <= lo: it has units
+    while (i < j) {
+      const int mid = (i + j + 1) >> 1;
+      if (before[mid] <= lo) i = mid; else j = mid - 1;
+    }
+    const unsigned long long off = lo - before[i];
+    load.enter(a, i);
+    const unsigned long long per = static_cast<unsigned long long>(load.nkt) * load.nrt;
+    load.head = static_cast<int>(off / per);
+    const unsigned rest = static_cast<unsigned>(off - load.head * per);
+    load.rt = rest / load.nkt;
+    load.kt = rest - load.rt * load.nkt;
+  }
+  __syncthreads();  // `before` gives way to the tiles
+  if (pieces < PIECES) {
+    // columns past a head's are zero for good: no copy touches them
+    for (int x = tid; x < STAGES * 2 * TK * (PIECES - pieces); x += THREADS) {
+      const int row = x / (PIECES - pieces), c = pieces + x % (PIECES - pieces);
+      *reinterpret_cast<uint4*>(sm + (row * ROW + ((c ^ (row & 7)) << 4))) = make_uint4(0, 0, 0, 0);
+    }
+  }
+  Place<M> at = load;
+  const int units = static_cast<int>(hi - lo);
+
+  // The pages of the tile at `load`, of the rows that this thread copies; kept a tile ahead of the copies.
+  int ids[COPIES];
+  auto look_up = [&] {
+#pragma unroll
+    for (int x = 0; x < COPIES; ++x) {
+      const int e = x * THREADS + tid, key = load.kt * TK + e / PIECES;
+      ids[x] = e < TK * PIECES && key < load.r.len
+                   ? a.table[static_cast<size_t>(load.req) * a.max_pages + (key >> a.cache.page_shift)]
+                   : -1;
+    }
+  };
+  auto copy = [&](int stage) {
+    const uint32_t ks = sb + stage * 2 * C::TILE, vs = ks + C::TILE;
+    const T* kc = static_cast<const T*>(a.k_cache) + load.head * a.cache.head_stride;
+    const T* vc = static_cast<const T*>(a.v_cache) + load.head * a.cache.head_stride;
+#pragma unroll
+    for (int x = 0; x < COPIES; ++x) {
+      const int e = x * THREADS + tid, row = e / PIECES, c = e - row * PIECES, key = load.kt * TK + row;
+      if (e >= TK * PIECES || c >= pieces) continue;
+      const int fresh = key - load.r.len;
+      const T *k = kc, *v = vc;
+      bool ok;
+      if (fresh < 0) {
+        ok = static_cast<unsigned>(ids[x]) < static_cast<unsigned>(a.cache.n_pages);
+        const long long off = ok ? ids[x] * a.cache.page_stride + (key & ((1 << a.cache.page_shift) - 1)) * a.cache.token_stride : 0;
+        k += off + 8 * c;
+        v += off + 8 * c;
+      } else {
+        ok = fresh < load.r.n;
+        if (ok) {
+          const long long row = load.r.row0 + fresh;
+          k = static_cast<const T*>(a.k_new) + row * a.k_new_stride + load.head * a.cache.dim + 8 * c;
+          v = static_cast<const T*>(a.v_new) + row * a.v_new_stride + load.head * a.cache.dim + 8 * c;
+        }
+      }
+      copy16(piece<ROW>(ks, row, c), k, ok);
+      copy16(piece<ROW>(vs, row, c), v, ok);
+    }
+  };
+
+  int loaded = 0;
+  look_up();
+  auto fill = [&](int stage) {  // the next tile's copies, if there is one
+    if (loaded < units) {
+      copy(stage);
+      if (tid < 2) flags[2 * stage + tid] = 0;
+      load.next(a);
+      if (++loaded < units) look_up();
+    }
+    copies_commit();
+  };
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) fill(s);
+  __syncthreads();  // the flags are clear, and the columns past a head's
+
+  uint32_t q[QREG ? DP / 16 : 1][4];
+  float o[DP / 8][4], m[2], l[2];
+  int node[2];               // new row of the lane's rows g, g + 8 (-1: none)
+  long long qoff[2];
+  bool begun = true;         // of the tile's keys the run has seen the first
+  auto query = [&](int c, uint32_t (&f)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = e & 1, d = 16 * c + 2 * t + 8 * (e >> 1);
+      f[e] = node[r] >= 0 && d < a.cache.dim ? *reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + qoff[r] + d) : 0u;
+    }
+  };
+
+  for (int u = 0; u < units; ++u) {
+    const int stage = u % STAGES;
+    if (u == 0 || at.kt == 0) {  // a new tile of rows
+      begun = at.kt == 0;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int x = at.rt * M + rw * 16 + g + 8 * r, n = x / a.group;
+        node[r] = n < at.r.n ? n : -1;
+        qoff[r] = (at.r.row0 + n) * a.q_stride + static_cast<long long>(at.head * a.group + x - n * a.group) * a.cache.dim;
+        m[r] = -INFINITY;
+        l[r] = 0.f;
+      }
+      if (QREG) {
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) query(c, q[c]);
+      }
+#pragma unroll
+      for (int j = 0; j < DP / 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
+    }
+    const uint32_t ks = sb + stage * 2 * C::TILE, vs = ks + C::TILE;
+    const int k0 = at.kt * TK;
+    const bool edge = k0 + TK > at.r.len;  // holds new rows, or ends
+    copies_wait<STAGES - 2>();
+    if (edge) {
+      // Values of new rows that are not finite would reach rows that do not see them (0 * NaN): they
+      // become zero here, each thread looking at what it copied, and are added back below.
+#pragma unroll
+      for (int x = 0; x < COPIES; ++x) {
+        const int e = x * THREADS + tid, row = e / PIECES, c = e - row * PIECES;
+        if (e >= TK * PIECES || c >= pieces || k0 + row < at.r.len || k0 + row >= at.r.len + at.r.n) continue;
+        uint32_t* w = reinterpret_cast<uint32_t*>(sm + (piece<ROW>(vs, row, c) - sb));
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t e16 = std::is_same<T, bf16>::value ? 0x7f80u : 0x7c00u;
+          const uint32_t x0 = w[i];
+          uint32_t keep = 0xffffffffu;
+          if ((x0 & e16) == e16) keep &= 0xffff0000u;
+          if ((x0 >> 16 & e16) == e16) keep &= 0x0000ffffu;
+          if (keep != 0xffffffffu) {
+            w[i] = x0 & keep;
+            odd = true;
+          }
+        }
+        if (odd) atomicOr(&flags[2 * stage + (row >> 5)], 1u << (row & 31));
+      }
+    }
+    __syncthreads();  // everyone's copies have landed, and the stage of the tile before is free
+    fill((u + STAGES - 1) % STAGES);
+
+    // scores of the warp's keys
+    float s[WK / 8][4];
+#pragma unroll
+    for (int j = 0; j < WK / 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[j][e] = 0.f;
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+      uint32_t f[4];
+      if (!QREG) query(c, f);
+#pragma unroll
+      for (int j = 0; j < WK / 16; ++j) {
+        uint32_t b[4];
+        const int row = kw * WK + 16 * j + (lane & 7) + ((lane & 16) >> 1);
+        ldmatrix4(b, piece<ROW>(ks, row, 2 * c + (lane >> 3 & 1)));
+        mma<T>(s[2 * j], QREG ? q[QREG ? c : 0] : f, b[0], b[1]);
+        mma<T>(s[2 * j + 1], QREG ? q[QREG ? c : 0] : f, b[2], b[3]);
+      }
+    }
+    if (edge) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const uint64_t bits = node[r] >= 0 ? seen(a, at.r, node[r], k0) >> (kw * WK) : 0;
+#pragma unroll
+        for (int j = 0; j < WK / 8; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (!(bits >> (8 * j + 2 * t + e) & 1)) s[j][2 * r + e] = -INFINITY;
+      }
+    }
+    // probabilities, running maximum and sum
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < WK / 8; ++j) mx = fmaxf(mx, fmaxf(s[j][2 * r], s[j][2 * r + 1]));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      const float top = fmaxf(m[r], mx), ref = top == -INFINITY ? 0.f : top;  // (nothing seen so far: P = 0)
+      const float alpha = ex2((m[r] - ref) * a.scale_log2), mo = SHIFT - ref * a.scale_log2;
+      m[r] = top;
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < WK / 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          s[j][2 * r + e] = ex2(fmaf(s[j][2 * r + e], a.scale_log2, mo));
+          sum += s[j][2 * r + e];
+        }
+      l[r] = l[r] * alpha + sum;
+#pragma unroll
+      for (int j = 0; j < DP / 8; ++j) {
+        o[j][2 * r] *= alpha;
+        o[j][2 * r + 1] *= alpha;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < WK / 16; ++j) {
+      uint32_t p[C::TERMS][4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float& x = s[2 * j + (e >> 1)][2 * (e & 1)];
+        float& y = s[2 * j + (e >> 1)][2 * (e & 1) + 1];
+        p[0][e] = pack2<T>(x, y);
+        if (C::TERMS == 2) {
+          const float2 h = unpack2<T>(p[0][e]);
+          p[C::TERMS - 1][e] = pack2<T>(x - h.x, y - h.y);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < DP / 16; ++c) {
+        uint32_t b[4];
+        const int row = kw * WK + 16 * j + (lane & 15);
+        ldmatrix4_trans(b, piece<ROW>(vs, row, 2 * c + (lane >> 4)));
+#pragma unroll
+        for (int x = 0; x < C::TERMS; ++x) {
+          mma<T>(o[2 * c], p[x], b[0], b[1]);
+          mma<T>(o[2 * c + 1], p[x], b[2], b[3]);
+        }
+      }
+    }
+    if (edge && (flags[2 * stage] | flags[2 * stage + 1])) {
+      // values that are not finite, for the rows that see them
+      for (int k = kw * WK; k < (kw + 1) * WK; ++k) {
+        if (!(flags[2 * stage + (k >> 5)] >> (k & 31) & 1)) continue;
+        const T* v = static_cast<const T*>(a.v_new) + (at.r.row0 + k0 + k - at.r.len) * a.v_new_stride + at.head * a.cache.dim;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+          if (node[r] >= 0 && seen(a, at.r, node[r], k0) >> k & 1) {
+#pragma unroll
+            for (int j = 0; j < DP / 8; ++j)
+              if (8 * j < a.cache.dim) {
+                const float2 x = unpack2<T>(*reinterpret_cast<const uint32_t*>(v + 8 * j + 2 * t));
+                if (!isfinite(x.x)) o[j][2 * r] += x.x;
+                if (!isfinite(x.y)) o[j][2 * r + 1] += x.y;
+              }
+          }
+      }
+    }
+
+    if (at.kt == at.nkt - 1 || u == units - 1) {  // the run has no more keys of this tile of rows
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+      }
+      if (KW > 1) {  // the warps of a row group, one after another into the first
+        float* meet = reinterpret_cast<float*>(sm + C::OFF_MEET);
+        float* mm = meet + M * C::MEET;
+        for (int w = 1; w < KW; ++w) {
+          if (kw == w) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const int row = rw * 16 + g + 8 * r;
+              if (t == 0) {
+                mm[2 * row] = m[r];
+                mm[2 * row + 1] = l[r];
+              }
+#pragma unroll
+              for (int j = 0; j < DP / 8; ++j)
+                *reinterpret_cast<float2*>(meet + row * C::MEET + 8 * j + 2 * t) = make_float2(o[j][2 * r], o[j][2 * r + 1]);
+            }
+          }
+          __syncthreads();
+          if (kw == 0) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const int row = rw * 16 + g + 8 * r;
+              const float m2 = mm[2 * row], l2 = mm[2 * row + 1];
+              const float top = fmaxf(m[r], m2), ref = top == -INFINITY ? 0.f : top;
+              const float f1 = ex2((m[r] - ref) * a.scale_log2), f2 = ex2((m2 - ref) * a.scale_log2);
+              m[r] = top;
+              l[r] = l[r] * f1 + l2 * f2;
+#pragma unroll
+              for (int j = 0; j < DP / 8; ++j) {
+                const float2 x = *reinterpret_cast<const float2*>(meet + row * C::MEET + 8 * j + 2 * t);
+                o[j][2 * r] = o[j][2 * r] * f1 + x.x * f2;
+                o[j][2 * r + 1] = o[j][2 * r + 1] * f1 + x.y * f2;
+              }
+            }
+          }
+          __syncthreads();
+        }
+      }
+      const bool whole = begun && at.kt == at.nkt - 1;
+      if (kw == 0) {
+        // a part: the first of the run, or the one it ends with
+        const int slot = 2 * blockIdx.x + (u - at.kt > 0 && begun ? 1 : 0);
+        float* part = a.parts + static_cast<size_t>(slot) * C::PART;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int row = rw * 16 + g + 8 * r, x = at.rt * M + row;
+          if (whole) {
+            if (node[r] < 0) continue;
+            const int h = at.head * a.group + x - node[r] * a.group;
+            const long long orow = at.r.row0 + node[r];
+            const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
+            T* dst = static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * a.cache.dim;
+#pragma unroll
+            for (int j = 0; j < DP / 8; ++j)
+              if (8 * j < a.cache.dim)
+                *reinterpret_cast<uint32_t*>(dst + 8 * j + 2 * t) = pack2<T>(o[j][2 * r] * inv, o[j][2 * r + 1] * inv);
+            if (a.lse && t == 0)
+              a.lse[orow * a.heads + h] = (m[r] * a.scale_log2 + (log2f(l[r]) - SHIFT)) * 0.6931471805599453f;
+          } else {
+            if (t == 0) {
+              part[M * DP + 2 * row] = m[r];
+              part[M * DP + 2 * row + 1] = l[r];
+            }
+#pragma unroll
+            for (int j = 0; j < DP / 8; ++j)
+              *reinterpret_cast<float2*>(part + row * DP + 8 * j + 2 * t) = make_float2(o[j][2 * r], o[j][2 * r + 1]);
+          }
+        }
+      }
+      if (!whole && begun && tid == 0) {
+        // the tile's last unit, and the CTA whose run holds it
+        const unsigned long long last = lo + u - at.kt + at.nkt - 1;
+        const unsigned long long end = ((last + 1) * ctas - 1) / total;
+        a.joins[blockIdx.x] = make_int4(at.req, at.head, at.rt, 2 * static_cast<int>(end) + (u - at.kt > 0 ? 1 : 0));
+      }
+    }
+    at.next(a);
+  }
+}
+
+// Joins the parts of the tile of rows that CTA c's run of the attention kernel begins: block (c, y)
+// takes every gridDim.y-th of its rows, its warps the parts in turn.
+template <typename T, int DP, int RW>
+__global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a) {
+  constexpr int M = 16 * RW, PART = Cfg<DP, RW>::PART, WARPS = 8, VEC = (DP + 31) / 32;
+  __shared__ float ms[WARPS], ls[WARPS], os[WARPS][DP];
+  const int c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int4 join = a.joins[c];
+  if (join.x < 0) return;
+  const Request r = request(a, join.x);
+  const int rows = min(M, r.n * a.group - join.z * M), n = (join.w >> 1) - c + 1;
+  // the tile's parts: CTA c's second or first, then the first ones of the CTAs behind it
+  const float* parts = a.parts + static_cast<size_t>(2 * c) * PART;
+  const int second = join.w & 1;
+  for (int row = blockIdx.y; row < rows; row += gridDim.y) {
+    float m = -INFINITY, l = 0.f, o[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) o[v] = 0.f;
+    for (int i = warp; i < n; i += WARPS) {
+      const float* p = parts + static_cast<size_t>(2 * i + (i == 0 ? second : 0)) * PART;
+      const float m2 = p[M * DP + 2 * row], l2 = p[M * DP + 2 * row + 1];
+      const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+      const float f1 = ex2((m - ref) * a.scale_log2), f2 = ex2((m2 - ref) * a.scale_log2);
+      m = top;
+      l = l * f1 + l2 * f2;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v)
+        if (32 * v + lane < DP) o[v] = o[v] * f1 + p[row * DP + 32 * v + lane] * f2;
+    }
+    if (lane == 0) {
+      ms[warp] = m;
+      ls[warp] = l;
+    }
+#pragma unroll
+    for (int v = 0; v < VEC; ++v)
+      if (32 * v + lane < DP) os[warp][32 * v + lane] = o[v];
+    __syncthreads();
+    float top = ms[0];
+#pragma unroll
+    for (int w = 1; w < WARPS; ++w) top = fmaxf(top, ms[w]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float f[WARPS], sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      f[w] = ex2((ms[w] - ref) * a.scale_log2);
+      sum += ls[w] * f[w];
+    }
+    const int x = join.z * M + row, node = x / a.group, h = join.y * a.group + x - node * a.group;
+    const long long orow = r.row0 + node;
+    const int d = 2 * threadIdx.x;
+    if (d < a.cache.dim) {
+      float y0 = 0.f, y1 = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        y0 += os[w][d] * f[w];
+        y1 += os[w][d + 1] * f[w];
+      }
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * a.cache.dim + d) =
+          pack2<T>(y0 * inv, y1 * inv);
+    }
+    if (a.lse && threadIdx.x == 0)
+      a.lse[orow * a.heads + h] = (top * a.scale_log2 + (log2f(sum) - SHIFT)) * 0.6931471805599453f;
+    __syncthreads();  // the sums are read before the next row's
+  }
+}
+
+bool valid(const ivit_attention_config& c, const ivit_cache_layout& l) {
+  return valid_cache(l) && c.n_req >= 1 && c.n_req <= MAX_REQ && c.heads >= 1 && c.heads <= 256 && c.heads % l.kv_heads == 0 &&
+         c.max_pages >= 1 && static_cast<long long>(c.max_pages) * l.page_size < (1LL << 31) - (1 << 20) && c.max_new >= 1 &&
+         c.max_new <= 65536 && c.mask_mode >= IVIT_MASK_CAUSAL && c.mask_mode <= IVIT_MASK_TREE && c.mask_words >= 0 &&
+         c.mask_words <= 32768 && (c.mask_mode != IVIT_MASK_TREE || c.mask_words > 0) && c.scale > 0.f && c.scale < 1e30f;
+}
+
+// Calls f with the type, the padded head width and the row groups of a tile as types: 16 rows while they hold
+// the most rows that share a key head, then 32, else 64.
+template <typename F>
+auto dispatch(const ivit_attention_config& c, const ivit_cache_layout& l, F f) {
+  const int rows = static_cast<int>(std::min<long long>(64, static_cast<long long>(c.max_new) * (c.heads / l.kv_heads)));
+  const auto groups = [&](auto type, auto dp) {
+    return rows <= 16   ? f(type, dp, std::integral_constant<int, 1>{})
+           : rows <= 32 ? f(type, dp, std::integral_constant<int, 2>{})
+                        : f(type, dp, std::integral_constant<int, 4>{});
+  };
+  const auto width = [&](auto type) {
+    return l.head_dim <= 64    ? groups(type, std::integral_constant<int, 64>{})
+           : l.head_dim <= 80  ? groups(type, std::integral_constant<int, 80>{})
+           : l.head_dim <= 128 ? groups(type, std::integral_constant<int, 128>{})
+                               : groups(type, std::integral_constant<int, 256>{});
+  };
+  return l.dtype == IVIT_BF16 ? width(bf16{}) : width(half{});
+}
+
+}  // namespace
+}  // namespace ivit
+
+extern "C" size_t ivit_tree_attention_workspace(const ivit_attention_config* cfg, const ivit_cache_layout* cache) {
+  using namespace ivit;
+  if (!cfg || !cache || !valid(*cfg, *cache)) return 0;
+  return dispatch(*cfg, *cache, [](auto, auto dp, auto rw) -> size_t {
+    return MAX_CTAS * (sizeof(int4) + 2 * sizeof(float) * Cfg<dp(), rw()>::PART);
+  });
+}
+
+extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_cache_layout* cache, int32_t n_rows,
+                                   const void* q_dev, int64_t q_stride, const void* k_new_dev, int64_t k_new_stride,
+                                   const void* v_new_dev, int64_t v_new_stride, const void* k_cache_dev,
+                                   const void* v_cache_dev, const int32_t* table_dev, const int32_t* len_dev,
+                                   const int32_t* cu_rows_dev, const uint32_t* mask_dev, void* out_dev, int64_t out_stride,
+                                   float* lse_dev, void* workspace_dev, void* stream) {
+  using namespace ivit;
+  if (!cfg || !cache || n_rows < 0)
+    return fail(IVIT_ERR_ARG, "ivit_tree_attention: null configuration or a negative row count");
+  if (!valid(*cfg, *cache))
+    return fail(IVIT_ERR_SHAPE,
+                "ivit_tree_attention: need 1..4096 requests, heads up to 256 and a multiple of the cache's, head_dim a "
+                "multiple of 8 up to 256, max_new 1..65536, a mask mode (trees with 1..32768 mask words), scale > 0 and a "
+                "supported cache layout");
+  if (n_rows == 0) return IVIT_OK;
+  if (!q_dev || !k_new_dev || !v_new_dev || !k_cache_dev || !v_cache_dev || !table_dev || !len_dev || !cu_rows_dev ||
+      !out_dev || !workspace_dev || (cfg->mask_mode == IVIT_MASK_TREE && !mask_dev))
+    return fail(IVIT_ERR_ARG, "ivit_tree_attention: null pointer");
+  if ((q_stride | k_new_stride | v_new_stride | out_stride) & 7 || q_stride < 0 || k_new_stride < 0 || v_new_stride < 0 ||
+      out_stride < 0)
+    return fail(IVIT_ERR_ARG, "ivit_tree_attention: row strides must be multiples of 8 elements");
+  if (!all_aligned({q_dev, k_new_dev, v_new_dev, k_cache_dev, v_cache_dev, out_dev, workspace_dev}, 16) ||
+      !all_aligned({table_dev, len_dev, cu_rows_dev, mask_dev, lse_dev}, 4))
+    return fail(IVIT_ERR_ARG, "ivit_tree_attention: arrays must be 16-byte aligned (table, lengths, offsets, mask and lse 4)");
+  const int sms = sm_count();
+  if (sms <= 0) return fail(IVIT_ERR_CUDA, "ivit_tree_attention: no CUDA device");
+  TreeArgs a = {};
+  a.q = q_dev;
+  a.k_new = k_new_dev;
+  a.v_new = v_new_dev;
+  a.k_cache = k_cache_dev;
+  a.v_cache = v_cache_dev;
+  a.table = table_dev;
+  a.len = len_dev;
+  a.cu = cu_rows_dev;
+  a.mask = mask_dev;
+  a.out = out_dev;
+  a.lse = lse_dev;
+  a.joins = static_cast<int4*>(workspace_dev);
+  a.parts = reinterpret_cast<float*>(a.joins + MAX_CTAS);
+  a.q_stride = q_stride;
+  a.k_new_stride = k_new_stride;
+  a.v_new_stride = v_new_stride;
+  a.out_stride = out_stride;
+  a.cache = paged(*cache);
+  a.n_req = cfg->n_req;
+  a.n_rows = n_rows;
+  a.heads = cfg->heads;
+  a.group = cfg->heads / cache->kv_heads;
+  a.max_pages = cfg->max_pages;
+  a.max_new = cfg->max_new;
+  a.mask_mode = cfg->mask_mode;
+  a.mask_words = cfg->mask_words;
+  a.scale_log2 = cfg->scale * 1.4426950408889634f;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = dispatch(*cfg, *cache, [&](auto type, auto dp, auto rw) {
+    using T = decltype(type);
+    using C = Cfg<dp(), rw()>;
+    const auto kernel = tree_attention_kernel<T, dp(), rw()>;
+    cudaError_t err = allow_smem<tree_attention_kernel<T, dp(), rw()>>(C::BYTES);
+    if (err != cudaSuccess) return err;
+    const int ctas = std::min(MAX_CTAS, C::CTAS * sms);
+    err = launch_ex(kernel, dim3(ctas), dim3(THREADS), C::BYTES, s, 1, a);
+    if (err != cudaSuccess) return err;
+    return launch_ex(tree_join_kernel<T, dp(), rw()>, dim3(ctas, 4), dim3(256), 0, s, 1, a);
+  });
+  return e == cudaSuccess ? IVIT_OK : fail_cuda(e);
+}
