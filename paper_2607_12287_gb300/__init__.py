@@ -34,6 +34,8 @@ EXPORTED = [
     "ivit_tree_attention_workspace", "ivit_tree_attention", "ivit_kv_write",
 ]
 IVIT_NOALLOC_MAX_TOKENS = 65536
+IVIT_BF16 = 0
+IVIT_FP16 = 1
 
 
 class IvitConfig(C.Structure):
@@ -146,6 +148,7 @@ def _tensor_type():
         import torch
         for name in ("uint8", "int32", "float32", "bfloat16", "float16"):
             _dtypes[name] = getattr(torch, name)
+        _dtypes[IVIT_BF16], _dtypes[IVIT_FP16] = torch.bfloat16, torch.float16  # (by the library's codes, too)
         t = _dtypes["tensor"] = torch.Tensor
     return t
 
@@ -323,8 +326,6 @@ def ivit_action_combine(x0, v0, v7, alpha, beta, b, xT, stream=None) -> None:
 
 # ------------------------------------------------------- language backbone
 
-IVIT_BF16 = 0
-IVIT_FP16 = 1
 IVIT_MASK_CAUSAL = 0
 IVIT_MASK_ALL = 1
 IVIT_MASK_TREE = 2
@@ -370,21 +371,36 @@ def make_attention_config(n_req: int, heads: int, max_pages: int, max_new: int, 
     return IvitAttentionConfig(n_req, heads, max_pages, max_new, _MASKS.get(mask, mask), mask_words, scale)
 
 
-def _rows(t, name: str, dtype: int, n_rows: int, heads: int, dim: int) -> int:
-    """The row stride of a tensor [rows, heads, dim] whose heads are contiguous in a row; rejects one that
-    the kernels would misread, as ``_require`` does."""
+def _arg(t, name: str, dtype_name: str, numel: int) -> Optional[int]:
+    """``_require``, and the pointer."""
+    if (type(t) is _dtypes.get("tensor") and t.is_cuda and t.dtype is _dtypes[dtype_name] and t.is_contiguous()
+            and t.numel() >= numel):
+        return t.data_ptr()
+    _require(t, name, dtype_name, numel)
+    return _ptr(t)
+
+
+def _typed(t, name: str, dtype: int) -> None:
+    """Rejects what is not a device tensor of the type ``dtype`` (IVIT_BF16 or IVIT_FP16)."""
+    if type(t) is _dtypes.get("tensor") and t.is_cuda and t.dtype is _dtypes[dtype]:
+        return
     if isinstance(t, (int, np.ndarray)) or t is None:
         raise TypeError(f"{name}: a CUDA tensor is required")
     if t.device.type != "cuda":
         raise ValueError(f"{name}: tensor on {t.device}; a CUDA tensor is required")
     _tensor_type()
-    if t.dtype is not _dtypes[_DTYPE_NAMES[dtype]]:
+    if t.dtype is not _dtypes[dtype]:
         raise TypeError(f"{name}: dtype {t.dtype}, expected torch.{_DTYPE_NAMES[dtype]}")
-    sh = t.shape
+
+
+def _rows(t, name: str, dtype: int, n_rows: int, heads: int, dim: int) -> int:
+    """The row stride of a tensor [rows, heads, dim] whose heads are contiguous in a row; rejects one that
+    the kernels would misread, as ``_require`` does."""
+    _typed(t, name, dtype)
+    sh, st = t.shape, t.stride()
     if len(sh) != 3 or sh[0] < n_rows or sh[1] != heads or sh[2] != dim:
         raise ValueError(f"{name}: shape {tuple(sh)}, expected [{n_rows}, {heads}, {dim}]")
-    st = t.stride()
-    if st[2] != 1 or (heads > 1 and st[1] != dim):
+    if st[2] != 1 or (st[1] != dim and heads > 1):
         raise ValueError(f"{name}: the heads of a row are not contiguous")
     return st[0] if sh[0] > 1 else heads * dim
 
@@ -395,19 +411,21 @@ def _row_count(t, name: str) -> int:
     return t.shape[0]
 
 
-def _cache(t, name: str, layout: IvitCacheLayout, layered: bool = False) -> None:
-    """Rejects a tensor that is not a cache of this layout (with a leading layer dimension if ``layered``)."""
+def _cache(t, name: str, layout: IvitCacheLayout) -> int:
+    """The pointer of a cache of this layout; rejects any other tensor."""
+    _typed(t, name, layout.dtype)
+    if t.shape != layout.shape or t.stride() != layout.strides:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} and strides {t.stride()} are not the layout's, {layout.shape} and "
+                         f"{layout.strides}")
+    return t.data_ptr()
+
+
+def _layers(t, name: str, dtype: int) -> tuple:
+    """Shape and strides of a tensor with a leading layer dimension."""
     if t is None or isinstance(t, (int, np.ndarray)):
         raise TypeError(f"{name}: a CUDA tensor is required")
-    if t.device.type != "cuda":
-        raise ValueError(f"{name}: tensor on {t.device}; a CUDA tensor is required")
-    _tensor_type()
-    if t.dtype is not _dtypes[_DTYPE_NAMES[layout.dtype]]:
-        raise TypeError(f"{name}: dtype {t.dtype}, expected torch.{_DTYPE_NAMES[layout.dtype]}")
-    sh, st = (t.shape[1:], t.stride()[1:]) if layered else (t.shape, t.stride())
-    if tuple(sh) != layout.shape or tuple(st) != layout.strides:
-        raise ValueError(f"{name}: shape {tuple(sh)} and strides {tuple(st)} are not the layout's, {layout.shape} and "
-                         f"{layout.strides}")
+    _typed(t, name, dtype)
+    return t.shape, t.stride()
 
 
 def ivit_step_plan(cfg: IvitPlanConfig, held, base, new, parent, ring, ring_in, table, cu_rows, req, slots, positions,
@@ -416,40 +434,30 @@ def ivit_step_plan(cfg: IvitPlanConfig, held, base, new, parent, ring, ring_in, 
     None): ``table`` [n_req, max_pages] and ``ring`` [n_pages] are updated, ``cu_rows`` [n_req + 1], the row arrays
     [max_rows], ``mask`` [max_rows, mask_words], ``ring_out`` [2] and ``status`` [1] written."""
     n, rows = cfg.n_req, cfg.max_rows
-    _require(held, "held", "int32", n)
-    _require(base, "base", "int32", n)
-    _require(new, "new", "int32", n)
-    _require(parent, "parent", "int32", rows)
-    _require(ring, "ring", "int32", cfg.n_pages)
-    _require(ring_in, "ring_in", "int32", 2)
-    _require(table, "table", "int32", n * cfg.max_pages)
-    _require(cu_rows, "cu_rows", "int32", n + 1)
-    _require(req, "req", "int32", rows)
-    _require(slots, "slots", "int32", rows)
-    _require(positions, "positions", "int32", rows)
-    _require(mask, "mask", "int32", rows * cfg.mask_words)
-    _require(ring_out, "ring_out", "int32", 2)
-    _require(status, "status", "int32", 1)
-    _check(load().ivit_step_plan(C.addressof(cfg), _ptr(held), _ptr(base), _ptr(new), _ptr(parent), _ptr(ring), _ptr(ring_in),
-                                 _ptr(table), _ptr(cu_rows), _ptr(req), _ptr(slots), _ptr(positions), _ptr(mask),
-                                 _ptr(ring_out), _ptr(status), _stream(stream)), None)
+    args = (C.addressof(cfg), _arg(held, "held", "int32", n), _arg(base, "base", "int32", n), _arg(new, "new",
+            "int32", n), _arg(parent, "parent", "int32", rows), _arg(ring, "ring", "int32", cfg.n_pages), _arg(ring_in,
+            "ring_in", "int32", 2), _arg(table, "table", "int32", n * cfg.max_pages), _arg(cu_rows, "cu_rows", "int32", n +
+            1), _arg(req, "req", "int32", rows), _arg(slots, "slots", "int32", rows), _arg(positions, "positions", "int32",
+            rows), _arg(mask, "mask", "int32", rows * cfg.mask_words), _arg(ring_out, "ring_out", "int32", 2), _arg(status,
+            "status", "int32", 1), _stream(stream))
+    _check(load().ivit_step_plan(*args), None)
 
 
-def _rope_inputs(cfg: IvitRopeConfig, n: int, q_weight, k_weight, positions, freq, axis) -> int:
-    """Checks what the rotation and its gradient have in common; the stride of the position axes."""
-    _require(q_weight, "q_weight", _DTYPE_NAMES[cfg.dtype], cfg.head_dim)
-    _require(k_weight, "k_weight", _DTYPE_NAMES[cfg.dtype], cfg.head_dim)
-    _require(freq, "freq", "float32", cfg.rot_dim // 2)
-    _require(axis, "axis", "int32", cfg.rot_dim // 2)
-    if positions is None or isinstance(positions, (int, np.ndarray)) or len(positions.shape) > 2:
+def _rope_inputs(cfg: IvitRopeConfig, n: int, q_weight, k_weight, positions, freq, axis) -> tuple:
+    """What the rotation and its gradient have in common, as the library takes it."""
+    pairs, dt, dim = cfg.rot_dim // 2, _DTYPE_NAMES[cfg.dtype], cfg.head_dim
+    if positions is None or isinstance(positions, (int, np.ndarray)):
         raise TypeError("positions: a CUDA tensor [rows] or [axes, rows] is required")
-    if len(positions.shape) == 1 or positions.shape[0] == 1:  # one position for all axes
-        _require(positions, "positions", "int32", n)
-        return 0
-    if positions.shape[0] < cfg.n_axes or positions.shape[1] < n:
-        raise ValueError(f"positions: shape {tuple(positions.shape)}, expected [{cfg.n_axes}, {n}]")
-    _require(positions, "positions", "int32", cfg.n_axes * n)
-    return positions.shape[1]
+    sh = positions.shape
+    if len(sh) == 1 or (len(sh) == 2 and sh[0] == 1):  # one position for all axes
+        stride, least = 0, n
+    elif len(sh) == 2 and sh[0] >= cfg.n_axes and sh[1] >= n:
+        stride, least = sh[1], sh[0] * sh[1]
+    else:
+        raise ValueError(f"positions: shape {tuple(sh)}, expected [{cfg.n_axes}, {n}]")
+    return (_arg(q_weight, "q_weight", dt, dim), _arg(k_weight, "k_weight", dt, dim),
+            _arg(positions, "positions", "int32", least), stride, _arg(freq, "freq", "float32", pairs),
+            _arg(axis, "axis", "int32", pairs))
 
 
 def ivit_qk_norm_rope(cfg: IvitRopeConfig, q, k, v, q_weight, k_weight, positions, freq, axis, q_out, k_out=None,
@@ -463,18 +471,17 @@ def ivit_qk_norm_rope(cfg: IvitRopeConfig, q, k, v, q_weight, k_weight, position
     qs = _rows(q, "q", dt, n, heads, dim)
     ks = _rows(k, "k", dt, n, kv, dim)
     qos = _rows(q_out, "q_out", dt, n, heads, dim)
-    kos = 0 if k_out is None else _rows(k_out, "k_out", dt, n, kv, dim)
-    vs, lay = 0, None
+    kos, ko = (0, None) if k_out is None else (_rows(k_out, "k_out", dt, n, kv, dim), k_out.data_ptr())
+    vs = lay = vp = kc = vc = sl = None
     if cache is not None:
-        vs = _rows(v, "v", dt, n, kv, dim)
-        _cache(k_cache, "k_cache", cache)
-        _cache(v_cache, "v_cache", cache)
-        _require(slots, "slots", "int32", n)
-        lay = C.addressof(cache)
-    ps = _rope_inputs(cfg, n, q_weight, k_weight, positions, freq, axis)
-    _check(load().ivit_qk_norm_rope(C.addressof(cfg), n, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(q_weight), _ptr(k_weight),
-                                    _ptr(positions), ps, _ptr(freq), _ptr(axis), _ptr(q_out), qos, _ptr(k_out), kos, lay,
-                                    _ptr(k_cache), _ptr(v_cache), _ptr(slots), _stream(stream)), None)
+        vs, vp = _rows(v, "v", dt, n, kv, dim), v.data_ptr()
+        kc, vc = _cache(k_cache, "k_cache", cache), _cache(v_cache, "v_cache", cache)
+        lay, sl = C.addressof(cache), _arg(slots, "slots", "int32", n)
+    elif not (v is k_cache is v_cache is slots is None):
+        raise ValueError("v, k_cache, v_cache and slots need the cache's layout")
+    args = (C.addressof(cfg), n, q.data_ptr(), qs, k.data_ptr(), ks, vp, vs or 0, *_rope_inputs(cfg, n, q_weight,
+            k_weight, positions, freq, axis), q_out.data_ptr(), qos, ko, kos, lay, kc, vc, sl, _stream(stream))
+    _check(load().ivit_qk_norm_rope(*args), None)
 
 
 def ivit_qk_norm_rope_backward_workspace(cfg: IvitRopeConfig) -> int:
@@ -493,15 +500,14 @@ def ivit_qk_norm_rope_backward(cfg: IvitRopeConfig, grad_q, grad_k, q, k, q_weig
     qs = _rows(q, "q", dt, n, heads, dim)
     ks = _rows(k, "k", dt, n, kv, dim)
     dqs, dks = _rows(dq, "dq", dt, n, heads, dim), _rows(dk, "dk", dt, n, kv, dim)
-    _require(dq_weight, "dq_weight", "float32", dim)
-    _require(dk_weight, "dk_weight", "float32", dim)
-    ps = _rope_inputs(cfg, n, q_weight, k_weight, positions, freq, axis)
-    if dq_weight is not None or dk_weight is not None:
-        _require(workspace, "workspace", "uint8", ivit_qk_norm_rope_backward_workspace(cfg))
-    _check(load().ivit_qk_norm_rope_backward(C.addressof(cfg), n, _ptr(grad_q), gqs, _ptr(grad_k), gks, _ptr(q), qs, _ptr(k), ks,
-                                             _ptr(q_weight), _ptr(k_weight), _ptr(positions), ps, _ptr(freq), _ptr(axis),
-                                             _ptr(dq), dqs, _ptr(dk), dks, _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace),
-                                             _stream(stream)), None)
+    dqw, dkw = _arg(dq_weight, "dq_weight", "float32", dim), _arg(dk_weight, "dk_weight", "float32", dim)
+    ws = None
+    if dqw or dkw:
+        ws = _arg(workspace, "workspace", "uint8", ivit_qk_norm_rope_backward_workspace(cfg))
+    args = (C.addressof(cfg), n, grad_q.data_ptr(), gqs, grad_k.data_ptr(), gks, q.data_ptr(), qs, k.data_ptr(), ks,
+            *_rope_inputs(cfg, n, q_weight, k_weight, positions, freq, axis), dq.data_ptr(), dqs, dk.data_ptr(), dks, dqw,
+            dkw, ws, _stream(stream))
+    _check(load().ivit_qk_norm_rope_backward(*args), None)
 
 
 def ivit_tree_attention_workspace(cfg: IvitAttentionConfig, cache: IvitCacheLayout) -> int:
@@ -519,45 +525,36 @@ def ivit_tree_attention(cfg: IvitAttentionConfig, cache: IvitCacheLayout, q, k_n
     ks = _rows(k_new, "k_new", dt, n, kv, dim)
     vs = _rows(v_new, "v_new", dt, n, kv, dim)
     os_ = _rows(out, "out", dt, n, heads, dim)
-    _cache(k_cache, "k_cache", cache)
-    _cache(v_cache, "v_cache", cache)
-    _require(table, "table", "int32", cfg.n_req * cfg.max_pages)
-    _require(lengths, "lengths", "int32", cfg.n_req)
-    _require(cu_rows, "cu_rows", "int32", cfg.n_req + 1)
-    if cfg.mask_mode == IVIT_MASK_TREE:
-        _require(mask, "mask", "int32", n * cfg.mask_words)
-    _require(lse, "lse", "float32", n * heads)
-    _require(workspace, "workspace", "uint8", ivit_tree_attention_workspace(cfg, cache))
-    _check(load().ivit_tree_attention(C.addressof(cfg), C.addressof(cache), n, _ptr(q), qs, _ptr(k_new), ks, _ptr(v_new), vs,
-                                      _ptr(k_cache), _ptr(v_cache), _ptr(table), _ptr(lengths), _ptr(cu_rows), _ptr(mask),
-                                      _ptr(out), os_, _ptr(lse), _ptr(workspace), _stream(stream)), None)
+    kc, vc, req = _cache(k_cache, "k_cache", cache), _cache(v_cache, "v_cache", cache), cfg.n_req
+    if cfg.mask_mode != IVIT_MASK_TREE:
+        mask = None
+    args = (C.addressof(cfg), C.addressof(cache), n, q.data_ptr(), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs,
+            kc, vc, _arg(table, "table", "int32", req * cfg.max_pages), _arg(lengths, "lengths", "int32", req),
+            _arg(cu_rows, "cu_rows", "int32", req + 1), _arg(mask, "mask", "int32", n * cfg.mask_words), out.data_ptr(),
+            os_, _arg(lse, "lse", "float32", n * heads), _arg(workspace, "workspace", "uint8",
+            ivit_tree_attention_workspace(cfg, cache)), _stream(stream))
+    _check(load().ivit_tree_attention(*args), None)
 
 
 def ivit_kv_write(cache: IvitCacheLayout, k, v, rows, slots, k_cache, v_cache, stream=None) -> None:
     """Rows ``rows`` (int32, -1: none) of k and v [layers, rows, kv_heads, head_dim] into the ``slots`` of the caches
     [layers, pages, page_size, kv_heads, head_dim] of all layers."""
-    for t, name in ((k, "k"), (v, "v")):
-        if t is None or isinstance(t, (int, np.ndarray)) or len(t.shape) != 4:
-            raise ValueError(f"{name}: a CUDA tensor [layers, rows, kv_heads, head_dim] is required")
-    layers, n_src = k.shape[0], k.shape[1]
-    strides = []
-    for t, name in ((k, "k"), (v, "v")):
-        if t.shape[0] != layers or t.shape[1] != n_src:
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [{layers}, {n_src}, ...]")
-        row = _rows(t[0] if layers else t.flatten(0, 1), name, cache.dtype, n_src, cache.kv_heads, cache.head_dim)
-        strides.append((row, t.stride()[0] if layers > 1 else 0))
-    if strides[0] != strides[1]:
-        raise ValueError("v: strides other than k's")
-    _cache(k_cache, "k_cache", cache, layered=True)
-    _cache(v_cache, "v_cache", cache, layered=True)
-    if k_cache.shape[0] < layers or v_cache.shape[0] < layers or k_cache.stride()[0] != v_cache.stride()[0]:
-        raise ValueError("k_cache, v_cache: fewer layers than k and v, or of different strides")
+    dt, kv, dim = cache.dtype, cache.kv_heads, cache.head_dim
+    (sh, st), (vsh, vst) = _layers(k, "k", dt), _layers(v, "v", dt)
+    if len(sh) != 4 or sh[2] != kv or sh[3] != dim or sh != vsh:
+        raise ValueError(f"k, v: shapes {tuple(sh)} and {tuple(vsh)}, expected [layers, rows, {kv}, {dim}]")
+    if st[3] != 1 or (st[2] != dim and kv > 1) or st != vst:
+        raise ValueError("k, v: the heads of a row are not contiguous, or the strides differ")
+    (csh, cst), (vcsh, vcst) = _layers(k_cache, "k_cache", dt), _layers(v_cache, "v_cache", dt)
+    layers, n_src = sh[0], sh[1]
+    if csh[1:] != cache.shape or cst[1:] != cache.strides or vcsh != csh or vcst != cst or csh[0] < layers:
+        raise ValueError(f"k_cache, v_cache: shapes {tuple(csh)} and {tuple(vcsh)} are not {layers} caches of the layout, "
+                         f"{cache.shape}, with strides {cache.strides}")
     n = rows.numel() if hasattr(rows, "numel") else 0
-    _require(rows, "rows", "int32", n)
-    _require(slots, "slots", "int32", n)
-    _check(load().ivit_kv_write(C.addressof(cache), layers, n, n_src, _ptr(k), _ptr(v), strides[0][0], strides[0][1],
-                                _ptr(rows), _ptr(slots), _ptr(k_cache), _ptr(v_cache), k_cache.stride()[0],
-                                _stream(stream)), None)
+    args = (C.addressof(cache), layers, n, n_src, k.data_ptr(), v.data_ptr(), st[1] if n_src > 1 else kv * dim,
+            st[0] if layers > 1 else 0, _arg(rows, "rows", "int32", n), _arg(slots, "slots", "int32", n),
+            k_cache.data_ptr(), v_cache.data_ptr(), cst[0] if layers > 1 else 0, _stream(stream))
+    _check(load().ivit_kv_write(*args), None)
 
 
 # ------------------------------------------------------------ convenience

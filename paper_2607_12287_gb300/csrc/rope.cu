@@ -12,6 +12,8 @@
 // memory a table would add.
 //
 // Bound: HBM for many rows, the launch and two dependent round trips for a few.
+#include <type_traits>
+
 #include "backbone.cuh"
 
 namespace ivit {
@@ -34,12 +36,13 @@ struct RopeArgs {
 };
 
 // Cosine and sine of p * f.  The product is carried in two fp32 terms and reduced by multiples of
-// 2 pi, itself in two terms (Cody and Waite), so that large positions keep their angle.
+// 2 pi, itself in two terms (Cody and Waite), so that large positions keep their angle; the fast
+// functions are then within 2^-21 of the true values.
 __device__ __forceinline__ void turn(int p, float f, float& c, float& s) {
   const float x = static_cast<float>(p), hi = x * f, lo = fmaf(x, f, -hi);
   const float n = rintf(hi * 0.15915494309189535f);
   const float r = fmaf(n, 1.7484555e-7f, fmaf(n, -6.2831854820251465f, hi)) + lo;
-  sincospif(r * 0.3183098861837907f, &s, &c);
+  __sincosf(r, &s, &c);
 }
 
 // Where a lane's values are: pieces of 4 at a and b; pairs (a[i], b[i]), or (a[0], a[1]) and so on when
@@ -105,25 +108,16 @@ __device__ __forceinline__ void angles(const RopeArgs& p, const Lane& ln, int ro
     turn(ax[i] == 1 ? at[1] : ax[i] == 2 ? at[2] : ax[i] == 3 ? at[3] : at[0], f[i], c[i], s[i]);
 }
 
-// Rotation of a lane's pairs by sign * angle.
-__device__ __forceinline__ void rotate(float (&a)[4], float (&b)[4], const float (&c)[4], const float (&s)[4], float sign,
-                                       bool interleaved) {
-  if (!interleaved) {
+// Rotation of a lane's pairs.
+template <bool INTERLEAVED>
+__device__ __forceinline__ void rotate(float (&a)[4], float (&b)[4], const float (&c)[4], const float (&s)[4]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float u = a[i], v = b[i], t = sign * s[i];
-      a[i] = u * c[i] - v * t;
-      b[i] = v * c[i] + u * t;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float& x = i < 2 ? a[2 * i] : b[2 * i - 4];
-      float& y = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
-      const float u = x, v = y, t = sign * s[i];
-      x = u * c[i] - v * t;
-      y = v * c[i] + u * t;
-    }
+  for (int i = 0; i < 4; ++i) {
+    float& x = !INTERLEAVED ? a[i] : i < 2 ? a[2 * i] : b[2 * i - 4];
+    float& y = !INTERLEAVED ? b[i] : i < 2 ? a[2 * i + 1] : b[2 * i - 3];
+    const float u = x, v = y;
+    x = u * c[i] - v * s[i];
+    y = v * c[i] + u * s[i];
   }
 }
 
@@ -146,35 +140,41 @@ __device__ __forceinline__ void load_weight(const void* w, const Lane& ln, float
   }
 }
 
-constexpr int STEPS = 4;  // steps of a warp whose loads are in flight together
+// Forward: a step of a warp is up to 32 / (D / 8) heads of one kind; the warps of a row take its steps
+// (queries, then keys, then values) in turn, STEPS at a time with their loads in flight together.
+constexpr int STEPS = 4;
 
-template <typename T>
-__global__ void __launch_bounds__(THREADS) qk_norm_rope_kernel(const RopeArgs p) {
+// NORM: there is a weight.
+template <typename T, bool NORM, bool INTERLEAVED>
+__global__ void __launch_bounds__(THREADS, 3) qk_norm_rope_kernel(const RopeArgs p) {
   const int warp = threadIdx.x >> 5;
   const Lane ln(p, threadIdx.x & 31);
   pdl_wait();
   pdl_launch_dependents();
   const int index = blockIdx.x * WARPS + warp, row = index / p.row_warps, part = index - row * p.row_warps;
   if (row >= p.n_rows) return;
-  // the row's heads in order: queries, keys, values
-  const T* q = static_cast<const T*>(p.q) + row * p.q_stride;
-  const T* k = static_cast<const T*>(p.k) + row * p.k_stride;
-  const T* v = static_cast<const T*>(p.v) + row * p.v_stride;
-  const int keys = p.heads + p.kv_heads, all = p.v ? keys + p.kv_heads : keys, step = p.row_warps * ln.heads;
+  const int q_steps = (p.heads + ln.heads - 1) / ln.heads, k_steps = (p.kv_heads + ln.heads - 1) / ln.heads;
+  const int steps = q_steps + (p.v ? 2 * k_steps : k_steps);
+  const int my = ln.group * p.dim;
+  const T* q = static_cast<const T*>(p.q) + row * p.q_stride + my;
+  const T* k = static_cast<const T*>(p.k) + row * p.k_stride + my;
+  const T* v = static_cast<const T*>(p.v) + row * p.v_stride + my;
   const int slot = p.slot ? p.slot[row] : -1;
   const bool cached = p.slot && p.cache.holds(slot);
-  const long long token = cached ? p.cache.token(slot) : 0;
   float c[4], s[4], qa[4], qb[4], ka[4], kb[4];
   bool first = true;
 
-  for (int base = part * ln.heads; base < all; base += STEPS * step) {
+  for (int base = part; base < steps; base += STEPS * p.row_warps) {
     uint2 ra[STEPS], rb[STEPS];
 #pragma unroll
     for (int u = 0; u < STEPS; ++u) {
-      const int x = base + u * step + ln.group;
+      const int st = base + u * p.row_warps;
+      if (st >= steps) break;  // (the same for the whole warp, as the kind of a step)
+      const bool query = st < q_steps, key = st < q_steps + k_steps;
+      const int h0 = (query ? st : key ? st - q_steps : st - q_steps - k_steps) * ln.heads;
+      const T* src = (query ? q : key ? k : v) + h0 * p.dim;
       ra[u] = rb[u] = make_uint2(0, 0);
-      if (ln.active && x < all) {
-        const T* src = x < p.heads ? q + x * p.dim : x < keys ? k + (x - p.heads) * p.dim : v + (x - keys) * p.dim;
+      if (ln.active && h0 + ln.group < (query ? p.heads : p.kv_heads)) {
         ra[u] = load4(src + ln.a);
         rb[u] = load4(src + ln.b);
       }
@@ -182,45 +182,45 @@ __global__ void __launch_bounds__(THREADS) qk_norm_rope_kernel(const RopeArgs p)
     if (first) {  // (behind the first loads)
       first = false;
       angles(p, ln, row, c, s);
-      load_weight<T>(p.q_weight, ln, qa, qb);
-      load_weight<T>(p.k_weight, ln, ka, kb);
+      if (NORM) {
+        load_weight<T>(p.q_weight, ln, qa, qb);
+        load_weight<T>(p.k_weight, ln, ka, kb);
+      }
     }
 #pragma unroll
     for (int u = 0; u < STEPS; ++u) {
-      if (base + u * step >= all) break;  // (the same for the whole warp)
-      const int x = base + u * step + ln.group;
-      const bool key = x >= p.heads;
-      float a[4], b[4];
-      unpack4<T>(ra[u], a);
-      unpack4<T>(rb[u], b);
-      if (p.q_weight || p.k_weight) {
-        float ss = 0.f;
+      const int st = base + u * p.row_warps;
+      if (st >= steps) break;
+      const bool query = st < q_steps, key = st < q_steps + k_steps;
+      const int h0 = (query ? st : key ? st - q_steps : st - q_steps - k_steps) * ln.heads;
+      if (key) {
+        float a[4], b[4];
+        unpack4<T>(ra[u], a);
+        unpack4<T>(rb[u], b);
+        if (NORM && (query ? p.q_weight : p.k_weight)) {
+          float ss = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
-        ss = ln.sum(ss);
-        if (key ? p.k_weight != nullptr : p.q_weight != nullptr) {
-          const float r = rsqrtf(ss / p.dim + p.eps);
+          for (int i = 0; i < 4; ++i) ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
+          const float r = rsqrtf(ln.sum(ss) / p.dim + p.eps);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            a[i] = a[i] * r * (key ? ka[i] : qa[i]);
-            b[i] = b[i] * r * (key ? kb[i] : qb[i]);
+            a[i] = a[i] * r * (query ? qa[i] : ka[i]);
+            b[i] = b[i] * r * (query ? qb[i] : kb[i]);
           }
         }
-      }
-      if (ln.rotated) rotate(a, b, c, s, 1.f, p.interleaved);
-      if (!ln.active || x >= all) continue;
-      if (x < keys) {
+        rotate<INTERLEAVED>(a, b, c, s);  // (by nothing where the lane's values are not rotated)
         ra[u] = pack4<T>(a);
         rb[u] = pack4<T>(b);
       }
-      const int h = x < p.heads ? x : x < keys ? x - p.heads : x - keys;
-      if (!key || (x < keys && p.k_out)) {
-        T* dst = key ? static_cast<T*>(p.k_out) + row * p.k_out_stride : static_cast<T*>(p.q_out) + row * p.q_out_stride;
-        store4(dst + h * p.dim + ln.a, ra[u]);
-        store4(dst + h * p.dim + ln.b, rb[u]);
+      if (!ln.active || h0 + ln.group >= (query ? p.heads : p.kv_heads)) continue;
+      const int to = h0 * p.dim + my;
+      if (query || (key && p.k_out)) {
+        T* dst = (query ? static_cast<T*>(p.q_out) + row * p.q_out_stride : static_cast<T*>(p.k_out) + row * p.k_out_stride) + to;
+        store4(dst + ln.a, ra[u]);
+        store4(dst + ln.b, rb[u]);
       }
-      if (key && cached) {
-        T* dst = static_cast<T*>(x < keys ? p.k_cache : p.v_cache) + token + h * p.cache.head_stride;
+      if (!query && cached) {
+        T* dst = static_cast<T*>(key ? p.k_cache : p.v_cache) + p.cache.token(slot) + (h0 + ln.group) * p.cache.head_stride;
         store4(dst + ln.a, ra[u]);
         store4(dst + ln.b, rb[u]);
       }
@@ -228,9 +228,69 @@ __global__ void __launch_bounds__(THREADS) qk_norm_rope_kernel(const RopeArgs p)
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(THREADS) qk_norm_rope_backward_kernel(const RopeArgs p) {
-  extern __shared__ float sm[];  // [THREADS][16] weight gradients of the lanes
+constexpr int BWD_STEPS = 2;
+
+// Gradients of the steps of one kind of a row; its heads at x, g and dx (lane's head included).
+template <typename T, bool NORM, bool INTERLEAVED>
+__device__ __forceinline__ void backward_steps(const RopeArgs& p, const Lane& ln, const T* x, const T* g, T* dx, int part, int heads,
+                                               const float (&c)[4], const float (&s)[4], const float (&wa)[4], const float (&wb)[4],
+                                               float per, float (&dw)[8]) {
+  const int step = p.row_warps * ln.heads;
+  for (int base = part * ln.heads; base < heads; base += BWD_STEPS * step) {
+    uint2 ga[BWD_STEPS], gb[BWD_STEPS], xa[BWD_STEPS], xb[BWD_STEPS];
+#pragma unroll
+    for (int u = 0; u < BWD_STEPS; ++u) {
+      const int h0 = base + u * step;
+      ga[u] = gb[u] = xa[u] = xb[u] = make_uint2(0, 0);
+      if (ln.active && h0 + ln.group < heads) {
+        ga[u] = load4(g + h0 * p.dim + ln.a);
+        gb[u] = load4(g + h0 * p.dim + ln.b);
+        if (NORM) {
+          xa[u] = load4(x + h0 * p.dim + ln.a);
+          xb[u] = load4(x + h0 * p.dim + ln.b);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < BWD_STEPS; ++u) {
+      const int h0 = base + u * step;
+      if (h0 >= heads) break;
+      float a[4], b[4];
+      unpack4<T>(ga[u], a);
+      unpack4<T>(gb[u], b);
+      rotate<INTERLEAVED>(a, b, c, s);
+      if (NORM) {
+        float ya[4], yb[4];
+        unpack4<T>(xa[u], ya);
+        unpack4<T>(xb[u], yb);
+        float ss = 0.f, dot = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          ss = fmaf(ya[i], ya[i], fmaf(yb[i], yb[i], ss));
+          dot = fmaf(a[i] * wa[i], ya[i], fmaf(b[i] * wb[i], yb[i], dot));
+        }
+        ss = ln.sum(ss);
+        dot = ln.sum(dot);
+        const float r = rsqrtf(ss * per + p.eps), m = r * r * r * dot * per;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          dw[i] = fmaf(a[i], ya[i] * r, dw[i]);
+          dw[4 + i] = fmaf(b[i], yb[i] * r, dw[4 + i]);
+          a[i] = a[i] * wa[i] * r - ya[i] * m;
+          b[i] = b[i] * wb[i] * r - yb[i] * m;
+        }
+      }
+      if (ln.active && h0 + ln.group < heads) {
+        store4(dx + h0 * p.dim + ln.a, pack4<T>(a));
+        store4(dx + h0 * p.dim + ln.b, pack4<T>(b));
+      }
+    }
+  }
+}
+
+template <typename T, bool QNORM, bool KNORM, bool INTERLEAVED>
+__global__ void __launch_bounds__(THREADS, 2) qk_norm_rope_backward_kernel(const RopeArgs p) {
+  extern __shared__ float sm[];  // [16][THREADS] weight gradients of the lanes
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Lane ln(p, lane);
   pdl_wait();
@@ -241,72 +301,23 @@ __global__ void __launch_bounds__(THREADS) qk_norm_rope_backward_kernel(const Ro
   float wa[2][4], wb[2][4];
   load_weight<T>(p.q_weight, ln, wa[0], wb[0]);
   load_weight<T>(p.k_weight, ln, wa[1], wb[1]);
-  const int step = p.row_warps * ln.heads;
   const float per = 1.f / p.dim;
+  const int my = ln.group * p.dim;
 
   for (int index = blockIdx.x * WARPS + warp; index < p.n_rows * p.row_warps; index += gridDim.x * WARPS) {
     const int row = index / p.row_warps, part = index - row * p.row_warps;
     float c[4], s[4];
     angles(p, ln, row, c, s);
 #pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
-      const T* x = kind ? static_cast<const T*>(p.k) + row * p.k_stride : static_cast<const T*>(p.q) + row * p.q_stride;
-      const T* g = kind ? static_cast<const T*>(p.grad_k) + row * p.grad_k_stride
-                        : static_cast<const T*>(p.grad_q) + row * p.grad_q_stride;
-      T* dx = kind ? static_cast<T*>(p.k_out) + row * p.k_out_stride : static_cast<T*>(p.q_out) + row * p.q_out_stride;
-      const bool norm = kind ? p.k_weight != nullptr : p.q_weight != nullptr;
-      const int heads = kind ? p.kv_heads : p.heads;
-      for (int base = part * ln.heads; base < heads; base += STEPS / 2 * step) {
-        uint2 ga[STEPS / 2], gb[STEPS / 2], xa[STEPS / 2], xb[STEPS / 2];
-#pragma unroll
-        for (int u = 0; u < STEPS / 2; ++u) {
-          const int h = base + u * step + ln.group;
-          ga[u] = gb[u] = xa[u] = xb[u] = make_uint2(0, 0);
-          if (ln.active && h < heads) {
-            ga[u] = load4(g + h * p.dim + ln.a);
-            gb[u] = load4(g + h * p.dim + ln.b);
-            if (norm) {
-              xa[u] = load4(x + h * p.dim + ln.a);
-              xb[u] = load4(x + h * p.dim + ln.b);
-            }
-          }
-        }
-#pragma unroll
-        for (int u = 0; u < STEPS / 2; ++u) {
-          if (base + u * step >= heads) break;
-          const int h = base + u * step + ln.group;
-          float a[4], b[4];
-          unpack4<T>(ga[u], a);
-          unpack4<T>(gb[u], b);
-          if (ln.rotated) rotate(a, b, c, s, -1.f, p.interleaved);
-          if (norm) {
-            float ya[4], yb[4];
-            unpack4<T>(xa[u], ya);
-            unpack4<T>(xb[u], yb);
-            float ss = 0.f, dot = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              ss = fmaf(ya[i], ya[i], fmaf(yb[i], yb[i], ss));
-              dot = fmaf(a[i] * wa[kind][i], ya[i], fmaf(b[i] * wb[kind][i], yb[i], dot));
-            }
-            ss = ln.sum(ss);
-            dot = ln.sum(dot);
-            const float r = rsqrtf(ss * per + p.eps), m = r * r * r * dot * per;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              dw[kind][i] = fmaf(a[i], ya[i] * r, dw[kind][i]);
-              dw[kind][4 + i] = fmaf(b[i], yb[i] * r, dw[kind][4 + i]);
-              a[i] = a[i] * wa[kind][i] * r - ya[i] * m;
-              b[i] = b[i] * wb[kind][i] * r - yb[i] * m;
-            }
-          }
-          if (ln.active && h < heads) {
-            store4(dx + h * p.dim + ln.a, pack4<T>(a));
-            store4(dx + h * p.dim + ln.b, pack4<T>(b));
-          }
-        }
-      }
-    }
+    for (int i = 0; i < 4; ++i) s[i] = -s[i];
+    backward_steps<T, QNORM, INTERLEAVED>(p, ln, static_cast<const T*>(p.q) + row * p.q_stride + my,
+                                          static_cast<const T*>(p.grad_q) + row * p.grad_q_stride + my,
+                                          static_cast<T*>(p.q_out) + row * p.q_out_stride + my, part, p.heads, c, s, wa[0], wb[0],
+                                          per, dw[0]);
+    backward_steps<T, KNORM, INTERLEAVED>(p, ln, static_cast<const T*>(p.k) + row * p.k_stride + my,
+                                          static_cast<const T*>(p.grad_k) + row * p.grad_k_stride + my,
+                                          static_cast<T*>(p.k_out) + row * p.k_out_stride + my, part, p.kv_heads, c, s, wa[1], wb[1],
+                                          per, dw[1]);
   }
   if (!p.partial) return;
   // the CTA's sums, over its warps and the heads of a step in order
@@ -364,6 +375,13 @@ int row_warps(long long rows, int steps, int ctas, int sms) {
   int w = 1;
   while (w < WARPS && w < steps && rows * w < static_cast<long long>(ctas) * sms * WARPS) w *= 2;
   return w;
+}
+
+// Calls f with the type and the order of the pairs as types.
+template <typename F>
+cudaError_t dispatch(const ivit_rope_config& c, F f) {
+  if (c.dtype == IVIT_BF16) return c.interleaved ? f(bf16{}, std::true_type{}) : f(bf16{}, std::false_type{});
+  return c.interleaved ? f(half{}, std::true_type{}) : f(half{}, std::false_type{});
 }
 
 RopeArgs common(const ivit_rope_config& c, int n_rows) {
@@ -431,12 +449,15 @@ extern "C" int ivit_qk_norm_rope(const ivit_rope_config* cfg, int32_t n_rows, co
   p.pos_stride = pos_stride;
   if (cache) p.cache = paged(*cache);
   const int per_step = 32 / (cfg->head_dim / 8), vectors = cfg->heads + cfg->kv_heads * (v_dev ? 2 : 1);
-  p.row_warps = row_warps(n_rows, (vectors + per_step - 1) / per_step, 4, sms);
+  p.row_warps = row_warps(n_rows, (vectors + per_step - 1) / per_step, 3, sms);
   const long long blocks = (static_cast<long long>(n_rows) * p.row_warps + WARPS - 1) / WARPS;
   const dim3 grid(static_cast<unsigned>(blocks));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = cfg->dtype == IVIT_BF16 ? launch_ex(qk_norm_rope_kernel<bf16>, grid, dim3(THREADS), 0, s, 1, p)
-                                                : launch_ex(qk_norm_rope_kernel<half>, grid, dim3(THREADS), 0, s, 1, p);
+  const cudaError_t e = dispatch(*cfg, [&](auto type, auto inter) {
+    using T = decltype(type);
+    return q_weight_dev || k_weight_dev ? launch_ex(qk_norm_rope_kernel<T, true, inter()>, grid, dim3(THREADS), 0, s, 1, p)
+                                        : launch_ex(qk_norm_rope_kernel<T, false, inter()>, grid, dim3(THREADS), 0, s, 1, p);
+  });
   return e == cudaSuccess ? IVIT_OK : fail_cuda(e);
 }
 
@@ -500,8 +521,14 @@ extern "C" int ivit_qk_norm_rope_backward(const ivit_rope_config* cfg, int32_t n
   cudaError_t e = cudaSuccess;
   if (grid > 0) {
     const size_t smem = weights ? sizeof(float) * 16 * THREADS : 0;
-    e = cfg->dtype == IVIT_BF16 ? launch_ex(qk_norm_rope_backward_kernel<bf16>, dim3(grid), dim3(THREADS), smem, s, 1, p)
-                                : launch_ex(qk_norm_rope_backward_kernel<half>, dim3(grid), dim3(THREADS), smem, s, 1, p);
+    e = dispatch(*cfg, [&](auto type, auto inter) {
+      using T = decltype(type);
+      const auto launch = [&](auto kernel) { return launch_ex(kernel, dim3(grid), dim3(THREADS), smem, s, 1, p); };
+      return q_weight_dev ? k_weight_dev ? launch(qk_norm_rope_backward_kernel<T, true, true, inter()>)
+                                         : launch(qk_norm_rope_backward_kernel<T, true, false, inter()>)
+             : k_weight_dev ? launch(qk_norm_rope_backward_kernel<T, false, true, inter()>)
+                            : launch(qk_norm_rope_backward_kernel<T, false, false, inter()>);
+    });
   }
   if (e == cudaSuccess && weights)
     e = launch_ex(weight_gradient_kernel, dim3((2 * cfg->head_dim + 31) / 32), dim3(THREADS), 0, s, 1,

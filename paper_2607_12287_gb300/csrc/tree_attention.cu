@@ -4,8 +4,8 @@
 //
 // over the keys j that a row sees: all cached ones, and the new rows that its mask names.
 //
-// Rows that share a key head (the new rows x the query heads of the group) form tiles of 16, 32 or
-// 64; a tile walks its keys -- the cached tokens and, behind them, the new rows -- 64 at a time.
+// Rows that share a key head (the new rows x the query heads of the group) form tiles of 16, 32, 64
+// or 128; a tile walks its keys -- the cached tokens and, behind them, the new rows -- 64 at a time.
 // All (request, key head, row tile, 64 keys) of the call, in this order, are cut into as many equal
 // runs as there are CTAs, two per SM, so that ragged lengths and few requests load the chip alike.
 // A run that holds a tile's keys only in part leaves its running maximum, sum and output (fp32) in
@@ -29,12 +29,14 @@
 namespace ivit {
 namespace {
 
-constexpr int THREADS = 128;
 constexpr int TK = 64;              // keys of a tile
 constexpr int MAX_REQ = 4096;
-constexpr int MAX_CTAS = 512;       // of the attention kernel: the workspace's parts
+constexpr int MAX_SMS = 256;        // the workspace has parts for that many
 // Probabilities are kept 2^SHIFT times too large, which keeps small fp16 ones normal.
 constexpr float SHIFT = 10.f;
+// A row's reference maximum moves when a tile exceeds it by more than 2^GROWTH, not before: the output is
+// rescaled a few times per run instead of for most tiles, and 2^(SHIFT + GROWTH) is an fp16 number.
+constexpr float GROWTH = 5.f;
 
 struct TreeArgs {
   const void *q, *k_new, *v_new, *k_cache, *v_cache;
@@ -134,18 +136,24 @@ struct Place {
 
 template <int DP, int RW>
 struct Cfg {
-  static constexpr int M = 16 * RW, KW = 4 / RW, WK = TK / KW;   // rows, warps along the keys, keys of a warp
-  static constexpr int ROW = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;  // bytes of a row in shared memory
+  static constexpr int M = 16 * RW, KW = RW < 4 ? 4 / RW : 1, WK = TK / KW;  // rows, warps along the keys, keys of a warp
+  static constexpr int THREADS = 32 * RW * KW;
+  static constexpr int ROW = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;         // bytes of a row in shared memory
   static constexpr int TILE = TK * ROW;
-  static constexpr int STAGES = 3;
-  static constexpr int CTAS = DP <= 128 ? 2 : 1;                 // per SM
+  static constexpr int CTAS = DP <= 128 && RW < 8 ? 2 : 1;                   // per SM
+  static constexpr bool QSMEM = DP > 128;                                    // queries in shared memory, not registers
+  static constexpr int STAGES = DP > 128 ? 2 : 3;
   static constexpr int TERMS = RW < 4 ? 2 : 1;
-  static constexpr int MEET = DP + 4;                            // floats of a row where the warps meet
-  static constexpr int OFF_MEET = STAGES * 2 * TILE;
+  // a copy of a tile: CP threads for the pieces of a row, RP rows at a time
+  static constexpr int CP = ROW / 16, RP = THREADS / CP, COPIES = TK / RP;
+  static constexpr int MEET = DP + 4;                                        // floats of a row where the warps meet
+  static constexpr int OFF_Q = STAGES * 2 * TILE;
+  static constexpr int OFF_MEET = OFF_Q + (QSMEM ? M * ROW : 0);
   static constexpr int OFF_FLAGS = OFF_MEET + (KW > 1 ? M * (MEET + 2) * 4 : 0);
   static constexpr int BYTES = OFF_FLAGS + STAGES * 8;
-  static constexpr int PART = M * (DP + 2);                      // floats of a part in the workspace
-  static_assert(MAX_REQ * 8 + 8 <= OFF_MEET, "the units before each request");
+  static constexpr int PART = M * (DP + 2);                                  // floats of a part in the workspace
+  static_assert(MAX_REQ * 8 <= OFF_Q, "the units before each request");
+  static_assert(BYTES <= (CTAS == 2 ? 113 : 227) * 1024 - 128, "shared memory of an SM");
 };
 
 // Shared-memory address of 16-byte piece c of a row.
@@ -174,11 +182,10 @@ __device__ __forceinline__ uint64_t seen(const TreeArgs& a, const Request& r, in
 }
 
 template <typename T, int DP, int RW>
-__global__ void __launch_bounds__(THREADS, Cfg<DP, RW>::CTAS) tree_attention_kernel(const TreeArgs a) {
+__global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_attention_kernel(const TreeArgs a) {
   using C = Cfg<DP, RW>;
-  constexpr int M = C::M, KW = C::KW, WK = C::WK, ROW = C::ROW, STAGES = C::STAGES;
-  constexpr int PIECES = DP / 8, COPIES = (TK * PIECES + THREADS - 1) / THREADS;
-  constexpr bool QREG = DP <= 128;   // queries in registers (else read again for every tile)
+  constexpr int M = C::M, KW = C::KW, WK = C::WK, ROW = C::ROW, STAGES = C::STAGES, THREADS = C::THREADS;
+  constexpr int PIECES = DP / 8, COPIES = C::COPIES, RP = C::RP;
   extern __shared__ __align__(128) uint8_t sm[];
   const uint32_t sb = smem_u32(sm);
   uint32_t* flags = reinterpret_cast<uint32_t*>(sm + C::OFF_FLAGS);  // [STAGES][2] keys whose values are not finite
@@ -247,43 +254,61 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, RW>::CTAS) tree_attention_ker
   Place<M> at = load;
   const int units = static_cast<int>(hi - lo);
 
-  // The pages of the tile at `load`, of the rows that this thread copies; kept a tile ahead of the copies.
+  // A copy's part of this thread: piece cp of the rows r0, r0 + RP, ... of a tile.
+  const int cp = tid % C::CP, r0 = tid / C::CP, page_mask = (1 << a.cache.page_shift) - 1;
+  const uint32_t to = r0 * ROW + ((cp ^ (r0 & 7)) << 4);
+  const auto place = [&](int x) {  // of its x-th row in a tile (8 rows repeat the swizzle)
+    return (RP % 8 == 0 ? to : to ^ ((x * RP & 7) << 4)) + x * RP * ROW;
+  };
+  // The pages of the tile at `load`, of those rows; kept a tile ahead of the copies.
   int ids[COPIES];
-  auto look_up = [&] {
+  const auto look_up = [&] {
+    const int* table = a.table + static_cast<size_t>(load.req) * a.max_pages;
+    const int key = load.kt * TK + r0;
+    if ((load.kt + 1) * TK <= load.r.len) {
 #pragma unroll
-    for (int x = 0; x < COPIES; ++x) {
-      const int e = x * THREADS + tid, key = load.kt * TK + e / PIECES;
-      ids[x] = e < TK * PIECES && key < load.r.len
-                   ? a.table[static_cast<size_t>(load.req) * a.max_pages + (key >> a.cache.page_shift)]
-                   : -1;
+      for (int x = 0; x < COPIES; ++x) ids[x] = table[(key + x * RP) >> a.cache.page_shift];
+    } else {
+#pragma unroll
+      for (int x = 0; x < COPIES; ++x) ids[x] = key + x * RP < load.r.len ? table[(key + x * RP) >> a.cache.page_shift] : -1;
     }
   };
-  auto copy = [&](int stage) {
+  const auto copy = [&](int stage) {
+    if (cp >= pieces) return;
     const uint32_t ks = sb + stage * 2 * C::TILE, vs = ks + C::TILE;
-    const T* kc = static_cast<const T*>(a.k_cache) + load.head * a.cache.head_stride;
-    const T* vc = static_cast<const T*>(a.v_cache) + load.head * a.cache.head_stride;
+    const long long head = load.head * a.cache.head_stride + 8 * cp;
+    const T *kc = static_cast<const T*>(a.k_cache) + head, *vc = static_cast<const T*>(a.v_cache) + head;
+    const int key = load.kt * TK + r0;
+    if ((load.kt + 1) * TK <= load.r.len) {
 #pragma unroll
-    for (int x = 0; x < COPIES; ++x) {
-      const int e = x * THREADS + tid, row = e / PIECES, c = e - row * PIECES, key = load.kt * TK + row;
-      if (e >= TK * PIECES || c >= pieces) continue;
-      const int fresh = key - load.r.len;
+      for (int x = 0; x < COPIES; ++x) {
+        const bool ok = static_cast<unsigned>(ids[x]) < static_cast<unsigned>(a.cache.n_pages);
+        const long long off = ids[x] * a.cache.page_stride + ((key + x * RP) & page_mask) * a.cache.token_stride;
+        copy16(ks + place(x), kc + (ok ? off : 0), ok);
+        copy16(vs + place(x), vc + (ok ? off : 0), ok);
+      }
+      return;
+    }
+#pragma unroll
+    for (int x = 0; x < COPIES; ++x) {  // the new rows, and what lies behind them (zeros)
+      const int fresh = key + x * RP - load.r.len;
       const T *k = kc, *v = vc;
       bool ok;
       if (fresh < 0) {
         ok = static_cast<unsigned>(ids[x]) < static_cast<unsigned>(a.cache.n_pages);
-        const long long off = ok ? ids[x] * a.cache.page_stride + (key & ((1 << a.cache.page_shift) - 1)) * a.cache.token_stride : 0;
-        k += off + 8 * c;
-        v += off + 8 * c;
+        const long long off = ok ? ids[x] * a.cache.page_stride + ((key + x * RP) & page_mask) * a.cache.token_stride : 0;
+        k += off;
+        v += off;
       } else {
         ok = fresh < load.r.n;
         if (ok) {
-          const long long row = load.r.row0 + fresh;
-          k = static_cast<const T*>(a.k_new) + row * a.k_new_stride + load.head * a.cache.dim + 8 * c;
-          v = static_cast<const T*>(a.v_new) + row * a.v_new_stride + load.head * a.cache.dim + 8 * c;
+          const long long row = load.r.row0 + fresh, col = load.head * a.cache.dim + 8 * cp;
+          k = static_cast<const T*>(a.k_new) + row * a.k_new_stride + col;
+          v = static_cast<const T*>(a.v_new) + row * a.v_new_stride + col;
         }
       }
-      copy16(piece<ROW>(ks, row, c), k, ok);
-      copy16(piece<ROW>(vs, row, c), v, ok);
+      copy16(ks + place(x), k, ok);
+      copy16(vs + place(x), v, ok);
     }
   };
 
@@ -302,34 +327,42 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, RW>::CTAS) tree_attention_ker
   for (int s = 0; s < STAGES - 1; ++s) fill(s);
   __syncthreads();  // the flags are clear, and the columns past a head's
 
-  uint32_t q[QREG ? DP / 16 : 1][4];
+  uint32_t q[C::QSMEM ? 1 : DP / 16][4];
   float o[DP / 8][4], m[2], l[2];
   int node[2];               // new row of the lane's rows g, g + 8 (-1: none)
-  long long qoff[2];
   bool begun = true;         // of the tile's keys the run has seen the first
-  auto query = [&](int c, uint32_t (&f)[4]) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int r = e & 1, d = 16 * c + 2 * t + 8 * (e >> 1);
-      f[e] = node[r] >= 0 && d < a.cache.dim ? *reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + qoff[r] + d) : 0u;
-    }
-  };
 
   for (int u = 0; u < units; ++u) {
     const int stage = u % STAGES;
     if (u == 0 || at.kt == 0) {  // a new tile of rows
       begun = at.kt == 0;
+      const T* from[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int x = at.rt * M + rw * 16 + g + 8 * r, n = x / a.group;
         node[r] = n < at.r.n ? n : -1;
-        qoff[r] = (at.r.row0 + n) * a.q_stride + static_cast<long long>(at.head * a.group + x - n * a.group) * a.cache.dim;
+        from[r] = static_cast<const T*>(a.q) + (at.r.row0 + n) * a.q_stride +
+                  static_cast<long long>(at.head * a.group + x - n * a.group) * a.cache.dim;
         m[r] = -INFINITY;
         l[r] = 0.f;
       }
-      if (QREG) {
+      if (!C::QSMEM) {
 #pragma unroll
-        for (int c = 0; c < DP / 16; ++c) query(c, q[c]);
+        for (int c = 0; c < DP / 16; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = e & 1, d = 16 * c + 2 * t + 8 * (e >> 1);
+            q[c][e] = node[r] >= 0 && d < a.cache.dim ? *reinterpret_cast<const uint32_t*>(from[r] + d) : 0u;
+          }
+      } else {
+        __syncthreads();  // the tile before has been multiplied
+        if (kw == 0) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            for (int c = t; c < PIECES; c += 4)
+              *reinterpret_cast<uint4*>(sm + C::OFF_Q + (piece<ROW>(0, rw * 16 + g + 8 * r, c))) =
+                  node[r] >= 0 && c < pieces ? *reinterpret_cast<const uint4*>(from[r] + 8 * c) : make_uint4(0, 0, 0, 0);
+        }
       }
 #pragma unroll
       for (int j = 0; j < DP / 8; ++j)
@@ -345,9 +378,9 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, RW>::CTAS) tree_attention_ker
       // become zero here, each thread looking at what it copied, and are added back below.
 #pragma unroll
       for (int x = 0; x < COPIES; ++x) {
-        const int e = x * THREADS + tid, row = e / PIECES, c = e - row * PIECES;
-        if (e >= TK * PIECES || c >= pieces || k0 + row < at.r.len || k0 + row >= at.r.len + at.r.n) continue;
-        uint32_t* w = reinterpret_cast<uint32_t*>(sm + (piece<ROW>(vs, row, c) - sb));
+        const int row = r0 + x * RP;
+        if (cp >= pieces || k0 + row < at.r.len || k0 + row >= at.r.len + at.r.n) continue;
+        uint32_t* w = reinterpret_cast<uint32_t*>(sm + (vs - sb) + place(x));
         bool odd = false;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -375,15 +408,14 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, RW>::CTAS) tree_attention_ker
       for (int e = 0; e < 4; ++e) s[j][e] = 0.f;
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) {
-      uint32_t f[4];
-      if (!QREG) query(c, f);
+      if (C::QSMEM) ldmatrix4(q[0], piece<ROW>(sb + C::OFF_Q, rw * 16 + (lane & 15), 2 * c + (lane >> 4)));
 #pragma unroll
       for (int j = 0; j < WK / 16; ++j) {
         uint32_t b[4];
         const int row = kw * WK + 16 * j + (lane & 7) + ((lane & 16) >> 1);
         ldmatrix4(b, piece<ROW>(ks, row, 2 * c + (lane >> 3 & 1)));
-        mma<T>(s[2 * j], QREG ? q[QREG ? c : 0] : f, b[0], b[1]);
-        mma<T>(s[2 * j + 1], QREG ? q[QREG ? c : 0] : f, b[2], b[3]);
+        mma<T>(s[2 * j], q[C::QSMEM ? 0 : c], b[0], b[1]);
+        mma<T>(s[2 * j + 1], q[C::QSMEM ? 0 : c], b[2], b[3]);
       }
     }
     if (edge) {
@@ -397,31 +429,44 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, RW>::CTAS) tree_attention_ker
             if (!(bits >> (8 * j + 2 * t + e) & 1)) s[j][2 * r + e] = -INFINITY;
       }
     }
-    // probabilities, running maximum and sum
+    // probabilities against the reference maximum, and their sum
+    float mx[2];
+    bool grow = false;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      float mx = -INFINITY;
+      mx[r] = s[0][2 * r];
 #pragma unroll
-      for (int j = 0; j < WK / 8; ++j) mx = fmaxf(mx, fmaxf(s[j][2 * r], s[j][2 * r + 1]));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-      const float top = fmaxf(m[r], mx), ref = top == -INFINITY ? 0.f : top;  // (nothing seen so far: P = 0)
-      const float alpha = ex2((m[r] - ref) * a.scale_log2), mo = SHIFT - ref * a.scale_log2;
-      m[r] = top;
-      float sum = 0.f;
+      for (int j = 0; j < WK / 8; ++j) mx[r] = fmaxf(mx[r], fmaxf(s[j][2 * r], s[j][2 * r + 1]));
+      mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
+      mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2));
+      grow |= (mx[r] - m[r]) * a.scale_log2 > GROWTH;
+    }
+    if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        if (!(mx[r] > m[r])) continue;
+        const float alpha = ex2((m[r] - mx[r]) * a.scale_log2);
+        m[r] = mx[r];
+        l[r] *= alpha;
+#pragma unroll
+        for (int j = 0; j < DP / 8; ++j) {
+          o[j][2 * r] *= alpha;
+          o[j][2 * r + 1] *= alpha;
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const float mo = SHIFT - (m[r] == -INFINITY ? 0.f : m[r] * a.scale_log2);  // (nothing seen so far: P = 0)
+      float sum[2] = {0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < WK / 8; ++j)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           s[j][2 * r + e] = ex2(fmaf(s[j][2 * r + e], a.scale_log2, mo));
-          sum += s[j][2 * r + e];
+          sum[e] += s[j][2 * r + e];
         }
-      l[r] = l[r] * alpha + sum;
-#pragma unroll
-      for (int j = 0; j < DP / 8; ++j) {
-        o[j][2 * r] *= alpha;
-        o[j][2 * r + 1] *= alpha;
-      }
+      l[r] += sum[0] + sum[1];
     }
 #pragma unroll
     for (int j = 0; j < WK / 16; ++j) {
@@ -553,12 +598,14 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, RW>::CTAS) tree_attention_ker
   }
 }
 
-// Joins the parts of the tile of rows that CTA c's run of the attention kernel begins: block (c, y)
-// takes every gridDim.y-th of its rows, its warps the parts in turn.
+// Joins the parts of the tile of rows that CTA c's run of the attention kernel begins, in the order of
+// their keys: block (c, y) takes every gridDim.y-th group of its rows.  Up to 8 parts are a warp's work,
+// a row each; more are shared by the block's warps, which meet in shared memory.
 template <typename T, int DP, int RW>
 __global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a) {
-  constexpr int M = 16 * RW, PART = Cfg<DP, RW>::PART, WARPS = 8, VEC = (DP + 31) / 32;
-  __shared__ float ms[WARPS], ls[WARPS], os[WARPS][DP];
+  constexpr int M = 16 * RW, PART = Cfg<DP, RW>::PART, WARPS = 8, VEC = (DP / 2 + 31) / 32;
+  __shared__ float ms[WARPS], ls[WARPS];
+  __shared__ float2 os[WARPS][DP / 2];
   const int c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();
   pdl_launch_dependents();
@@ -569,56 +616,69 @@ __global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a) {
   // the tile's parts: CTA c's second or first, then the first ones of the CTAs behind it
   const float* parts = a.parts + static_cast<size_t>(2 * c) * PART;
   const int second = join.w & 1;
-  for (int row = blockIdx.y; row < rows; row += gridDim.y) {
-    float m = -INFINITY, l = 0.f, o[VEC];
+  const bool shared = n > WARPS;
+
+  for (int row0 = blockIdx.y * (shared ? 1 : WARPS); row0 < rows; row0 += gridDim.y * (shared ? 1 : WARPS)) {
+    const int row = shared ? row0 : row0 + warp;
+    if (row >= rows) break;  // (all of the block, or a warp that no other waits for)
+    float m = -INFINITY, l = 0.f;
+    float2 o[VEC];
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) o[v] = 0.f;
-    for (int i = warp; i < n; i += WARPS) {
+    for (int v = 0; v < VEC; ++v) o[v] = make_float2(0.f, 0.f);
+#pragma unroll 4
+    for (int i = shared ? warp : 0; i < n; i += shared ? WARPS : 1) {
       const float* p = parts + static_cast<size_t>(2 * i + (i == 0 ? second : 0)) * PART;
-      const float m2 = p[M * DP + 2 * row], l2 = p[M * DP + 2 * row + 1];
-      const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
-      const float f1 = ex2((m - ref) * a.scale_log2), f2 = ex2((m2 - ref) * a.scale_log2);
+      const float2 ml = *reinterpret_cast<const float2*>(p + M * DP + 2 * row);
+      const float top = fmaxf(m, ml.x), ref = top == -INFINITY ? 0.f : top;
+      const float f1 = ex2((m - ref) * a.scale_log2), f2 = ex2((ml.x - ref) * a.scale_log2);
       m = top;
-      l = l * f1 + l2 * f2;
+      l = l * f1 + ml.y * f2;
 #pragma unroll
       for (int v = 0; v < VEC; ++v)
-        if (32 * v + lane < DP) o[v] = o[v] * f1 + p[row * DP + 32 * v + lane] * f2;
+        if (32 * v + lane < DP / 2) {
+          const float2 x = reinterpret_cast<const float2*>(p + row * DP)[32 * v + lane];
+          o[v].x = o[v].x * f1 + x.x * f2;
+          o[v].y = o[v].y * f1 + x.y * f2;
+        }
     }
-    if (lane == 0) {
-      ms[warp] = m;
-      ls[warp] = l;
-    }
+    if (shared) {
+      if (lane == 0) {
+        ms[warp] = m;
+        ls[warp] = l;
+      }
 #pragma unroll
-    for (int v = 0; v < VEC; ++v)
-      if (32 * v + lane < DP) os[warp][32 * v + lane] = o[v];
-    __syncthreads();
-    float top = ms[0];
+      for (int v = 0; v < VEC; ++v)
+        if (32 * v + lane < DP / 2) os[warp][32 * v + lane] = o[v];
+      __syncthreads();
+      if (warp == 0) {
 #pragma unroll
-    for (int w = 1; w < WARPS; ++w) top = fmaxf(top, ms[w]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    float f[WARPS], sum = 0.f;
+        for (int w = 1; w < WARPS; ++w) {
+          const float top = fmaxf(m, ms[w]), ref = top == -INFINITY ? 0.f : top;
+          const float f1 = ex2((m - ref) * a.scale_log2), f2 = ex2((ms[w] - ref) * a.scale_log2);
+          m = top;
+          l = l * f1 + ls[w] * f2;
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
-      f[w] = ex2((ms[w] - ref) * a.scale_log2);
-      sum += ls[w] * f[w];
+          for (int v = 0; v < VEC; ++v)
+            if (32 * v + lane < DP / 2) {
+              const float2 x = os[w][32 * v + lane];
+              o[v].x = o[v].x * f1 + x.x * f2;
+              o[v].y = o[v].y * f1 + x.y * f2;
+            }
+        }
+      }
+      __syncthreads();  // the sums are read before the next row's
+      if (warp != 0) continue;
     }
     const int x = join.z * M + row, node = x / a.group, h = join.y * a.group + x - node * a.group;
     const long long orow = r.row0 + node;
-    const int d = 2 * threadIdx.x;
-    if (d < a.cache.dim) {
-      float y0 = 0.f, y1 = 0.f;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* dst = static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * a.cache.dim;
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w) {
-        y0 += os[w][d] * f[w];
-        y1 += os[w][d + 1] * f[w];
-      }
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * a.cache.dim + d) =
-          pack2<T>(y0 * inv, y1 * inv);
+    for (int v = 0; v < VEC; ++v) {
+      const int d = 2 * (32 * v + lane);
+      if (d < a.cache.dim) *reinterpret_cast<uint32_t*>(dst + d) = pack2<T>(o[v].x * inv, o[v].y * inv);
     }
-    if (a.lse && threadIdx.x == 0)
-      a.lse[orow * a.heads + h] = (top * a.scale_log2 + (log2f(sum) - SHIFT)) * 0.6931471805599453f;
-    __syncthreads();  // the sums are read before the next row's
+    if (a.lse && lane == 0) a.lse[orow * a.heads + h] = (m * a.scale_log2 + (log2f(l) - SHIFT)) * 0.6931471805599453f;
   }
 }
 
@@ -629,15 +689,16 @@ bool valid(const ivit_attention_config& c, const ivit_cache_layout& l) {
          c.mask_words <= 32768 && (c.mask_mode != IVIT_MASK_TREE || c.mask_words > 0) && c.scale > 0.f && c.scale < 1e30f;
 }
 
-// Calls f with the type, the padded head width and the row groups of a tile as types: 16 rows while they hold
-// the most rows that share a key head, then 32, else 64.
+// Calls f with the type, the padded head width and the row groups of a tile as types: the smallest of 16, 32, 64
+// and 128 rows that holds the most rows that share a key head, else 128.
 template <typename F>
 auto dispatch(const ivit_attention_config& c, const ivit_cache_layout& l, F f) {
-  const int rows = static_cast<int>(std::min<long long>(64, static_cast<long long>(c.max_new) * (c.heads / l.kv_heads)));
+  const int rows = static_cast<int>(std::min<long long>(128, static_cast<long long>(c.max_new) * (c.heads / l.kv_heads)));
   const auto groups = [&](auto type, auto dp) {
     return rows <= 16   ? f(type, dp, std::integral_constant<int, 1>{})
            : rows <= 32 ? f(type, dp, std::integral_constant<int, 2>{})
-                        : f(type, dp, std::integral_constant<int, 4>{});
+           : rows <= 64 ? f(type, dp, std::integral_constant<int, 4>{})
+                        : f(type, dp, std::integral_constant<int, 8>{});
   };
   const auto width = [&](auto type) {
     return l.head_dim <= 64    ? groups(type, std::integral_constant<int, 64>{})
@@ -655,7 +716,8 @@ extern "C" size_t ivit_tree_attention_workspace(const ivit_attention_config* cfg
   using namespace ivit;
   if (!cfg || !cache || !valid(*cfg, *cache)) return 0;
   return dispatch(*cfg, *cache, [](auto, auto dp, auto rw) -> size_t {
-    return MAX_CTAS * (sizeof(int4) + 2 * sizeof(float) * Cfg<dp(), rw()>::PART);
+    using C = Cfg<dp(), rw()>;
+    return C::CTAS * MAX_SMS * (sizeof(int4) + 2 * sizeof(float) * C::PART);
   });
 }
 
@@ -698,7 +760,6 @@ extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_
   a.out = out_dev;
   a.lse = lse_dev;
   a.joins = static_cast<int4*>(workspace_dev);
-  a.parts = reinterpret_cast<float*>(a.joins + MAX_CTAS);
   a.q_stride = q_stride;
   a.k_new_stride = k_new_stride;
   a.v_new_stride = v_new_stride;
@@ -720,8 +781,9 @@ extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_
     const auto kernel = tree_attention_kernel<T, dp(), rw()>;
     cudaError_t err = allow_smem<tree_attention_kernel<T, dp(), rw()>>(C::BYTES);
     if (err != cudaSuccess) return err;
-    const int ctas = std::min(MAX_CTAS, C::CTAS * sms);
-    err = launch_ex(kernel, dim3(ctas), dim3(THREADS), C::BYTES, s, 1, a);
+    const int ctas = C::CTAS * std::min(MAX_SMS, sms);
+    a.parts = reinterpret_cast<float*>(a.joins + C::CTAS * MAX_SMS);
+    err = launch_ex(kernel, dim3(ctas), dim3(C::THREADS), C::BYTES, s, 1, a);
     if (err != cudaSuccess) return err;
     return launch_ex(tree_join_kernel<T, dp(), rw()>, dim3(ctas, 4), dim3(256), 0, s, 1, a);
   });
