@@ -42,20 +42,6 @@ __device__ __forceinline__ uint32_t pack2<half>(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&b);
 }
 
-// Four values of 8 bytes.
-template <typename T>
-__device__ __forceinline__ void unpack4(const uint2& u, float (&x)[4]) {
-  const float2 a = unpack2<T>(u.x), b = unpack2<T>(u.y);
-  x[0] = a.x;
-  x[1] = a.y;
-  x[2] = b.x;
-  x[3] = b.y;
-}
-template <typename T>
-__device__ __forceinline__ uint2 pack4(const float (&x)[4]) {
-  return make_uint2(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]));
-}
-
 // A paged cache of one layer (ivit_cache_layout), page size as a shift.
 struct PagedCache {
   int n_pages, page_shift, heads, dim;

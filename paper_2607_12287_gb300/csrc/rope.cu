@@ -4,14 +4,15 @@
 //   y = x r w, r = 1 / sqrt(mean(x^2) + eps);   (u, v) -> (u c - v s, v c + u s), angle pos * freq;
 //   backward, with g' the gradient rotated back:  dw = sum g' x r,  dx = r g' w - x r^3 sum(g' w x) / D.
 //
-// A row is one warp's work, or that of 2, 4 or 8 warps when there are few rows.  A lane holds 8
-// values of a head in two pieces of 4, chosen so that both halves of its 4 pairs are its own (no
-// exchange for the rotation) and its 4 cosines and sines serve all of the row's heads; D / 8 lanes
-// make a head, 32 / (D / 8) heads a step of the warp, and the loads of several steps are in flight
-// together.  The cosines and sines are computed, not read: 4 per lane and row are less than the
-// memory a table would add.
+// A lane holds 8 values of a head in two pieces of 4, chosen so that both halves of its 4 pairs are its
+// own: no exchange for the rotation.  D / 8 lanes make a head; the 32 / (D / 8) groups of a warp take a
+// row each and walk its heads together, so that a lane's 4 cosines and sines (computed: a table would
+// add to the memory read) serve all heads of its row, every step of the warp is of one kind (query, key
+// or value), and no step is partly empty.  The loads of several heads are in flight together.  With few
+// rows their heads are split over more warps, down to one head each.
 //
 // Bound: HBM for many rows, the launch and two dependent round trips for a few.
+#include <algorithm>
 #include <type_traits>
 
 #include "backbone.cuh"
@@ -32,7 +33,8 @@ struct RopeArgs {
   long long q_stride, k_stride, v_stride, q_out_stride, k_out_stride, grad_q_stride, grad_k_stride, pos_stride;
   PagedCache cache;
   int n_rows, heads, kv_heads, dim, rot, n_axes, interleaved, row_warps;
-  float eps;
+  int row_sets;          // groups of as many rows as a warp takes
+  float eps, per_dim;    // per_dim: 1 / dim
 };
 
 // Cosine and sine of p * f.  The product is carried in two fp32 terms and reduced by multiples of
@@ -45,14 +47,16 @@ __device__ __forceinline__ void turn(int p, float f, float& c, float& s) {
   __sincosf(r, &s, &c);
 }
 
-// Where a lane's values are: pieces of 4 at a and b; pairs (a[i], b[i]), or (a[0], a[1]) and so on when
-// interleaved; lanes past rot / 8 hold values that are not rotated.
+// A lane's place in a head: pieces of 4 values at a and b, whose pairs are (a[i], b[i]), or (a[0], a[1]) and so
+// on when interleaved; lanes past rot / 8 hold values that are not rotated.  L: lanes of a head, 0: not a
+// power of two of 8 to 32.
+template <int L>
 struct Lane {
-  int group, l, per_head, heads, a, b;  // head of a step, lane of the head, lanes of a head, heads of a step
+  int group, l, per_head, heads, a, b;  // row of the warp's, lane of the head, lanes of a head, rows of a warp
   bool active, rotated;
 
   __device__ __forceinline__ Lane(const RopeArgs& p, int lane) {
-    per_head = p.dim >> 3;
+    per_head = L ? L : p.dim >> 3;
     heads = 32 / per_head;
     group = lane / per_head;
     l = lane - group * per_head;
@@ -69,10 +73,9 @@ struct Lane {
 
   // The sum over a head's lanes, in each of them.
   __device__ __forceinline__ float sum(float v) const {
-    if ((per_head & (per_head - 1)) == 0) {
+    if constexpr (L > 0) {
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1)
-        if (o < per_head) v += __shfl_xor_sync(0xffffffffu, v, o);
+      for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
       return v;
     }
 #pragma unroll
@@ -85,39 +88,52 @@ struct Lane {
   }
 };
 
-__device__ __forceinline__ void angles(const RopeArgs& p, const Lane& ln, int row, float (&c)[4], float (&s)[4]) {
+// Cosines and sines of a lane's pairs (0 and 1, 2 and 3), of no angle where they are not rotated.
+template <int L>
+__device__ __forceinline__ void angles(const RopeArgs& p, const Lane<L>& ln, int row, float2 (&c)[2], float2 (&s)[2]) {
+  float c4[4] = {1.f, 1.f, 1.f, 1.f}, s4[4] = {0.f, 0.f, 0.f, 0.f};
+  if (ln.rotated) {
+    int at[4] = {p.pos[row], 0, 0, 0};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    c[i] = 1.f;
-    s[i] = 0.f;
+    for (int x = 1; x < 4; ++x)
+      if (x < p.n_axes) at[x] = p.pos[x * p.pos_stride + row];
+    float f[4];
+    int ax[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[i] = p.freq[4 * ln.l + i];
+      ax[i] = p.n_axes > 1 ? p.axis[4 * ln.l + i] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      turn(ax[i] == 1 ? at[1] : ax[i] == 2 ? at[2] : ax[i] == 3 ? at[3] : at[0], f[i], c4[i], s4[i]);
   }
-  if (!ln.rotated) return;
-  int at[4] = {p.pos[row], 0, 0, 0};
 #pragma unroll
-  for (int x = 1; x < 4; ++x)
-    if (x < p.n_axes) at[x] = p.pos[x * p.pos_stride + row];
-  float f[4];
-  int ax[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[i] = p.freq[4 * ln.l + i];
-    ax[i] = p.n_axes > 1 ? p.axis[4 * ln.l + i] : 0;
+  for (int i = 0; i < 2; ++i) {
+    c[i] = make_float2(c4[2 * i], c4[2 * i + 1]);
+    s[i] = make_float2(s4[2 * i], s4[2 * i + 1]);
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    turn(ax[i] == 1 ? at[1] : ax[i] == 2 ? at[2] : ax[i] == 3 ? at[3] : at[0], f[i], c[i], s[i]);
 }
 
-// Rotation of a lane's pairs.
-template <bool INTERLEAVED>
-__device__ __forceinline__ void rotate(float (&a)[4], float (&b)[4], const float (&c)[4], const float (&s)[4]) {
+// A lane's 8 values as 16 bits: the words of piece a and of piece b; and as the first and second values of its
+// pairs, in fp32.
+template <typename T, bool INTERLEAVED>
+__device__ __forceinline__ void unpack(const uint2& a, const uint2& b, float2 (&u)[2], float2 (&v)[2]) {
+  const float2 x[4] = {unpack2<T>(a.x), unpack2<T>(a.y), unpack2<T>(b.x), unpack2<T>(b.y)};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float& x = !INTERLEAVED ? a[i] : i < 2 ? a[2 * i] : b[2 * i - 4];
-    float& y = !INTERLEAVED ? b[i] : i < 2 ? a[2 * i + 1] : b[2 * i - 3];
-    const float u = x, v = y;
-    x = u * c[i] - v * s[i];
-    y = v * c[i] + u * s[i];
+  for (int i = 0; i < 2; ++i) {
+    u[i] = INTERLEAVED ? make_float2(x[2 * i].x, x[2 * i + 1].x) : x[i];
+    v[i] = INTERLEAVED ? make_float2(x[2 * i].y, x[2 * i + 1].y) : x[2 + i];
+  }
+}
+template <typename T, bool INTERLEAVED>
+__device__ __forceinline__ void pack(const float2 (&u)[2], const float2 (&v)[2], uint2& a, uint2& b) {
+  if (INTERLEAVED) {
+    a = make_uint2(pack2<T>(u[0].x, v[0].x), pack2<T>(u[0].y, v[0].y));
+    b = make_uint2(pack2<T>(u[1].x, v[1].x), pack2<T>(u[1].y, v[1].y));
+  } else {
+    a = make_uint2(pack2<T>(u[0].x, u[0].y), pack2<T>(u[1].x, u[1].y));
+    b = make_uint2(pack2<T>(v[0].x, v[0].y), pack2<T>(v[1].x, v[1].y));
   }
 }
 
@@ -130,211 +146,270 @@ __device__ __forceinline__ void store4(T* p, const uint2& u) {
   *reinterpret_cast<uint2*>(p) = u;
 }
 
-template <typename T>
-__device__ __forceinline__ void load_weight(const void* w, const Lane& ln, float (&a)[4], float (&b)[4]) {
+// A norm's weights at a lane's values (1 without one).
+template <typename T, bool INTERLEAVED, int L>
+__device__ __forceinline__ void load_weight(const void* w, const Lane<L>& ln, float2 (&u)[2], float2 (&v)[2]) {
+  u[0] = u[1] = v[0] = v[1] = make_float2(1.f, 1.f);
+  if (w && ln.active) unpack<T, INTERLEAVED>(load4(static_cast<const T*>(w) + ln.a), load4(static_cast<const T*>(w) + ln.b), u, v);
+}
+
+__device__ __forceinline__ float2 neg(float2 x) { return make_float2(-x.x, -x.y); }
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// What turns a lane's values into its outputs: weight times cosine and sine, or the weights alone where the
+// values are not rotated.
+struct Turn {
+  float2 uc[2], us[2], vc[2], vs[2];
+
+  __device__ __forceinline__ void set(const float2 (&wu)[2], const float2 (&wv)[2], const float2 (&c)[2], const float2 (&s)[2]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) a[i] = b[i] = 1.f;
-  if (w && ln.active) {
-    unpack4<T>(load4(static_cast<const T*>(w) + ln.a), a);
-    unpack4<T>(load4(static_cast<const T*>(w) + ln.b), b);
+    for (int i = 0; i < 2; ++i) {
+      uc[i] = mul_f32x2(wu[i], c[i]);
+      us[i] = mul_f32x2(wu[i], s[i]);
+      vc[i] = mul_f32x2(wv[i], c[i]);
+      vs[i] = neg(mul_f32x2(wv[i], s[i]));
+    }
+  }
+  // (the two products of a value of a pair are not taken where there is no pair: infinity times 0)
+  __device__ __forceinline__ void apply(float2 (&u)[2], float2 (&v)[2], bool rotated) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float2 x = mul_f32x2(u[i], uc[i]), y = mul_f32x2(v[i], vc[i]);
+      if (rotated) {
+        x = fma_f32x2(v[i], vs[i], x);
+        y = fma_f32x2(u[i], us[i], y);
+      }
+      u[i] = x;
+      v[i] = y;
+    }
+  }
+};
+
+constexpr int AHEAD = 4;  // heads whose loads are in flight together
+
+// What of a row the warp takes: of n heads that begin with the row's head number `before`, every row_warps-th.
+__device__ __forceinline__ int first_head(const RopeArgs& p, int part, int before) {
+  const int h = (part - before) % p.row_warps;
+  return h < 0 ? h + p.row_warps : h;
+}
+
+// Norm and rotation of n heads at src to dst (strides in elements) and, if there is one, to dst2.
+template <typename T, int L, bool INTERLEAVED>
+__device__ __forceinline__ void forward_heads(const RopeArgs& p, const Lane<L>& ln, bool on, bool norm, const T* src, T* dst,
+                                              long long dst_stride, T* dst2, long long dst2_stride, int h0, int n,
+                                              const Turn& turn) {
+  const int step = p.row_warps, stride = step * p.dim;
+  src += h0 * p.dim;
+  for (int h = h0; h < n; h += AHEAD * step, src += AHEAD * stride) {
+    uint2 ra[AHEAD], rb[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      ra[i] = rb[i] = make_uint2(0, 0);
+      if (on && h + i * step < n) {
+        ra[i] = load4(src + i * stride + ln.a);
+        rb[i] = load4(src + i * stride + ln.b);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (h + i * step >= n) break;
+      float2 x[2], y[2];
+      unpack<T, INTERLEAVED>(ra[i], rb[i], x, y);
+      float r = 1.f;
+      if (norm) {
+        float2 ss = mul_f32x2(x[0], x[0]);
+        ss = fma_f32x2(x[1], x[1], ss);
+        ss = fma_f32x2(y[0], y[0], ss);
+        ss = fma_f32x2(y[1], y[1], ss);
+        r = rsqrtf(fmaf(ln.sum(ss.x + ss.y), p.per_dim, p.eps));
+      }
+      turn.apply(x, y, ln.rotated);
+      if (norm) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          x[e] = mul_f32x2(x[e], both(r));
+          y[e] = mul_f32x2(y[e], both(r));
+        }
+      }
+      if (on) {
+        uint2 oa, ob;
+        pack<T, INTERLEAVED>(x, y, oa, ob);
+        if (dst) {
+          T* to = dst + (h + i * step) * dst_stride;
+          store4(to + ln.a, oa);
+          store4(to + ln.b, ob);
+        }
+        if (dst2) {
+          T* to = dst2 + (h + i * step) * dst2_stride;
+          store4(to + ln.a, oa);
+          store4(to + ln.b, ob);
+        }
+      }
+    }
   }
 }
 
-// Forward: a step of a warp is up to 32 / (D / 8) heads of one kind; the warps of a row take its steps
-// (queries, then keys, then values) in turn, STEPS at a time with their loads in flight together.
-constexpr int STEPS = 4;
-
-// NORM: there is a weight.
-template <typename T, bool NORM, bool INTERLEAVED>
+template <typename T, int L, bool INTERLEAVED>
 __global__ void __launch_bounds__(THREADS, 3) qk_norm_rope_kernel(const RopeArgs p) {
-  const int warp = threadIdx.x >> 5;
-  const Lane ln(p, threadIdx.x & 31);
+  const Lane<L> ln(p, threadIdx.x & 31);
   pdl_wait();
   pdl_launch_dependents();
-  const int index = blockIdx.x * WARPS + warp, row = index / p.row_warps, part = index - row * p.row_warps;
-  if (row >= p.n_rows) return;
-  const int q_steps = (p.heads + ln.heads - 1) / ln.heads, k_steps = (p.kv_heads + ln.heads - 1) / ln.heads;
-  const int steps = q_steps + (p.v ? 2 * k_steps : k_steps);
-  const int my = ln.group * p.dim;
-  const T* q = static_cast<const T*>(p.q) + row * p.q_stride + my;
-  const T* k = static_cast<const T*>(p.k) + row * p.k_stride + my;
-  const T* v = static_cast<const T*>(p.v) + row * p.v_stride + my;
+  const int index = blockIdx.x * WARPS + (threadIdx.x >> 5), set = index / p.row_warps, part = index - set * p.row_warps;
+  const long long mine = static_cast<long long>(set) * ln.heads + ln.group;
+  const bool on = ln.active && mine < p.n_rows;
+  const int row = on ? static_cast<int>(mine) : 0;
+  if (!__any_sync(0xffffffffu, on)) return;
+  float2 c[2], s[2], wu[2], wv[2];
+  angles(p, ln, row, c, s);
+  Turn turn;
+  load_weight<T, INTERLEAVED>(p.q_weight, ln, wu, wv);
+  turn.set(wu, wv, c, s);
+  forward_heads<T, L, INTERLEAVED>(p, ln, on, p.q_weight != nullptr, static_cast<const T*>(p.q) + row * p.q_stride,
+                                   static_cast<T*>(p.q_out) + row * p.q_out_stride, p.dim, nullptr, 0, part, p.heads, turn);
+  load_weight<T, INTERLEAVED>(p.k_weight, ln, wu, wv);
+  turn.set(wu, wv, c, s);
   const int slot = p.slot ? p.slot[row] : -1;
   const bool cached = p.slot && p.cache.holds(slot);
-  float c[4], s[4], qa[4], qb[4], ka[4], kb[4];
-  bool first = true;
+  const long long token = cached ? p.cache.token(slot) : 0;
+  forward_heads<T, L, INTERLEAVED>(p, ln, on, p.k_weight != nullptr, static_cast<const T*>(p.k) + row * p.k_stride,
+                                   p.k_out ? static_cast<T*>(p.k_out) + row * p.k_out_stride : nullptr, p.dim,
+                                   cached ? static_cast<T*>(p.k_cache) + token : nullptr, p.cache.head_stride,
+                                   first_head(p, part, p.heads), p.kv_heads, turn);
+  if (!p.v) return;
+  const T* v = static_cast<const T*>(p.v) + row * p.v_stride;
+  T* to = static_cast<T*>(p.v_cache) + token;
+  for (int h = first_head(p, part, p.heads + p.kv_heads); h < p.kv_heads; h += AHEAD * p.row_warps) {
+    uint2 ra[AHEAD], rb[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (on && cached && h + i * p.row_warps < p.kv_heads) {
+        ra[i] = load4(v + (h + i * p.row_warps) * p.dim + ln.a);
+        rb[i] = load4(v + (h + i * p.row_warps) * p.dim + ln.b);
+      }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (on && cached && h + i * p.row_warps < p.kv_heads) {
+        store4(to + (h + i * p.row_warps) * p.cache.head_stride + ln.a, ra[i]);
+        store4(to + (h + i * p.row_warps) * p.cache.head_stride + ln.b, rb[i]);
+      }
+  }
+}
 
-  for (int base = part; base < steps; base += STEPS * p.row_warps) {
-    uint2 ra[STEPS], rb[STEPS];
+constexpr int BWD_AHEAD = 2;
+
+// Gradients of n heads of a row, at x, g and dx.  dw: of the lane's first and second values.
+template <typename T, int L, bool INTERLEAVED>
+__device__ __forceinline__ void backward_heads(const RopeArgs& p, const Lane<L>& ln, bool on, bool norm, const T* x, const T* g,
+                                               T* dx, int first, int n, const float2 (&c)[2], const float2 (&s)[2],
+                                               const float2 (&wu)[2], const float2 (&wv)[2], float2 (&dw)[4]) {
+  const int step = p.row_warps;
+  for (int h = first; h < n; h += BWD_AHEAD * step) {
+    uint2 ga[BWD_AHEAD], gb[BWD_AHEAD], xa[BWD_AHEAD], xb[BWD_AHEAD];
 #pragma unroll
-    for (int u = 0; u < STEPS; ++u) {
-      const int st = base + u * p.row_warps;
-      if (st >= steps) break;  // (the same for the whole warp, as the kind of a step)
-      const bool query = st < q_steps, key = st < q_steps + k_steps;
-      const int h0 = (query ? st : key ? st - q_steps : st - q_steps - k_steps) * ln.heads;
-      const T* src = (query ? q : key ? k : v) + h0 * p.dim;
-      ra[u] = rb[u] = make_uint2(0, 0);
-      if (ln.active && h0 + ln.group < (query ? p.heads : p.kv_heads)) {
-        ra[u] = load4(src + ln.a);
-        rb[u] = load4(src + ln.b);
-      }
-    }
-    if (first) {  // (behind the first loads)
-      first = false;
-      angles(p, ln, row, c, s);
-      if (NORM) {
-        load_weight<T>(p.q_weight, ln, qa, qb);
-        load_weight<T>(p.k_weight, ln, ka, kb);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < STEPS; ++u) {
-      const int st = base + u * p.row_warps;
-      if (st >= steps) break;
-      const bool query = st < q_steps, key = st < q_steps + k_steps;
-      const int h0 = (query ? st : key ? st - q_steps : st - q_steps - k_steps) * ln.heads;
-      if (key) {
-        float a[4], b[4];
-        unpack4<T>(ra[u], a);
-        unpack4<T>(rb[u], b);
-        if (NORM && (query ? p.q_weight : p.k_weight)) {
-          float ss = 0.f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
-          const float r = rsqrtf(ln.sum(ss) / p.dim + p.eps);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            a[i] = a[i] * r * (query ? qa[i] : ka[i]);
-            b[i] = b[i] * r * (query ? qb[i] : kb[i]);
-          }
+    for (int i = 0; i < BWD_AHEAD; ++i) {
+      const int at = (h + i * step) * p.dim;
+      ga[i] = gb[i] = xa[i] = xb[i] = make_uint2(0, 0);
+      if (on && h + i * step < n) {
+        ga[i] = load4(g + at + ln.a);
+        gb[i] = load4(g + at + ln.b);
+        if (norm) {
+          xa[i] = load4(x + at + ln.a);
+          xb[i] = load4(x + at + ln.b);
         }
-        rotate<INTERLEAVED>(a, b, c, s);  // (by nothing where the lane's values are not rotated)
-        ra[u] = pack4<T>(a);
-        rb[u] = pack4<T>(b);
       }
-      if (!ln.active || h0 + ln.group >= (query ? p.heads : p.kv_heads)) continue;
-      const int to = h0 * p.dim + my;
-      if (query || (key && p.k_out)) {
-        T* dst = (query ? static_cast<T*>(p.q_out) + row * p.q_out_stride : static_cast<T*>(p.k_out) + row * p.k_out_stride) + to;
-        store4(dst + ln.a, ra[u]);
-        store4(dst + ln.b, rb[u]);
+    }
+#pragma unroll
+    for (int i = 0; i < BWD_AHEAD; ++i) {
+      if (h + i * step >= n) break;
+      float2 u[2], v[2];
+      unpack<T, INTERLEAVED>(ga[i], gb[i], u, v);
+      if (ln.rotated) {  // back, by -a
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float2 t = fma_f32x2(v[e], s[e], mul_f32x2(u[e], c[e]));
+          v[e] = fma_f32x2(neg(u[e]), s[e], mul_f32x2(v[e], c[e]));
+          u[e] = t;
+        }
       }
-      if (!query && cached) {
-        T* dst = static_cast<T*>(key ? p.k_cache : p.v_cache) + p.cache.token(slot) + (h0 + ln.group) * p.cache.head_stride;
-        store4(dst + ln.a, ra[u]);
-        store4(dst + ln.b, rb[u]);
+      if (norm) {
+        float2 xu[2], xv[2], ss = make_float2(0.f, 0.f), dot = ss, tu[2], tv[2];
+        unpack<T, INTERLEAVED>(xa[i], xb[i], xu, xv);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          ss = fma_f32x2(xu[e], xu[e], ss);
+          ss = fma_f32x2(xv[e], xv[e], ss);
+          tu[e] = mul_f32x2(u[e], xu[e]);
+          tv[e] = mul_f32x2(v[e], xv[e]);
+          dot = fma_f32x2(tu[e], wu[e], dot);
+          dot = fma_f32x2(tv[e], wv[e], dot);
+        }
+        const float r = rsqrtf(fmaf(ln.sum(ss.x + ss.y), p.per_dim, p.eps));
+        const float m = -r * r * r * ln.sum(dot.x + dot.y) * p.per_dim;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          dw[e] = fma_f32x2(tu[e], both(r), dw[e]);
+          dw[2 + e] = fma_f32x2(tv[e], both(r), dw[2 + e]);
+          u[e] = fma_f32x2(xu[e], both(m), mul_f32x2(mul_f32x2(u[e], wu[e]), both(r)));
+          v[e] = fma_f32x2(xv[e], both(m), mul_f32x2(mul_f32x2(v[e], wv[e]), both(r)));
+        }
+      }
+      if (on) {
+        uint2 oa, ob;
+        pack<T, INTERLEAVED>(u, v, oa, ob);
+        store4(dx + (h + i * step) * p.dim + ln.a, oa);
+        store4(dx + (h + i * step) * p.dim + ln.b, ob);
       }
     }
   }
 }
 
-constexpr int BWD_STEPS = 2;
-
-// Gradients of the steps of one kind of a row; its heads at x, g and dx (lane's head included).
-template <typename T, bool NORM, bool INTERLEAVED>
-__device__ __forceinline__ void backward_steps(const RopeArgs& p, const Lane& ln, const T* x, const T* g, T* dx, int part, int heads,
-                                               const float (&c)[4], const float (&s)[4], const float (&wa)[4], const float (&wb)[4],
-                                               float per, float (&dw)[8]) {
-  const int step = p.row_warps * ln.heads;
-  for (int base = part * ln.heads; base < heads; base += BWD_STEPS * step) {
-    uint2 ga[BWD_STEPS], gb[BWD_STEPS], xa[BWD_STEPS], xb[BWD_STEPS];
-#pragma unroll
-    for (int u = 0; u < BWD_STEPS; ++u) {
-      const int h0 = base + u * step;
-      ga[u] = gb[u] = xa[u] = xb[u] = make_uint2(0, 0);
-      if (ln.active && h0 + ln.group < heads) {
-        ga[u] = load4(g + h0 * p.dim + ln.a);
-        gb[u] = load4(g + h0 * p.dim + ln.b);
-        if (NORM) {
-          xa[u] = load4(x + h0 * p.dim + ln.a);
-          xb[u] = load4(x + h0 * p.dim + ln.b);
-        }
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < BWD_STEPS; ++u) {
-      const int h0 = base + u * step;
-      if (h0 >= heads) break;
-      float a[4], b[4];
-      unpack4<T>(ga[u], a);
-      unpack4<T>(gb[u], b);
-      rotate<INTERLEAVED>(a, b, c, s);
-      if (NORM) {
-        float ya[4], yb[4];
-        unpack4<T>(xa[u], ya);
-        unpack4<T>(xb[u], yb);
-        float ss = 0.f, dot = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          ss = fmaf(ya[i], ya[i], fmaf(yb[i], yb[i], ss));
-          dot = fmaf(a[i] * wa[i], ya[i], fmaf(b[i] * wb[i], yb[i], dot));
-        }
-        ss = ln.sum(ss);
-        dot = ln.sum(dot);
-        const float r = rsqrtf(ss * per + p.eps), m = r * r * r * dot * per;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          dw[i] = fmaf(a[i], ya[i] * r, dw[i]);
-          dw[4 + i] = fmaf(b[i], yb[i] * r, dw[4 + i]);
-          a[i] = a[i] * wa[i] * r - ya[i] * m;
-          b[i] = b[i] * wb[i] * r - yb[i] * m;
-        }
-      }
-      if (ln.active && h0 + ln.group < heads) {
-        store4(dx + h0 * p.dim + ln.a, pack4<T>(a));
-        store4(dx + h0 * p.dim + ln.b, pack4<T>(b));
-      }
-    }
-  }
-}
-
-template <typename T, bool QNORM, bool KNORM, bool INTERLEAVED>
+template <typename T, int L, bool INTERLEAVED>
 __global__ void __launch_bounds__(THREADS, 2) qk_norm_rope_backward_kernel(const RopeArgs p) {
   extern __shared__ float sm[];  // [16][THREADS] weight gradients of the lanes
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const Lane ln(p, lane);
+  const Lane<L> ln(p, lane);
   pdl_wait();
   pdl_launch_dependents();
-  float dw[2][8];  // of a lane's 8 values: queries, keys
+  float2 dw[2][4];  // of a lane's 8 values: queries, keys
 #pragma unroll
-  for (int i = 0; i < 8; ++i) dw[0][i] = dw[1][i] = 0.f;
-  float wa[2][4], wb[2][4];
-  load_weight<T>(p.q_weight, ln, wa[0], wb[0]);
-  load_weight<T>(p.k_weight, ln, wa[1], wb[1]);
-  const float per = 1.f / p.dim;
-  const int my = ln.group * p.dim;
+  for (int i = 0; i < 4; ++i) dw[0][i] = dw[1][i] = make_float2(0.f, 0.f);
+  float2 wu[2][2], wv[2][2];
+  load_weight<T, INTERLEAVED>(p.q_weight, ln, wu[0], wv[0]);
+  load_weight<T, INTERLEAVED>(p.k_weight, ln, wu[1], wv[1]);
 
-  for (int index = blockIdx.x * WARPS + warp; index < p.n_rows * p.row_warps; index += gridDim.x * WARPS) {
-    const int row = index / p.row_warps, part = index - row * p.row_warps;
-    float c[4], s[4];
+  for (int index = blockIdx.x * WARPS + warp; index < p.row_sets * p.row_warps; index += gridDim.x * WARPS) {
+    const int set = index / p.row_warps, part = index - set * p.row_warps;
+    const long long mine = static_cast<long long>(set) * ln.heads + ln.group;
+    const bool on = ln.active && mine < p.n_rows;
+    const int row = on ? static_cast<int>(mine) : 0;
+    float2 c[2], s[2];
     angles(p, ln, row, c, s);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = -s[i];
-    backward_steps<T, QNORM, INTERLEAVED>(p, ln, static_cast<const T*>(p.q) + row * p.q_stride + my,
-                                          static_cast<const T*>(p.grad_q) + row * p.grad_q_stride + my,
-                                          static_cast<T*>(p.q_out) + row * p.q_out_stride + my, part, p.heads, c, s, wa[0], wb[0],
-                                          per, dw[0]);
-    backward_steps<T, KNORM, INTERLEAVED>(p, ln, static_cast<const T*>(p.k) + row * p.k_stride + my,
-                                          static_cast<const T*>(p.grad_k) + row * p.grad_k_stride + my,
-                                          static_cast<T*>(p.k_out) + row * p.k_out_stride + my, part, p.kv_heads, c, s, wa[1], wb[1],
-                                          per, dw[1]);
+    backward_heads<T, L, INTERLEAVED>(p, ln, on, p.q_weight != nullptr, static_cast<const T*>(p.q) + row * p.q_stride,
+                                      static_cast<const T*>(p.grad_q) + row * p.grad_q_stride,
+                                      static_cast<T*>(p.q_out) + row * p.q_out_stride, part, p.heads, c, s, wu[0], wv[0], dw[0]);
+    backward_heads<T, L, INTERLEAVED>(p, ln, on, p.k_weight != nullptr, static_cast<const T*>(p.k) + row * p.k_stride,
+                                      static_cast<const T*>(p.grad_k) + row * p.grad_k_stride,
+                                      static_cast<T*>(p.k_out) + row * p.k_out_stride, first_head(p, part, p.heads), p.kv_heads,
+                                      c, s, wu[1], wv[1], dw[1]);
   }
   if (!p.partial) return;
   // the CTA's sums, over its warps and the heads of a step in order
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    sm[(i * 2 + 0) * THREADS + threadIdx.x] = dw[0][i];
-    sm[(i * 2 + 1) * THREADS + threadIdx.x] = dw[1][i];
-  }
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+      sm[(4 * i + kind) * THREADS + threadIdx.x] = dw[kind][i].x;
+      sm[(4 * i + 2 + kind) * THREADS + threadIdx.x] = dw[kind][i].y;
+    }
   __syncthreads();
   const int lanes = ln.per_head;
   for (int e = threadIdx.x; e < 16 * lanes; e += THREADS) {
-    const int i = e / (2 * lanes), kind = e / lanes & 1, l = e % lanes;
+    const int i = e / (2 * lanes), kind = e / lanes & 1, l = e % lanes;  // i: first values 0 to 3, then second ones
     float sum = 0.f;
     for (int w = 0; w < WARPS; ++w)
       for (int g = 0; g < ln.heads; ++g) sum += sm[(i * 2 + kind) * THREADS + w * 32 + g * lanes + l];
-    const bool rotated = l < p.rot >> 3 && !p.interleaved;
-    const int d = rotated ? (i < 4 ? 4 * l + i : p.rot / 2 + 4 * l + i - 4) : 8 * l + i;
+    const bool split = l < p.rot >> 3 && !INTERLEAVED;
+    const int d = INTERLEAVED ? 8 * l + 2 * (i & 3) + (i >> 2) : split ? (i < 4 ? 4 * l + i : p.rot / 2 + 4 * l + i - 4) : 8 * l + i;
     p.partial[(static_cast<size_t>(blockIdx.x) * 2 + kind) * p.dim + d] = sum;
   }
 }
@@ -369,19 +444,26 @@ bool valid(const ivit_rope_config& c) {
 const char* kShape = "need heads and kv_heads 1..256, head_dim a multiple of 8 up to 256, rot_dim a multiple of 8 up to "
                      "it, 1..4 axes, interleaved 0 or 1, dtype IVIT_BF16 or IVIT_FP16, eps >= 0";
 
-// Warps of a row: as many as it takes to give each of the chip's warp slots (of `ctas` per SM) a row's part,
-// up to the steps that a row has.
-int row_warps(long long rows, int steps, int ctas, int sms) {
-  int w = 1;
-  while (w < WARPS && w < steps && rows * w < static_cast<long long>(ctas) * sms * WARPS) w *= 2;
-  return w;
+// Warps that share a set of rows: as many as it takes to give each of the chip's warp slots (`ctas` CTAs per
+// SM) work, up to the row's heads.
+int row_warps(int row_sets, int heads, int ctas, int sms) {
+  const long long slots = static_cast<long long>(ctas) * sms * WARPS;
+  return static_cast<int>(std::max<long long>(1, std::min<long long>(heads, slots / std::max(1, row_sets))));
 }
 
-// Calls f with the type and the order of the pairs as types.
+// Calls f with the type, the lanes of a head (0: not a power of two of 8 to 32) and the order of the pairs as types.
 template <typename F>
 cudaError_t dispatch(const ivit_rope_config& c, F f) {
-  if (c.dtype == IVIT_BF16) return c.interleaved ? f(bf16{}, std::true_type{}) : f(bf16{}, std::false_type{});
-  return c.interleaved ? f(half{}, std::true_type{}) : f(half{}, std::false_type{});
+  const auto order = [&](auto type, auto lanes) {
+    return c.interleaved ? f(type, lanes, std::true_type{}) : f(type, lanes, std::false_type{});
+  };
+  const auto width = [&](auto type) {
+    return c.head_dim == 64    ? order(type, std::integral_constant<int, 8>{})
+           : c.head_dim == 128 ? order(type, std::integral_constant<int, 16>{})
+           : c.head_dim == 256 ? order(type, std::integral_constant<int, 32>{})
+                               : order(type, std::integral_constant<int, 0>{});
+  };
+  return c.dtype == IVIT_BF16 ? width(bf16{}) : width(half{});
 }
 
 RopeArgs common(const ivit_rope_config& c, int n_rows) {
@@ -394,6 +476,9 @@ RopeArgs common(const ivit_rope_config& c, int n_rows) {
   p.n_axes = c.n_axes;
   p.interleaved = c.interleaved;
   p.eps = c.eps;
+  p.per_dim = 1.f / c.head_dim;
+  const int rows = 32 / (c.head_dim / 8);
+  p.row_sets = n_rows / rows + (n_rows % rows != 0);
   return p;
 }
 
@@ -448,15 +533,12 @@ extern "C" int ivit_qk_norm_rope(const ivit_rope_config* cfg, int32_t n_rows, co
   p.k_out_stride = k_out_stride;
   p.pos_stride = pos_stride;
   if (cache) p.cache = paged(*cache);
-  const int per_step = 32 / (cfg->head_dim / 8), vectors = cfg->heads + cfg->kv_heads * (v_dev ? 2 : 1);
-  p.row_warps = row_warps(n_rows, (vectors + per_step - 1) / per_step, 3, sms);
-  const long long blocks = (static_cast<long long>(n_rows) * p.row_warps + WARPS - 1) / WARPS;
+  p.row_warps = row_warps(p.row_sets, cfg->heads + cfg->kv_heads * (v_dev ? 2 : 1), 3, sms);
+  const long long blocks = (static_cast<long long>(p.row_sets) * p.row_warps + WARPS - 1) / WARPS;
   const dim3 grid(static_cast<unsigned>(blocks));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = dispatch(*cfg, [&](auto type, auto inter) {
-    using T = decltype(type);
-    return q_weight_dev || k_weight_dev ? launch_ex(qk_norm_rope_kernel<T, true, inter()>, grid, dim3(THREADS), 0, s, 1, p)
-                                        : launch_ex(qk_norm_rope_kernel<T, false, inter()>, grid, dim3(THREADS), 0, s, 1, p);
+  const cudaError_t e = dispatch(*cfg, [&](auto type, auto lanes, auto inter) {
+    return launch_ex(qk_norm_rope_kernel<decltype(type), lanes(), inter()>, grid, dim3(THREADS), 0, s, 1, p);
   });
   return e == cudaSuccess ? IVIT_OK : fail_cuda(e);
 }
@@ -513,21 +595,15 @@ extern "C" int ivit_qk_norm_rope_backward(const ivit_rope_config* cfg, int32_t n
   p.q_out_stride = dq_stride;
   p.k_out_stride = dk_stride;
   p.pos_stride = pos_stride;
-  const int per_step = 32 / (cfg->head_dim / 8);
-  p.row_warps = row_warps(n_rows, (cfg->heads + per_step - 1) / per_step, 4, sms);
-  const long long blocks = (static_cast<long long>(n_rows) * p.row_warps + WARPS - 1) / WARPS;
-  const int most = min(BWD_CTAS_MAX, 4 * sms), grid = static_cast<int>(blocks < most ? blocks : most);
+  p.row_warps = row_warps(p.row_sets, cfg->heads + cfg->kv_heads, 2, sms);
+  const long long blocks = (static_cast<long long>(p.row_sets) * p.row_warps + WARPS - 1) / WARPS;
+  const int most = min(BWD_CTAS_MAX, 2 * sms), grid = static_cast<int>(blocks < most ? blocks : most);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   if (grid > 0) {
     const size_t smem = weights ? sizeof(float) * 16 * THREADS : 0;
-    e = dispatch(*cfg, [&](auto type, auto inter) {
-      using T = decltype(type);
-      const auto launch = [&](auto kernel) { return launch_ex(kernel, dim3(grid), dim3(THREADS), smem, s, 1, p); };
-      return q_weight_dev ? k_weight_dev ? launch(qk_norm_rope_backward_kernel<T, true, true, inter()>)
-                                         : launch(qk_norm_rope_backward_kernel<T, true, false, inter()>)
-             : k_weight_dev ? launch(qk_norm_rope_backward_kernel<T, false, true, inter()>)
-                            : launch(qk_norm_rope_backward_kernel<T, false, false, inter()>);
+    e = dispatch(*cfg, [&](auto type, auto lanes, auto inter) {
+      return launch_ex(qk_norm_rope_backward_kernel<decltype(type), lanes(), inter()>, dim3(grid), dim3(THREADS), smem, s, 1, p);
     });
   }
   if (e == cudaSuccess && weights)
