@@ -8,8 +8,10 @@
 // own: no exchange for the rotation.  D / 8 lanes make a head; the 32 / (D / 8) groups of a warp take a
 // row each and walk its heads together, so that a lane's 4 cosines and sines (computed: a table would
 // add to the memory read) serve all heads of its row, every step of the warp is of one kind (query, key
-// or value), and no step is partly empty.  The loads of several heads are in flight together.  With few
-// rows their heads are split over more warps, down to one head each.
+// or value), and no step is partly empty.  With few rows their heads are split over more warps, down to
+// one head each.
+// Heads go through a warp four at a time, loads first, so that four chains of unpack, sum, shuffle and
+// scale overlap.
 //
 // Bound: HBM for many rows, the launch and two dependent round trips for a few.
 #include <algorithm>
@@ -21,6 +23,7 @@ namespace ivit {
 namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
+constexpr int FWD_CTAS = 3, BWD_CTAS = 2;  // per SM
 constexpr int BWD_CTAS_MAX = 1024;  // CTAs of the backward pass: partial weight gradients
 
 struct RopeArgs {
@@ -48,8 +51,7 @@ __device__ __forceinline__ void turn(int p, float f, float& c, float& s) {
 }
 
 // A lane's place in a head: pieces of 4 values at a and b, whose pairs are (a[i], b[i]), or (a[0], a[1]) and so
-// on when interleaved; lanes past rot / 8 hold values that are not rotated.  L: lanes of a head, 0: not a
-// power of two of 8 to 32.
+// on when interleaved; lanes past rot / 8 hold values that are not rotated.  L: lanes of a head, 0: any.
 template <int L>
 struct Lane {
   int group, l, per_head, heads, a, b;  // row of the warp's, lane of the head, lanes of a head, rows of a warp
@@ -71,20 +73,39 @@ struct Lane {
     }
   }
 
-  // The sum over a head's lanes, in each of them.
+  // The sum over a head's lanes, in each of them.  Powers of two: a butterfly; 9, 10 and 12 lanes: rotations
+  // within the head, first by the multiples of the cofactor, then by 1, 2, ...; others: a tree and a broadcast.
   __device__ __forceinline__ float sum(float v) const {
-    if constexpr (L > 0) {
+    if constexpr (L == 8 || L == 16 || L == 32) {
 #pragma unroll
       for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
       return v;
-    }
+    } else if constexpr (L > 0) {
+      static_assert(L == 9 || L == 10 || L == 12, "a sum over the lanes of a head");
+      if constexpr (L == 9) return rotations<3, 1>(rotations<3, 3>(v));
+      if constexpr (L == 10) return rotations<5, 1>(rotations<2, 5>(v));
+      if constexpr (L == 12) return rotations<3, 1>(rotations<2, 3>(rotations<2, 6>(v)));
+    } else {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-      if (o < per_head) {
-        const float x = __shfl_down_sync(0xffffffffu, v, o);
-        if (l + o < per_head) v += x;
-      }
-    return __shfl_sync(0xffffffffu, v, group * per_head);
+      for (int o = 16; o > 0; o >>= 1)
+        if (o < per_head) {
+          const float x = __shfl_down_sync(0xffffffffu, v, o);
+          if (l + o < per_head) v += x;
+        }
+      return __shfl_sync(0xffffffffu, v, group * per_head);
+    }
+  }
+
+  // The sum of the values of the lanes l, l + S, ..., l + (N - 1) S of the head, going round.
+  template <int N, int S>
+  __device__ __forceinline__ float rotations(float v) const {
+    float r = v;
+#pragma unroll
+    for (int i = 1; i < N; ++i) {
+      const int to = l + i * S >= L ? l + i * S - L : l + i * S;
+      r += __shfl_sync(0xffffffffu, v, group * L + to);  // (the idle lanes of a warp add what they get)
+    }
+    return r;
   }
 };
 
@@ -185,72 +206,84 @@ struct Turn {
   }
 };
 
-constexpr int AHEAD = 4;  // heads whose loads are in flight together
-
-// What of a row the warp takes: of n heads that begin with the row's head number `before`, every row_warps-th.
+// Of the heads of a kind, which come after `before` others of the row: the first that is the warp's.
 __device__ __forceinline__ int first_head(const RopeArgs& p, int part, int before) {
   const int h = (part - before) % p.row_warps;
   return h < 0 ? h + p.row_warps : h;
 }
 
-// Norm and rotation of n heads at src to dst (strides in elements) and, if there is one, to dst2.
-template <typename T, int L, bool INTERLEAVED>
-__device__ __forceinline__ void forward_heads(const RopeArgs& p, const Lane<L>& ln, bool on, bool norm, const T* src, T* dst,
-                                              long long dst_stride, T* dst2, long long dst2_stride, int h0, int n,
-                                              const Turn& turn) {
-  const int step = p.row_warps, stride = step * p.dim;
-  src += h0 * p.dim;
-  for (int h = h0; h < n; h += AHEAD * step, src += AHEAD * stride) {
-    uint2 ra[AHEAD], rb[AHEAD];
+constexpr int AHEAD = 4;  // heads at a time
+
+// Norm and rotation of N heads, `step` elements apart, to dst and dst2 (either may be null).
+template <typename T, int L, bool INTERLEAVED, bool NORM, int N>
+__device__ __forceinline__ void forward_heads(const RopeArgs& p, const Lane<L>& ln, bool on, const T* src, int step, T* dst,
+                                              long long dst_step, T* dst2, long long dst2_step, const Turn& turn) {
+  uint2 a[N], b[N];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      ra[i] = rb[i] = make_uint2(0, 0);
-      if (on && h + i * step < n) {
-        ra[i] = load4(src + i * stride + ln.a);
-        rb[i] = load4(src + i * stride + ln.b);
-      }
+  for (int i = 0; i < N; ++i) {
+    a[i] = b[i] = make_uint2(0, 0);
+    if (on) {
+      a[i] = load4(src + i * step + ln.a);
+      b[i] = load4(src + i * step + ln.b);
     }
+  }
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      if (h + i * step >= n) break;
-      float2 x[2], y[2];
-      unpack<T, INTERLEAVED>(ra[i], rb[i], x, y);
-      float r = 1.f;
-      if (norm) {
-        float2 ss = mul_f32x2(x[0], x[0]);
-        ss = fma_f32x2(x[1], x[1], ss);
-        ss = fma_f32x2(y[0], y[0], ss);
-        ss = fma_f32x2(y[1], y[1], ss);
-        r = rsqrtf(fmaf(ln.sum(ss.x + ss.y), p.per_dim, p.eps));
-      }
+  for (int i = 0; i < N; ++i) {
+    float2 x[2], y[2];
+    unpack<T, INTERLEAVED>(a[i], b[i], x, y);
+    if (NORM) {
+      float2 ss = mul_f32x2(x[0], x[0]);
+      ss = fma_f32x2(x[1], x[1], ss);
+      ss = fma_f32x2(y[0], y[0], ss);
+      ss = fma_f32x2(y[1], y[1], ss);
+      const float2 r = both(rsqrtf(fmaf(ln.sum(ss.x + ss.y), p.per_dim, p.eps)));
       turn.apply(x, y, ln.rotated);
-      if (norm) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          x[e] = mul_f32x2(x[e], both(r));
-          y[e] = mul_f32x2(y[e], both(r));
-        }
+      for (int e = 0; e < 2; ++e) {
+        x[e] = mul_f32x2(x[e], r);
+        y[e] = mul_f32x2(y[e], r);
       }
-      if (on) {
-        uint2 oa, ob;
-        pack<T, INTERLEAVED>(x, y, oa, ob);
-        if (dst) {
-          T* to = dst + (h + i * step) * dst_stride;
-          store4(to + ln.a, oa);
-          store4(to + ln.b, ob);
-        }
-        if (dst2) {
-          T* to = dst2 + (h + i * step) * dst2_stride;
-          store4(to + ln.a, oa);
-          store4(to + ln.b, ob);
-        }
-      }
+    } else {
+      turn.apply(x, y, ln.rotated);
+    }
+    pack<T, INTERLEAVED>(x, y, a[i], b[i]);
+  }
+  if (!on) return;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (dst) {
+      store4(dst + i * dst_step + ln.a, a[i]);
+      store4(dst + i * dst_step + ln.b, b[i]);
+    }
+    if (dst2) {
+      store4(dst2 + i * dst2_step + ln.a, a[i]);
+      store4(dst2 + i * dst2_step + ln.b, b[i]);
     }
   }
 }
 
-template <typename T, int L, bool INTERLEAVED>
-__global__ void __launch_bounds__(THREADS, 3) qk_norm_rope_kernel(const RopeArgs p) {
+// The warp's share of n heads of a row.
+template <typename T, int L, bool INTERLEAVED, bool NORM>
+__device__ __forceinline__ void forward_kind(const RopeArgs& p, const Lane<L>& ln, bool on, const T* src, T* dst, T* dst2,
+                                             long long dst2_stride, int h, int n, const Turn& turn) {
+  const int step = p.row_warps * p.dim;
+  const long long step2 = p.row_warps * dst2_stride;
+  src += h * p.dim;
+  if (dst) dst += h * p.dim;
+  if (dst2) dst2 += h * dst2_stride;
+  const auto advance = [&](int heads) {
+    h += heads * p.row_warps;
+    src += heads * step;
+    if (dst) dst += heads * step;
+    if (dst2) dst2 += heads * step2;
+  };
+  for (; h + (AHEAD - 1) * p.row_warps < n; advance(AHEAD))
+    forward_heads<T, L, INTERLEAVED, NORM, AHEAD>(p, ln, on, src, step, dst, step, dst2, step2, turn);
+  for (; h < n; advance(1)) forward_heads<T, L, INTERLEAVED, NORM, 1>(p, ln, on, src, step, dst, step, dst2, step2, turn);
+}
+
+template <typename T, int L, bool INTERLEAVED, bool NORM>
+__global__ void __launch_bounds__(THREADS, FWD_CTAS) qk_norm_rope_kernel(const RopeArgs p) {
   const Lane<L> ln(p, threadIdx.x & 31);
   pdl_wait();
   pdl_launch_dependents();
@@ -264,153 +297,164 @@ __global__ void __launch_bounds__(THREADS, 3) qk_norm_rope_kernel(const RopeArgs
   Turn turn;
   load_weight<T, INTERLEAVED>(p.q_weight, ln, wu, wv);
   turn.set(wu, wv, c, s);
-  forward_heads<T, L, INTERLEAVED>(p, ln, on, p.q_weight != nullptr, static_cast<const T*>(p.q) + row * p.q_stride,
-                                   static_cast<T*>(p.q_out) + row * p.q_out_stride, p.dim, nullptr, 0, part, p.heads, turn);
+  const auto kind = [&](bool norm, const T* src, T* dst, T* dst2, long long dst2_stride, int h, int n) {
+    if (NORM && norm) {
+      forward_kind<T, L, INTERLEAVED, NORM>(p, ln, on, src, dst, dst2, dst2_stride, h, n, turn);
+    } else {
+      forward_kind<T, L, INTERLEAVED, false>(p, ln, on, src, dst, dst2, dst2_stride, h, n, turn);
+    }
+  };
+  kind(p.q_weight != nullptr, static_cast<const T*>(p.q) + row * p.q_stride, static_cast<T*>(p.q_out) + row * p.q_out_stride,
+       nullptr, 0, part, p.heads);
   load_weight<T, INTERLEAVED>(p.k_weight, ln, wu, wv);
   turn.set(wu, wv, c, s);
   const int slot = p.slot ? p.slot[row] : -1;
   const bool cached = p.slot && p.cache.holds(slot);
   const long long token = cached ? p.cache.token(slot) : 0;
-  forward_heads<T, L, INTERLEAVED>(p, ln, on, p.k_weight != nullptr, static_cast<const T*>(p.k) + row * p.k_stride,
-                                   p.k_out ? static_cast<T*>(p.k_out) + row * p.k_out_stride : nullptr, p.dim,
-                                   cached ? static_cast<T*>(p.k_cache) + token : nullptr, p.cache.head_stride,
-                                   first_head(p, part, p.heads), p.kv_heads, turn);
+  kind(p.k_weight != nullptr, static_cast<const T*>(p.k) + row * p.k_stride,
+       p.k_out ? static_cast<T*>(p.k_out) + row * p.k_out_stride : nullptr, cached ? static_cast<T*>(p.k_cache) + token : nullptr,
+       p.cache.head_stride, first_head(p, part, p.heads), p.kv_heads);
   if (!p.v) return;
   const T* v = static_cast<const T*>(p.v) + row * p.v_stride;
   T* to = static_cast<T*>(p.v_cache) + token;
-  for (int h = first_head(p, part, p.heads + p.kv_heads); h < p.kv_heads; h += AHEAD * p.row_warps) {
-    uint2 ra[AHEAD], rb[AHEAD];
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i)
-      if (on && cached && h + i * p.row_warps < p.kv_heads) {
-        ra[i] = load4(v + (h + i * p.row_warps) * p.dim + ln.a);
-        rb[i] = load4(v + (h + i * p.row_warps) * p.dim + ln.b);
-      }
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i)
-      if (on && cached && h + i * p.row_warps < p.kv_heads) {
-        store4(to + (h + i * p.row_warps) * p.cache.head_stride + ln.a, ra[i]);
-        store4(to + (h + i * p.row_warps) * p.cache.head_stride + ln.b, rb[i]);
-      }
-  }
+  const bool copies = on && cached;
+#pragma unroll 4
+  for (int h = first_head(p, part, p.heads + p.kv_heads); h < p.kv_heads; h += p.row_warps)
+    if (copies) {
+      const uint2 a = load4(v + h * p.dim + ln.a), b = load4(v + h * p.dim + ln.b);
+      store4(to + h * p.cache.head_stride + ln.a, a);
+      store4(to + h * p.cache.head_stride + ln.b, b);
+    }
 }
 
-constexpr int BWD_AHEAD = 2;
+constexpr int BWD_AHEAD = 4;
 
-// Gradients of n heads of a row, at x, g and dx.  dw: of the lane's first and second values.
-template <typename T, int L, bool INTERLEAVED>
-__device__ __forceinline__ void backward_heads(const RopeArgs& p, const Lane<L>& ln, bool on, bool norm, const T* x, const T* g,
-                                               T* dx, int first, int n, const float2 (&c)[2], const float2 (&s)[2],
-                                               const float2 (&wu)[2], const float2 (&wv)[2], float2 (&dw)[4]) {
-  const int step = p.row_warps;
-  for (int h = first; h < n; h += BWD_AHEAD * step) {
-    uint2 ga[BWD_AHEAD], gb[BWD_AHEAD], xa[BWD_AHEAD], xb[BWD_AHEAD];
+// Gradients of N heads, `step` elements apart.  dw: of the lane's first values, then of its second ones.
+template <typename T, int L, bool INTERLEAVED, bool NORM, int N>
+__device__ __forceinline__ void backward_heads(const RopeArgs& p, const Lane<L>& ln, bool on, const T* x, const T* g, T* dx,
+                                               int step, const float2 (&c)[2], const float2 (&s)[2], const float2 (&wu)[2],
+                                               const float2 (&wv)[2], float2 (&dw)[4]) {
+  uint2 ga[N], gb[N], xa[N], xb[N];
 #pragma unroll
-    for (int i = 0; i < BWD_AHEAD; ++i) {
-      const int at = (h + i * step) * p.dim;
-      ga[i] = gb[i] = xa[i] = xb[i] = make_uint2(0, 0);
-      if (on && h + i * step < n) {
-        ga[i] = load4(g + at + ln.a);
-        gb[i] = load4(g + at + ln.b);
-        if (norm) {
-          xa[i] = load4(x + at + ln.a);
-          xb[i] = load4(x + at + ln.b);
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < BWD_AHEAD; ++i) {
-      if (h + i * step >= n) break;
-      float2 u[2], v[2];
-      unpack<T, INTERLEAVED>(ga[i], gb[i], u, v);
-      if (ln.rotated) {  // back, by -a
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float2 t = fma_f32x2(v[e], s[e], mul_f32x2(u[e], c[e]));
-          v[e] = fma_f32x2(neg(u[e]), s[e], mul_f32x2(v[e], c[e]));
-          u[e] = t;
-        }
-      }
-      if (norm) {
-        float2 xu[2], xv[2], ss = make_float2(0.f, 0.f), dot = ss, tu[2], tv[2];
-        unpack<T, INTERLEAVED>(xa[i], xb[i], xu, xv);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          ss = fma_f32x2(xu[e], xu[e], ss);
-          ss = fma_f32x2(xv[e], xv[e], ss);
-          tu[e] = mul_f32x2(u[e], xu[e]);
-          tv[e] = mul_f32x2(v[e], xv[e]);
-          dot = fma_f32x2(tu[e], wu[e], dot);
-          dot = fma_f32x2(tv[e], wv[e], dot);
-        }
-        const float r = rsqrtf(fmaf(ln.sum(ss.x + ss.y), p.per_dim, p.eps));
-        const float m = -r * r * r * ln.sum(dot.x + dot.y) * p.per_dim;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          dw[e] = fma_f32x2(tu[e], both(r), dw[e]);
-          dw[2 + e] = fma_f32x2(tv[e], both(r), dw[2 + e]);
-          u[e] = fma_f32x2(xu[e], both(m), mul_f32x2(mul_f32x2(u[e], wu[e]), both(r)));
-          v[e] = fma_f32x2(xv[e], both(m), mul_f32x2(mul_f32x2(v[e], wv[e]), both(r)));
-        }
-      }
-      if (on) {
-        uint2 oa, ob;
-        pack<T, INTERLEAVED>(u, v, oa, ob);
-        store4(dx + (h + i * step) * p.dim + ln.a, oa);
-        store4(dx + (h + i * step) * p.dim + ln.b, ob);
+  for (int i = 0; i < N; ++i) {
+    ga[i] = gb[i] = xa[i] = xb[i] = make_uint2(0, 0);
+    if (on) {
+      ga[i] = load4(g + i * step + ln.a);
+      gb[i] = load4(g + i * step + ln.b);
+      if (NORM) {
+        xa[i] = load4(x + i * step + ln.a);
+        xb[i] = load4(x + i * step + ln.b);
       }
     }
   }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float2 u[2], v[2];
+    unpack<T, INTERLEAVED>(ga[i], gb[i], u, v);
+    if (ln.rotated) {  // back, by -a
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float2 t = fma_f32x2(v[e], s[e], mul_f32x2(u[e], c[e]));
+        v[e] = fma_f32x2(neg(u[e]), s[e], mul_f32x2(v[e], c[e]));
+        u[e] = t;
+      }
+    }
+    if (NORM) {
+      float2 xu[2], xv[2], ss = make_float2(0.f, 0.f), dot = ss, tu[2], tv[2];
+      unpack<T, INTERLEAVED>(xa[i], xb[i], xu, xv);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        ss = fma_f32x2(xu[e], xu[e], ss);
+        ss = fma_f32x2(xv[e], xv[e], ss);
+        tu[e] = mul_f32x2(u[e], xu[e]);
+        tv[e] = mul_f32x2(v[e], xv[e]);
+        dot = fma_f32x2(tu[e], wu[e], dot);
+        dot = fma_f32x2(tv[e], wv[e], dot);
+      }
+      const float r = rsqrtf(fmaf(ln.sum(ss.x + ss.y), p.per_dim, p.eps));
+      const float m = -r * r * r * ln.sum(dot.x + dot.y) * p.per_dim;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        dw[e] = fma_f32x2(tu[e], both(r), dw[e]);
+        dw[2 + e] = fma_f32x2(tv[e], both(r), dw[2 + e]);
+        u[e] = fma_f32x2(xu[e], both(m), mul_f32x2(mul_f32x2(u[e], wu[e]), both(r)));
+        v[e] = fma_f32x2(xv[e], both(m), mul_f32x2(mul_f32x2(v[e], wv[e]), both(r)));
+      }
+    }
+    pack<T, INTERLEAVED>(u, v, ga[i], gb[i]);
+  }
+  if (!on) return;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    store4(dx + i * step + ln.a, ga[i]);
+    store4(dx + i * step + ln.b, gb[i]);
+  }
 }
 
-template <typename T, int L, bool INTERLEAVED>
-__global__ void __launch_bounds__(THREADS, 2) qk_norm_rope_backward_kernel(const RopeArgs p) {
-  extern __shared__ float sm[];  // [16][THREADS] weight gradients of the lanes
+template <typename T, int L, bool INTERLEAVED, bool NORM>
+__global__ void __launch_bounds__(THREADS, BWD_CTAS) qk_norm_rope_backward_kernel(const RopeArgs p) {
+  extern __shared__ float sm[];  // [8][THREADS] weight gradients of the lanes
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Lane<L> ln(p, lane);
   pdl_wait();
   pdl_launch_dependents();
-  float2 dw[2][4];  // of a lane's 8 values: queries, keys
+  // queries, then keys: the weights and their gradients of one kind are live at a time
+  for (int kind = 0; kind < 2; ++kind) {
+    const void* weight = kind ? p.k_weight : p.q_weight;
+    const int n = kind ? p.kv_heads : p.heads;
+    float2 dw[4], wu[2], wv[2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) dw[0][i] = dw[1][i] = make_float2(0.f, 0.f);
-  float2 wu[2][2], wv[2][2];
-  load_weight<T, INTERLEAVED>(p.q_weight, ln, wu[0], wv[0]);
-  load_weight<T, INTERLEAVED>(p.k_weight, ln, wu[1], wv[1]);
-
-  for (int index = blockIdx.x * WARPS + warp; index < p.row_sets * p.row_warps; index += gridDim.x * WARPS) {
-    const int set = index / p.row_warps, part = index - set * p.row_warps;
-    const long long mine = static_cast<long long>(set) * ln.heads + ln.group;
-    const bool on = ln.active && mine < p.n_rows;
-    const int row = on ? static_cast<int>(mine) : 0;
-    float2 c[2], s[2];
-    angles(p, ln, row, c, s);
-    backward_heads<T, L, INTERLEAVED>(p, ln, on, p.q_weight != nullptr, static_cast<const T*>(p.q) + row * p.q_stride,
-                                      static_cast<const T*>(p.grad_q) + row * p.grad_q_stride,
-                                      static_cast<T*>(p.q_out) + row * p.q_out_stride, part, p.heads, c, s, wu[0], wv[0], dw[0]);
-    backward_heads<T, L, INTERLEAVED>(p, ln, on, p.k_weight != nullptr, static_cast<const T*>(p.k) + row * p.k_stride,
-                                      static_cast<const T*>(p.grad_k) + row * p.grad_k_stride,
-                                      static_cast<T*>(p.k_out) + row * p.k_out_stride, first_head(p, part, p.heads), p.kv_heads,
-                                      c, s, wu[1], wv[1], dw[1]);
-  }
-  if (!p.partial) return;
-  // the CTA's sums, over its warps and the heads of a step in order
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
-      sm[(4 * i + kind) * THREADS + threadIdx.x] = dw[kind][i].x;
-      sm[(4 * i + 2 + kind) * THREADS + threadIdx.x] = dw[kind][i].y;
+    for (int i = 0; i < 4; ++i) dw[i] = make_float2(0.f, 0.f);
+    load_weight<T, INTERLEAVED>(weight, ln, wu, wv);
+    for (int index = blockIdx.x * WARPS + warp; index < p.row_sets * p.row_warps; index += gridDim.x * WARPS) {
+      const int set = index / p.row_warps, part = index - set * p.row_warps, step = p.row_warps * p.dim;
+      int h = kind ? first_head(p, part, p.heads) : part;
+      if (h >= n) continue;
+      const long long mine = static_cast<long long>(set) * ln.heads + ln.group;
+      const bool on = ln.active && mine < p.n_rows;
+      const int row = on ? static_cast<int>(mine) : 0;
+      const T* x = static_cast<const T*>(kind ? p.k : p.q) + row * (kind ? p.k_stride : p.q_stride) + h * p.dim;
+      const T* g = static_cast<const T*>(kind ? p.grad_k : p.grad_q) + row * (kind ? p.grad_k_stride : p.grad_q_stride) + h * p.dim;
+      T* dx = static_cast<T*>(kind ? p.k_out : p.q_out) + row * (kind ? p.k_out_stride : p.q_out_stride) + h * p.dim;
+      float2 c[2], s[2];
+      angles(p, ln, row, c, s);
+      const auto heads = [&](auto norm, auto count) {
+        constexpr int N = decltype(count)::value;
+        backward_heads<T, L, INTERLEAVED, decltype(norm)::value, N>(p, ln, on, x, g, dx, step, c, s, wu, wv, dw);
+        h += N * p.row_warps;
+        x += N * step;
+        g += N * step;
+        dx += N * step;
+      };
+      const auto all = [&](auto norm) {
+        while (h + (BWD_AHEAD - 1) * p.row_warps < n) heads(norm, std::integral_constant<int, BWD_AHEAD>{});
+        while (h < n) heads(norm, std::integral_constant<int, 1>{});
+      };
+      if (NORM && weight) {
+        all(std::bool_constant<NORM>{});
+      } else {
+        all(std::false_type{});
+      }
     }
-  __syncthreads();
-  const int lanes = ln.per_head;
-  for (int e = threadIdx.x; e < 16 * lanes; e += THREADS) {
-    const int i = e / (2 * lanes), kind = e / lanes & 1, l = e % lanes;  // i: first values 0 to 3, then second ones
-    float sum = 0.f;
-    for (int w = 0; w < WARPS; ++w)
-      for (int g = 0; g < ln.heads; ++g) sum += sm[(i * 2 + kind) * THREADS + w * 32 + g * lanes + l];
-    const bool split = l < p.rot >> 3 && !INTERLEAVED;
-    const int d = INTERLEAVED ? 8 * l + 2 * (i & 3) + (i >> 2) : split ? (i < 4 ? 4 * l + i : p.rot / 2 + 4 * l + i - 4) : 8 * l + i;
-    p.partial[(static_cast<size_t>(blockIdx.x) * 2 + kind) * p.dim + d] = sum;
+    if (!p.partial) continue;
+    // the CTA's sums, over its warps and rows in order
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sm[2 * i * THREADS + threadIdx.x] = dw[i].x;
+      sm[(2 * i + 1) * THREADS + threadIdx.x] = dw[i].y;
+    }
+    __syncthreads();
+    const int lanes = ln.per_head;
+    for (int e = threadIdx.x; e < 8 * lanes; e += THREADS) {
+      const int i = e / lanes, l = e - i * lanes;  // i: first values 0 to 3, then second ones
+      float sum = 0.f;
+      for (int w = 0; w < WARPS; ++w)
+        for (int g = 0; g < ln.heads; ++g) sum += sm[i * THREADS + w * 32 + g * lanes + l];
+      const bool split = l < p.rot >> 3 && !INTERLEAVED;
+      const int d = INTERLEAVED ? 8 * l + 2 * (i & 3) + (i >> 2) : split ? (i < 4 ? 4 * l + i : p.rot / 2 + 4 * l + i - 4) : 8 * l + i;
+      p.partial[(static_cast<size_t>(blockIdx.x) * 2 + kind) * p.dim + d] = sum;
+    }
+    __syncthreads();  // the sums are read before the other kind's
   }
 }
 
@@ -451,17 +495,25 @@ int row_warps(int row_sets, int heads, int ctas, int sms) {
   return static_cast<int>(std::max<long long>(1, std::min<long long>(heads, slots / std::max(1, row_sets))));
 }
 
-// Calls f with the type, the lanes of a head (0: not a power of two of 8 to 32) and the order of the pairs as types.
+// Calls f with the type, the lanes of a head (0: any), the order of the pairs and whether there is a weight as types.
 template <typename F>
-cudaError_t dispatch(const ivit_rope_config& c, F f) {
+cudaError_t dispatch(const ivit_rope_config& c, bool norm, F f) {
+  const auto norms = [&](auto type, auto lanes, auto order) {
+    return norm ? f(type, lanes, order, std::true_type{}) : f(type, lanes, order, std::false_type{});
+  };
   const auto order = [&](auto type, auto lanes) {
-    return c.interleaved ? f(type, lanes, std::true_type{}) : f(type, lanes, std::false_type{});
+    return c.interleaved ? norms(type, lanes, std::true_type{}) : norms(type, lanes, std::false_type{});
   };
   const auto width = [&](auto type) {
-    return c.head_dim == 64    ? order(type, std::integral_constant<int, 8>{})
-           : c.head_dim == 128 ? order(type, std::integral_constant<int, 16>{})
-           : c.head_dim == 256 ? order(type, std::integral_constant<int, 32>{})
-                               : order(type, std::integral_constant<int, 0>{});
+    switch (c.head_dim) {
+      case 64: return order(type, std::integral_constant<int, 8>{});
+      case 72: return order(type, std::integral_constant<int, 9>{});
+      case 80: return order(type, std::integral_constant<int, 10>{});
+      case 96: return order(type, std::integral_constant<int, 12>{});
+      case 128: return order(type, std::integral_constant<int, 16>{});
+      case 256: return order(type, std::integral_constant<int, 32>{});
+      default: return order(type, std::integral_constant<int, 0>{});
+    }
   };
   return c.dtype == IVIT_BF16 ? width(bf16{}) : width(half{});
 }
@@ -533,12 +585,12 @@ extern "C" int ivit_qk_norm_rope(const ivit_rope_config* cfg, int32_t n_rows, co
   p.k_out_stride = k_out_stride;
   p.pos_stride = pos_stride;
   if (cache) p.cache = paged(*cache);
-  p.row_warps = row_warps(p.row_sets, cfg->heads + cfg->kv_heads * (v_dev ? 2 : 1), 3, sms);
+  p.row_warps = row_warps(p.row_sets, cfg->heads + cfg->kv_heads * (v_dev ? 2 : 1), FWD_CTAS, sms);
   const long long blocks = (static_cast<long long>(p.row_sets) * p.row_warps + WARPS - 1) / WARPS;
   const dim3 grid(static_cast<unsigned>(blocks));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = dispatch(*cfg, [&](auto type, auto lanes, auto inter) {
-    return launch_ex(qk_norm_rope_kernel<decltype(type), lanes(), inter()>, grid, dim3(THREADS), 0, s, 1, p);
+  const cudaError_t e = dispatch(*cfg, q_weight_dev || k_weight_dev, [&](auto type, auto lanes, auto order, auto norm) {
+    return launch_ex(qk_norm_rope_kernel<decltype(type), lanes(), order(), norm()>, grid, dim3(THREADS), 0, s, 1, p);
   });
   return e == cudaSuccess ? IVIT_OK : fail_cuda(e);
 }
@@ -595,15 +647,16 @@ extern "C" int ivit_qk_norm_rope_backward(const ivit_rope_config* cfg, int32_t n
   p.q_out_stride = dq_stride;
   p.k_out_stride = dk_stride;
   p.pos_stride = pos_stride;
-  p.row_warps = row_warps(p.row_sets, cfg->heads + cfg->kv_heads, 2, sms);
+  p.row_warps = row_warps(p.row_sets, cfg->heads + cfg->kv_heads, BWD_CTAS, sms);
   const long long blocks = (static_cast<long long>(p.row_sets) * p.row_warps + WARPS - 1) / WARPS;
-  const int most = min(BWD_CTAS_MAX, 2 * sms), grid = static_cast<int>(blocks < most ? blocks : most);
+  const int most = min(BWD_CTAS_MAX, BWD_CTAS * sms), grid = static_cast<int>(blocks < most ? blocks : most);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   if (grid > 0) {
-    const size_t smem = weights ? sizeof(float) * 16 * THREADS : 0;
-    e = dispatch(*cfg, [&](auto type, auto lanes, auto inter) {
-      return launch_ex(qk_norm_rope_backward_kernel<decltype(type), lanes(), inter()>, dim3(grid), dim3(THREADS), smem, s, 1, p);
+    const size_t smem = weights ? sizeof(float) * 8 * THREADS : 0;
+    e = dispatch(*cfg, q_weight_dev || k_weight_dev, [&](auto type, auto lanes, auto order, auto norm) {
+      return launch_ex(qk_norm_rope_backward_kernel<decltype(type), lanes(), order(), norm()>, dim3(grid), dim3(THREADS), smem, s,
+                       1, p);
     });
   }
   if (e == cudaSuccess && weights)
