@@ -16,8 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT_DIR, "libivit.so")
 SOURCES = ["gemm.cu", "gemm_pair.cu", "ops.cu", "attention.cu", "attention_rows.cu", "persistent.cu", "stream.cu", "engine.cu", "noalloc.cu",
-           "action.cu", "step_plan.cu", "rope.cu", "tree_attention.cu", "kv_write.cu"]
-HEADERS = ["ptx.cuh", "internal.h", "select.cuh", "attention.cuh", "gelu.cuh", "backbone.cuh"]
+           "action.cu", "step_plan.cu", "rope.cu", "tree_attention.cu", "tree_attention_tc.cu", "kv_write.cu"]
+HEADERS = ["ptx.cuh", "internal.h", "select.cuh", "attention.cuh", "gelu.cuh", "backbone.cuh", "tree_attention.cuh"]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include")]

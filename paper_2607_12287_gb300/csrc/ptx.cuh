@@ -482,6 +482,11 @@ __device__ __forceinline__ void fence_proxy_async_global() {
   asm volatile("fence.proxy.async.global;" ::: "memory");
 }
 
+// The same for shared memory.
+__device__ __forceinline__ void fence_proxy_async_smem() {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+
 // ------------------------------------------------------------- kernel timeline
 // Optional per-launch stamps (the library's timeline mode): thread 0 of CTA b writes
 // the global time after the kernel's wait on the previous kernel to s[2b] and the time

@@ -23,33 +23,16 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "attention.cuh"
-#include "backbone.cuh"
+#include "tree_attention.cuh"
 
 namespace ivit {
 namespace {
 
 constexpr int TK = 64;              // keys of a tile
-constexpr int MAX_REQ = 4096;
-constexpr int MAX_SMS = 256;        // the workspace has parts for that many
-// Probabilities are kept 2^SHIFT times too large, which keeps small fp16 ones normal.
-constexpr float SHIFT = 10.f;
-// A row's reference maximum moves when a tile exceeds it by more than 2^GROWTH, not before: the output is
-// rescaled a few times per run instead of for most tiles, and 2^(SHIFT + GROWTH) is an fp16 number.
-constexpr float GROWTH = 5.f;
+constexpr int TC_ROWS = 64;         // more rows per key head than this take the tcgen05 kernel
 
-struct TreeArgs {
-  const void *q, *k_new, *v_new, *k_cache, *v_cache;
-  const int *table, *len, *cu;
-  const uint32_t* mask;
-  void* out;
-  float *lse, *parts;
-  int4* joins;                      // [CTAs] the tile that CTA c's run begins and others go on with: request (-1:
-                                    // none), key head, row tile, 2 * last CTA + whether it is c's second part
-  long long q_stride, k_new_stride, v_new_stride, out_stride;
-  PagedCache cache;
-  int n_req, n_rows, heads, group, max_pages, max_new, mask_mode, mask_words;
-  float scale_log2;                 // scale * log2(e)
+struct Keys64 {
+  static __device__ __forceinline__ int tiles(const TreeRequest& r) { return (r.len + r.n + TK - 1) / TK; }
 };
 
 template <typename T>
@@ -88,52 +71,6 @@ __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// Rows and cached tokens of a request, within the bounds the host vouches for.
-struct Request {
-  int row0, n, len;
-};
-
-__device__ __forceinline__ Request request(const TreeArgs& a, int i) {
-  Request r;
-  const int lo = a.cu[i], hi = a.cu[i + 1], most = a.max_pages << a.cache.page_shift;
-  r.row0 = min(max(lo, 0), a.n_rows);
-  r.n = min(max(min(hi, a.n_rows) - r.row0, 0), a.max_new);
-  r.len = min(max(a.len[i], 0), most);
-  return r;
-}
-
-__device__ __forceinline__ int key_tiles(const Request& r) { return r.n > 0 ? (r.len + r.n + TK - 1) / TK : 0; }
-
-template <int M>
-__device__ __forceinline__ int row_tiles(const TreeArgs& a, const Request& r) {
-  return (r.n * a.group + M - 1) / M;
-}
-
-// A place in the order of units (request, key head, row tile, key tile).
-template <int M>
-struct Place {
-  Request r;
-  int req, head, rt, kt, nkt, nrt;
-
-  __device__ __forceinline__ void enter(const TreeArgs& a, int i) {  // the first unit of request i or later
-    for (req = i; req < a.n_req; ++req) {
-      r = request(a, req);
-      if (r.n > 0) break;
-    }
-    nkt = key_tiles(r);
-    nrt = row_tiles<M>(a, r);
-    head = rt = kt = 0;
-  }
-  __device__ __forceinline__ void next(const TreeArgs& a) {
-    if (++kt < nkt) return;
-    kt = 0;
-    if (++rt < nrt) return;
-    rt = 0;
-    if (++head < a.cache.heads) return;
-    enter(a, req + 1);
-  }
-};
-
 template <int DP, int RW>
 struct Cfg {
   static constexpr int M = 16 * RW, KW = RW < 4 ? 4 / RW : 1, WK = TK / KW;  // rows, warps along the keys, keys of a warp
@@ -151,8 +88,8 @@ struct Cfg {
   static constexpr int OFF_MEET = OFF_Q + (QSMEM ? M * ROW : 0);
   static constexpr int OFF_FLAGS = OFF_MEET + (KW > 1 ? M * (MEET + 2) * 4 : 0);
   static constexpr int BYTES = OFF_FLAGS + STAGES * 8;
-  static constexpr int PART = M * (DP + 2);                                  // floats of a part in the workspace
-  static_assert(MAX_REQ * 8 <= OFF_Q, "the units before each request");
+  static constexpr int PART = tree_part_floats(M, DP);
+  static_assert(TREE_MAX_REQ * 8 <= OFF_Q, "the units before each request");
   static_assert(BYTES <= (CTAS == 2 ? 113 : 227) * 1024 - 128, "shared memory of an SM");
 };
 
@@ -163,7 +100,7 @@ __device__ __forceinline__ uint32_t piece(uint32_t tile, int row, int c) {
 }
 
 // Which of the 64 keys from k0 on new row `node` of the request sees (bit j: key k0 + j).
-__device__ __forceinline__ uint64_t seen(const TreeArgs& a, const Request& r, int node, int k0) {
+__device__ __forceinline__ uint64_t seen(const TreeArgs& a, const TreeRequest& r, int node, int k0) {
   const auto low = [](int n) { return n >= 64 ? ~0ull : n > 0 ? (1ull << n) - 1 : 0ull; };
   const int first = k0 - r.len;  // new row of bit 0 (negative: cached tokens up to there)
   if (a.mask_mode == IVIT_MASK_CAUSAL) return low(node + 1 - first);
@@ -195,55 +132,11 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
   pdl_wait();
   pdl_launch_dependents();
 
-  // units before each request, and this CTA's run [lo, hi)
-  __shared__ unsigned long long carry[THREADS / 32];
-  unsigned long long* before = reinterpret_cast<unsigned long long*>(sm);
-  unsigned long long total = 0;
-  for (int i0 = 0; i0 < a.n_req; i0 += THREADS) {
-    const int i = i0 + tid;
-    unsigned long long n = 0;
-    if (i < a.n_req) {
-      const Request r = request(a, i);
-      n = static_cast<unsigned long long>(key_tiles(r)) * row_tiles<M>(a, r) * a.cache.heads;
-    }
-    unsigned long long run = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const unsigned long long up = __shfl_up_sync(0xffffffffu, run, o);
-      if (lane >= o) run += up;
-    }
-    if (lane == 31) carry[warp] = run;
-    __syncthreads();
-    unsigned long long ahead = total;
-#pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-      if (w < warp) ahead += carry[w];
-      total += carry[w];
-    }
-    if (i < a.n_req) before[i] = ahead + run - n;
-    __syncthreads();
-  }
-  // (no more runs than units, so that no run is empty between two that share a tile)
-  const unsigned long long ctas = total < gridDim.x ? total : gridDim.x;
-  if (tid == 0) a.joins[blockIdx.x].x = -1;
-  if (blockIdx.x >= ctas) return;
-  const unsigned long long lo = total * blockIdx.x / ctas, hi = total * (blockIdx.x + 1) / ctas;
-  Place<M> load;
-  {
-    int i = 0, j = a.n_req - 1;  // last request with before <= lo: it has units
-    while (i < j) {
-      const int mid = (i + j + 1) >> 1;
-      if (before[mid] <= lo) i = mid; else j = mid - 1;
-    }
-    const unsigned long long off = lo - before[i];
-    load.enter(a, i);
-    const unsigned long long per = static_cast<unsigned long long>(load.nkt) * load.nrt;
-    load.head = static_cast<int>(off / per);
-    const unsigned rest = static_cast<unsigned>(off - load.head * per);
-    load.rt = rest / load.nkt;
-    load.kt = rest - load.rt * load.nkt;
-  }
-  __syncthreads();  // `before` gives way to the tiles
+  if (blockIdx.x == 0 && tid == 0) *a.err = 0;  // (nothing here waits on a barrier that could fail)
+  TreeRun<Keys64> run{};
+  if (!run.find<THREADS>(a, reinterpret_cast<unsigned long long*>(sm))) return;
+  TreePlace<Keys64> load = run.at, at = run.at;
+  const int units = static_cast<int>(run.hi - run.lo);
   if (pieces < PIECES) {
     // columns past a head's are zero for good: no copy touches them
     for (int x = tid; x < STAGES * 2 * TK * (PIECES - pieces); x += THREADS) {
@@ -251,8 +144,6 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
       *reinterpret_cast<uint4*>(sm + (row * ROW + ((c ^ (row & 7)) << 4))) = make_uint4(0, 0, 0, 0);
     }
   }
-  Place<M> at = load;
-  const int units = static_cast<int>(hi - lo);
 
   // A copy's part of this thread: piece cp of the rows r0, r0 + RP, ... of a tile.
   const int cp = tid % C::CP, r0 = tid / C::CP, page_mask = (1 << a.cache.page_shift) - 1;
@@ -400,115 +291,117 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
     __syncthreads();  // everyone's copies have landed, and the stage of the tile before is free
     fill((u + STAGES - 1) % STAGES);
 
-    // scores of the warp's keys
-    float s[WK / 8][4];
-#pragma unroll
-    for (int j = 0; j < WK / 8; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[j][e] = 0.f;
-#pragma unroll
-    for (int c = 0; c < DP / 16; ++c) {
-      if (C::QSMEM) ldmatrix4(q[0], piece<ROW>(sb + C::OFF_Q, rw * 16 + (lane & 15), 2 * c + (lane >> 4)));
-#pragma unroll
-      for (int j = 0; j < WK / 16; ++j) {
-        uint32_t b[4];
-        const int row = kw * WK + 16 * j + (lane & 7) + ((lane & 16) >> 1);
-        ldmatrix4(b, piece<ROW>(ks, row, 2 * c + (lane >> 3 & 1)));
-        mma<T>(s[2 * j], q[C::QSMEM ? 0 : c], b[0], b[1]);
-        mma<T>(s[2 * j + 1], q[C::QSMEM ? 0 : c], b[2], b[3]);
-      }
-    }
-    if (edge) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const uint64_t bits = node[r] >= 0 ? seen(a, at.r, node[r], k0) >> (kw * WK) : 0;
-#pragma unroll
-        for (int j = 0; j < WK / 8; ++j)
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (!(bits >> (8 * j + 2 * t + e) & 1)) s[j][2 * r + e] = -INFINITY;
-      }
-    }
-    // probabilities against the reference maximum, and their sum
-    float mx[2];
-    bool grow = false;
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      mx[r] = s[0][2 * r];
-#pragma unroll
-      for (int j = 0; j < WK / 8; ++j) mx[r] = fmaxf(mx[r], fmaxf(s[j][2 * r], s[j][2 * r + 1]));
-      mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
-      mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2));
-      grow |= (mx[r] - m[r]) * a.scale_log2 > GROWTH;
-    }
-    if (__any_sync(0xffffffffu, grow)) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        if (!(mx[r] > m[r])) continue;
-        const float alpha = ex2((m[r] - mx[r]) * a.scale_log2);
-        m[r] = mx[r];
-        l[r] *= alpha;
-#pragma unroll
-        for (int j = 0; j < DP / 8; ++j) {
-          o[j][2 * r] *= alpha;
-          o[j][2 * r + 1] *= alpha;
-        }
-      }
-    }
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const float mo = SHIFT - (m[r] == -INFINITY ? 0.f : m[r] * a.scale_log2);  // (nothing seen so far: P = 0)
-      float sum[2] = {0.f, 0.f};
+    if (at.rt * M + rw * 16 < at.r.n * a.group) {  // (else the warp's rows are all padding)
+      // scores of the warp's keys
+      float s[WK / 8][4];
 #pragma unroll
       for (int j = 0; j < WK / 8; ++j)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          s[j][2 * r + e] = ex2(fmaf(s[j][2 * r + e], a.scale_log2, mo));
-          sum[e] += s[j][2 * r + e];
-        }
-      l[r] += sum[0] + sum[1];
-    }
-#pragma unroll
-    for (int j = 0; j < WK / 16; ++j) {
-      uint32_t p[C::TERMS][4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float& x = s[2 * j + (e >> 1)][2 * (e & 1)];
-        float& y = s[2 * j + (e >> 1)][2 * (e & 1) + 1];
-        p[0][e] = pack2<T>(x, y);
-        if (C::TERMS == 2) {
-          const float2 h = unpack2<T>(p[0][e]);
-          p[C::TERMS - 1][e] = pack2<T>(x - h.x, y - h.y);
-        }
-      }
+        for (int e = 0; e < 4; ++e) s[j][e] = 0.f;
 #pragma unroll
       for (int c = 0; c < DP / 16; ++c) {
-        uint32_t b[4];
-        const int row = kw * WK + 16 * j + (lane & 15);
-        ldmatrix4_trans(b, piece<ROW>(vs, row, 2 * c + (lane >> 4)));
+        if (C::QSMEM) ldmatrix4(q[0], piece<ROW>(sb + C::OFF_Q, rw * 16 + (lane & 15), 2 * c + (lane >> 4)));
 #pragma unroll
-        for (int x = 0; x < C::TERMS; ++x) {
-          mma<T>(o[2 * c], p[x], b[0], b[1]);
-          mma<T>(o[2 * c + 1], p[x], b[2], b[3]);
+        for (int j = 0; j < WK / 16; ++j) {
+          uint32_t b[4];
+          const int row = kw * WK + 16 * j + (lane & 7) + ((lane & 16) >> 1);
+          ldmatrix4(b, piece<ROW>(ks, row, 2 * c + (lane >> 3 & 1)));
+          mma<T>(s[2 * j], q[C::QSMEM ? 0 : c], b[0], b[1]);
+          mma<T>(s[2 * j + 1], q[C::QSMEM ? 0 : c], b[2], b[3]);
         }
       }
-    }
-    if (edge && (flags[2 * stage] | flags[2 * stage + 1])) {
-      // values that are not finite, for the rows that see them
-      for (int k = kw * WK; k < (kw + 1) * WK; ++k) {
-        if (!(flags[2 * stage + (k >> 5)] >> (k & 31) & 1)) continue;
-        const T* v = static_cast<const T*>(a.v_new) + (at.r.row0 + k0 + k - at.r.len) * a.v_new_stride + at.head * a.cache.dim;
+      if (edge) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r)
-          if (node[r] >= 0 && seen(a, at.r, node[r], k0) >> k & 1) {
+        for (int r = 0; r < 2; ++r) {
+          const uint64_t bits = node[r] >= 0 ? seen(a, at.r, node[r], k0) >> (kw * WK) : 0;
 #pragma unroll
-            for (int j = 0; j < DP / 8; ++j)
-              if (8 * j < a.cache.dim) {
-                const float2 x = unpack2<T>(*reinterpret_cast<const uint32_t*>(v + 8 * j + 2 * t));
-                if (!isfinite(x.x)) o[j][2 * r] += x.x;
-                if (!isfinite(x.y)) o[j][2 * r + 1] += x.y;
-              }
+          for (int j = 0; j < WK / 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              if (!(bits >> (8 * j + 2 * t + e) & 1)) s[j][2 * r + e] = -INFINITY;
+        }
+      }
+      // probabilities against the reference maximum, and their sum
+      float mx[2];
+      bool grow = false;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        mx[r] = s[0][2 * r];
+#pragma unroll
+        for (int j = 0; j < WK / 8; ++j) mx[r] = fmaxf(mx[r], fmaxf(s[j][2 * r], s[j][2 * r + 1]));
+        mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
+        mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2));
+        grow |= (mx[r] - m[r]) * a.scale_log2 > TREE_GROWTH;
+      }
+      if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          if (!(mx[r] > m[r])) continue;
+          const float alpha = ex2((m[r] - mx[r]) * a.scale_log2);
+          m[r] = mx[r];
+          l[r] *= alpha;
+#pragma unroll
+          for (int j = 0; j < DP / 8; ++j) {
+            o[j][2 * r] *= alpha;
+            o[j][2 * r + 1] *= alpha;
           }
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const float mo = TREE_SHIFT - (m[r] == -INFINITY ? 0.f : m[r] * a.scale_log2);  // (nothing seen so far: P = 0)
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < WK / 8; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            s[j][2 * r + e] = ex2(fmaf(s[j][2 * r + e], a.scale_log2, mo));
+            sum[e] += s[j][2 * r + e];
+          }
+        l[r] += sum[0] + sum[1];
+      }
+#pragma unroll
+      for (int j = 0; j < WK / 16; ++j) {
+        uint32_t p[C::TERMS][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float& x = s[2 * j + (e >> 1)][2 * (e & 1)];
+          float& y = s[2 * j + (e >> 1)][2 * (e & 1) + 1];
+          p[0][e] = pack2<T>(x, y);
+          if (C::TERMS == 2) {
+            const float2 h = unpack2<T>(p[0][e]);
+            p[C::TERMS - 1][e] = pack2<T>(x - h.x, y - h.y);
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) {
+          uint32_t b[4];
+          const int row = kw * WK + 16 * j + (lane & 15);
+          ldmatrix4_trans(b, piece<ROW>(vs, row, 2 * c + (lane >> 4)));
+#pragma unroll
+          for (int x = 0; x < C::TERMS; ++x) {
+            mma<T>(o[2 * c], p[x], b[0], b[1]);
+            mma<T>(o[2 * c + 1], p[x], b[2], b[3]);
+          }
+        }
+      }
+      if (edge && (flags[2 * stage] | flags[2 * stage + 1])) {
+        // values that are not finite, for the rows that see them
+        for (int k = kw * WK; k < (kw + 1) * WK; ++k) {
+          if (!(flags[2 * stage + (k >> 5)] >> (k & 31) & 1)) continue;
+          const T* v = static_cast<const T*>(a.v_new) + (at.r.row0 + k0 + k - at.r.len) * a.v_new_stride + at.head * a.cache.dim;
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            if (node[r] >= 0 && seen(a, at.r, node[r], k0) >> k & 1) {
+#pragma unroll
+              for (int j = 0; j < DP / 8; ++j)
+                if (8 * j < a.cache.dim) {
+                  const float2 x = unpack2<T>(*reinterpret_cast<const uint32_t*>(v + 8 * j + 2 * t));
+                  if (!isfinite(x.x)) o[j][2 * r] += x.x;
+                  if (!isfinite(x.y)) o[j][2 * r + 1] += x.y;
+                }
+            }
+        }
       }
     }
 
@@ -575,7 +468,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
               if (8 * j < a.cache.dim)
                 *reinterpret_cast<uint32_t*>(dst + 8 * j + 2 * t) = pack2<T>(o[j][2 * r] * inv, o[j][2 * r + 1] * inv);
             if (a.lse && t == 0)
-              a.lse[orow * a.heads + h] = (m[r] * a.scale_log2 + (log2f(l[r]) - SHIFT)) * 0.6931471805599453f;
+              a.lse[orow * a.heads + h] = (m[r] * a.scale_log2 + (log2f(l[r]) - TREE_SHIFT)) * 0.6931471805599453f;
           } else {
             if (t == 0) {
               part[M * DP + 2 * row] = m[r];
@@ -587,12 +480,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
           }
         }
       }
-      if (!whole && begun && tid == 0) {
-        // the tile's last unit, and the CTA whose run holds it
-        const unsigned long long last = lo + u - at.kt + at.nkt - 1;
-        const unsigned long long end = ((last + 1) * ctas - 1) / total;
-        a.joins[blockIdx.x] = make_int4(at.req, at.head, at.rt, 2 * static_cast<int>(end) + (u - at.kt > 0 ? 1 : 0));
-      }
+      if (!whole && begun && tid == 0) run.note_join(a, at, run.lo + u - at.kt);
     }
     at.next(a);
   }
@@ -601,9 +489,9 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
 // Joins the parts of the tile of rows that CTA c's run of the attention kernel begins, in the order of
 // their keys: block (c, y) takes every gridDim.y-th group of its rows.  Up to 8 parts are a warp's work,
 // a row each; more are shared by the block's warps, which meet in shared memory.
-template <typename T, int DP, int RW>
+template <typename T, int DP, int M>
 __global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a) {
-  constexpr int M = 16 * RW, PART = Cfg<DP, RW>::PART, WARPS = 8, VEC = (DP / 2 + 31) / 32;
+  constexpr int PART = tree_part_floats(M, DP), WARPS = 8, VEC = (DP / 2 + 31) / 32;
   __shared__ float ms[WARPS], ls[WARPS];
   __shared__ float2 os[WARPS][DP / 2];
   const int c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -611,8 +499,8 @@ __global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a) {
   pdl_launch_dependents();
   const int4 join = a.joins[c];
   if (join.x < 0) return;
-  const Request r = request(a, join.x);
-  const int rows = min(M, r.n * a.group - join.z * M), n = (join.w >> 1) - c + 1;
+  const TreeRequest r = tree_request(a, join.x);
+  const int rows = min(a.tile_rows, r.n * a.group - join.z * a.tile_rows), n = (join.w >> 1) - c + 1;
   // the tile's parts: CTA c's second or first, then the first ones of the CTAs behind it
   const float* parts = a.parts + static_cast<size_t>(2 * c) * PART;
   const int second = join.w & 1;
@@ -669,7 +557,7 @@ __global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a) {
       __syncthreads();  // the sums are read before the next row's
       if (warp != 0) continue;
     }
-    const int x = join.z * M + row, node = x / a.group, h = join.y * a.group + x - node * a.group;
+    const int x = join.z * a.tile_rows + row, node = x / a.group, h = join.y * a.group + x - node * a.group;
     const long long orow = r.row0 + node;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     T* dst = static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * a.cache.dim;
@@ -678,35 +566,74 @@ __global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a) {
       const int d = 2 * (32 * v + lane);
       if (d < a.cache.dim) *reinterpret_cast<uint32_t*>(dst + d) = pack2<T>(o[v].x * inv, o[v].y * inv);
     }
-    if (a.lse && lane == 0) a.lse[orow * a.heads + h] = (m * a.scale_log2 + (log2f(l) - SHIFT)) * 0.6931471805599453f;
+    if (a.lse && lane == 0) a.lse[orow * a.heads + h] = (m * a.scale_log2 + (log2f(l) - TREE_SHIFT)) * 0.6931471805599453f;
   }
 }
 
 bool valid(const ivit_attention_config& c, const ivit_cache_layout& l) {
-  return valid_cache(l) && c.n_req >= 1 && c.n_req <= MAX_REQ && c.heads >= 1 && c.heads <= 256 && c.heads % l.kv_heads == 0 &&
+  return valid_cache(l) && c.n_req >= 1 && c.n_req <= TREE_MAX_REQ && c.heads >= 1 && c.heads <= 256 && c.heads % l.kv_heads == 0 &&
          c.max_pages >= 1 && static_cast<long long>(c.max_pages) * l.page_size < (1LL << 31) - (1 << 20) && c.max_new >= 1 &&
          c.max_new <= 65536 && c.mask_mode >= IVIT_MASK_CAUSAL && c.mask_mode <= IVIT_MASK_TREE && c.mask_words >= 0 &&
          c.mask_words <= 32768 && (c.mask_mode != IVIT_MASK_TREE || c.mask_words > 0) && c.scale > 0.f && c.scale < 1e30f;
 }
 
-// Calls f with the type, the padded head width and the row groups of a tile as types: the smallest of 16, 32, 64
-// and 128 rows that holds the most rows that share a key head, else 128.
-template <typename F>
-auto dispatch(const ivit_attention_config& c, const ivit_cache_layout& l, F f) {
-  const int rows = static_cast<int>(std::min<long long>(128, static_cast<long long>(c.max_new) * (c.heads / l.kv_heads)));
-  const auto groups = [&](auto type, auto dp) {
-    return rows <= 16   ? f(type, dp, std::integral_constant<int, 1>{})
-           : rows <= 32 ? f(type, dp, std::integral_constant<int, 2>{})
-           : rows <= 64 ? f(type, dp, std::integral_constant<int, 4>{})
-                        : f(type, dp, std::integral_constant<int, 8>{});
+// Which kernel, and its sizes: tiles of 16 * rw rows of mma.sync, or with tc the tcgen05 kernel's of up to 128.
+struct Plan {
+  bool tc;
+  int dp, rw, tile_rows, ctas_per_sm, part_floats;
+};
+
+template <int DP, int RW>
+Plan plan_of() {
+  using C = Cfg<DP, RW>;
+  return {false, DP, RW, C::M, C::CTAS, C::PART};
+}
+
+Plan plan(const ivit_attention_config& c, const ivit_cache_layout& l) {
+  const int group = c.heads / l.kv_heads;
+  const int rows = static_cast<int>(std::min<long long>(128, static_cast<long long>(c.max_new) * group));  // that share a key head
+  const int dp = l.head_dim <= 64 ? 64 : l.head_dim <= 80 ? 80 : l.head_dim <= 128 ? 128 : 256;
+  if (rows > TC_ROWS && dp <= 128 && group <= 128 && l.page_size >= 8 && l.head_stride > 0 && l.token_stride > 0 &&
+      l.page_stride > 0)
+    return {true, dp, 0, tree_tc_rows(group), 2, tree_part_floats(128, dp)};
+  // the smallest tile that holds the rows
+  const auto groups = [&](auto d) {
+    constexpr int DP = decltype(d)::value;
+    return rows <= 16 ? plan_of<DP, 1>() : rows <= 32 ? plan_of<DP, 2>() : rows <= 64 ? plan_of<DP, 4>() : plan_of<DP, 8>();
   };
-  const auto width = [&](auto type) {
-    return l.head_dim <= 64    ? groups(type, std::integral_constant<int, 64>{})
-           : l.head_dim <= 80  ? groups(type, std::integral_constant<int, 80>{})
-           : l.head_dim <= 128 ? groups(type, std::integral_constant<int, 128>{})
-                               : groups(type, std::integral_constant<int, 256>{});
+  return dp == 64    ? groups(std::integral_constant<int, 64>{})
+         : dp == 80  ? groups(std::integral_constant<int, 80>{})
+         : dp == 128 ? groups(std::integral_constant<int, 128>{})
+                     : groups(std::integral_constant<int, 256>{});
+}
+
+template <typename T, int DP, int RW>
+cudaError_t launch_rows(const TreeArgs& a, int ctas, cudaStream_t s) {
+  using C = Cfg<DP, RW>;
+  const cudaError_t e = allow_smem<tree_attention_kernel<T, DP, RW>>(C::BYTES);
+  return e != cudaSuccess ? e : launch_ex(tree_attention_kernel<T, DP, RW>, dim3(ctas), dim3(C::THREADS), C::BYTES, s, 1, a);
+}
+
+// The kernel of the plan, then the join.
+template <typename T, int DP>
+cudaError_t launch(const Plan& p, const TreeArgs& a, int dtype, int ctas, cudaStream_t s) {
+  const auto join = [&](auto m) {
+    return launch_ex(tree_join_kernel<T, DP, decltype(m)::value>, dim3(ctas, 4), dim3(256), 0, s, 1, a);
   };
-  return l.dtype == IVIT_BF16 ? width(bf16{}) : width(half{});
+  cudaError_t e;
+  if (p.tc) {
+    e = launch_tree_attention_tc(a, dtype, DP, ctas, s);
+  } else {
+    e = p.rw == 1   ? launch_rows<T, DP, 1>(a, ctas, s)
+        : p.rw == 2 ? launch_rows<T, DP, 2>(a, ctas, s)
+        : p.rw == 4 ? launch_rows<T, DP, 4>(a, ctas, s)
+                    : launch_rows<T, DP, 8>(a, ctas, s);
+  }
+  if (e != cudaSuccess) return e;
+  return p.rw == 1   ? join(std::integral_constant<int, 16>{})
+         : p.rw == 2 ? join(std::integral_constant<int, 32>{})
+         : p.rw == 4 ? join(std::integral_constant<int, 64>{})
+                     : join(std::integral_constant<int, 128>{});
 }
 
 }  // namespace
@@ -715,10 +642,9 @@ auto dispatch(const ivit_attention_config& c, const ivit_cache_layout& l, F f) {
 extern "C" size_t ivit_tree_attention_workspace(const ivit_attention_config* cfg, const ivit_cache_layout* cache) {
   using namespace ivit;
   if (!cfg || !cache || !valid(*cfg, *cache)) return 0;
-  return dispatch(*cfg, *cache, [](auto, auto dp, auto rw) -> size_t {
-    using C = Cfg<dp(), rw()>;
-    return C::CTAS * MAX_SMS * (sizeof(int4) + 2 * sizeof(float) * C::PART);
-  });
+  const Plan p = plan(*cfg, *cache);
+  // the error word, then of each CTA a join and two parts
+  return 16 + static_cast<size_t>(p.ctas_per_sm) * TREE_MAX_SMS * (sizeof(int4) + 2 * sizeof(float) * p.part_floats);
 }
 
 extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_cache_layout* cache, int32_t n_rows,
@@ -759,7 +685,6 @@ extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_
   a.mask = mask_dev;
   a.out = out_dev;
   a.lse = lse_dev;
-  a.joins = static_cast<int4*>(workspace_dev);
   a.q_stride = q_stride;
   a.k_new_stride = k_new_stride;
   a.v_new_stride = v_new_stride;
@@ -775,17 +700,19 @@ extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_
   a.mask_words = cfg->mask_words;
   a.scale_log2 = cfg->scale * 1.4426950408889634f;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = dispatch(*cfg, *cache, [&](auto type, auto dp, auto rw) {
+  const Plan p = plan(*cfg, *cache);
+  const int ctas = p.ctas_per_sm * std::min(TREE_MAX_SMS, sms);
+  a.tile_rows = p.tile_rows;
+  a.err = static_cast<int*>(workspace_dev);
+  a.joins = static_cast<int4*>(workspace_dev) + 1;
+  a.parts = reinterpret_cast<float*>(a.joins + p.ctas_per_sm * TREE_MAX_SMS);
+  const auto width = [&](auto type) {
     using T = decltype(type);
-    using C = Cfg<dp(), rw()>;
-    const auto kernel = tree_attention_kernel<T, dp(), rw()>;
-    cudaError_t err = allow_smem<tree_attention_kernel<T, dp(), rw()>>(C::BYTES);
-    if (err != cudaSuccess) return err;
-    const int ctas = C::CTAS * std::min(MAX_SMS, sms);
-    a.parts = reinterpret_cast<float*>(a.joins + C::CTAS * MAX_SMS);
-    err = launch_ex(kernel, dim3(ctas), dim3(C::THREADS), C::BYTES, s, 1, a);
-    if (err != cudaSuccess) return err;
-    return launch_ex(tree_join_kernel<T, dp(), rw()>, dim3(ctas, 4), dim3(256), 0, s, 1, a);
-  });
+    return p.dp == 64    ? launch<T, 64>(p, a, cache->dtype, ctas, s)
+           : p.dp == 80  ? launch<T, 80>(p, a, cache->dtype, ctas, s)
+           : p.dp == 128 ? launch<T, 128>(p, a, cache->dtype, ctas, s)
+                         : launch<T, 256>(p, a, cache->dtype, ctas, s);
+  };
+  const cudaError_t e = cache->dtype == IVIT_BF16 ? width(bf16{}) : width(half{});
   return e == cudaSuccess ? IVIT_OK : fail_cuda(e);
 }

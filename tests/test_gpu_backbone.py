@@ -368,6 +368,11 @@ ATTENTION = [  # cached, new, heads, kv, dim, page, type, order
     ([100, 300], [17, 5], 5, 1, 256, 128, "float16", "head"), ([257], [3], 2, 2, 256, 16, "bfloat16", "token"),
     ([90, 10], [70, 130], 3, 3, 40, 16, "bfloat16", "token"), ([2000, 3, 777], [4, 4, 4], 8, 8, 8, 1024, "float16", "token"),
     ([33], [7], 32, 1, 200, 4, "bfloat16", "head"),
+    # many rows per key head: tcgen05 tiles, last blocks of every kind, groups that do not divide 128
+    ([300, 95, 96, 97, 0], [65, 96, 20, 1, 130], 8, 4, 72, 8, "bfloat16", "token"),
+    ([191, 192, 500], [128, 33, 97], 5, 1, 80, 128, "float16", "head"), ([700], [256], 2, 2, 64, 64, "bfloat16", "token"),
+    ([0, 0, 127, 128, 129], [140, 3, 128, 129, 70], 2, 2, 64, 16, "float16", "token"),
+    ([0, 64, 200], [75, 64, 1], 7, 1, 128, 16, "bfloat16", "token"), ([500], [65], 6, 2, 112, 256, "bfloat16", "head"),
 ]
 
 
