@@ -29,9 +29,10 @@ namespace ivit {
 namespace {
 
 constexpr int TK = 64;              // keys of a tile
-constexpr int TC_ROWS = 64;         // more rows per key head than this take the tcgen05 kernel
+constexpr int TC_ROWS = 16, TC_ROWS_64 = 64;  // more rows per key head than this take the tcgen05 kernel (heads up to 64)
 
 struct Keys64 {
+  static constexpr int LEAST = 1;
   static __device__ __forceinline__ int tiles(const TreeRequest& r) { return (r.len + r.n + TK - 1) / TK; }
 };
 
@@ -75,22 +76,24 @@ template <int DP, int RW>
 struct Cfg {
   static constexpr int M = 16 * RW, KW = RW < 4 ? 4 / RW : 1, WK = TK / KW;  // rows, warps along the keys, keys of a warp
   static constexpr int THREADS = 32 * RW * KW;
+  // One row group: no two warps share keys, each copies its own, and the walk has no barrier.
+  static constexpr bool ALONE = RW == 1;
   static constexpr int ROW = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;         // bytes of a row in shared memory
   static constexpr int TILE = TK * ROW;
-  static constexpr int CTAS = DP <= 128 && RW < 8 ? 2 : 1;                   // per SM
+  static constexpr int CTAS = ALONE ? (DP <= 64 ? 4 : 2) : DP <= 128 && RW < 8 ? 2 : 1;  // per SM
   static constexpr bool QSMEM = DP > 128;                                    // queries in shared memory, not registers
-  static constexpr int STAGES = DP > 128 ? 2 : 3;
+  static constexpr int STAGES = ALONE ? (DP <= 128 ? 3 : 1) : DP > 128 ? 2 : 3;
   static constexpr int TERMS = RW < 4 ? 2 : 1;
-  // a copy of a tile: CP threads for the pieces of a row, RP rows at a time
-  static constexpr int CP = ROW / 16, RP = THREADS / CP, COPIES = TK / RP;
+  // a copy of a tile (of the warp's keys if it is alone): CP lanes for the pieces of a row, RP rows at a time
+  static constexpr int CP = ROW / 16, RP = (ALONE ? 32 : THREADS) / CP, COPIES = (ALONE ? WK : TK) / RP;
   static constexpr int MEET = DP + 4;                                        // floats of a row where the warps meet
   static constexpr int OFF_Q = STAGES * 2 * TILE;
   static constexpr int OFF_MEET = OFF_Q + (QSMEM ? M * ROW : 0);
   static constexpr int OFF_FLAGS = OFF_MEET + (KW > 1 ? M * (MEET + 2) * 4 : 0);
-  static constexpr int BYTES = OFF_FLAGS + STAGES * 8;
+  static constexpr int BYTES = OFF_FLAGS + 4 * 16;
   static constexpr int PART = tree_part_floats(M, DP);
   static_assert(TREE_MAX_REQ * 8 <= OFF_Q, "the units before each request");
-  static_assert(BYTES <= (CTAS == 2 ? 113 : 227) * 1024 - 128, "shared memory of an SM");
+  static_assert(CTAS * (BYTES + 1024 + 128) <= 228 * 1024, "shared memory of an SM");
 };
 
 // Shared-memory address of 16-byte piece c of a row.
@@ -125,7 +128,8 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
   constexpr int PIECES = DP / 8, COPIES = C::COPIES, RP = C::RP;
   extern __shared__ __align__(128) uint8_t sm[];
   const uint32_t sb = smem_u32(sm);
-  uint32_t* flags = reinterpret_cast<uint32_t*>(sm + C::OFF_FLAGS);  // [STAGES][2] keys whose values are not finite
+  // [tile % 4][16 keys] whose values are not finite; cleared two tiles ahead, a barrier away from their use
+  uint32_t* flags = reinterpret_cast<uint32_t*>(sm + C::OFF_FLAGS);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int rw = warp / KW, kw = warp % KW;  // row group and key group of the warp
   const int pieces = a.cache.dim >> 3;
@@ -146,7 +150,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
   }
 
   // A copy's part of this thread: piece cp of the rows r0, r0 + RP, ... of a tile.
-  const int cp = tid % C::CP, r0 = tid / C::CP, page_mask = (1 << a.cache.page_shift) - 1;
+  const int cp = tid % C::CP, r0 = C::ALONE ? warp * WK + lane / C::CP : tid / C::CP, page_mask = (1 << a.cache.page_shift) - 1;
   const uint32_t to = r0 * ROW + ((cp ^ (r0 & 7)) << 4);
   const auto place = [&](int x) {  // of its x-th row in a tile (8 rows repeat the swizzle)
     return (RP % 8 == 0 ? to : to ^ ((x * RP & 7) << 4)) + x * RP * ROW;
@@ -203,19 +207,19 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
     }
   };
 
+  if (tid < 16) flags[tid] = 0;
   int loaded = 0;
   look_up();
   auto fill = [&](int stage) {  // the next tile's copies, if there is one
     if (loaded < units) {
       copy(stage);
-      if (tid < 2) flags[2 * stage + tid] = 0;
       load.next(a);
       if (++loaded < units) look_up();
     }
     copies_commit();
   };
-#pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s) fill(s);
+#pragma unroll 1
+  for (int s = 0; s < (STAGES > 1 ? STAGES - 1 : 1); ++s) fill(s);
   __syncthreads();  // the flags are clear, and the columns past a head's
 
   uint32_t q[C::QSMEM ? 1 : DP / 16][4];
@@ -225,7 +229,8 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
 
   for (int u = 0; u < units; ++u) {
     const int stage = u % STAGES;
-    if (u == 0 || at.kt == 0) {  // a new tile of rows
+    const bool fresh_rows = u == 0 || at.kt == 0;
+    if (fresh_rows) {  // a new tile of rows
       begun = at.kt == 0;
       const T* from[2];
 #pragma unroll
@@ -263,7 +268,8 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
     const uint32_t ks = sb + stage * 2 * C::TILE, vs = ks + C::TILE;
     const int k0 = at.kt * TK;
     const bool edge = k0 + TK > at.r.len;  // holds new rows, or ends
-    copies_wait<STAGES - 2>();
+    uint32_t* odd_keys = flags + 4 * (u & 3);
+    copies_wait<(STAGES > 2 ? STAGES - 2 : 0)>();
     if (edge) {
       // Values of new rows that are not finite would reach rows that do not see them (0 * NaN): they
       // become zero here, each thread looking at what it copied, and are added back below.
@@ -285,11 +291,17 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
             odd = true;
           }
         }
-        if (odd) atomicOr(&flags[2 * stage + (row >> 5)], 1u << (row & 31));
+        if (odd) atomicOr(&odd_keys[row >> 4], 1u << (row & 15));
       }
     }
-    __syncthreads();  // everyone's copies have landed, and the stage of the tile before is free
-    fill((u + STAGES - 1) % STAGES);
+    // everyone's copies (of this warp's keys) have landed, and the stage of the tile before is free
+    if (C::ALONE && !(C::QSMEM && fresh_rows)) {
+      __syncwarp();
+    } else {
+      __syncthreads();
+    }
+    if (lane == 0 && warp < 4) flags[4 * (u + 2 & 3) + warp] = 0;
+    if (STAGES > 1) fill((u + STAGES - 1) % STAGES);
 
     if (at.rt * M + rw * 16 < at.r.n * a.group) {  // (else the warp's rows are all padding)
       // scores of the warp's keys
@@ -385,10 +397,10 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
           }
         }
       }
-      if (edge && (flags[2 * stage] | flags[2 * stage + 1])) {
+      if (edge && (C::ALONE ? odd_keys[kw] : odd_keys[0] | odd_keys[1] | odd_keys[2] | odd_keys[3])) {
         // values that are not finite, for the rows that see them
         for (int k = kw * WK; k < (kw + 1) * WK; ++k) {
-          if (!(flags[2 * stage + (k >> 5)] >> (k & 31) & 1)) continue;
+          if (!(odd_keys[k >> 4] >> (k & 15) & 1)) continue;
           const T* v = static_cast<const T*>(a.v_new) + (at.r.row0 + k0 + k - at.r.len) * a.v_new_stride + at.head * a.cache.dim;
 #pragma unroll
           for (int r = 0; r < 2; ++r)
@@ -414,6 +426,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
       if (KW > 1) {  // the warps of a row group, one after another into the first
         float* meet = reinterpret_cast<float*>(sm + C::OFF_MEET);
         float* mm = meet + M * C::MEET;
+#pragma unroll 1
         for (int w = 1; w < KW; ++w) {
           if (kw == w) {
 #pragma unroll
@@ -483,90 +496,133 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
       if (!whole && begun && tid == 0) run.note_join(a, at, run.lo + u - at.kt);
     }
     at.next(a);
+    if (STAGES == 1) {  // (the warp's own keys: it alone reads them)
+      __syncwarp();
+      fill(0);
+    }
   }
 }
 
-// Joins the parts of the tile of rows that CTA c's run of the attention kernel begins, in the order of
-// their keys: block (c, y) takes every gridDim.y-th group of its rows.  Up to 8 parts are a warp's work,
-// a row each; more are shared by the block's warps, which meet in shared memory.
+// Joins the parts of a tile of rows that several runs have, in the order of their keys.  Blocks (i, y) look
+// for the i-th such tile among the runs' notes.  Up to FEW parts, a thread takes 4 columns of a row and
+// reads four parts at a time; more parts are shared by the warps of a block, a row at a time, which meet in
+// shared memory.
 template <typename T, int DP, int M>
-__global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a) {
-  constexpr int PART = tree_part_floats(M, DP), WARPS = 8, VEC = (DP / 2 + 31) / 32;
-  __shared__ float ms[WARPS], ls[WARPS];
-  __shared__ float2 os[WARPS][DP / 2];
-  const int c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+__global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a, int ctas) {
+  constexpr int PART = tree_part_floats(M, DP), WARPS = 8, VEC = (DP / 4 + 31) / 32, FEW = 16, NOTES = 4;
+  static_assert(NOTES * 256 >= 4 * TREE_MAX_SMS, "the notes of all CTAs");
+  __shared__ float2 ml_of[WARPS];
+  __shared__ float4 o_of[WARPS][DP / 4];
+  __shared__ int found[NOTES][WARPS], which;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) which = -1;
   pdl_wait();
   pdl_launch_dependents();
-  const int4 join = a.joins[c];
-  if (join.x < 0) return;
-  const TreeRequest r = tree_request(a, join.x);
-  const int rows = min(a.tile_rows, r.n * a.group - join.z * a.tile_rows), n = (join.w >> 1) - c + 1;
+  bool has[NOTES];
+  unsigned mine[NOTES];
+#pragma unroll
+  for (int k = 0; k < NOTES; ++k) has[k] = 256 * k + tid < ctas && a.joins[2 * (256 * k + tid)].x >= 0;
+#pragma unroll
+  for (int k = 0; k < NOTES; ++k) {
+    mine[k] = __ballot_sync(0xffffffffu, has[k]);
+    if (lane == 0) found[k][warp] = __popc(mine[k]);
+  }
+  __syncthreads();
+  int before = 0;
+#pragma unroll
+  for (int k = 0; k < NOTES; ++k) {
+    int rank = before + __popc(mine[k] & ((1u << lane) - 1));
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      if (w < warp) rank += found[k][w];
+      before += found[k][w];
+    }
+    if (has[k] && rank == static_cast<int>(blockIdx.x)) which = 256 * k + tid;
+  }
+  __syncthreads();
+  const int c = which;
+  if (c < 0) return;
+  const int4 note = a.joins[2 * c], rest = a.joins[2 * c + 1];
+  const int head = note.x, x0 = note.y, row0 = note.z, n = (note.w >> 1) - c + 1, rows = rest.x;
   // the tile's parts: CTA c's second or first, then the first ones of the CTAs behind it
   const float* parts = a.parts + static_cast<size_t>(2 * c) * PART;
-  const int second = join.w & 1;
-  const bool shared = n > WARPS;
-
-  for (int row0 = blockIdx.y * (shared ? 1 : WARPS); row0 < rows; row0 += gridDim.y * (shared ? 1 : WARPS)) {
-    const int row = shared ? row0 : row0 + warp;
-    if (row >= rows) break;  // (all of the block, or a warp that no other waits for)
-    float m = -INFINITY, l = 0.f;
-    float2 o[VEC];
+  const auto part = [&](int i) { return parts + static_cast<size_t>(2 * i + (i == 0 ? note.w & 1 : 0)) * PART; };
+  // parts i, i + step, i + 2 step, i + 3 step of columns 4 col .. 4 col + 3 of a row, into (m, l, o)
+  const auto add4 = [&](int i, int step, int row, int col, float& m, float& l, float4& o) {
+    float2 ml[4];
+    float4 x[4];
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) o[v] = make_float2(0.f, 0.f);
-#pragma unroll 4
-    for (int i = shared ? warp : 0; i < n; i += shared ? WARPS : 1) {
-      const float* p = parts + static_cast<size_t>(2 * i + (i == 0 ? second : 0)) * PART;
-      const float2 ml = *reinterpret_cast<const float2*>(p + M * DP + 2 * row);
-      const float top = fmaxf(m, ml.x), ref = top == -INFINITY ? 0.f : top;
-      const float f1 = ex2((m - ref) * a.scale_log2), f2 = ex2((ml.x - ref) * a.scale_log2);
-      m = top;
-      l = l * f1 + ml.y * f2;
-#pragma unroll
-      for (int v = 0; v < VEC; ++v)
-        if (32 * v + lane < DP / 2) {
-          const float2 x = reinterpret_cast<const float2*>(p + row * DP)[32 * v + lane];
-          o[v].x = o[v].x * f1 + x.x * f2;
-          o[v].y = o[v].y * f1 + x.y * f2;
-        }
-    }
-    if (shared) {
-      if (lane == 0) {
-        ms[warp] = m;
-        ls[warp] = l;
+    for (int k = 0; k < 4; ++k) {
+      ml[k] = make_float2(-INFINITY, 0.f);
+      x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i + k * step < n) {
+        const float* p = part(i + k * step);
+        ml[k] = *reinterpret_cast<const float2*>(p + M * DP + 2 * row);
+        x[k] = reinterpret_cast<const float4*>(p + row * DP)[col];
       }
-#pragma unroll
-      for (int v = 0; v < VEC; ++v)
-        if (32 * v + lane < DP / 2) os[warp][32 * v + lane] = o[v];
-      __syncthreads();
-      if (warp == 0) {
-#pragma unroll
-        for (int w = 1; w < WARPS; ++w) {
-          const float top = fmaxf(m, ms[w]), ref = top == -INFINITY ? 0.f : top;
-          const float f1 = ex2((m - ref) * a.scale_log2), f2 = ex2((ms[w] - ref) * a.scale_log2);
-          m = top;
-          l = l * f1 + ls[w] * f2;
-#pragma unroll
-          for (int v = 0; v < VEC; ++v)
-            if (32 * v + lane < DP / 2) {
-              const float2 x = os[w][32 * v + lane];
-              o[v].x = o[v].x * f1 + x.x * f2;
-              o[v].y = o[v].y * f1 + x.y * f2;
-            }
-        }
-      }
-      __syncthreads();  // the sums are read before the next row's
-      if (warp != 0) continue;
     }
-    const int x = join.z * a.tile_rows + row, node = x / a.group, h = join.y * a.group + x - node * a.group;
-    const long long orow = r.row0 + node;
+    const float top = fmaxf(fmaxf(m, fmaxf(ml[0].x, ml[1].x)), fmaxf(ml[2].x, ml[3].x)), ref = top == -INFINITY ? 0.f : top;
+    const float f = ex2((m - ref) * a.scale_log2);
+    m = top;
+    l *= f;
+    o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i + k * step < n) {
+        const float g = ex2((ml[k].x - ref) * a.scale_log2);
+        l += ml[k].y * g;
+        o = make_float4(o.x + x[k].x * g, o.y + x[k].y * g, o.z + x[k].z * g, o.w + x[k].w * g);
+      }
+  };
+  const auto write = [&](int row, int col, float m, float l, const float4& o) {
+    const int x = x0 + row, node = x / a.group, h = head * a.group + x - node * a.group;
+    const long long orow = row0 + node;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    T* dst = static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * a.cache.dim;
+    if (4 * col < a.cache.dim)
+      *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * a.cache.dim + 4 * col) =
+          make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
+    if (a.lse && col == 0) a.lse[orow * a.heads + h] = (m * a.scale_log2 + (log2f(l) - TREE_SHIFT)) * 0.6931471805599453f;
+  };
+
+  if (n <= FEW) {
+    for (int e = blockIdx.y * 256 + tid; e < rows * (DP / 4); e += gridDim.y * 256) {
+      const int row = e / (DP / 4), col = e - row * (DP / 4);
+      float m = -INFINITY, l = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < n; i += 4) add4(i, 1, row, col, m, l, o);
+      write(row, col, m, l, o);
+    }
+    return;
+  }
+  for (int row = blockIdx.y; row < rows; row += gridDim.y) {
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      const int d = 2 * (32 * v + lane);
-      if (d < a.cache.dim) *reinterpret_cast<uint32_t*>(dst + d) = pack2<T>(o[v].x * inv, o[v].y * inv);
+      const int col = 32 * v + lane;
+      float m = -INFINITY, l = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (col < DP / 4) {
+        for (int i = warp; i < n; i += 4 * WARPS) add4(i, WARPS, row, col, m, l, o);
+        o_of[warp][col] = o;
+      }
+      if (col == 0) ml_of[warp] = make_float2(m, l);
     }
-    if (a.lse && lane == 0) a.lse[orow * a.heads + h] = (m * a.scale_log2 + (log2f(l) - TREE_SHIFT)) * 0.6931471805599453f;
+    __syncthreads();
+    if (tid < DP / 4) {
+      float m = -INFINITY, l = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) m = fmaxf(m, ml_of[w].x);
+      const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        const float g = ex2((ml_of[w].x - ref) * a.scale_log2);
+        const float4 x = o_of[w][tid];
+        l += ml_of[w].y * g;
+        o = make_float4(o.x + x.x * g, o.y + x.y * g, o.z + x.z * g, o.w + x.w * g);
+      }
+      write(row, tid, m, l, o);
+    }
+    __syncthreads();  // the sums are read before the next row's
   }
 }
 
@@ -593,7 +649,7 @@ Plan plan(const ivit_attention_config& c, const ivit_cache_layout& l) {
   const int group = c.heads / l.kv_heads;
   const int rows = static_cast<int>(std::min<long long>(128, static_cast<long long>(c.max_new) * group));  // that share a key head
   const int dp = l.head_dim <= 64 ? 64 : l.head_dim <= 80 ? 80 : l.head_dim <= 128 ? 128 : 256;
-  if (rows > TC_ROWS && dp <= 128 && group <= 128 && l.page_size >= 8 && l.head_stride > 0 && l.token_stride > 0 &&
+  if (rows > (dp <= 64 ? TC_ROWS_64 : TC_ROWS) && dp <= 128 && group <= 128 && l.page_size >= 8 && l.head_stride > 0 && l.token_stride > 0 &&
       l.page_stride > 0)
     return {true, dp, 0, tree_tc_rows(group), 2, tree_part_floats(128, dp)};
   // the smallest tile that holds the rows
@@ -618,7 +674,13 @@ cudaError_t launch_rows(const TreeArgs& a, int ctas, cudaStream_t s) {
 template <typename T, int DP>
 cudaError_t launch(const Plan& p, const TreeArgs& a, int dtype, int ctas, cudaStream_t s) {
   const auto join = [&](auto m) {
-    return launch_ex(tree_join_kernel<T, DP, decltype(m)::value>, dim3(ctas, 4), dim3(256), 0, s, 1, a);
+    // at most one joined tile per run and tile of rows; a thread for 4 columns of a row, up to some 16 blocks per SM
+    const long long most = static_cast<long long>(a.max_new) * a.group;  // rows that share a key head
+    const long long tiles = static_cast<long long>(a.n_req) * a.cache.heads * ((most + a.tile_rows - 1) / a.tile_rows);
+    const int x = static_cast<int>(std::min<long long>(tiles, ctas)), rows = static_cast<int>(std::min<long long>(a.tile_rows, most));
+    const int blocks = ctas > 8 * x ? rows : (rows * (DP / 4) + 255) / 256;  // (many parts: a block for a row)
+    const int y = std::max(1, std::min(blocks, 8 * ctas / x));
+    return launch_ex(tree_join_kernel<T, DP, decltype(m)::value>, dim3(x, y), dim3(256), 0, s, 1, a, ctas);
   };
   cudaError_t e;
   if (p.tc) {
@@ -643,8 +705,8 @@ extern "C" size_t ivit_tree_attention_workspace(const ivit_attention_config* cfg
   using namespace ivit;
   if (!cfg || !cache || !valid(*cfg, *cache)) return 0;
   const Plan p = plan(*cfg, *cache);
-  // the error word, then of each CTA a join and two parts
-  return 16 + static_cast<size_t>(p.ctas_per_sm) * TREE_MAX_SMS * (sizeof(int4) + 2 * sizeof(float) * p.part_floats);
+  // the error word, then of each CTA a note and two parts
+  return 16 + static_cast<size_t>(p.ctas_per_sm) * TREE_MAX_SMS * (2 * sizeof(int4) + 2 * sizeof(float) * p.part_floats);
 }
 
 extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_cache_layout* cache, int32_t n_rows,
@@ -705,7 +767,7 @@ extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_
   a.tile_rows = p.tile_rows;
   a.err = static_cast<int*>(workspace_dev);
   a.joins = static_cast<int4*>(workspace_dev) + 1;
-  a.parts = reinterpret_cast<float*>(a.joins + p.ctas_per_sm * TREE_MAX_SMS);
+  a.parts = reinterpret_cast<float*>(a.joins + 2 * p.ctas_per_sm * TREE_MAX_SMS);
   const auto width = [&](auto type) {
     using T = decltype(type);
     return p.dp == 64    ? launch<T, 64>(p, a, cache->dtype, ctas, s)

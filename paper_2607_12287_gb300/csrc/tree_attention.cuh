@@ -22,8 +22,9 @@ struct TreeArgs {
   void* out;
   float *lse, *parts;
   int* err;                         // device error word of the tcgen05 kernel's bounded waits
-  int4* joins;                      // [CTAs] the tile that CTA c's run begins and others go on with: request (-1:
-                                    // none), key head, row tile, 2 * last CTA + whether it is c's second part
+  int4* joins;                      // [CTAs][2] the tile that CTA c's run begins and others go on with: key head
+                                    // (-1: none), first of its rows in the request, the request's first row,
+                                    // 2 * last CTA + whether it is c's second part; rows of the tile
   long long q_stride, k_new_stride, v_new_stride, out_stride;
   PagedCache cache;
   int n_req, n_rows, heads, group, max_pages, max_new, mask_mode, mask_words;
@@ -58,7 +59,7 @@ __device__ __forceinline__ int tree_row_tiles(const TreeArgs& a, const TreeReque
 }
 
 // A place in the order of units (request, key head, row tile, key tile).  Keys::tiles(r): key tiles of a
-// request with rows.
+// request with rows.  Keys::LEAST: of a run.
 template <class Keys>
 struct TreePlace {
   TreeRequest r;
@@ -85,8 +86,9 @@ struct TreePlace {
   }
 };
 
-// The units [lo, hi) of this CTA out of `total` in `ctas` equal runs, and where they begin.  No more runs
-// than units, so that no run is empty between two that share a tile: the CTAs past `ctas` have none.
+// The units [lo, hi) of this CTA out of `total` in `ctas` equal runs, and where they begin.  A run has at
+// least Keys::LEAST units but for the last few (none is empty between two that share a tile, and parts stay
+// cheap beside the work on them): the CTAs past `ctas` have none.
 // `before` [n_req] is scratch in shared memory, free again after the call.
 template <class Keys>
 struct TreeRun {
@@ -122,8 +124,9 @@ struct TreeRun {
       if (i < a.n_req) before[i] = ahead + run - n;
       __syncthreads();
     }
-    ctas = total < gridDim.x ? total : gridDim.x;
-    if (tid == 0) a.joins[blockIdx.x].x = -1;
+    const unsigned long long most = (total + Keys::LEAST - 1) / Keys::LEAST;
+    ctas = most < gridDim.x ? most : gridDim.x;
+    if (tid == 0) a.joins[2 * blockIdx.x].x = -1;
     if (blockIdx.x >= ctas) return false;
     lo = total * blockIdx.x / ctas;
     hi = total * (blockIdx.x + 1) / ctas;
@@ -147,7 +150,9 @@ struct TreeRun {
   // `unit`: the run's unit that is the tile's first.
   __device__ __forceinline__ void note_join(const TreeArgs& a, const TreePlace<Keys>& p, unsigned long long unit) const {
     const unsigned long long last = unit + p.nkt - 1, end = ((last + 1) * ctas - 1) / total;  // the CTA that has it
-    a.joins[blockIdx.x] = make_int4(p.req, p.head, p.rt, 2 * static_cast<int>(end) + (unit > lo ? 1 : 0));
+    const int x0 = p.rt * a.tile_rows;
+    a.joins[2 * blockIdx.x] = make_int4(p.head, x0, p.r.row0, 2 * static_cast<int>(end) + (unit > lo ? 1 : 0));
+    a.joins[2 * blockIdx.x + 1] = make_int4(min(a.tile_rows, p.r.n * a.group - x0), 0, 0, 0);
   }
 };
 
