@@ -89,7 +89,7 @@ struct Cfg {
   static constexpr int MEET = DP + 4;                                        // floats of a row where the warps meet
   static constexpr int OFF_Q = STAGES * 2 * TILE;
   static constexpr int OFF_MEET = OFF_Q + (QSMEM ? M * ROW : 0);
-  static constexpr int OFF_FLAGS = OFF_MEET + (KW > 1 ? M * (MEET + 2) * 4 : 0);
+  static constexpr int OFF_FLAGS = OFF_MEET + (ALONE ? KW * M * 8 : KW > 1 ? M * (MEET + 2) * 4 : 0);
   static constexpr int BYTES = OFF_FLAGS + 4 * 16;
   static constexpr int PART = tree_part_floats(M, DP);
   static_assert(TREE_MAX_REQ * 8 <= OFF_Q, "the units before each request");
@@ -225,6 +225,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
   uint32_t q[C::QSMEM ? 1 : DP / 16][4];
   float o[DP / 8][4], m[2], l[2];
   int node[2];               // new row of the lane's rows g, g + 8 (-1: none)
+  bool two = true;           // the warp has rows past its first 8
   bool begun = true;         // of the tile's keys the run has seen the first
 
   for (int u = 0; u < units; ++u) {
@@ -232,6 +233,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
     const bool fresh_rows = u == 0 || at.kt == 0;
     if (fresh_rows) {  // a new tile of rows
       begun = at.kt == 0;
+      two = at.rt * M + rw * 16 + 8 < at.r.n * a.group;
       const T* from[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
@@ -244,12 +246,14 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
       }
       if (!C::QSMEM) {
 #pragma unroll
-        for (int c = 0; c < DP / 16; ++c)
+        for (int r = 0; r < 2; ++r)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = e & 1, d = 16 * c + 2 * t + 8 * (e >> 1);
-            q[c][e] = node[r] >= 0 && d < a.cache.dim ? *reinterpret_cast<const uint32_t*>(from[r] + d) : 0u;
-          }
+          for (int e = r; e < 4; e += 2)
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c) {
+              const int d = 16 * c + 2 * t + 8 * (e >> 1);
+              q[c][e] = (r == 0 || two) && node[r] >= 0 && d < a.cache.dim ? *reinterpret_cast<const uint32_t*>(from[r] + d) : 0u;
+            }
       } else {
         __syncthreads();  // the tile before has been multiplied
         if (kw == 0) {
@@ -338,6 +342,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
       bool grow = false;
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
+        if (r == 1 && !two) break;
         mx[r] = s[0][2 * r];
 #pragma unroll
         for (int j = 0; j < WK / 8; ++j) mx[r] = fmaxf(mx[r], fmaxf(s[j][2 * r], s[j][2 * r + 1]));
@@ -348,7 +353,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
       if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          if (!(mx[r] > m[r])) continue;
+          if ((r == 1 && !two) || !(mx[r] > m[r])) continue;
           const float alpha = ex2((m[r] - mx[r]) * a.scale_log2);
           m[r] = mx[r];
           l[r] *= alpha;
@@ -361,6 +366,11 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
       }
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
+        if (r == 1 && !two) {
+#pragma unroll
+          for (int j = 0; j < WK / 8; ++j) s[j][2] = s[j][3] = 0.f;
+          break;
+        }
         const float mo = TREE_SHIFT - (m[r] == -INFINITY ? 0.f : m[r] * a.scale_log2);  // (nothing seen so far: P = 0)
         float sum[2] = {0.f, 0.f};
 #pragma unroll
@@ -423,73 +433,140 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
       }
-      if (KW > 1) {  // the warps of a row group, one after another into the first
-        float* meet = reinterpret_cast<float*>(sm + C::OFF_MEET);
-        float* mm = meet + M * C::MEET;
-#pragma unroll 1
-        for (int w = 1; w < KW; ++w) {
-          if (kw == w) {
+      const bool whole = begun && at.kt == at.nkt - 1;
+      // a part: the first of the run, or the one it ends with
+      float* part = a.parts + static_cast<size_t>(2 * blockIdx.x + (u - at.kt > 0 && begun ? 1 : 0)) * C::PART;
+      const auto out_of = [&](int row, int node, int& h, long long& orow) {  // of a row of the tile
+        h = at.head * a.group + at.rt * M + row - node * a.group;
+        orow = at.r.row0 + node;
+        return static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * a.cache.dim;
+      };
+      if constexpr (C::ALONE) {
+        // Each warp leaves its output in the place of its own keys and values of this tile (rows 0 - 7 and 8 - 15;
+        // pieces of a row turn with it, so that the rows do not meet in a bank); all threads add them up.
+        constexpr int COLS = DP / 4;
+        float2* ml = reinterpret_cast<float2*>(sm + C::OFF_MEET);  // [KW][M]
+        const auto at_row = [&](int w, int row) {
+          return sm + stage * 2 * C::TILE + (row >> 3) * C::TILE + w * WK * ROW + (row & 7) * DP * 4;
+        };
+        __syncwarp();
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-              const int row = rw * 16 + g + 8 * r;
+        for (int r = 0; r < 2; ++r) {
+          if (r == 1 && !two) break;
+          if (t == 0) ml[warp * M + g + 8 * r] = make_float2(m[r], l[r]);
+          uint8_t* dst = at_row(warp, g + 8 * r);
+#pragma unroll
+          for (int j = 0; j < DP / 8; ++j) {
+            const int c = 2 * j + (t >> 1) + g;
+            *reinterpret_cast<float2*>(dst + 16 * (c >= COLS ? c - COLS : c) + 8 * (t & 1)) = make_float2(o[j][2 * r], o[j][2 * r + 1]);
+          }
+        }
+        __syncthreads();
+        const int rows = min(M, at.r.n * a.group - at.rt * M);
+#pragma unroll 1
+        for (int e = tid; e < rows * COLS; e += THREADS) {
+          const int row = e / COLS, col = e - row * COLS, turned = col + (row & 7);
+          float top = -INFINITY, sum = 0.f;
+          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+          float2 w[KW];
+#pragma unroll
+          for (int k = 0; k < KW; ++k) {
+            w[k] = ml[k * M + row];
+            top = fmaxf(top, w[k].x);
+          }
+          const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+          for (int k = 0; k < KW; ++k) {
+            const float4 x = *reinterpret_cast<const float4*>(at_row(k, row) + 16 * (turned >= COLS ? turned - COLS : turned));
+            const float f = ex2((w[k].x - ref) * a.scale_log2);
+            sum += w[k].y * f;
+            y = make_float4(y.x + x.x * f, y.y + x.y * f, y.z + x.z * f, y.w + x.w * f);
+          }
+          if (whole) {
+            int h;
+            long long orow;
+            T* dst = out_of(row, (at.rt * M + row) / a.group, h, orow) + 4 * col;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            if (4 * col < a.cache.dim)
+              *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<T>(y.x * inv, y.y * inv), pack2<T>(y.z * inv, y.w * inv));
+            if (a.lse && col == 0)
+              a.lse[orow * a.heads + h] = (top * a.scale_log2 + (log2f(sum) - TREE_SHIFT)) * 0.6931471805599453f;
+          } else {
+            reinterpret_cast<float4*>(part + row * DP)[col] = y;
+            if (col == 0) *reinterpret_cast<float2*>(part + M * DP + 2 * row) = make_float2(top, sum);
+          }
+        }
+        __syncthreads();  // the stage is free
+        for (int x = lane; x < 2 * WK * (PIECES - pieces); x += 32) {  // the columns past a head's are zero again
+          const int row = x / (PIECES - pieces), c = pieces + x % (PIECES - pieces);
+          const uint32_t tile = stage * 2 * C::TILE + (row >= WK ? C::TILE : 0);
+          *reinterpret_cast<uint4*>(sm + piece<ROW>(tile, warp * WK + (row & (WK - 1)), c)) = make_uint4(0, 0, 0, 0);
+        }
+      } else {
+        if constexpr (KW > 1) {  // the warps of a row group, one after another into the first
+          float* meet = reinterpret_cast<float*>(sm + C::OFF_MEET);
+          float* mm = meet + M * C::MEET;
+#pragma unroll 1
+          for (int w = 1; w < KW; ++w) {
+            if (kw == w) {
+#pragma unroll
+              for (int r = 0; r < 2; ++r) {
+                const int row = rw * 16 + g + 8 * r;
+                if (t == 0) {
+                  mm[2 * row] = m[r];
+                  mm[2 * row + 1] = l[r];
+                }
+#pragma unroll
+                for (int j = 0; j < DP / 8; ++j)
+                  *reinterpret_cast<float2*>(meet + row * C::MEET + 8 * j + 2 * t) = make_float2(o[j][2 * r], o[j][2 * r + 1]);
+              }
+            }
+            __syncthreads();
+            if (kw == 0) {
+#pragma unroll
+              for (int r = 0; r < 2; ++r) {
+                const int row = rw * 16 + g + 8 * r;
+                const float m2 = mm[2 * row], l2 = mm[2 * row + 1];
+                const float top = fmaxf(m[r], m2), ref = top == -INFINITY ? 0.f : top;
+                const float f1 = ex2((m[r] - ref) * a.scale_log2), f2 = ex2((m2 - ref) * a.scale_log2);
+                m[r] = top;
+                l[r] = l[r] * f1 + l2 * f2;
+#pragma unroll
+                for (int j = 0; j < DP / 8; ++j) {
+                  const float2 x = *reinterpret_cast<const float2*>(meet + row * C::MEET + 8 * j + 2 * t);
+                  o[j][2 * r] = o[j][2 * r] * f1 + x.x * f2;
+                  o[j][2 * r + 1] = o[j][2 * r + 1] * f1 + x.y * f2;
+                }
+              }
+            }
+            __syncthreads();
+          }
+        }
+        if (kw == 0) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const int row = rw * 16 + g + 8 * r;
+            if (whole) {
+              if (node[r] < 0) continue;
+              int h;
+              long long orow;
+              T* dst = out_of(row, node[r], h, orow);
+              const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
+#pragma unroll
+              for (int j = 0; j < DP / 8; ++j)
+                if (8 * j < a.cache.dim)
+                  *reinterpret_cast<uint32_t*>(dst + 8 * j + 2 * t) = pack2<T>(o[j][2 * r] * inv, o[j][2 * r + 1] * inv);
+              if (a.lse && t == 0)
+                a.lse[orow * a.heads + h] = (m[r] * a.scale_log2 + (log2f(l[r]) - TREE_SHIFT)) * 0.6931471805599453f;
+            } else {
               if (t == 0) {
-                mm[2 * row] = m[r];
-                mm[2 * row + 1] = l[r];
+                part[M * DP + 2 * row] = m[r];
+                part[M * DP + 2 * row + 1] = l[r];
               }
 #pragma unroll
               for (int j = 0; j < DP / 8; ++j)
-                *reinterpret_cast<float2*>(meet + row * C::MEET + 8 * j + 2 * t) = make_float2(o[j][2 * r], o[j][2 * r + 1]);
+                *reinterpret_cast<float2*>(part + row * DP + 8 * j + 2 * t) = make_float2(o[j][2 * r], o[j][2 * r + 1]);
             }
-          }
-          __syncthreads();
-          if (kw == 0) {
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-              const int row = rw * 16 + g + 8 * r;
-              const float m2 = mm[2 * row], l2 = mm[2 * row + 1];
-              const float top = fmaxf(m[r], m2), ref = top == -INFINITY ? 0.f : top;
-              const float f1 = ex2((m[r] - ref) * a.scale_log2), f2 = ex2((m2 - ref) * a.scale_log2);
-              m[r] = top;
-              l[r] = l[r] * f1 + l2 * f2;
-#pragma unroll
-              for (int j = 0; j < DP / 8; ++j) {
-                const float2 x = *reinterpret_cast<const float2*>(meet + row * C::MEET + 8 * j + 2 * t);
-                o[j][2 * r] = o[j][2 * r] * f1 + x.x * f2;
-                o[j][2 * r + 1] = o[j][2 * r + 1] * f1 + x.y * f2;
-              }
-            }
-          }
-          __syncthreads();
-        }
-      }
-      const bool whole = begun && at.kt == at.nkt - 1;
-      if (kw == 0) {
-        // a part: the first of the run, or the one it ends with
-        const int slot = 2 * blockIdx.x + (u - at.kt > 0 && begun ? 1 : 0);
-        float* part = a.parts + static_cast<size_t>(slot) * C::PART;
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int row = rw * 16 + g + 8 * r, x = at.rt * M + row;
-          if (whole) {
-            if (node[r] < 0) continue;
-            const int h = at.head * a.group + x - node[r] * a.group;
-            const long long orow = at.r.row0 + node[r];
-            const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
-            T* dst = static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * a.cache.dim;
-#pragma unroll
-            for (int j = 0; j < DP / 8; ++j)
-              if (8 * j < a.cache.dim)
-                *reinterpret_cast<uint32_t*>(dst + 8 * j + 2 * t) = pack2<T>(o[j][2 * r] * inv, o[j][2 * r + 1] * inv);
-            if (a.lse && t == 0)
-              a.lse[orow * a.heads + h] = (m[r] * a.scale_log2 + (log2f(l[r]) - TREE_SHIFT)) * 0.6931471805599453f;
-          } else {
-            if (t == 0) {
-              part[M * DP + 2 * row] = m[r];
-              part[M * DP + 2 * row + 1] = l[r];
-            }
-#pragma unroll
-            for (int j = 0; j < DP / 8; ++j)
-              *reinterpret_cast<float2*>(part + row * DP + 8 * j + 2 * t) = make_float2(o[j][2 * r], o[j][2 * r + 1]);
           }
         }
       }

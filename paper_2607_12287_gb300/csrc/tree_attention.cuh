@@ -90,9 +90,14 @@ struct TreePlace {
 // least Keys::LEAST units but for the last few (none is empty between two that share a tile, and parts stay
 // cheap beside the work on them): the CTAs past `ctas` have none.
 // `before` [n_req] is scratch in shared memory, free again after the call.
+// (a division of 64-bit numbers is a subroutine; nearly all are small)
+__device__ __forceinline__ unsigned long long tree_div(unsigned long long a, unsigned long long b) {
+  return (a | b) >> 32 ? a / b : static_cast<unsigned>(a) / static_cast<unsigned>(b);
+}
+
 template <class Keys>
 struct TreeRun {
-  unsigned long long lo, hi, total, ctas;
+  unsigned long long lo, hi, total, ctas, least, more;
   TreePlace<Keys> at;
 
   template <int THREADS>
@@ -128,8 +133,11 @@ struct TreeRun {
     ctas = most < gridDim.x ? most : gridDim.x;
     if (tid == 0) a.joins[2 * blockIdx.x].x = -1;
     if (blockIdx.x >= ctas) return false;
-    lo = total * blockIdx.x / ctas;
-    hi = total * (blockIdx.x + 1) / ctas;
+    // the first `more` runs have one unit more than the others
+    least = tree_div(total, ctas);
+    more = total - least * ctas;
+    lo = least * blockIdx.x + min(static_cast<unsigned long long>(blockIdx.x), more);
+    hi = lo + least + (blockIdx.x < more ? 1 : 0);
     int i = 0, j = a.n_req - 1;  // last request with before <= lo: it has units
     while (i < j) {
       const int mid = (i + j + 1) >> 1;
@@ -137,11 +145,10 @@ struct TreeRun {
     }
     const unsigned long long off = lo - before[i];
     at.enter(a, i);
-    const unsigned long long per = static_cast<unsigned long long>(at.nkt) * at.nrt;
-    at.head = static_cast<int>(off / per);
-    const unsigned rest = static_cast<unsigned>(off - at.head * per);
-    at.rt = rest / at.nkt;
-    at.kt = rest - at.rt * at.nkt;
+    const unsigned long long tiles = tree_div(off, at.nkt);  // of rows, before this one
+    at.kt = static_cast<int>(off - tiles * at.nkt);
+    at.head = static_cast<int>(tree_div(tiles, at.nrt));
+    at.rt = static_cast<int>(tiles - static_cast<unsigned long long>(at.head) * at.nrt);
     __syncthreads();
     return true;
   }
@@ -149,7 +156,8 @@ struct TreeRun {
   // Notes that the run begins the tile of rows at `p` (as its second part or its first) and another ends it;
   // `unit`: the run's unit that is the tile's first.
   __device__ __forceinline__ void note_join(const TreeArgs& a, const TreePlace<Keys>& p, unsigned long long unit) const {
-    const unsigned long long last = unit + p.nkt - 1, end = ((last + 1) * ctas - 1) / total;  // the CTA that has it
+    const unsigned long long last = unit + p.nkt - 1, longer = more * (least + 1);  // the CTA that has it:
+    const unsigned long long end = last < longer ? tree_div(last, least + 1) : more + tree_div(last - longer, least);
     const int x0 = p.rt * a.tile_rows;
     a.joins[2 * blockIdx.x] = make_int4(p.head, x0, p.r.row0, 2 * static_cast<int>(end) + (unit > lo ? 1 : 0));
     a.joins[2 * blockIdx.x + 1] = make_int4(min(a.tile_rows, p.r.n * a.group - x0), 0, 0, 0);

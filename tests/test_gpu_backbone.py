@@ -384,10 +384,13 @@ def test_tree_attention(pkg, lengths, new, heads, kv, dim, page, dtype, order, m
     run_attention(pkg, c, mask, trees(r, new) if mask == "tree" else None)
 
 
-def test_many_short_requests(pkg):
+@pytest.mark.parametrize("dim,most_new,n", [(64, 2, 700), (72, 2, 700), (40, 2, 700), (96, 2, 500), (256, 2, 300), (72, 20, 200),
+                                            (96, 70, 40)])
+def test_many_short_requests(pkg, dim, most_new, n):
+    # every CTA goes through several tiles of rows
     r = np.random.default_rng(2)
-    lengths, new = r.integers(0, 40, 700), r.integers(0, 3, 700)
-    c = attention_case(r, lengths, new, 2, 1, 64, 8, "bfloat16")
+    lengths, new = r.integers(0, 90, n), r.integers(0, most_new + 1, n)
+    c = attention_case(r, lengths, new, 6, 3, dim, 8, "bfloat16")
     run_attention(pkg, c, "causal", lse=False)
 
 
