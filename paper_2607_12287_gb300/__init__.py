@@ -181,11 +181,19 @@ def _require(t, name: str, dtype_name: str, numel: int) -> None:
 _dims = {}
 
 
+_current = []  # torch's raw stream and device lookups, once the first call has found them
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
+        if _current:  # (without building a Stream object)
+            return _current[0](_current[1]())
         import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # (without building a Stream object)
-        return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
+        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+        stream = torch.cuda.current_stream().cuda_stream
+        if raw and device and raw(device()) == stream:
+            _current.extend((raw, device))
+        return stream
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -393,16 +401,21 @@ def _typed(t, name: str, dtype: int) -> None:
         raise TypeError(f"{name}: dtype {t.dtype}, expected torch.{_DTYPE_NAMES[dtype]}")
 
 
-def _rows(t, name: str, dtype: int, n_rows: int, heads: int, dim: int) -> int:
-    """The row stride of a tensor [rows, heads, dim] whose heads are contiguous in a row; rejects one that
-    the kernels would misread, as ``_require`` does."""
+def _rows(t, name: str, dtype: int, shape: tuple) -> tuple:
+    """Pointer and row stride of a tensor [rows, heads, head_dim] of at least ``shape``'s rows whose heads are
+    contiguous in a row; rejects one that the kernels would misread, as ``_require`` does."""
+    if type(t) is _dtypes.get("tensor") and t.is_cuda and t.dtype is _dtypes[dtype] and t.shape == shape:
+        s0, s1, s2 = t.stride()  # the common case: the checks below without formatting names
+        if s2 == 1 and s1 == shape[2] and shape[0] > 1:
+            return t.data_ptr(), s0
     _typed(t, name, dtype)
+    n_rows, heads, dim = shape
     sh, st = t.shape, t.stride()
     if len(sh) != 3 or sh[0] < n_rows or sh[1] != heads or sh[2] != dim:
-        raise ValueError(f"{name}: shape {tuple(sh)}, expected [{n_rows}, {heads}, {dim}]")
+        raise ValueError(f"{name}: shape {tuple(sh)}, expected {list(shape)}")
     if st[2] != 1 or (st[1] != dim and heads > 1):
         raise ValueError(f"{name}: the heads of a row are not contiguous")
-    return st[0] if sh[0] > 1 else heads * dim
+    return t.data_ptr(), st[0] if sh[0] > 1 else heads * dim
 
 
 def _row_count(t, name: str) -> int:
@@ -433,13 +446,13 @@ def ivit_step_plan(cfg: IvitPlanConfig, held, base, new, parent, ring, ring_in, 
     """Pages, slots, positions and tree masks of a step (int32 tensors; parent, req, positions and mask may be
     None): ``table`` [n_req, max_pages] and ``ring`` [n_pages] are updated, ``cu_rows`` [n_req + 1], the row arrays
     [max_rows], ``mask`` [max_rows, mask_words], ``ring_out`` [2] and ``status`` [1] written."""
-    n, rows = cfg.n_req, cfg.max_rows
-    args = (C.addressof(cfg), _arg(held, "held", "int32", n), _arg(base, "base", "int32", n), _arg(new, "new",
-            "int32", n), _arg(parent, "parent", "int32", rows), _arg(ring, "ring", "int32", cfg.n_pages), _arg(ring_in,
-            "ring_in", "int32", 2), _arg(table, "table", "int32", n * cfg.max_pages), _arg(cu_rows, "cu_rows", "int32", n +
-            1), _arg(req, "req", "int32", rows), _arg(slots, "slots", "int32", rows), _arg(positions, "positions", "int32",
-            rows), _arg(mask, "mask", "int32", rows * cfg.mask_words), _arg(ring_out, "ring_out", "int32", 2), _arg(status,
-            "status", "int32", 1), _stream(stream))
+    n, rows, i32 = cfg.n_req, cfg.max_rows, "int32"
+    args = (C.addressof(cfg), _arg(held, "held", i32, n), _arg(base, "base", i32, n), _arg(new, "new", i32, n),
+            _arg(parent, "parent", i32, rows), _arg(ring, "ring", i32, cfg.n_pages), _arg(ring_in, "ring_in", i32, 2),
+            _arg(table, "table", i32, n * cfg.max_pages), _arg(cu_rows, "cu_rows", i32, n + 1),
+            _arg(req, "req", i32, rows), _arg(slots, "slots", i32, rows), _arg(positions, "positions", i32, rows),
+            _arg(mask, "mask", i32, rows * cfg.mask_words), _arg(ring_out, "ring_out", i32, 2),
+            _arg(status, "status", i32, 1), _stream(stream))
     _check(load().ivit_step_plan(*args), None)
 
 
@@ -466,21 +479,21 @@ def ivit_qk_norm_rope(cfg: IvitRopeConfig, q, k, v, q_weight, k_weight, position
     """Norm (where there is a weight) and rotation of q [rows, heads, head_dim] and k [rows, kv_heads, head_dim]
     into ``q_out``, ``k_out`` and, with ``cache``, of k and v into the ``slots`` of the paged caches.
     ``positions``: int32 [rows] or [axes, rows]; ``freq``, ``axis``: of each pair."""
-    n = _row_count(q, "q")
-    dt, heads, kv, dim = cfg.dtype, cfg.heads, cfg.kv_heads, cfg.head_dim
-    qs = _rows(q, "q", dt, n, heads, dim)
-    ks = _rows(k, "k", dt, n, kv, dim)
-    qos = _rows(q_out, "q_out", dt, n, heads, dim)
-    kos, ko = (0, None) if k_out is None else (_rows(k_out, "k_out", dt, n, kv, dim), k_out.data_ptr())
-    vs = lay = vp = kc = vc = sl = None
+    n, dt, dim = _row_count(q, "q"), cfg.dtype, cfg.head_dim
+    q_shape, k_shape = (n, cfg.heads, dim), (n, cfg.kv_heads, dim)
+    vp = lay = kc = vc = sl = ko = None
+    vs = kos = 0
+    if k_out is not None:
+        ko, kos = _rows(k_out, "k_out", dt, k_shape)
     if cache is not None:
-        vs, vp = _rows(v, "v", dt, n, kv, dim), v.data_ptr()
+        vp, vs = _rows(v, "v", dt, k_shape)
         kc, vc = _cache(k_cache, "k_cache", cache), _cache(v_cache, "v_cache", cache)
         lay, sl = C.addressof(cache), _arg(slots, "slots", "int32", n)
     elif not (v is k_cache is v_cache is slots is None):
         raise ValueError("v, k_cache, v_cache and slots need the cache's layout")
-    args = (C.addressof(cfg), n, q.data_ptr(), qs, k.data_ptr(), ks, vp, vs or 0, *_rope_inputs(cfg, n, q_weight,
-            k_weight, positions, freq, axis), q_out.data_ptr(), qos, ko, kos, lay, kc, vc, sl, _stream(stream))
+    args = (C.addressof(cfg), n, *_rows(q, "q", dt, q_shape), *_rows(k, "k", dt, k_shape), vp, vs,
+            *_rope_inputs(cfg, n, q_weight, k_weight, positions, freq, axis), *_rows(q_out, "q_out", dt, q_shape), ko, kos,
+            lay, kc, vc, sl, _stream(stream))
     _check(load().ivit_qk_norm_rope(*args), None)
 
 
@@ -493,20 +506,16 @@ def ivit_qk_norm_rope_backward(cfg: IvitRopeConfig, grad_q, grad_k, q, k, q_weig
                                dq_weight=None, dk_weight=None, workspace=None, stream=None) -> None:
     """Gradients of ``ivit_qk_norm_rope``: ``dq``, ``dk`` and the weights' fp32
     [head_dim] (or None)."""
-    n = _row_count(q, "q")
-    dt, heads, kv, dim = cfg.dtype, cfg.heads, cfg.kv_heads, cfg.head_dim
-    gqs = _rows(grad_q, "grad_q", dt, n, heads, dim)
-    gks = _rows(grad_k, "grad_k", dt, n, kv, dim)
-    qs = _rows(q, "q", dt, n, heads, dim)
-    ks = _rows(k, "k", dt, n, kv, dim)
-    dqs, dks = _rows(dq, "dq", dt, n, heads, dim), _rows(dk, "dk", dt, n, kv, dim)
+    n, dt, dim = _row_count(q, "q"), cfg.dtype, cfg.head_dim
+    q_shape, k_shape = (n, cfg.heads, dim), (n, cfg.kv_heads, dim)
     dqw, dkw = _arg(dq_weight, "dq_weight", "float32", dim), _arg(dk_weight, "dk_weight", "float32", dim)
     ws = None
     if dqw or dkw:
         ws = _arg(workspace, "workspace", "uint8", ivit_qk_norm_rope_backward_workspace(cfg))
-    args = (C.addressof(cfg), n, grad_q.data_ptr(), gqs, grad_k.data_ptr(), gks, q.data_ptr(), qs, k.data_ptr(), ks,
-            *_rope_inputs(cfg, n, q_weight, k_weight, positions, freq, axis), dq.data_ptr(), dqs, dk.data_ptr(), dks, dqw,
-            dkw, ws, _stream(stream))
+    args = (C.addressof(cfg), n, *_rows(grad_q, "grad_q", dt, q_shape), *_rows(grad_k, "grad_k", dt, k_shape),
+            *_rows(q, "q", dt, q_shape), *_rows(k, "k", dt, k_shape),
+            *_rope_inputs(cfg, n, q_weight, k_weight, positions, freq, axis), *_rows(dq, "dq", dt, q_shape),
+            *_rows(dk, "dk", dt, k_shape), dqw, dkw, ws, _stream(stream))
     _check(load().ivit_qk_norm_rope_backward(*args), None)
 
 
@@ -519,20 +528,16 @@ def ivit_tree_attention(cfg: IvitAttentionConfig, cache: IvitCacheLayout, q, k_n
                         cu_rows, mask, out, lse=None, workspace=None, stream=None) -> None:
     """Attention of the new rows q [rows, heads, head_dim] over the cached tokens of their requests and over the new
     keys and values [rows, kv_heads, head_dim] that the mask lets them see; ``lse`` fp32 [rows, heads] or None."""
-    n = _row_count(q, "q")
-    dt, heads, kv, dim = cache.dtype, cfg.heads, cache.kv_heads, cache.head_dim
-    qs = _rows(q, "q", dt, n, heads, dim)
-    ks = _rows(k_new, "k_new", dt, n, kv, dim)
-    vs = _rows(v_new, "v_new", dt, n, kv, dim)
-    os_ = _rows(out, "out", dt, n, heads, dim)
-    kc, vc, req = _cache(k_cache, "k_cache", cache), _cache(v_cache, "v_cache", cache), cfg.n_req
+    n, dt, dim, heads, req = _row_count(q, "q"), cache.dtype, cache.head_dim, cfg.heads, cfg.n_req
+    q_shape, k_shape = (n, heads, dim), (n, cache.kv_heads, dim)
     if cfg.mask_mode != IVIT_MASK_TREE:
         mask = None
-    args = (C.addressof(cfg), C.addressof(cache), n, q.data_ptr(), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs,
-            kc, vc, _arg(table, "table", "int32", req * cfg.max_pages), _arg(lengths, "lengths", "int32", req),
-            _arg(cu_rows, "cu_rows", "int32", req + 1), _arg(mask, "mask", "int32", n * cfg.mask_words), out.data_ptr(),
-            os_, _arg(lse, "lse", "float32", n * heads), _arg(workspace, "workspace", "uint8",
-            ivit_tree_attention_workspace(cfg, cache)), _stream(stream))
+    args = (C.addressof(cfg), C.addressof(cache), n, *_rows(q, "q", dt, q_shape), *_rows(k_new, "k_new", dt, k_shape),
+            *_rows(v_new, "v_new", dt, k_shape), _cache(k_cache, "k_cache", cache), _cache(v_cache, "v_cache", cache),
+            _arg(table, "table", "int32", req * cfg.max_pages), _arg(lengths, "lengths", "int32", req),
+            _arg(cu_rows, "cu_rows", "int32", req + 1), _arg(mask, "mask", "int32", n * cfg.mask_words),
+            *_rows(out, "out", dt, q_shape), _arg(lse, "lse", "float32", n * heads),
+            _arg(workspace, "workspace", "uint8", ivit_tree_attention_workspace(cfg, cache)), _stream(stream))
     _check(load().ivit_tree_attention(*args), None)
 
 
