@@ -6,9 +6,9 @@
 //
 // Rows that share a key head (the new rows x the query heads of the group) form tiles of 16, 32, 64
 // or 128; a tile walks its keys -- the cached tokens and, behind them, the new rows -- 64 at a time.
-// All (request, key head, row tile, 64 keys) of the call, in this order, are cut into as many equal
-// runs as there are CTAs, two per SM, so that ragged lengths and few requests load the chip alike.
-// A run that holds a tile's keys only in part leaves its running maximum, sum and output (fp32) in
+// All (request, row tile, 64 keys) of a key head, in this order, are cut into as many equal runs as
+// there are CTAs for the head, so that ragged lengths and few requests load the chip alike.  A run
+// that holds a tile's keys only in part leaves its running maximum, sum and output (fp32) in
 // the workspace, and a second kernel joins the parts of a tile in the order of their keys.
 //
 // A CTA of four warps: 16-byte asynchronous copies fill a ring of K and V tiles in shared memory
@@ -78,14 +78,17 @@ struct Cfg {
   static constexpr int THREADS = 32 * RW * KW;
   // One row group: no two warps share keys, each copies its own, and the walk has no barrier.
   static constexpr bool ALONE = RW == 1;
-  static constexpr int ROW = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;         // bytes of a row in shared memory
+  // Bytes of a row in shared memory: 8 rows of ldmatrix must not meet in a bank, by a swizzle of the pieces of
+  // rows of 64, 128 and 256 values, by an odd number of pieces for 80 and 96.
+  static constexpr bool PADDED = DP == 80 || DP == 96;
+  static constexpr int ROW = 2 * DP + (PADDED ? 16 : 0);
   static constexpr int TILE = TK * ROW;
   static constexpr int CTAS = ALONE ? (DP <= 64 ? 4 : 2) : DP <= 128 && RW < 8 ? 2 : 1;  // per SM
   static constexpr bool QSMEM = DP > 128;                                    // queries in shared memory, not registers
   static constexpr int STAGES = ALONE ? (DP <= 128 ? 3 : 1) : DP > 128 ? 2 : 3;
   static constexpr int TERMS = RW < 4 ? 2 : 1;
   // a copy of a tile (of the warp's keys if it is alone): CP lanes for the pieces of a row, RP rows at a time
-  static constexpr int CP = ROW / 16, RP = (ALONE ? 32 : THREADS) / CP, COPIES = (ALONE ? WK : TK) / RP;
+  static constexpr int CP = DP <= 64 ? 8 : DP <= 128 ? 16 : 32, RP = (ALONE ? 32 : THREADS) / CP, COPIES = (ALONE ? WK : TK) / RP;
   static constexpr int MEET = DP + 4;                                        // floats of a row where the warps meet
   static constexpr int OFF_Q = STAGES * 2 * TILE;
   static constexpr int OFF_MEET = OFF_Q + (QSMEM ? M * ROW : 0);
@@ -97,9 +100,9 @@ struct Cfg {
 };
 
 // Shared-memory address of 16-byte piece c of a row.
-template <int ROW>
+template <class C>
 __device__ __forceinline__ uint32_t piece(uint32_t tile, int row, int c) {
-  return tile + row * ROW + ((c ^ (row & 7)) << 4);
+  return tile + row * C::ROW + ((C::PADDED ? c : c ^ (row & 7)) << 4);
 }
 
 // Which of the 64 keys from k0 on new row `node` of the request sees (bit j: key k0 + j).
@@ -121,7 +124,8 @@ __device__ __forceinline__ uint64_t seen(const TreeArgs& a, const TreeRequest& r
   return bits & low(r.n - first);
 }
 
-template <typename T, int DP, int RW>
+// ONE_PAGE: the 16 keys of a warp that is alone are of one page.
+template <typename T, int DP, int RW, bool ONE_PAGE>
 __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_attention_kernel(const TreeArgs a) {
   using C = Cfg<DP, RW>;
   constexpr int M = C::M, KW = C::KW, WK = C::WK, ROW = C::ROW, STAGES = C::STAGES, THREADS = C::THREADS;
@@ -145,27 +149,28 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
     // columns past a head's are zero for good: no copy touches them
     for (int x = tid; x < STAGES * 2 * TK * (PIECES - pieces); x += THREADS) {
       const int row = x / (PIECES - pieces), c = pieces + x % (PIECES - pieces);
-      *reinterpret_cast<uint4*>(sm + (row * ROW + ((c ^ (row & 7)) << 4))) = make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4*>(sm + piece<C>(0, row, c)) = make_uint4(0, 0, 0, 0);
     }
   }
 
   // A copy's part of this thread: piece cp of the rows r0, r0 + RP, ... of a tile.
   const int cp = tid % C::CP, r0 = C::ALONE ? warp * WK + lane / C::CP : tid / C::CP, page_mask = (1 << a.cache.page_shift) - 1;
-  const uint32_t to = r0 * ROW + ((cp ^ (r0 & 7)) << 4);
+  const uint32_t to = piece<C>(0, r0, cp);
   const auto place = [&](int x) {  // of its x-th row in a tile (8 rows repeat the swizzle)
-    return (RP % 8 == 0 ? to : to ^ ((x * RP & 7) << 4)) + x * RP * ROW;
+    return (C::PADDED || RP % 8 == 0 ? to : to ^ ((x * RP & 7) << 4)) + x * RP * ROW;
   };
   // The pages of the tile at `load`, of those rows; kept a tile ahead of the copies.
-  int ids[COPIES];
+  constexpr int IDS = ONE_PAGE ? 1 : COPIES;
+  int ids[IDS];
   const auto look_up = [&] {
     const int* table = a.table + static_cast<size_t>(load.req) * a.max_pages;
-    const int key = load.kt * TK + r0;
+    const int key = load.kt * TK + (ONE_PAGE ? warp * WK : r0);
     if ((load.kt + 1) * TK <= load.r.len) {
 #pragma unroll
-      for (int x = 0; x < COPIES; ++x) ids[x] = table[(key + x * RP) >> a.cache.page_shift];
+      for (int x = 0; x < IDS; ++x) ids[x] = table[(key + x * RP) >> a.cache.page_shift];
     } else {
 #pragma unroll
-      for (int x = 0; x < COPIES; ++x) ids[x] = key + x * RP < load.r.len ? table[(key + x * RP) >> a.cache.page_shift] : -1;
+      for (int x = 0; x < IDS; ++x) ids[x] = key + x * RP < load.r.len ? table[(key + x * RP) >> a.cache.page_shift] : -1;
     }
   };
   const auto copy = [&](int stage) {
@@ -174,13 +179,21 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
     const long long head = load.head * a.cache.head_stride + 8 * cp;
     const T *kc = static_cast<const T*>(a.k_cache) + head, *vc = static_cast<const T*>(a.v_cache) + head;
     const int key = load.kt * TK + r0;
+    const auto cached = [&](int x, bool& ok) {  // where the x-th row is in the caches (row 0 if its page is outside)
+      const int id = ids[ONE_PAGE ? 0 : x];
+      ok = static_cast<unsigned>(id) < static_cast<unsigned>(a.cache.n_pages);
+      return ok ? id * a.cache.page_stride + ((key + x * RP) & page_mask) * a.cache.token_stride : 0;
+    };
     if ((load.kt + 1) * TK <= load.r.len) {
+      bool ok;
+      long long off = cached(0, ok);
+      const long long step = RP * a.cache.token_stride;
 #pragma unroll
       for (int x = 0; x < COPIES; ++x) {
-        const bool ok = static_cast<unsigned>(ids[x]) < static_cast<unsigned>(a.cache.n_pages);
-        const long long off = ids[x] * a.cache.page_stride + ((key + x * RP) & page_mask) * a.cache.token_stride;
-        copy16(ks + place(x), kc + (ok ? off : 0), ok);
-        copy16(vs + place(x), vc + (ok ? off : 0), ok);
+        if (!ONE_PAGE && x > 0) off = cached(x, ok);
+        copy16(ks + place(x), kc + off, ok);
+        copy16(vs + place(x), vc + off, ok);
+        if (ONE_PAGE) off += step;
       }
       return;
     }
@@ -190,8 +203,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
       const T *k = kc, *v = vc;
       bool ok;
       if (fresh < 0) {
-        ok = static_cast<unsigned>(ids[x]) < static_cast<unsigned>(a.cache.n_pages);
-        const long long off = ok ? ids[x] * a.cache.page_stride + ((key + x * RP) & page_mask) * a.cache.token_stride : 0;
+        const long long off = cached(x, ok);
         k += off;
         v += off;
       } else {
@@ -260,7 +272,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
 #pragma unroll
           for (int r = 0; r < 2; ++r)
             for (int c = t; c < PIECES; c += 4)
-              *reinterpret_cast<uint4*>(sm + C::OFF_Q + (piece<ROW>(0, rw * 16 + g + 8 * r, c))) =
+              *reinterpret_cast<uint4*>(sm + C::OFF_Q + (piece<C>(0, rw * 16 + g + 8 * r, c))) =
                   node[r] >= 0 && c < pieces ? *reinterpret_cast<const uint4*>(from[r] + 8 * c) : make_uint4(0, 0, 0, 0);
         }
       }
@@ -316,12 +328,12 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
         for (int e = 0; e < 4; ++e) s[j][e] = 0.f;
 #pragma unroll
       for (int c = 0; c < DP / 16; ++c) {
-        if (C::QSMEM) ldmatrix4(q[0], piece<ROW>(sb + C::OFF_Q, rw * 16 + (lane & 15), 2 * c + (lane >> 4)));
+        if (C::QSMEM) ldmatrix4(q[0], piece<C>(sb + C::OFF_Q, rw * 16 + (lane & 15), 2 * c + (lane >> 4)));
 #pragma unroll
         for (int j = 0; j < WK / 16; ++j) {
           uint32_t b[4];
           const int row = kw * WK + 16 * j + (lane & 7) + ((lane & 16) >> 1);
-          ldmatrix4(b, piece<ROW>(ks, row, 2 * c + (lane >> 3 & 1)));
+          ldmatrix4(b, piece<C>(ks, row, 2 * c + (lane >> 3 & 1)));
           mma<T>(s[2 * j], q[C::QSMEM ? 0 : c], b[0], b[1]);
           mma<T>(s[2 * j + 1], q[C::QSMEM ? 0 : c], b[2], b[3]);
         }
@@ -366,11 +378,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
       }
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        if (r == 1 && !two) {
-#pragma unroll
-          for (int j = 0; j < WK / 8; ++j) s[j][2] = s[j][3] = 0.f;
-          break;
-        }
+        if (r == 1 && !two) break;
         const float mo = TREE_SHIFT - (m[r] == -INFINITY ? 0.f : m[r] * a.scale_log2);  // (nothing seen so far: P = 0)
         float sum[2] = {0.f, 0.f};
 #pragma unroll
@@ -387,6 +395,10 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
         uint32_t p[C::TERMS][4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
+          if ((e & 1) && !two) {
+            p[0][e] = p[C::TERMS - 1][e] = 0u;
+            continue;
+          }
           float& x = s[2 * j + (e >> 1)][2 * (e & 1)];
           float& y = s[2 * j + (e >> 1)][2 * (e & 1) + 1];
           p[0][e] = pack2<T>(x, y);
@@ -399,7 +411,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
         for (int c = 0; c < DP / 16; ++c) {
           uint32_t b[4];
           const int row = kw * WK + 16 * j + (lane & 15);
-          ldmatrix4_trans(b, piece<ROW>(vs, row, 2 * c + (lane >> 4)));
+          ldmatrix4_trans(b, piece<C>(vs, row, 2 * c + (lane >> 4)));
 #pragma unroll
           for (int x = 0; x < C::TERMS; ++x) {
             mma<T>(o[2 * c], p[x], b[0], b[1]);
@@ -500,7 +512,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
         for (int x = lane; x < 2 * WK * (PIECES - pieces); x += 32) {  // the columns past a head's are zero again
           const int row = x / (PIECES - pieces), c = pieces + x % (PIECES - pieces);
           const uint32_t tile = stage * 2 * C::TILE + (row >= WK ? C::TILE : 0);
-          *reinterpret_cast<uint4*>(sm + piece<ROW>(tile, warp * WK + (row & (WK - 1)), c)) = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(sm + piece<C>(tile, warp * WK + (row & (WK - 1)), c)) = make_uint4(0, 0, 0, 0);
         }
       } else {
         if constexpr (KW > 1) {  // the warps of a row group, one after another into the first
@@ -620,10 +632,10 @@ __global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a, int ct
   const int c = which;
   if (c < 0) return;
   const int4 note = a.joins[2 * c], rest = a.joins[2 * c + 1];
-  const int head = note.x, x0 = note.y, row0 = note.z, n = (note.w >> 1) - c + 1, rows = rest.x;
-  // the tile's parts: CTA c's second or first, then the first ones of the CTAs behind it
+  const int head = note.x, x0 = note.y, row0 = note.z, n = note.w >> 1, rows = rest.x;
+  // the tile's parts: CTA c's second or first, then the first ones of the head's CTAs behind it
   const float* parts = a.parts + static_cast<size_t>(2 * c) * PART;
-  const auto part = [&](int i) { return parts + static_cast<size_t>(2 * i + (i == 0 ? note.w & 1 : 0)) * PART; };
+  const auto part = [&](int i) { return parts + static_cast<size_t>(2 * i * a.cache.heads + (i == 0 ? note.w & 1 : 0)) * PART; };
   // parts i, i + step, i + 2 step, i + 3 step of columns 4 col .. 4 col + 3 of a row, into (m, l, o)
   const auto add4 = [&](int i, int step, int row, int col, float& m, float& l, float4& o) {
     float2 ml[4];
@@ -725,10 +737,10 @@ Plan plan_of() {
 Plan plan(const ivit_attention_config& c, const ivit_cache_layout& l) {
   const int group = c.heads / l.kv_heads;
   const int rows = static_cast<int>(std::min<long long>(128, static_cast<long long>(c.max_new) * group));  // that share a key head
-  const int dp = l.head_dim <= 64 ? 64 : l.head_dim <= 80 ? 80 : l.head_dim <= 128 ? 128 : 256;
+  const int dp = l.head_dim <= 64 ? 64 : l.head_dim <= 80 ? 80 : l.head_dim <= 96 ? 96 : l.head_dim <= 128 ? 128 : 256;
   if (rows > (dp <= 64 ? TC_ROWS_64 : TC_ROWS) && dp <= 128 && group <= 128 && l.page_size >= 8 && l.head_stride > 0 && l.token_stride > 0 &&
       l.page_stride > 0)
-    return {true, dp, 0, tree_tc_rows(group), 2, tree_part_floats(128, dp)};
+    return {true, dp == 96 ? 128 : dp, 0, tree_tc_rows(group), 2, tree_part_floats(128, dp == 96 ? 128 : dp)};
   // the smallest tile that holds the rows
   const auto groups = [&](auto d) {
     constexpr int DP = decltype(d)::value;
@@ -736,15 +748,17 @@ Plan plan(const ivit_attention_config& c, const ivit_cache_layout& l) {
   };
   return dp == 64    ? groups(std::integral_constant<int, 64>{})
          : dp == 80  ? groups(std::integral_constant<int, 80>{})
+         : dp == 96  ? groups(std::integral_constant<int, 96>{})
          : dp == 128 ? groups(std::integral_constant<int, 128>{})
                      : groups(std::integral_constant<int, 256>{});
 }
 
-template <typename T, int DP, int RW>
+template <typename T, int DP, int RW, bool ONE_PAGE = false>
 cudaError_t launch_rows(const TreeArgs& a, int ctas, cudaStream_t s) {
   using C = Cfg<DP, RW>;
-  const cudaError_t e = allow_smem<tree_attention_kernel<T, DP, RW>>(C::BYTES);
-  return e != cudaSuccess ? e : launch_ex(tree_attention_kernel<T, DP, RW>, dim3(ctas), dim3(C::THREADS), C::BYTES, s, 1, a);
+  const auto kernel = tree_attention_kernel<T, DP, RW, ONE_PAGE>;
+  const cudaError_t e = allow_smem<tree_attention_kernel<T, DP, RW, ONE_PAGE>>(C::BYTES);
+  return e != cudaSuccess ? e : launch_ex(kernel, dim3(ctas), dim3(C::THREADS), C::BYTES, s, 1, a);
 }
 
 // The kernel of the plan, then the join.
@@ -763,7 +777,7 @@ cudaError_t launch(const Plan& p, const TreeArgs& a, int dtype, int ctas, cudaSt
   if (p.tc) {
     e = launch_tree_attention_tc(a, dtype, DP, ctas, s);
   } else {
-    e = p.rw == 1   ? launch_rows<T, DP, 1>(a, ctas, s)
+    e = p.rw == 1   ? (a.cache.page_shift >= 4 ? launch_rows<T, DP, 1, true>(a, ctas, s) : launch_rows<T, DP, 1>(a, ctas, s))
         : p.rw == 2 ? launch_rows<T, DP, 2>(a, ctas, s)
         : p.rw == 4 ? launch_rows<T, DP, 4>(a, ctas, s)
                     : launch_rows<T, DP, 8>(a, ctas, s);
@@ -840,7 +854,8 @@ extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_
   a.scale_log2 = cfg->scale * 1.4426950408889634f;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const Plan p = plan(*cfg, *cache);
-  const int ctas = p.ctas_per_sm * std::min(TREE_MAX_SMS, sms);
+  // whole runs of all key heads, at least one (more CTAs than fit at a time wait for a place, not for each other)
+  const int ctas = std::max(1, p.ctas_per_sm * std::min(TREE_MAX_SMS, sms) / cache->kv_heads) * cache->kv_heads;
   a.tile_rows = p.tile_rows;
   a.err = static_cast<int*>(workspace_dev);
   a.joins = static_cast<int4*>(workspace_dev) + 1;
@@ -849,6 +864,7 @@ extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_
     using T = decltype(type);
     return p.dp == 64    ? launch<T, 64>(p, a, cache->dtype, ctas, s)
            : p.dp == 80  ? launch<T, 80>(p, a, cache->dtype, ctas, s)
+           : p.dp == 96  ? launch<T, 96>(p, a, cache->dtype, ctas, s)
            : p.dp == 128 ? launch<T, 128>(p, a, cache->dtype, ctas, s)
                          : launch<T, 256>(p, a, cache->dtype, ctas, s);
   };

@@ -24,7 +24,7 @@ struct TreeArgs {
   int* err;                         // device error word of the tcgen05 kernel's bounded waits
   int4* joins;                      // [CTAs][2] the tile that CTA c's run begins and others go on with: key head
                                     // (-1: none), first of its rows in the request, the request's first row,
-                                    // 2 * last CTA + whether it is c's second part; rows of the tile
+                                    // 2 * its parts + whether the first is c's second; rows of the tile
   long long q_stride, k_new_stride, v_new_stride, out_stride;
   PagedCache cache;
   int n_req, n_rows, heads, group, max_pages, max_new, mask_mode, mask_words;
@@ -58,8 +58,8 @@ __device__ __forceinline__ int tree_row_tiles(const TreeArgs& a, const TreeReque
   return (r.n * a.group + a.tile_rows - 1) / a.tile_rows;
 }
 
-// A place in the order of units (request, key head, row tile, key tile).  Keys::tiles(r): key tiles of a
-// request with rows.  Keys::LEAST: of a run.
+// A place in a head's order of units (request, row tile, key tile).  Keys::tiles(r): key tiles of a request
+// with rows.  Keys::LEAST: units of a run.
 template <class Keys>
 struct TreePlace {
   TreeRequest r;
@@ -72,45 +72,44 @@ struct TreePlace {
     }
     nkt = Keys::tiles(r);
     nrt = tree_row_tiles(a, r);
-    head = rt = kt = 0;
+    rt = kt = 0;
   }
   __device__ __forceinline__ void next_rows(const TreeArgs& a) {  // the first key tile of the next tile of rows
     kt = 0;
-    if (++rt < nrt) return;
-    rt = 0;
-    if (++head < a.cache.heads) return;
-    enter(a, req + 1);
+    if (++rt == nrt) enter(a, req + 1);
   }
   __device__ __forceinline__ void next(const TreeArgs& a) {
     if (++kt == nkt) next_rows(a);
   }
 };
 
-// The units [lo, hi) of this CTA out of `total` in `ctas` equal runs, and where they begin.  A run has at
-// least Keys::LEAST units but for the last few (none is empty between two that share a tile, and parts stay
-// cheap beside the work on them): the CTAs past `ctas` have none.
-// `before` [n_req] is scratch in shared memory, free again after the call.
 // (a division of 64-bit numbers is a subroutine; nearly all are small)
 __device__ __forceinline__ unsigned long long tree_div(unsigned long long a, unsigned long long b) {
   return (a | b) >> 32 ? a / b : static_cast<unsigned>(a) / static_cast<unsigned>(b);
 }
 
+// The units [lo, hi) of this CTA: its key head's units, `total` of them, are cut into equal runs, and CTA c has
+// run c / heads of head c % heads.  So the CTAs that read the heads of the same tokens, which lie side by side
+// in the cache, do it at the same time: a head's 128 or 160 bytes of a token alone make poor use of DRAM.  A
+// run has at least Keys::LEAST units but for the last few (none is empty between two that share a tile, and
+// parts stay cheap beside the work on them).  `before` [n_req] is scratch in shared memory, free again after
+// the call.
 template <class Keys>
 struct TreeRun {
-  unsigned long long lo, hi, total, ctas, least, more;
+  unsigned long long lo, hi, least, more;
   TreePlace<Keys> at;
 
   template <int THREADS>
   __device__ __forceinline__ bool find(const TreeArgs& a, unsigned long long* before) {
     __shared__ unsigned long long carry[THREADS / 32];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    total = 0;
+    unsigned long long total = 0;
     for (int i0 = 0; i0 < a.n_req; i0 += THREADS) {
       const int i = i0 + tid;
       unsigned long long n = 0;
       if (i < a.n_req) {
         const TreeRequest r = tree_request(a, i);
-        if (r.n > 0) n = static_cast<unsigned long long>(Keys::tiles(r)) * tree_row_tiles(a, r) * a.cache.heads;
+        if (r.n > 0) n = static_cast<unsigned long long>(Keys::tiles(r)) * tree_row_tiles(a, r);
       }
       unsigned long long run = n;
 #pragma unroll
@@ -129,15 +128,15 @@ struct TreeRun {
       if (i < a.n_req) before[i] = ahead + run - n;
       __syncthreads();
     }
-    const unsigned long long most = (total + Keys::LEAST - 1) / Keys::LEAST;
-    ctas = most < gridDim.x ? most : gridDim.x;
     if (tid == 0) a.joins[2 * blockIdx.x].x = -1;
-    if (blockIdx.x >= ctas) return false;
+    const unsigned run = blockIdx.x / a.cache.heads, all = gridDim.x / a.cache.heads;
+    const unsigned long long most = tree_div(total + Keys::LEAST - 1, Keys::LEAST), runs = most < all ? most : all;
+    if (run >= runs) return false;
     // the first `more` runs have one unit more than the others
-    least = tree_div(total, ctas);
-    more = total - least * ctas;
-    lo = least * blockIdx.x + min(static_cast<unsigned long long>(blockIdx.x), more);
-    hi = lo + least + (blockIdx.x < more ? 1 : 0);
+    least = tree_div(total, runs);
+    more = total - least * runs;
+    lo = least * run + min(static_cast<unsigned long long>(run), more);
+    hi = lo + least + (run < more ? 1 : 0);
     int i = 0, j = a.n_req - 1;  // last request with before <= lo: it has units
     while (i < j) {
       const int mid = (i + j + 1) >> 1;
@@ -145,21 +144,21 @@ struct TreeRun {
     }
     const unsigned long long off = lo - before[i];
     at.enter(a, i);
-    const unsigned long long tiles = tree_div(off, at.nkt);  // of rows, before this one
-    at.kt = static_cast<int>(off - tiles * at.nkt);
-    at.head = static_cast<int>(tree_div(tiles, at.nrt));
-    at.rt = static_cast<int>(tiles - static_cast<unsigned long long>(at.head) * at.nrt);
+    at.rt = static_cast<int>(tree_div(off, at.nkt));
+    at.kt = static_cast<int>(off - static_cast<unsigned long long>(at.rt) * at.nkt);
+    at.head = blockIdx.x - run * a.cache.heads;
     __syncthreads();
     return true;
   }
 
   // Notes that the run begins the tile of rows at `p` (as its second part or its first) and another ends it;
-  // `unit`: the run's unit that is the tile's first.
+  // `unit`: the head's unit that is the tile's first.
   __device__ __forceinline__ void note_join(const TreeArgs& a, const TreePlace<Keys>& p, unsigned long long unit) const {
-    const unsigned long long last = unit + p.nkt - 1, longer = more * (least + 1);  // the CTA that has it:
-    const unsigned long long end = last < longer ? tree_div(last, least + 1) : more + tree_div(last - longer, least);
+    const unsigned long long last = unit + p.nkt - 1, longer = more * (least + 1);
+    const unsigned long long end = last < longer ? tree_div(last, least + 1) : more + tree_div(last - longer, least);  // its run
+    const int parts = static_cast<int>(end) - static_cast<int>(blockIdx.x / a.cache.heads) + 1;
     const int x0 = p.rt * a.tile_rows;
-    a.joins[2 * blockIdx.x] = make_int4(p.head, x0, p.r.row0, 2 * static_cast<int>(end) + (unit > lo ? 1 : 0));
+    a.joins[2 * blockIdx.x] = make_int4(p.head, x0, p.r.row0, 2 * parts + (unit > lo ? 1 : 0));
     a.joins[2 * blockIdx.x + 1] = make_int4(min(a.tile_rows, p.r.n * a.group - x0), 0, 0, 0);
   }
 };

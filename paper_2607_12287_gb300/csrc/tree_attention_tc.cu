@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(THREADS, 2)
 
   if (warp == 4) {
     fence_proxy_async_smem();  // (the ring was scratch)
-    const uint64_t policy = l2_policy_evict_normal();
+    const uint64_t policy = l2_policy_evict_first();
     const uint32_t q_bytes = a.tile_rows * (128 + W2 * 2);
     const int boxes = KB >> box_shift, page_mask = (1 << a.cache.page_shift) - 1;
     TreePlace<B> p = run.at;
