@@ -62,9 +62,15 @@ __device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr)
                : "memory");
 }
 
-// 16 bytes to shared memory, or zeros (nothing is read) if not `ok`.
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool ok) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+// 16 bytes to shared memory, or zeros (nothing is read) if not `ok`.  HINT: with an L2 policy.  Keys and values pass
+// through L2 once: asked to leave it first, they do not push out the parts of the runs, nor the kernels' own instructions.
+template <bool HINT>
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool ok, uint64_t policy) {
+  if (HINT)
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0), "l"(policy)
+                 : "memory");
+  else
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -83,10 +89,11 @@ struct Cfg {
   static constexpr bool PADDED = DP == 80 || DP == 96;
   static constexpr int ROW = 2 * DP + (PADDED ? 16 : 0);
   static constexpr int TILE = TK * ROW;
-  static constexpr int CTAS = ALONE ? (DP <= 64 ? 4 : 2) : DP <= 128 && RW < 8 ? 2 : 1;  // per SM
+  static constexpr int CTAS = ALONE ? (DP <= 64 ? 4 : DP <= 80 ? 3 : 2) : DP <= 128 && RW < 8 ? 2 : 1;  // per SM
   static constexpr bool QSMEM = DP > 128;                                    // queries in shared memory, not registers
   static constexpr int STAGES = ALONE ? (DP <= 128 ? 3 : 1) : DP > 128 ? 2 : 3;
   static constexpr int TERMS = RW < 4 ? 2 : 1;
+  static constexpr bool HINT = ALONE && DP <= 128;                           // (64 requests, heads of 64: 70 -> 64 us)
   // a copy of a tile (of the warp's keys if it is alone): CP lanes for the pieces of a row, RP rows at a time
   static constexpr int CP = DP <= 64 ? 8 : DP <= 128 ? 16 : 32, RP = (ALONE ? 32 : THREADS) / CP, COPIES = (ALONE ? WK : TK) / RP;
   static constexpr int MEET = DP + 4;                                        // floats of a row where the warps meet
@@ -173,6 +180,7 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
       for (int x = 0; x < IDS; ++x) ids[x] = key + x * RP < load.r.len ? table[(key + x * RP) >> a.cache.page_shift] : -1;
     }
   };
+  const uint64_t policy = C::HINT ? l2_policy_evict_first() : 0;
   const auto copy = [&](int stage) {
     if (cp >= pieces) return;
     const uint32_t ks = sb + stage * 2 * C::TILE, vs = ks + C::TILE;
@@ -191,8 +199,8 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
 #pragma unroll
       for (int x = 0; x < COPIES; ++x) {
         if (!ONE_PAGE && x > 0) off = cached(x, ok);
-        copy16(ks + place(x), kc + off, ok);
-        copy16(vs + place(x), vc + off, ok);
+        copy16<C::HINT>(ks + place(x), kc + off, ok, policy);
+        copy16<C::HINT>(vs + place(x), vc + off, ok, policy);
         if (ONE_PAGE) off += step;
       }
       return;
@@ -214,8 +222,8 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
           v = static_cast<const T*>(a.v_new) + row * a.v_new_stride + col;
         }
       }
-      copy16(ks + place(x), k, ok);
-      copy16(vs + place(x), v, ok);
+      copy16<C::HINT>(ks + place(x), k, ok, policy);
+      copy16<C::HINT>(vs + place(x), v, ok, policy);
     }
   };
 
