@@ -459,23 +459,25 @@ __global__ void __launch_bounds__(THREADS, BWD_CTAS) qk_norm_rope_backward_kerne
 }
 
 // Sums of the CTAs' partial weight gradients, 32 values per CTA, in an order that depends on n alone.
-__global__ void __launch_bounds__(THREADS) weight_gradient_kernel(const float* partial, int n, int dim, float* dq, float* dk) {
-  __shared__ float sm[WARPS][32];
+constexpr int SUM_WARPS = 32;
+__global__ void __launch_bounds__(32 * SUM_WARPS) weight_gradient_kernel(const float* partial, int n, int dim, float* dq, float* dk) {
+  __shared__ float sm[SUM_WARPS][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
   pdl_wait();
   pdl_launch_dependents();
   float sum = 0.f;
   if (e < 2 * dim)
 #pragma unroll 8
-    for (int i = warp; i < n; i += WARPS) sum += partial[static_cast<size_t>(i) * 2 * dim + e];
+    for (int i = warp; i < n; i += SUM_WARPS) sum += partial[static_cast<size_t>(i) * 2 * dim + e];
   sm[warp][lane] = sum;
   __syncthreads();
-  if (warp == 0 && e < 2 * dim) {
+  // warp w adds up value w of the 32
+  sum = sm[lane][warp];
 #pragma unroll
-    for (int w = 1; w < WARPS; ++w) sum += sm[w][lane];
-    float* out = e < dim ? dq : dk;
-    if (out) out[e < dim ? e : e - dim] = sum;
-  }
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  const int d = blockIdx.x * 32 + warp;
+  float* out = d < dim ? dq : dk;
+  if (lane == 0 && d < 2 * dim && out) out[d < dim ? d : d - dim] = sum;
 }
 
 bool valid(const ivit_rope_config& c) {
@@ -660,7 +662,7 @@ extern "C" int ivit_qk_norm_rope_backward(const ivit_rope_config* cfg, int32_t n
     });
   }
   if (e == cudaSuccess && weights)
-    e = launch_ex(weight_gradient_kernel, dim3((2 * cfg->head_dim + 31) / 32), dim3(THREADS), 0, s, 1,
+    e = launch_ex(weight_gradient_kernel, dim3((2 * cfg->head_dim + 31) / 32), dim3(32 * SUM_WARPS), 0, s, 1,
                   static_cast<const float*>(p.partial), grid, cfg->head_dim, dq_weight_dev, dk_weight_dev);
   return e == cudaSuccess ? IVIT_OK : fail_cuda(e);
 }
