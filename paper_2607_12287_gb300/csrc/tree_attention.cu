@@ -600,12 +600,13 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
   }
 }
 
-// Joins the parts of a tile of rows that several runs have, in the order of their keys.  Blocks (i, y) look
-// for the i-th such tile among the runs' notes.  Up to FEW parts, a thread takes 4 columns of a row and
+// Joins the parts of a tile of rows that several runs have, in the order of their keys.  Blocks (i, y) take the
+// tile that CTA i's run begins or, where the call has few tiles (`search`), look for the i-th of them among the
+// runs' notes.  Up to FEW parts, a thread takes 4 columns of a row and
 // reads four parts at a time; more parts are shared by the warps of a block, a row at a time, which meet in
 // shared memory.
 template <typename T, int DP, int M>
-__global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a, int ctas) {
+__global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a, int ctas, bool search) {
   constexpr int PART = tree_part_floats(M, DP), WARPS = 8, VEC = (DP / 4 + 31) / 32, FEW = 16, NOTES = 4;
   static_assert(NOTES * 256 >= 4 * TREE_MAX_SMS, "the notes of all CTAs");
   __shared__ float2 ml_of[WARPS];
@@ -615,31 +616,35 @@ __global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a, int ct
   if (tid == 0) which = -1;
   pdl_wait();
   pdl_launch_dependents();
-  bool has[NOTES];
-  unsigned mine[NOTES];
+  int c = blockIdx.x;
+  if (search) {
+    bool has[NOTES];
+    unsigned mine[NOTES];
 #pragma unroll
-  for (int k = 0; k < NOTES; ++k) has[k] = 256 * k + tid < ctas && a.joins[2 * (256 * k + tid)].x >= 0;
+    for (int k = 0; k < NOTES; ++k) has[k] = 256 * k + tid < ctas && a.joins[2 * (256 * k + tid)].x >= 0;
 #pragma unroll
-  for (int k = 0; k < NOTES; ++k) {
-    mine[k] = __ballot_sync(0xffffffffu, has[k]);
-    if (lane == 0) found[k][warp] = __popc(mine[k]);
-  }
-  __syncthreads();
-  int before = 0;
-#pragma unroll
-  for (int k = 0; k < NOTES; ++k) {
-    int rank = before + __popc(mine[k] & ((1u << lane) - 1));
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
-      if (w < warp) rank += found[k][w];
-      before += found[k][w];
+    for (int k = 0; k < NOTES; ++k) {
+      mine[k] = __ballot_sync(0xffffffffu, has[k]);
+      if (lane == 0) found[k][warp] = __popc(mine[k]);
     }
-    if (has[k] && rank == static_cast<int>(blockIdx.x)) which = 256 * k + tid;
+    __syncthreads();
+    int before = 0;
+#pragma unroll
+    for (int k = 0; k < NOTES; ++k) {
+      int rank = before + __popc(mine[k] & ((1u << lane) - 1));
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        if (w < warp) rank += found[k][w];
+        before += found[k][w];
+      }
+      if (has[k] && rank == static_cast<int>(blockIdx.x)) which = 256 * k + tid;
+    }
+    __syncthreads();
+    c = which;
+    if (c < 0) return;
   }
-  __syncthreads();
-  const int c = which;
-  if (c < 0) return;
   const int4 note = a.joins[2 * c], rest = a.joins[2 * c + 1];
+  if (note.x < 0) return;
   const int head = note.x, x0 = note.y, row0 = note.z, n = note.w >> 1, rows = rest.x;
   // the tile's parts: CTA c's second or first, then the first ones of the head's CTAs behind it
   const float* parts = a.parts + static_cast<size_t>(2 * c) * PART;
@@ -776,10 +781,11 @@ cudaError_t launch(const Plan& p, const TreeArgs& a, int dtype, int ctas, cudaSt
     // at most one joined tile per run and tile of rows; a thread for 4 columns of a row, up to some 16 blocks per SM
     const long long most = static_cast<long long>(a.max_new) * a.group;  // rows that share a key head
     const long long tiles = static_cast<long long>(a.n_req) * a.cache.heads * ((most + a.tile_rows - 1) / a.tile_rows);
-    const int x = static_cast<int>(std::min<long long>(tiles, ctas)), rows = static_cast<int>(std::min<long long>(a.tile_rows, most));
+    const bool search = 4 * tiles < ctas;
+    const int x = search ? static_cast<int>(tiles) : ctas, rows = static_cast<int>(std::min<long long>(a.tile_rows, most));
     const int blocks = ctas > 8 * x ? rows : (rows * (DP / 4) + 255) / 256;  // (many parts: a block for a row)
     const int y = std::max(1, std::min(blocks, 8 * ctas / x));
-    return launch_ex(tree_join_kernel<T, DP, decltype(m)::value>, dim3(x, y), dim3(256), 0, s, 1, a, ctas);
+    return launch_ex(tree_join_kernel<T, DP, decltype(m)::value>, dim3(x, y), dim3(256), 0, s, 1, a, ctas, search);
   };
   cudaError_t e;
   if (p.tc) {
