@@ -370,10 +370,13 @@ typedef struct ivit_attention_config {
  * table_dev int32 [n_req][max_pages]; len_dev int32 [n_req] (more than the table holds counts as
  * that much, pages outside the cache read as zeros); cu_rows_dev int32 [n_req + 1];
  * mask_dev uint32 [n_rows][mask_words] for IVIT_MASK_TREE, else NULL; out [n_rows][heads]
- * [head_dim], lse_dev fp32 [n_rows][heads] or NULL.  Row strides as in ivit_qk_norm_rope; rows
- * that belong to no request are left as they are.  workspace_dev: 16-byte aligned,
- * ivit_tree_attention_workspace(cfg, cache) bytes (0: invalid arguments), of no meaning between
- * calls; calls that overlap on the GPU need one each. */
+ * [head_dim], lse_dev fp32 [n_rows][heads] or NULL.  Row strides as in ivit_qk_norm_rope, but
+ * positive; rows that belong to no request are left as they are.  max_new is a bound that the
+ * caller vouches for; it chooses the kernel (tcgen05 for more than 16 rows per key head, where
+ * heads are at most 128 wide and pages of at least 8 tokens).  workspace_dev: 16-byte aligned,
+ * ivit_tree_attention_workspace(cfg, cache) bytes (0: invalid arguments), needs no
+ * initialisation; calls that overlap on the GPU need one each.  Its first int32 is 0 after a
+ * call, or not if one of the kernel's bounded waits expired (then outputs are not valid). */
 size_t ivit_tree_attention_workspace(const ivit_attention_config* cfg, const ivit_cache_layout* cache);
 int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_cache_layout* cache, int32_t n_rows,
                         const void* q_dev, int64_t q_stride, const void* k_new_dev, int64_t k_new_stride,

@@ -29,7 +29,11 @@ namespace ivit {
 namespace {
 
 constexpr int TK = 64;              // keys of a tile
-constexpr int TC_ROWS = 16, TC_ROWS_64 = 64;  // more rows per key head than this take the tcgen05 kernel (heads up to 64)
+// More rows per key head than this take the tcgen05 kernel where it can (heads of up to 128, pages of 8 tokens and more,
+// groups of up to 128).  Both sides, 16 requests of up to 8192 tokens, us: 32 rows of heads of 128 58 (tcgen05) and 70, 64
+// rows 60 and 79, 124 rows 64 and 137; heads of 64, 32 rows 31 and 33, 64 rows 32 and 35; one request of 1000 tokens, 32
+// rows, 12.3 and 11.6.
+constexpr int TC_ROWS = 16;
 
 struct Keys64 {
   static constexpr int LEAST = 1;
@@ -752,7 +756,7 @@ Plan plan(const ivit_attention_config& c, const ivit_cache_layout& l) {
   const int group = c.heads / l.kv_heads;
   const int rows = static_cast<int>(std::min<long long>(128, static_cast<long long>(c.max_new) * group));  // that share a key head
   const int dp = l.head_dim <= 64 ? 64 : l.head_dim <= 80 ? 80 : l.head_dim <= 96 ? 96 : l.head_dim <= 128 ? 128 : 256;
-  if (rows > (dp <= 64 ? TC_ROWS_64 : TC_ROWS) && dp <= 128 && group <= 128 && l.page_size >= 8 && l.head_stride > 0 && l.token_stride > 0 &&
+  if (rows > TC_ROWS && dp <= 128 && group <= 128 && l.page_size >= 8 && l.head_stride > 0 && l.token_stride > 0 &&
       l.page_stride > 0)
     return {true, dp == 96 ? 128 : dp, 0, tree_tc_rows(group), 2, tree_part_floats(128, dp == 96 ? 128 : dp)};
   // the smallest tile that holds the rows
@@ -833,9 +837,9 @@ extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_
   if (!q_dev || !k_new_dev || !v_new_dev || !k_cache_dev || !v_cache_dev || !table_dev || !len_dev || !cu_rows_dev ||
       !out_dev || !workspace_dev || (cfg->mask_mode == IVIT_MASK_TREE && !mask_dev))
     return fail(IVIT_ERR_ARG, "ivit_tree_attention: null pointer");
-  if ((q_stride | k_new_stride | v_new_stride | out_stride) & 7 || q_stride < 0 || k_new_stride < 0 || v_new_stride < 0 ||
-      out_stride < 0)
-    return fail(IVIT_ERR_ARG, "ivit_tree_attention: row strides must be multiples of 8 elements");
+  if ((q_stride | k_new_stride | v_new_stride | out_stride) & 7 || q_stride <= 0 || k_new_stride <= 0 || v_new_stride <= 0 ||
+      out_stride <= 0)
+    return fail(IVIT_ERR_ARG, "ivit_tree_attention: row strides must be positive multiples of 8 elements");
   if (!all_aligned({q_dev, k_new_dev, v_new_dev, k_cache_dev, v_cache_dev, out_dev, workspace_dev}, 16) ||
       !all_aligned({table_dev, len_dev, cu_rows_dev, mask_dev, lse_dev}, 4))
     return fail(IVIT_ERR_ARG, "ivit_tree_attention: arrays must be 16-byte aligned (table, lengths, offsets, mask and lse 4)");

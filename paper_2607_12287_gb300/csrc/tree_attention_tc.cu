@@ -51,7 +51,7 @@ struct Cfg {
 
 template <int KB>
 struct Blocks {
-  static constexpr int LEAST = 256 / KB;
+  static constexpr int LEAST = 128 / KB;
   static __device__ __forceinline__ int cached(const TreeRequest& r) { return (r.len + KB - 1) / KB; }
   static __device__ __forceinline__ int tiles(const TreeRequest& r) { return cached(r) + (r.n + KB - 1) / KB; }
 };

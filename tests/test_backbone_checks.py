@@ -161,7 +161,7 @@ def test_attention_pointers_and_strides(lib):
     assert attention(lib, attention_config(), layout(), n=-1) == pkg.IVIT_ERR_ARG
     for change in (dict(q=None), dict(k=None), dict(vc=None), dict(table=None), dict(len=None), dict(cu=None), dict(mask=None),
                    dict(out=None), dict(ws=None), dict(q=ODD4), dict(kc=ODD4), dict(ws=ODD4), dict(mask=ODD), dict(lse=ODD),
-                   dict(qs=4), dict(os=-8)):
+                   dict(qs=4), dict(os=-8), dict(ks=0), dict(vs=0)):
         assert attention(lib, attention_config(), layout(), **change) == pkg.IVIT_ERR_ARG, change
     assert attention(lib, attention_config(), layout(), n=0, q=None) == pkg.IVIT_OK
 

@@ -337,6 +337,7 @@ def run_attention(pkg, c, mask, vis=None, lse=True, check=True, scale=None, max_
     ws = torch.full((pkg.ivit_tree_attention_workspace(cfg, lay),), 255, dtype=torch.uint8, device="cuda")
     pkg.ivit_tree_attention(cfg, lay, c["q"], c["k"], c["v"], c["kc"], c["vc"], i32(c["table"]), i32(c["lengths"]), i32(c["cu"]),
                             packed, out, got_lse, ws)
+    assert int(ws[:4].view(torch.int32)) == 0  # no wait of the kernel expired
     if not check:
         return out, got_lse
     sees = {"causal": lambda i, n: np.tril(np.ones((n, n), bool)), "all": lambda i, n: np.ones((n, n), bool),
