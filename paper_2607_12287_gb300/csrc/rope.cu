@@ -13,7 +13,10 @@
 // Heads go through a warp four at a time, loads first, so that four chains of unpack, sum, shuffle and
 // scale overlap.
 //
-// Bound: HBM for many rows, the launch and two dependent round trips for a few.
+// Bound: HBM for many rows, the launch and two dependent round trips for a few.  Measured: 32768 rows of 16 + 16
+// heads of 72 58.5 us (5.2 TB/s read and written), gradients of 16385 rows of 32 + 8 heads of 128 94 us (5.4 TB/s),
+// 8 rows of 32 + 8 heads of 128 into the cache 2.7 us.  A step of the warp over heads of one row, with the
+// cosines in every group, took 140 us instead of 58.5 (the groups' last steps partly empty, 290 instructions a step).
 #include <algorithm>
 #include <type_traits>
 

@@ -11,15 +11,19 @@
 // that holds a tile's keys only in part leaves its running maximum, sum and output (fp32) in
 // the workspace, and a second kernel joins the parts of a tile in the order of their keys.
 //
-// A CTA of four warps: 16-byte asynchronous copies fill a ring of K and V tiles in shared memory
-// (swizzled; the pages are looked up one tile ahead), mma.m16n8k16 multiplies.  Row groups of 16 are
-// split over the warps and, for 16 and 32 rows, the 64 keys too (KW warps with a running maximum,
-// sum and output each, which meet in shared memory at the end).  Probabilities enter the product
-// with V as two 16-bit terms (their fp32 value but for 16 of 24 bits and more) up to 32 rows, where
-// the bytes of the cache bound the kernel and the second product is free, and rounded to one
-// above; sums use their fp32 values.
+// Tiles of 16 rows (a step of one token, small trees): the 64 keys of a tile belong to the four warps, 16 each.  A
+// warp copies its own keys and values with 16-byte asynchronous copies into its part of a ring of tiles in shared
+// memory, looks the pages up a tile ahead, and walks on without a barrier; its running maximum, sum and output
+// meet the others' at the end of a tile of rows.  Products by mma.m16n8k16; probabilities enter the one with V
+// as two 16-bit terms (16 bits and more of their fp32 value), which is free beside the cache's bytes.
+// Tiles of 32 to 128 rows are for what the tcgen05 kernel (tree_attention_tc.cu) does not take: heads wider than
+// 128, pages of fewer than 8 tokens, groups of more than 128 heads.  Row groups of 16 are split over four or
+// eight warps that share the keys, the 64 keys too for 32 rows; probabilities are rounded once from 64 rows on.
+// Sums use the fp32 values everywhere.
 //
-// Bound: the cache's bytes for few rows per key head, mma.sync's rate for many.
+// Bound: the cache's bytes for few rows per key head (32 requests of up to 16384 tokens, 32 + 8 heads of 128, 168 us:
+// 6600 GB/s; 64 of up to 8192, 16 + 4 heads of 64, 49.5 us: 5500 GB/s), the chain of dependent reads of a start
+// for short ones (one request of 1041 tokens 7.4 us), mma.sync's rate for many rows.
 #include <algorithm>
 #include <type_traits>
 
