@@ -330,9 +330,10 @@ int ivit_qk_norm_rope(const ivit_rope_config* cfg, int32_t n_rows, const void* q
 /* Gradients of the above: from grad_q, grad_k (of q_out, k_out) and the inputs q, k to dq, dk
  * (which may be grad_q, grad_k, or q, k, with the same strides) and, where
  * there is a weight, dq_weight_dev, dk_weight_dev fp32 [head_dim] (or NULL), summed over rows
- * and heads in an order that depends on the sizes alone.  workspace_dev: 16-byte aligned,
- * ivit_qk_norm_rope_backward_workspace(cfg) bytes (0: cfg is invalid), of no meaning between
- * calls; calls that overlap on the GPU need one each. */
+ * and heads in an order that depends on the sizes alone.  workspace_dev (needed for weight
+ * gradients alone): 16-byte aligned, workspace_bytes at least
+ * ivit_qk_norm_rope_backward_workspace(cfg) (which gives 0 for an invalid cfg), of no meaning
+ * between calls; calls that overlap on the GPU need one each. */
 size_t ivit_qk_norm_rope_backward_workspace(const ivit_rope_config* cfg);
 int ivit_qk_norm_rope_backward(const ivit_rope_config* cfg, int32_t n_rows, const void* grad_q_dev,
                                int64_t grad_q_stride, const void* grad_k_dev, int64_t grad_k_stride,
@@ -341,7 +342,7 @@ int ivit_qk_norm_rope_backward(const ivit_rope_config* cfg, int32_t n_rows, cons
                                int64_t pos_stride, const float* freq_dev, const int32_t* axis_dev,
                                void* dq_dev, int64_t dq_stride, void* dk_dev, int64_t dk_stride,
                                float* dq_weight_dev, float* dk_weight_dev, void* workspace_dev,
-                               void* stream);
+                               size_t workspace_bytes, void* stream);
 
 #define IVIT_MASK_CAUSAL 0     /* a row sees itself and the request's rows before it */
 #define IVIT_MASK_ALL 1        /* a row sees all of the request's rows */
@@ -374,8 +375,8 @@ typedef struct ivit_attention_config {
  * positive; rows that belong to no request are left as they are.  max_new is a bound that the
  * caller vouches for; it chooses the kernel (tcgen05 for more than 16 rows per key head, where
  * heads are at most 128 wide and pages of at least 8 tokens).  workspace_dev: 16-byte aligned,
- * ivit_tree_attention_workspace(cfg, cache) bytes (0: invalid arguments), needs no
- * initialisation; calls that overlap on the GPU need one each.  Its first int32 is 0 after a
+ * workspace_bytes at least ivit_tree_attention_workspace(cfg, cache) (0: invalid arguments), needs
+ * no initialisation; calls that overlap on the GPU need one each.  Its first int32 is 0 after a
  * call, or not if one of the kernel's bounded waits expired (then outputs are not valid). */
 size_t ivit_tree_attention_workspace(const ivit_attention_config* cfg, const ivit_cache_layout* cache);
 int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_cache_layout* cache, int32_t n_rows,
@@ -383,7 +384,8 @@ int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_cache_layou
                         const void* v_new_dev, int64_t v_new_stride, const void* k_cache_dev,
                         const void* v_cache_dev, const int32_t* table_dev, const int32_t* len_dev,
                         const int32_t* cu_rows_dev, const uint32_t* mask_dev, void* out_dev,
-                        int64_t out_stride, float* lse_dev, void* workspace_dev, void* stream);
+                        int64_t out_stride, float* lse_dev, void* workspace_dev, size_t workspace_bytes,
+                        void* stream);
 
 /* Row src_row_dev[i] of k and v ([n_layers][n_src][kv_heads][head_dim], row and layer strides in
  * elements, multiples of 8) into slot slot_dev[i] of every layer's cache (k_cache_dev,

@@ -118,10 +118,10 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     L.ivit_qk_norm_rope_backward_workspace.restype = C.c_size_t
     L.ivit_qk_norm_rope_backward_workspace.argtypes = [P]
     L.ivit_qk_norm_rope_backward.argtypes = [P, I32, P, I64, P, I64, P, I64, P, I64, P, P, P, I64, P, P, P, I64, P, I64, P,
-                                             P, P, P]
+                                             P, P, C.c_size_t, P]
     L.ivit_tree_attention_workspace.restype = C.c_size_t
     L.ivit_tree_attention_workspace.argtypes = [P, P]
-    L.ivit_tree_attention.argtypes = [P, P, I32, P, I64, P, I64, P, I64, P, P, P, P, P, P, P, I64, P, P, P]
+    L.ivit_tree_attention.argtypes = [P, P, I32, P, I64, P, I64, P, I64, P, P, P, P, P, P, P, I64, P, P, C.c_size_t, P]
     L.ivit_kv_write.argtypes = [P, I32, I32, I32, P, P, I64, I64, P, P, P, P, I64, P]
     _lib = L
     return L
@@ -418,7 +418,16 @@ def _rows(t, name: str, dtype: int, shape: tuple) -> tuple:
     return t.data_ptr(), st[0] if sh[0] > 1 else heads * dim
 
 
+def _workspace(t) -> tuple:
+    """Pointer and bytes (the library compares them with what it needs)."""
+    return _arg(t, "workspace", "uint8", 0), 0 if t is None else t.numel()
+
+
 def _row_count(t, name: str) -> int:
+    if type(t) is _dtypes.get("tensor"):
+        sh = t.shape
+        if len(sh) == 3:
+            return sh[0]
     if t is None or isinstance(t, (int, np.ndarray)) or len(t.shape) != 3:
         raise ValueError(f"{name}: a CUDA tensor [rows, heads, head_dim] is required")
     return t.shape[0]
@@ -509,13 +518,10 @@ def ivit_qk_norm_rope_backward(cfg: IvitRopeConfig, grad_q, grad_k, q, k, q_weig
     n, dt, dim = _row_count(q, "q"), cfg.dtype, cfg.head_dim
     q_shape, k_shape = (n, cfg.heads, dim), (n, cfg.kv_heads, dim)
     dqw, dkw = _arg(dq_weight, "dq_weight", "float32", dim), _arg(dk_weight, "dk_weight", "float32", dim)
-    ws = None
-    if dqw or dkw:
-        ws = _arg(workspace, "workspace", "uint8", ivit_qk_norm_rope_backward_workspace(cfg))
     args = (C.addressof(cfg), n, *_rows(grad_q, "grad_q", dt, q_shape), *_rows(grad_k, "grad_k", dt, k_shape),
             *_rows(q, "q", dt, q_shape), *_rows(k, "k", dt, k_shape),
             *_rope_inputs(cfg, n, q_weight, k_weight, positions, freq, axis), *_rows(dq, "dq", dt, q_shape),
-            *_rows(dk, "dk", dt, k_shape), dqw, dkw, ws, _stream(stream))
+            *_rows(dk, "dk", dt, k_shape), dqw, dkw, *_workspace(workspace), _stream(stream))
     _check(load().ivit_qk_norm_rope_backward(*args), None)
 
 
@@ -537,7 +543,7 @@ def ivit_tree_attention(cfg: IvitAttentionConfig, cache: IvitCacheLayout, q, k_n
             _arg(table, "table", "int32", req * cfg.max_pages), _arg(lengths, "lengths", "int32", req),
             _arg(cu_rows, "cu_rows", "int32", req + 1), _arg(mask, "mask", "int32", n * cfg.mask_words),
             *_rows(out, "out", dt, q_shape), _arg(lse, "lse", "float32", n * heads),
-            _arg(workspace, "workspace", "uint8", ivit_tree_attention_workspace(cfg, cache)), _stream(stream))
+            *_workspace(workspace), _stream(stream))
     _check(load().ivit_tree_attention(*args), None)
 
 

@@ -611,7 +611,8 @@ extern "C" int ivit_qk_norm_rope_backward(const ivit_rope_config* cfg, int32_t n
                                           const void* q_weight_dev, const void* k_weight_dev, const int32_t* pos_dev,
                                           int64_t pos_stride, const float* freq_dev, const int32_t* axis_dev,
                                           void* dq_dev, int64_t dq_stride, void* dk_dev, int64_t dk_stride,
-                                          float* dq_weight_dev, float* dk_weight_dev, void* workspace_dev, void* stream) {
+                                          float* dq_weight_dev, float* dk_weight_dev, void* workspace_dev,
+                                          size_t workspace_bytes, void* stream) {
   using namespace ivit;
   if (!cfg || n_rows < 0)
     return fail(IVIT_ERR_ARG, "ivit_qk_norm_rope_backward: null configuration or a negative row count");
@@ -622,7 +623,8 @@ extern "C" int ivit_qk_norm_rope_backward(const ivit_rope_config* cfg, int32_t n
   if (n_rows > 0 && (!grad_q_dev || !grad_k_dev || !q_dev || !k_dev || !pos_dev || !dq_dev || !dk_dev ||
                      (cfg->rot_dim > 0 && (!freq_dev || !axis_dev))))
     return fail(IVIT_ERR_ARG, "ivit_qk_norm_rope_backward: null pointer");
-  if (weights && !workspace_dev) return fail(IVIT_ERR_ARG, "ivit_qk_norm_rope_backward: null workspace");
+  if (weights && (!workspace_dev || workspace_bytes < ivit_qk_norm_rope_backward_workspace(cfg)))
+    return fail(IVIT_ERR_ARG, "ivit_qk_norm_rope_backward: the workspace is null or too small");
   if ((grad_q_stride | grad_k_stride | q_stride | k_stride | dq_stride | dk_stride) & 7 || grad_q_stride < 0 ||
       grad_k_stride < 0 || q_stride < 0 || k_stride < 0 || dq_stride < 0 || dk_stride < 0 || pos_stride < 0)
     return fail(IVIT_ERR_ARG, "ivit_qk_norm_rope_backward: row strides must be multiples of 8 elements");

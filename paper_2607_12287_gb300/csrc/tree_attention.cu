@@ -775,6 +775,11 @@ Plan plan(const ivit_attention_config& c, const ivit_cache_layout& l) {
                      : groups(std::integral_constant<int, 256>{});
 }
 
+// The error word, then of each CTA a note and two parts.
+size_t workspace_of(const Plan& p) {
+  return 16 + static_cast<size_t>(p.ctas_per_sm) * TREE_MAX_SMS * (2 * sizeof(int4) + 2 * sizeof(float) * p.part_floats);
+}
+
 template <typename T, int DP, int RW, bool ONE_PAGE = false>
 cudaError_t launch_rows(const TreeArgs& a, int ctas, cudaStream_t s) {
   using C = Cfg<DP, RW>;
@@ -816,11 +821,7 @@ cudaError_t launch(const Plan& p, const TreeArgs& a, int dtype, int ctas, cudaSt
 }  // namespace ivit
 
 extern "C" size_t ivit_tree_attention_workspace(const ivit_attention_config* cfg, const ivit_cache_layout* cache) {
-  using namespace ivit;
-  if (!cfg || !cache || !valid(*cfg, *cache)) return 0;
-  const Plan p = plan(*cfg, *cache);
-  // the error word, then of each CTA a note and two parts
-  return 16 + static_cast<size_t>(p.ctas_per_sm) * TREE_MAX_SMS * (2 * sizeof(int4) + 2 * sizeof(float) * p.part_floats);
+  return cfg && cache && ivit::valid(*cfg, *cache) ? ivit::workspace_of(ivit::plan(*cfg, *cache)) : 0;
 }
 
 extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_cache_layout* cache, int32_t n_rows,
@@ -828,7 +829,7 @@ extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_
                                    const void* v_new_dev, int64_t v_new_stride, const void* k_cache_dev,
                                    const void* v_cache_dev, const int32_t* table_dev, const int32_t* len_dev,
                                    const int32_t* cu_rows_dev, const uint32_t* mask_dev, void* out_dev, int64_t out_stride,
-                                   float* lse_dev, void* workspace_dev, void* stream) {
+                                   float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
   using namespace ivit;
   if (!cfg || !cache || n_rows < 0)
     return fail(IVIT_ERR_ARG, "ivit_tree_attention: null configuration or a negative row count");
@@ -847,6 +848,8 @@ extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_
   if (!all_aligned({q_dev, k_new_dev, v_new_dev, k_cache_dev, v_cache_dev, out_dev, workspace_dev}, 16) ||
       !all_aligned({table_dev, len_dev, cu_rows_dev, mask_dev, lse_dev}, 4))
     return fail(IVIT_ERR_ARG, "ivit_tree_attention: arrays must be 16-byte aligned (table, lengths, offsets, mask and lse 4)");
+  const Plan p = plan(*cfg, *cache);
+  if (workspace_bytes < workspace_of(p)) return fail(IVIT_ERR_ARG, "ivit_tree_attention: the workspace is too small");
   const int sms = sm_count();
   if (sms <= 0) return fail(IVIT_ERR_CUDA, "ivit_tree_attention: no CUDA device");
   TreeArgs a = {};
@@ -876,7 +879,6 @@ extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_
   a.mask_words = cfg->mask_words;
   a.scale_log2 = cfg->scale * 1.4426950408889634f;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const Plan p = plan(*cfg, *cache);
   // whole runs of all key heads, at least one (more CTAs than fit at a time wait for a place, not for each other)
   const int ctas = std::max(1, p.ctas_per_sm * std::min(TREE_MAX_SMS, sms) / cache->kv_heads) * cache->kv_heads;
   a.tile_rows = p.tile_rows;

@@ -88,7 +88,7 @@ def rope(lib, cfg, lay=None, n=3, **change):
 
 def rope_backward(lib, cfg, n=3, **change):
     a = dict(gq=OK, gqs=512, gk=OK, gks=512, q=OK, qs=512, k=OK, ks=512, qw=OK, kw=OK, pos=OK, ps=3, freq=OK, axis=OK, dq=OK,
-             dqs=512, dk=OK, dks=512, dqw=OK, dkw=OK, ws=OK)
+             dqs=512, dk=OK, dks=512, dqw=OK, dkw=OK, ws=OK, wb=1 << 40)
     a.update(change)
     return lib.ivit_qk_norm_rope_backward(C.addressof(cfg) if cfg else None, n, *a.values(), None)
 
@@ -115,7 +115,8 @@ def test_rope_pointers_and_strides(lib):
     for change in (dict(v=None), dict(kc=None), dict(vc=None), dict(slot=None), dict(vs=4), dict(vc=ODD4), dict(slot=ODD)):
         assert rope(lib, cfg, layout(), **change) == pkg.IVIT_ERR_ARG, change
     for change in (dict(gq=None), dict(dk=None), dict(q=None), dict(ws=None), dict(dqw=OK, qw=None), dict(gq=ODD4), dict(ws=ODD4),
-                   dict(dqs=12), dict(dkw=ODD), dict(gks=-8)):
+                   dict(dqs=12), dict(dkw=ODD), dict(gks=-8),
+                   dict(wb=lib.ivit_qk_norm_rope_backward_workspace(C.addressof(cfg)) - 1)):
         assert rope_backward(lib, cfg, **change) == pkg.IVIT_ERR_ARG, change
     assert rope(lib, cfg, n=0, q=None) == pkg.IVIT_OK
 
@@ -125,7 +126,7 @@ def test_cache_layouts(lib, field, value):
     lay = layout(**{field: value})
     assert rope(lib, pkg.make_rope_config(8, 2, 64), lay) == pkg.IVIT_ERR_SHAPE
     assert attention(lib, attention_config(), lay) == pkg.IVIT_ERR_SHAPE
-    assert lib.ivit_tree_attention_workspace(C.addressof(attention_config()), C.addressof(lay)) == 0
+    assert workspace(lib, attention_config(), lay) == 0
     assert write(lib, lay) == pkg.IVIT_ERR_SHAPE
 
 
@@ -141,8 +142,12 @@ def attention_config(**change):
     return cfg
 
 
+def workspace(lib, cfg, lay):
+    return lib.ivit_tree_attention_workspace(C.addressof(cfg), C.addressof(lay))
+
+
 def attention(lib, cfg, lay, n=9, **change):
-    a = dict(q=OK, qs=512, k=OK, ks=128, v=OK, vs=128, kc=OK, vc=OK, table=OK, len=OK, cu=OK, mask=OK, out=OK, os=512, lse=OK, ws=OK)
+    a = dict(q=OK, qs=512, k=OK, ks=128, v=OK, vs=128, kc=OK, vc=OK, table=OK, len=OK, cu=OK, mask=OK, out=OK, os=512, lse=OK, ws=OK, wb=1 << 40)
     a.update(change)
     return lib.ivit_tree_attention(C.addressof(cfg) if cfg else None, C.addressof(lay) if lay else None, n, *a.values(), None)
 
@@ -153,7 +158,7 @@ def attention(lib, cfg, lay, n=9, **change):
                                          ("scale", float("nan")), ("scale", float("inf"))])
 def test_attention_configuration(lib, field, value):
     assert attention(lib, attention_config(**{field: value}), layout()) == pkg.IVIT_ERR_SHAPE
-    assert lib.ivit_tree_attention_workspace(C.addressof(attention_config(**{field: value})), C.addressof(layout())) == 0
+    assert workspace(lib, attention_config(**{field: value}), layout()) == 0
 
 
 def test_attention_pointers_and_strides(lib):
@@ -161,7 +166,8 @@ def test_attention_pointers_and_strides(lib):
     assert attention(lib, attention_config(), layout(), n=-1) == pkg.IVIT_ERR_ARG
     for change in (dict(q=None), dict(k=None), dict(vc=None), dict(table=None), dict(len=None), dict(cu=None), dict(mask=None),
                    dict(out=None), dict(ws=None), dict(q=ODD4), dict(kc=ODD4), dict(ws=ODD4), dict(mask=ODD), dict(lse=ODD),
-                   dict(qs=4), dict(os=-8), dict(ks=0), dict(vs=0)):
+                   dict(qs=4), dict(os=-8), dict(ks=0), dict(vs=0),
+                   dict(wb=workspace(lib, attention_config(), layout()) - 1)):
         assert attention(lib, attention_config(), layout(), **change) == pkg.IVIT_ERR_ARG, change
     assert attention(lib, attention_config(), layout(), n=0, q=None) == pkg.IVIT_OK
 

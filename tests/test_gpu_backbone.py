@@ -374,6 +374,11 @@ ATTENTION = [  # cached, new, heads, kv, dim, page, type, order
     ([191, 192, 500], [128, 33, 97], 5, 1, 80, 128, "float16", "head"), ([700], [256], 2, 2, 64, 64, "bfloat16", "token"),
     ([0, 0, 127, 128, 129], [140, 3, 128, 129, 70], 2, 2, 64, 16, "float16", "token"),
     ([0, 64, 200], [75, 64, 1], 7, 1, 128, 16, "bfloat16", "token"), ([500], [65], 6, 2, 112, 256, "bfloat16", "head"),
+    # what tcgen05 does not take (small pages, wide heads): tiles of 16, 32 and 64 rows
+    ([64, 128], [16, 7], 1, 1, 80, 4, "bfloat16", "token"), ([70, 200], [20, 9], 2, 2, 64, 4, "bfloat16", "token"),
+    ([70, 0, 130], [50, 3, 1], 1, 1, 128, 2, "float16", "token"), ([66], [12], 8, 4, 96, 4, "bfloat16", "token"),
+    ([300, 40], [40, 17], 1, 1, 96, 1, "float16", "head"), ([90, 65], [30, 2], 1, 1, 256, 16, "bfloat16", "token"),
+    ([90, 65], [60, 2], 1, 1, 256, 8, "float16", "head"), ([129], [100], 2, 1, 128, 4, "bfloat16", "token"),
 ]
 
 
@@ -406,12 +411,13 @@ def test_rows_that_see_nothing(pkg):
         assert float(out[:5].abs().max()) == 0 and float(lse[:5].max()) == -np.inf
 
 
-@pytest.mark.parametrize("new", [4, 20, 100])
+@pytest.mark.parametrize("new,page,dim", [(4, 16, 64), (20, 16, 64), (100, 16, 64), (4, 4, 64), (10, 4, 64), (20, 4, 64), (100, 4, 64),
+                                          (4, 16, 256), (30, 16, 256), (60, 8, 128), (90, 8, 80)])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
-def test_what_a_row_does_not_see_does_not_reach_it(pkg, new, bad):
+def test_what_a_row_does_not_see_does_not_reach_it(pkg, new, page, dim, bad):
     import torch
     r = np.random.default_rng(new)
-    c = attention_case(r, [70], [new], 4, 2, 64, 16, "float16")
+    c = attention_case(r, [70], [new], 4, 2, dim, page, "float16")
     vis = [np.tril(np.ones((new, new), bool))]
     vis[0][:, 2] = False
     vis[0][new - 1, 2] = True          # only the last row sees draft 2
@@ -420,7 +426,7 @@ def test_what_a_row_does_not_see_does_not_reach_it(pkg, new, bad):
     c["k"][3] = c["k"][3]              # (its key is as it was)
     out, lse = run_attention(pkg, c, "tree", vis, check=False)
     assert torch.equal(lse, clean_lse)
-    others = torch.ones(new, 4, 64, dtype=torch.bool)
+    others = torch.ones(new, 4, dim, dtype=torch.bool)
     others[new - 1, 2:, 5] = False     # (query heads 2 and 3 read key head 1)
     assert torch.equal(out.cpu()[others], clean.cpu()[others])
     hit = out[new - 1, 2:, 5].float().cpu().numpy()
@@ -442,7 +448,8 @@ def test_large_scores_and_growing_maximum(pkg):
     run_attention(pkg, c, "causal", scale=0.125)
 
 
-def test_offsets_past_32_bits(pkg):
+@pytest.mark.parametrize("group", [1, 8])
+def test_offsets_past_32_bits(pkg, group):
     # pages at the far end of a cache of more than 2^32 elements
     import torch
     page, kv, dim = 16, 8, 128
@@ -450,7 +457,7 @@ def test_offsets_past_32_bits(pkg):
     r = np.random.default_rng(7)
     if torch.cuda.mem_get_info()[0] < 5 * pages * page * kv * dim:
         pytest.skip("needs 22 GB of device memory")
-    c = attention_case(r, [300], [3], 8, 8, dim, page, "bfloat16")
+    c = attention_case(r, [300], [3], 8 * group, 8, dim, page, "bfloat16")
     small = [c["kc"], c["vc"]]
     far = (pages - 1 - np.arange(small[0].shape[0])).astype(np.int64)
     big = torch.empty((pages, page, kv, dim), dtype=torch.bfloat16, device="cuda")
@@ -462,9 +469,9 @@ def test_offsets_past_32_bits(pkg):
     want, _ = run_attention(pkg, c, "causal")
     used = c["table"] >= 0
     far_table = np.where(used, far[np.maximum(c["table"], 0)], -1)
-    cfg = pkg.make_attention_config(1, 8, far_table.shape[1], 3, "causal", 0, dim ** -0.5)
+    cfg = pkg.make_attention_config(1, 8 * group, far_table.shape[1], 3, "causal", 0, dim ** -0.5)
     ws = torch.empty(pkg.ivit_tree_attention_workspace(cfg, lay), dtype=torch.uint8, device="cuda")
-    out = torch.empty((3, 8, dim), dtype=torch.bfloat16, device="cuda")
+    out = torch.empty((3, 8 * group, dim), dtype=torch.bfloat16, device="cuda")
     # values: the same table over a view that begins 2 * len(far) pages lower
     k_far = big[2 * len(far):]
     lay2 = pkg.make_cache_layout(k_far)
