@@ -610,15 +610,15 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
 
 // Joins the parts of a tile of rows that several runs have, in the order of their keys.  Blocks (i, y) take the
 // tile that CTA i's run begins or, where the call has few tiles (`search`), look for the i-th of them among the
-// runs' notes.  Up to FEW parts, a thread takes 4 columns of a row and
-// reads four parts at a time; more parts are shared by the warps of a block, a row at a time, which meet in
-// shared memory.
-template <typename T, int DP, int M>
+// runs' notes.  A thread has 4 columns of a row, an element of the parts.  Up to FEW parts, it reads four parts
+// at a time; more parts are shared by the warps of a block, 32 elements at a time, which meet in shared memory.
+// TC: the parts are the tcgen05 kernel's.
+template <typename T, int DP, int M, bool TC>
 __global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a, int ctas, bool search) {
-  constexpr int PART = tree_part_floats(M, DP), WARPS = 8, VEC = (DP / 4 + 31) / 32, FEW = 16, NOTES = 4;
+  constexpr int PART = tree_part_floats(M, DP), WARPS = 8, FEW = 16, NOTES = 4;
   static_assert(NOTES * 256 >= 4 * TREE_MAX_SMS, "the notes of all CTAs");
-  __shared__ float2 ml_of[WARPS];
-  __shared__ float4 o_of[WARPS][DP / 4];
+  __shared__ float2 ml_of[WARPS][32];
+  __shared__ float4 o_of[WARPS][32];
   __shared__ int found[NOTES][WARPS], which;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) which = -1;
@@ -658,8 +658,15 @@ __global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a, int ct
   // the tile's parts: CTA c's second or first, then the first ones of the head's CTAs behind it
   const float* parts = a.parts + static_cast<size_t>(2 * c) * PART;
   const auto part = [&](int i) { return parts + static_cast<size_t>(2 * i * a.cache.heads + (i == 0 ? note.w & 1 : 0)) * PART; };
-  // parts i, i + step, i + 2 step, i + 3 step of columns 4 col .. 4 col + 3 of a row, into (m, l, o)
-  const auto add4 = [&](int i, int step, int row, int col, float& m, float& l, float4& o) {
+  const int elements = TC ? (rows + 7) / 8 * (2 * DP) : rows * (DP / 4);
+  const auto place = [&](int e, int& row, int& col) {  // columns 4 col .. 4 col + 3 of a row; whether it is one of the tile's
+    const int g = e / (TC ? 2 * DP : DP / 4), w = e - g * (TC ? 2 * DP : DP / 4);
+    row = TC ? 8 * g + (w & 7) : g;
+    col = TC ? w >> 3 : w;
+    return e < elements && row < rows;
+  };
+  // element e of parts i, i + step, i + 2 step, i + 3 step, into (m, l, o)
+  const auto add4 = [&](int i, int step, int e, int row, float& m, float& l, float4& o) {
     float2 ml[4];
     float4 x[4];
 #pragma unroll
@@ -669,7 +676,7 @@ __global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a, int ct
       if (i + k * step < n) {
         const float* p = part(i + k * step);
         ml[k] = *reinterpret_cast<const float2*>(p + M * DP + 2 * row);
-        x[k] = reinterpret_cast<const float4*>(p + row * DP)[col];
+        x[k] = reinterpret_cast<const float4*>(p)[e];
       }
     }
     const float top = fmaxf(fmaxf(m, fmaxf(ml[0].x, ml[1].x)), fmaxf(ml[2].x, ml[3].x)), ref = top == -INFINITY ? 0.f : top;
@@ -696,44 +703,43 @@ __global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a, int ct
   };
 
   if (n <= FEW) {
-    for (int e = blockIdx.y * 256 + tid; e < rows * (DP / 4); e += gridDim.y * 256) {
-      const int row = e / (DP / 4), col = e - row * (DP / 4);
+    for (int e = blockIdx.y * 256 + tid; e < elements; e += gridDim.y * 256) {
+      int row, col;
+      if (!place(e, row, col)) continue;
       float m = -INFINITY, l = 0.f;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i = 0; i < n; i += 4) add4(i, 1, row, col, m, l, o);
+      for (int i = 0; i < n; i += 4) add4(i, 1, e, row, m, l, o);
       write(row, col, m, l, o);
     }
     return;
   }
-  for (int row = blockIdx.y; row < rows; row += gridDim.y) {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      const int col = 32 * v + lane;
-      float m = -INFINITY, l = 0.f;
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (col < DP / 4) {
-        for (int i = warp; i < n; i += 4 * WARPS) add4(i, WARPS, row, col, m, l, o);
-        o_of[warp][col] = o;
-      }
-      if (col == 0) ml_of[warp] = make_float2(m, l);
-    }
+  for (int first = blockIdx.y * 32; first < elements; first += gridDim.y * 32) {
+    int row, col;
+    const bool has = place(first + lane, row, col);
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (has)
+      for (int i = warp; i < n; i += 4 * WARPS) add4(i, WARPS, first + lane, row, m, l, o);
+    ml_of[warp][lane] = make_float2(m, l);
+    o_of[warp][lane] = o;
     __syncthreads();
-    if (tid < DP / 4) {
-      float m = -INFINITY, l = 0.f;
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (warp == 0 && has) {
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w) m = fmaxf(m, ml_of[w].x);
+      for (int w = 1; w < WARPS; ++w) m = fmaxf(m, ml_of[w][lane].x);
       const float ref = m == -INFINITY ? 0.f : m;
+      l = 0.f;
+      o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < WARPS; ++w) {
-        const float g = ex2((ml_of[w].x - ref) * a.scale_log2);
-        const float4 x = o_of[w][tid];
-        l += ml_of[w].y * g;
+        const float2 ml = ml_of[w][lane];
+        const float4 x = o_of[w][lane];
+        const float g = ex2((ml.x - ref) * a.scale_log2);
+        l += ml.y * g;
         o = make_float4(o.x + x.x * g, o.y + x.y * g, o.z + x.z * g, o.w + x.w * g);
       }
-      write(row, tid, m, l, o);
+      write(row, col, m, l, o);
     }
-    __syncthreads();  // the sums are read before the next row's
+    __syncthreads();  // the sums are read before the next ones
   }
 }
 
@@ -791,30 +797,33 @@ cudaError_t launch_rows(const TreeArgs& a, int ctas, cudaStream_t s) {
 // The kernel of the plan, then the join.
 template <typename T, int DP>
 cudaError_t launch(const Plan& p, const TreeArgs& a, int dtype, int ctas, cudaStream_t s) {
-  const auto join = [&](auto m) {
+  const auto join = [&](auto m, auto tc) {
     // at most one joined tile per run and tile of rows; a thread for 4 columns of a row, up to some 16 blocks per SM
     const long long most = static_cast<long long>(a.max_new) * a.group;  // rows that share a key head
     const long long tiles = static_cast<long long>(a.n_req) * a.cache.heads * ((most + a.tile_rows - 1) / a.tile_rows);
     const bool search = 4 * tiles < ctas;
     const int x = search ? static_cast<int>(tiles) : ctas, rows = static_cast<int>(std::min<long long>(a.tile_rows, most));
-    const int blocks = ctas > 8 * x ? rows : (rows * (DP / 4) + 255) / 256;  // (many parts: a block for a row)
+    const int elements = p.tc ? (rows + 7) / 8 * 2 * DP : rows * (DP / 4);
+    const int blocks = ctas > 8 * x ? (elements + 31) / 32 : (elements + 255) / 256;  // (many parts: 32 elements each)
     const int y = std::max(1, std::min(blocks, 8 * ctas / x));
-    return launch_ex(tree_join_kernel<T, DP, decltype(m)::value>, dim3(x, y), dim3(256), 0, s, 1, a, ctas, search);
+    return launch_ex(tree_join_kernel<T, DP, decltype(m)::value, decltype(tc)::value>, dim3(x, y), dim3(256), 0, s, 1, a, ctas, search);
   };
   cudaError_t e;
-  if (p.tc) {
-    e = launch_tree_attention_tc(a, dtype, DP, ctas, s);
-  } else {
-    e = p.rw == 1   ? (a.cache.page_shift >= 4 ? launch_rows<T, DP, 1, true>(a, ctas, s) : launch_rows<T, DP, 1>(a, ctas, s))
-        : p.rw == 2 ? launch_rows<T, DP, 2>(a, ctas, s)
-        : p.rw == 4 ? launch_rows<T, DP, 4>(a, ctas, s)
-                    : launch_rows<T, DP, 8>(a, ctas, s);
+  if constexpr (DP <= 128 && DP != 96) {
+    if (p.tc) {
+      e = launch_tree_attention_tc(a, dtype, DP, ctas, s);
+      return e != cudaSuccess ? e : join(std::integral_constant<int, 128>{}, std::true_type{});
+    }
   }
+  e = p.rw == 1   ? (a.cache.page_shift >= 4 ? launch_rows<T, DP, 1, true>(a, ctas, s) : launch_rows<T, DP, 1>(a, ctas, s))
+      : p.rw == 2 ? launch_rows<T, DP, 2>(a, ctas, s)
+      : p.rw == 4 ? launch_rows<T, DP, 4>(a, ctas, s)
+                  : launch_rows<T, DP, 8>(a, ctas, s);
   if (e != cudaSuccess) return e;
-  return p.rw == 1   ? join(std::integral_constant<int, 16>{})
-         : p.rw == 2 ? join(std::integral_constant<int, 32>{})
-         : p.rw == 4 ? join(std::integral_constant<int, 64>{})
-                     : join(std::integral_constant<int, 128>{});
+  return p.rw == 1   ? join(std::integral_constant<int, 16>{}, std::false_type{})
+         : p.rw == 2 ? join(std::integral_constant<int, 32>{}, std::false_type{})
+         : p.rw == 4 ? join(std::integral_constant<int, 64>{}, std::false_type{})
+                     : join(std::integral_constant<int, 128>{}, std::false_type{});
 }
 
 }  // namespace

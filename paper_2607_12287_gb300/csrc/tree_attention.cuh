@@ -32,7 +32,8 @@ struct TreeArgs {
   float scale_log2;                 // scale * log2(e)
 };
 
-// Floats of a part in the workspace: output [m][dp], then running maximum and sum of each row.
+// Floats of a part in the workspace: output [m][dp] (of the tcgen05 kernel [m / 8][dp / 4][8][4]), then running maximum
+// and sum of each row.
 __host__ __device__ constexpr int tree_part_floats(int m, int dp) { return m * (dp + 2); }
 
 // The tcgen05 kernel: widths up to 128 (dp 64, 80 or 128), pages of 8 tokens and more, groups of up to 128

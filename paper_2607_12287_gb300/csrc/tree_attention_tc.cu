@@ -1,7 +1,8 @@
 // The form of ivit_tree_attention for many rows per key head (see tree_attention.cu for the operation), on
 // the tensor cores.  A tile is up to 128 rows (new row x head of the group) of one request and key head; it
-// walks the request's keys in blocks of KB (128, 96 or 64 by head width, so that S, P and O of a block fit
-// in 256 tensor-memory columns): first the cached tokens, then the new rows, each with a last block that may
+// walks the request's keys in blocks of KB (96 for heads up to 80, else 64: S, P and O of a block fit in 256
+// tensor-memory columns and a row of S in registers; 128 at heads of 64 spilled, 50 against 40 us over up to
+// 4096 tokens of eight requests of up to 256 rows and 16 heads; 64 for all 42): first the cached tokens, then the new rows, each with a last block that may
 // be partly empty.  The blocks of the call are cut into equal runs, two CTAs per SM, as in tree_attention.cu;
 // while one CTA's warps take exponentials the other's MMAs run.
 //
@@ -18,10 +19,15 @@
 //          with V must not meet: rows past the block's keys, and new rows' values that are not finite, which
 //          (0 * NaN) would reach rows that do not see them; rows that do see them get them back at the end.
 //
-// Bound: the cache's bytes for up to about 128 rows, the chain of handshakes of a block (1.4 us at KB = 96) for more.
-// Measured: 16 trees of up to 31 drafts over up to 8192 tokens, 32 + 8 heads of 128, 63.5 us (mma.sync 137); eight
-// requests of up to 256 rows over up to 2048 tokens, 16 heads of 72, 36 us (73), over up to 8192 tokens 71 us
-// (447 TFLOP/s).
+// A tile that another run shares leaves its part in groups of 8 rows, 4 columns of each side by side, so that a
+// warp's store (lane = row) is whole lines: row after row took 3 us of a CTA instead of 1.5.
+//
+// Bound: the cache's bytes for up to about 128 rows, for more the chain of a block (1.3 us at KB = 96, two CTAs
+// at a time): two thirds of it are the exponentials of both CTAs.  A quarter of them by a polynomial on the FMA
+// pipe was slower (35 -> 38 us: registers).
+// Measured: 16 trees of up to 31 drafts over up to 8192 tokens, 32 + 8 heads of 128, 61.6 us (mma.sync 137); eight
+// requests of up to 256 rows over up to 2048 tokens, 16 heads of 72, 34 us (73), over up to 8192 tokens 68 us
+// (465 TFLOP/s).
 #include <cudaTypedefs.h>
 
 #include <type_traits>
@@ -37,7 +43,7 @@ constexpr int SMEM_HALF = 113 * 1024;  // two CTAs share an SM
 
 template <int DP>
 struct Cfg {
-  static constexpr int KB = attention_key_block(DP);
+  static constexpr int KB = DP <= 80 ? 96 : 64;
   static constexpr int W2 = attention_slice2(DP);  // columns past the first 64
   static constexpr int Q1 = AQ * 128, Q2 = AQ * W2 * 2;                                // bytes of the slices of Q
   static constexpr int T1 = KB * 128, TILE = (T1 + KB * W2 * 2 + 1023) / 1024 * 1024;  // of a K or V block
@@ -177,9 +183,10 @@ __global__ void __launch_bounds__(THREADS, 2)
       mbar_init(t_empty + 8 * i, 1);
     }
     fence_mbar_init();
-    tma_prefetch_desc(&maps.q.lo);
-    tma_prefetch_desc(&maps.k.lo);
-    tma_prefetch_desc(&maps.v.lo);
+    for (const Maps* m : {&maps.q, &maps.k, &maps.v, &maps.k_new, &maps.v_new}) {
+      tma_prefetch_desc(&m->lo);
+      if (W2 > 0) tma_prefetch_desc(&m->hi);
+    }
     *sh_abort = 0;
     *sh_odd = 0;
   }
@@ -468,8 +475,9 @@ __global__ void __launch_bounds__(THREADS, 2)
             }
           } else {
 #pragma unroll
-            for (int e = 0; e < 16; e += 4)
-              *reinterpret_cast<uint4*>(part + row * DP + d + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            for (int e = 0; e < 16; e += 4)  // (a warp's stores are whole lines)
+              *reinterpret_cast<uint4*>(part + (row >> 3) * (8 * DP) + 8 * (d + e) + 4 * (row & 7)) =
+                  make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
         }
         if (valid && whole && a.lse) a.lse[orow * a.heads + h] = (m_ref * sc + (log2f(sum) - TREE_SHIFT)) * 0.6931471805599453f;
