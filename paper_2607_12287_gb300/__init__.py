@@ -140,16 +140,19 @@ def _ptr(t) -> Optional[int]:
 
 
 _dtypes = {}  # torch dtypes by name, and torch.Tensor: filled on the first check (torch is imported late)
+_Tensor = _Int32 = None  # torch.Tensor and torch.int32 from then on
 
 
 def _tensor_type():
+    global _Tensor, _Int32
     t = _dtypes.get("tensor")
     if t is None:
         import torch
         for name in ("uint8", "int32", "float32", "bfloat16", "float16"):
             _dtypes[name] = getattr(torch, name)
         _dtypes[IVIT_BF16], _dtypes[IVIT_FP16] = torch.bfloat16, torch.float16  # (by the library's codes, too)
-        t = _dtypes["tensor"] = torch.Tensor
+        _Int32 = torch.int32
+        t = _Tensor = _dtypes["tensor"] = torch.Tensor
     return t
 
 
@@ -381,16 +384,24 @@ def make_attention_config(n_req: int, heads: int, max_pages: int, max_new: int, 
 
 def _arg(t, name: str, dtype_name: str, numel: int) -> Optional[int]:
     """``_require``, and the pointer."""
-    if (type(t) is _dtypes.get("tensor") and t.is_cuda and t.dtype is _dtypes[dtype_name] and t.is_contiguous()
-            and t.numel() >= numel):
+    if type(t) is _Tensor and t.is_cuda and t.dtype is _dtypes[dtype_name] and t.is_contiguous() and t.numel() >= numel:
         return t.data_ptr()
     _require(t, name, dtype_name, numel)
     return _ptr(t)
 
 
+def _i32(t, name: str, numel: int) -> Optional[int]:
+    """``_arg`` of an int32 array, which most are."""
+    if type(t) is _Tensor and t.is_cuda and t.dtype is _Int32 and t.is_contiguous() and t.numel() >= numel:
+        return t.data_ptr()
+    if t is None:
+        return None
+    return _arg(t, name, "int32", numel)
+
+
 def _typed(t, name: str, dtype: int) -> None:
     """Rejects what is not a device tensor of the type ``dtype`` (IVIT_BF16 or IVIT_FP16)."""
-    if type(t) is _dtypes.get("tensor") and t.is_cuda and t.dtype is _dtypes[dtype]:
+    if type(t) is _Tensor and t.is_cuda and t.dtype is _dtypes[dtype]:
         return
     if isinstance(t, (int, np.ndarray)) or t is None:
         raise TypeError(f"{name}: a CUDA tensor is required")
@@ -404,7 +415,7 @@ def _typed(t, name: str, dtype: int) -> None:
 def _rows(t, name: str, dtype: int, shape: tuple) -> tuple:
     """Pointer and row stride of a tensor [rows, heads, head_dim] of at least ``shape``'s rows whose heads are
     contiguous in a row; rejects one that the kernels would misread, as ``_require`` does."""
-    if type(t) is _dtypes.get("tensor") and t.is_cuda and t.dtype is _dtypes[dtype] and t.shape == shape:
+    if type(t) is _Tensor and t.is_cuda and t.dtype is _dtypes[dtype] and t.shape == shape:
         s0, s1, s2 = t.stride()  # the common case: the checks below without formatting names
         if s2 == 1 and s1 == shape[2] and shape[0] > 1:
             return t.data_ptr(), s0
@@ -424,7 +435,7 @@ def _workspace(t) -> tuple:
 
 
 def _row_count(t, name: str) -> int:
-    if type(t) is _dtypes.get("tensor"):
+    if type(t) is _Tensor:
         sh = t.shape
         if len(sh) == 3:
             return sh[0]
@@ -435,6 +446,9 @@ def _row_count(t, name: str) -> int:
 
 def _cache(t, name: str, layout: IvitCacheLayout) -> int:
     """The pointer of a cache of this layout; rejects any other tensor."""
+    if (type(t) is _Tensor and t.is_cuda and t.dtype is _dtypes[layout.dtype] and t.shape == layout.shape
+            and t.stride() == layout.strides):
+        return t.data_ptr()
     _typed(t, name, layout.dtype)
     if t.shape != layout.shape or t.stride() != layout.strides:
         raise ValueError(f"{name}: shape {tuple(t.shape)} and strides {t.stride()} are not the layout's, {layout.shape} and "
@@ -455,13 +469,13 @@ def ivit_step_plan(cfg: IvitPlanConfig, held, base, new, parent, ring, ring_in, 
     """Pages, slots, positions and tree masks of a step (int32 tensors; parent, req, positions and mask may be
     None): ``table`` [n_req, max_pages] and ``ring`` [n_pages] are updated, ``cu_rows`` [n_req + 1], the row arrays
     [max_rows], ``mask`` [max_rows, mask_words], ``ring_out`` [2] and ``status`` [1] written."""
-    n, rows, i32 = cfg.n_req, cfg.max_rows, "int32"
-    args = (C.addressof(cfg), _arg(held, "held", i32, n), _arg(base, "base", i32, n), _arg(new, "new", i32, n),
-            _arg(parent, "parent", i32, rows), _arg(ring, "ring", i32, cfg.n_pages), _arg(ring_in, "ring_in", i32, 2),
-            _arg(table, "table", i32, n * cfg.max_pages), _arg(cu_rows, "cu_rows", i32, n + 1),
-            _arg(req, "req", i32, rows), _arg(slots, "slots", i32, rows), _arg(positions, "positions", i32, rows),
-            _arg(mask, "mask", i32, rows * cfg.mask_words), _arg(ring_out, "ring_out", i32, 2),
-            _arg(status, "status", i32, 1), _stream(stream))
+    n, rows = cfg.n_req, cfg.max_rows
+    args = (C.addressof(cfg), _i32(held, "held", n), _i32(base, "base", n), _i32(new, "new", n),
+            _i32(parent, "parent", rows), _i32(ring, "ring", cfg.n_pages), _i32(ring_in, "ring_in", 2),
+            _i32(table, "table", n * cfg.max_pages), _i32(cu_rows, "cu_rows", n + 1),
+            _i32(req, "req", rows), _i32(slots, "slots", rows), _i32(positions, "positions", rows),
+            _i32(mask, "mask", rows * cfg.mask_words), _i32(ring_out, "ring_out", 2),
+            _i32(status, "status", 1), _stream(stream))
     _check(load().ivit_step_plan(*args), None)
 
 
@@ -478,8 +492,8 @@ def _rope_inputs(cfg: IvitRopeConfig, n: int, q_weight, k_weight, positions, fre
     else:
         raise ValueError(f"positions: shape {tuple(sh)}, expected [{cfg.n_axes}, {n}]")
     return (_arg(q_weight, "q_weight", dt, dim), _arg(k_weight, "k_weight", dt, dim),
-            _arg(positions, "positions", "int32", least), stride, _arg(freq, "freq", "float32", pairs),
-            _arg(axis, "axis", "int32", pairs))
+            _i32(positions, "positions", least), stride, _arg(freq, "freq", "float32", pairs),
+            _i32(axis, "axis", pairs))
 
 
 def ivit_qk_norm_rope(cfg: IvitRopeConfig, q, k, v, q_weight, k_weight, positions, freq, axis, q_out, k_out=None,
@@ -497,7 +511,7 @@ def ivit_qk_norm_rope(cfg: IvitRopeConfig, q, k, v, q_weight, k_weight, position
     if cache is not None:
         vp, vs = _rows(v, "v", dt, k_shape)
         kc, vc = _cache(k_cache, "k_cache", cache), _cache(v_cache, "v_cache", cache)
-        lay, sl = C.addressof(cache), _arg(slots, "slots", "int32", n)
+        lay, sl = C.addressof(cache), _i32(slots, "slots", n)
     elif not (v is k_cache is v_cache is slots is None):
         raise ValueError("v, k_cache, v_cache and slots need the cache's layout")
     args = (C.addressof(cfg), n, *_rows(q, "q", dt, q_shape), *_rows(k, "k", dt, k_shape), vp, vs,
@@ -540,8 +554,8 @@ def ivit_tree_attention(cfg: IvitAttentionConfig, cache: IvitCacheLayout, q, k_n
         mask = None
     args = (C.addressof(cfg), C.addressof(cache), n, *_rows(q, "q", dt, q_shape), *_rows(k_new, "k_new", dt, k_shape),
             *_rows(v_new, "v_new", dt, k_shape), _cache(k_cache, "k_cache", cache), _cache(v_cache, "v_cache", cache),
-            _arg(table, "table", "int32", req * cfg.max_pages), _arg(lengths, "lengths", "int32", req),
-            _arg(cu_rows, "cu_rows", "int32", req + 1), _arg(mask, "mask", "int32", n * cfg.mask_words),
+            _i32(table, "table", req * cfg.max_pages), _i32(lengths, "lengths", req),
+            _i32(cu_rows, "cu_rows", req + 1), _i32(mask, "mask", n * cfg.mask_words),
             *_rows(out, "out", dt, q_shape), _arg(lse, "lse", "float32", n * heads),
             *_workspace(workspace), _stream(stream))
     _check(load().ivit_tree_attention(*args), None)
@@ -563,7 +577,7 @@ def ivit_kv_write(cache: IvitCacheLayout, k, v, rows, slots, k_cache, v_cache, s
                          f"{cache.shape}, with strides {cache.strides}")
     n = rows.numel() if hasattr(rows, "numel") else 0
     args = (C.addressof(cache), layers, n, n_src, k.data_ptr(), v.data_ptr(), st[1] if n_src > 1 else kv * dim,
-            st[0] if layers > 1 else 0, _arg(rows, "rows", "int32", n), _arg(slots, "slots", "int32", n),
+            st[0] if layers > 1 else 0, _i32(rows, "rows", n), _i32(slots, "slots", n),
             k_cache.data_ptr(), v_cache.data_ptr(), cst[0] if layers > 1 else 0, _stream(stream))
     _check(load().ivit_kv_write(*args), None)
 
