@@ -374,7 +374,7 @@ typedef struct ivit_attention_config {
  * [head_dim], lse_dev fp32 [n_rows][heads] or NULL.  Row strides as in ivit_qk_norm_rope, but
  * positive; rows that belong to no request are left as they are.  max_new is a bound that the
  * caller vouches for; it chooses the kernel (tcgen05 for more than 16 rows per key head, where
- * heads are at most 128 wide and pages of at least 8 tokens).  workspace_dev: 16-byte aligned,
+ * pages have at least 8 tokens and key heads at most 128 query heads).  workspace_dev: 16-byte aligned,
  * workspace_bytes at least ivit_tree_attention_workspace(cfg, cache) (0: invalid arguments), needs
  * no initialisation; calls that overlap on the GPU need one each.  Its first int32 is 0 after a
  * call, or not if one of the kernel's bounded waits expired (then outputs are not valid). */

@@ -16,14 +16,14 @@
 // memory, looks the pages up a tile ahead, and walks on without a barrier; its running maximum, sum and output
 // meet the others' at the end of a tile of rows.  Products by mma.m16n8k16; probabilities enter the one with V
 // as two 16-bit terms (16 bits and more of their fp32 value), which is free beside the cache's bytes.
-// Tiles of 32 to 128 rows are for what the tcgen05 kernel (tree_attention_tc.cu) does not take: heads wider than
-// 128, pages of fewer than 8 tokens, groups of more than 128 heads.  Row groups of 16 are split over four or
+// Tiles of 32 to 128 rows are for what the tcgen05 kernel (tree_attention_tc.cu) does not take: pages of fewer
+// than 8 tokens, groups of more than 128 heads.  Row groups of 16 are split over four or
 // eight warps that share the keys, the 64 keys too for 32 rows; probabilities are rounded once from 64 rows on.
 // Sums use the fp32 values everywhere.
 //
 // Bound: the cache's bytes for few rows per key head (32 requests of up to 16384 tokens, 32 + 8 heads of 128, 168 us:
 // 6600 GB/s; 64 of up to 8192, 16 + 4 heads of 64, 49.5 us: 5500 GB/s), the chain of dependent reads of a start
-// for short ones (one request of 1041 tokens 7.4 us), mma.sync's rate for many rows.
+// for short ones (one request of 1041 tokens 7.7 us), mma.sync's rate for many rows.
 #include <algorithm>
 #include <type_traits>
 
@@ -33,10 +33,11 @@ namespace ivit {
 namespace {
 
 constexpr int TK = 64;              // keys of a tile
-// More rows per key head than this take the tcgen05 kernel where it can (heads of up to 128, pages of 8 tokens and more,
-// groups of up to 128).  Both sides, 16 requests of up to 8192 tokens, us: 32 rows of heads of 128 58 (tcgen05) and 70, 64
-// rows 60 and 79, 124 rows 64 and 137; heads of 64, 32 rows 31 and 33, 64 rows 32 and 35; one request of 1000 tokens, 32
-// rows, 12.3 and 11.6.
+// More rows per key head than this take the tcgen05 kernel where it can (pages of 8 tokens and more, groups of up to 128).
+// Both sides, 16 requests of up to 8192 tokens, us: 32 rows of heads of 128 58 (tcgen05) and 70, 64 rows 60 and 79, 124
+// rows 62 and 137; heads of 64, 32 rows 31 and 33, 64 rows 32 and 35; up to 4096 tokens, heads of 256, 32 rows 30 and 41,
+// 64 rows 30 and 45, 124 rows 33 and 53; one request of 1000 tokens, 32 rows of 128, 12.3 and 11.6, of 600 tokens, 32
+// rows of 256, 15.4 and 13.7 (lengths are not known when the call is made).
 constexpr int TC_ROWS = 16;
 
 struct Keys64 {
@@ -766,9 +767,10 @@ Plan plan(const ivit_attention_config& c, const ivit_cache_layout& l) {
   const int group = c.heads / l.kv_heads;
   const int rows = static_cast<int>(std::min<long long>(128, static_cast<long long>(c.max_new) * group));  // that share a key head
   const int dp = l.head_dim <= 64 ? 64 : l.head_dim <= 80 ? 80 : l.head_dim <= 96 ? 96 : l.head_dim <= 128 ? 128 : 256;
-  if (rows > TC_ROWS && dp <= 128 && group <= 128 && l.page_size >= 8 && l.head_stride > 0 && l.token_stride > 0 &&
-      l.page_stride > 0)
-    return {true, dp == 96 ? 128 : dp, 0, tree_tc_rows(group), 2, tree_part_floats(128, dp == 96 ? 128 : dp)};
+  if (rows > TC_ROWS && group <= 128 && l.page_size >= 8 && l.head_stride > 0 && l.token_stride > 0 && l.page_stride > 0) {
+    const int wide = dp == 96 ? 128 : dp;
+    return {true, wide, 0, tree_tc_rows(group), wide <= 128 ? 2 : 1, tree_part_floats(128, wide)};
+  }
   // the smallest tile that holds the rows
   const auto groups = [&](auto d) {
     constexpr int DP = decltype(d)::value;
@@ -809,7 +811,7 @@ cudaError_t launch(const Plan& p, const TreeArgs& a, int dtype, int ctas, cudaSt
     return launch_ex(tree_join_kernel<T, DP, decltype(m)::value, decltype(tc)::value>, dim3(x, y), dim3(256), 0, s, 1, a, ctas, search);
   };
   cudaError_t e;
-  if constexpr (DP <= 128 && DP != 96) {
+  if constexpr (DP != 96) {
     if (p.tc) {
       e = launch_tree_attention_tc(a, dtype, DP, ctas, s);
       return e != cudaSuccess ? e : join(std::integral_constant<int, 128>{}, std::true_type{});

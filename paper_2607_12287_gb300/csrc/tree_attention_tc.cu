@@ -1,16 +1,17 @@
 // The form of ivit_tree_attention for many rows per key head (see tree_attention.cu for the operation), on
 // the tensor cores.  A tile is up to 128 rows (new row x head of the group) of one request and key head; it
-// walks the request's keys in blocks of KB (96 for heads up to 80, else 64: S, P and O of a block fit in 256
-// tensor-memory columns and a row of S in registers; 128 at heads of 64 spilled, 50 against 40 us over up to
-// 4096 tokens of eight requests of up to 256 rows and 16 heads; 64 for all 42): first the cached tokens, then the new rows, each with a last block that may
-// be partly empty.  The blocks of the call are cut into equal runs, two CTAs per SM, as in tree_attention.cu;
-// while one CTA's warps take exponentials the other's MMAs run.
+// walks the request's keys in blocks of KB: first the cached tokens, then the new rows, each with a last block
+// that may be partly empty.  The blocks of the call are cut into equal runs, two CTAs per SM, as in
+// tree_attention.cu; while one CTA's warps take exponentials the other's MMAs run.  (Heads above 128: one CTA,
+// for O takes 256 columns of tensor memory and two blocks of K and V take 128 KB.)  KB is 96 for heads up to 80,
+// else 64: S, P and O of a block fit in 256 columns of tensor memory and a row of S in registers (heads of 64,
+// eight requests of up to 256 rows over up to 4096 tokens, 16 heads: 40 us, 42 at KB = 64, 50 at 128, which spills).
 //
 // Warps of a CTA:
 //   4      TMA: Q tile (a box of heads x new rows, which is the tile's order of rows), then K and V blocks
 //          through a ring.  A cached block is fetched page by page (or in boxes of the largest power of two
-//          that divides KB, for larger pages), a block of new rows in one box.  Columns 0..63 of a head form
-//          one slice with 128-byte swizzle, the rest a second one as narrow as a swizzle allows.
+//          that divides KB, for larger pages), a block of new rows in one box.  64 columns of a head form a
+//          slice with 128-byte swizzle, 16 that are left (heads up to 80) one with 32-byte swizzle.
 //   5      MMA: S = Q K^T of block i + 1 is issued before O += P V of block i; P is read from tensor memory,
 //          V is the B operand in MN-major form.
 //   0 - 3  softmax, thread = row = tensor-memory lane: S into registers, masked where the block holds keys
@@ -20,14 +21,14 @@
 //          (0 * NaN) would reach rows that do not see them; rows that do see them get them back at the end.
 //
 // A tile that another run shares leaves its part in groups of 8 rows, 4 columns of each side by side, so that a
-// warp's store (lane = row) is whole lines: row after row took 3 us of a CTA instead of 1.5.
+// warp's store (lane = row) is whole lines (34.2 us for the eight requests below; row after row 36.3).
 //
 // Bound: the cache's bytes for up to about 128 rows, for more the chain of a block (1.3 us at KB = 96, two CTAs
 // at a time): two thirds of it are the exponentials of both CTAs.  A quarter of them by a polynomial on the FMA
 // pipe was slower (35 -> 38 us: registers).
 // Measured: 16 trees of up to 31 drafts over up to 8192 tokens, 32 + 8 heads of 128, 61.6 us (mma.sync 137); eight
 // requests of up to 256 rows over up to 2048 tokens, 16 heads of 72, 34 us (73), over up to 8192 tokens 68 us
-// (465 TFLOP/s).
+// (465 TFLOP/s); 16 requests of 16 drafts over up to 4096 tokens, 16 + 2 heads of 256, 33 us (53).
 #include <cudaTypedefs.h>
 
 #include <type_traits>
@@ -39,19 +40,19 @@ namespace {
 
 constexpr int AQ = 128;                // rows of a tile (MMA M)
 constexpr int THREADS = 192;
-constexpr int SMEM_HALF = 113 * 1024;  // two CTAs share an SM
 
 template <int DP>
 struct Cfg {
   static constexpr int KB = DP <= 80 ? 96 : 64;
-  static constexpr int W2 = attention_slice2(DP);  // columns past the first 64
-  static constexpr int Q1 = AQ * 128, Q2 = AQ * W2 * 2;                                // bytes of the slices of Q
-  static constexpr int T1 = KB * 128, TILE = (T1 + KB * W2 * 2 + 1023) / 1024 * 1024;  // of a K or V block
-  static constexpr int T_BYTES = T1 + KB * W2 * 2;
-  static constexpr int TM_O = KB, TM_P = KB + DP, TM_COLS = 256;                       // S at column 0
+  static constexpr int CTAS = DP <= 128 ? 2 : 1;                // of an SM
+  static constexpr int FULL = DP / 64, TAIL = DP % 64;          // slices of 64 columns, and columns of a narrow last one
+  static constexpr int Q1 = AQ * 128, T1 = KB * 128;            // bytes of a full slice of Q, of a K or V block
+  static constexpr int Q_ROW = FULL * 128 + TAIL * 2;
+  static constexpr int T_BYTES = KB * Q_ROW, TILE = (T_BYTES + 1023) / 1024 * 1024;
+  static constexpr int TM_O = KB, TM_P = KB + DP, TM_COLS = 512 / CTAS;  // S at column 0
   static_assert(TM_P + KB / 2 <= TM_COLS, "tensor memory of one CTA");
-  static constexpr int OFF_RING = Q1 + Q2;
-  static constexpr int FIT = (SMEM_HALF - OFF_RING - 1024 - 512) / TILE, RING = FIT < 8 ? FIT : 8;
+  static constexpr int OFF_RING = AQ * Q_ROW;
+  static constexpr int FIT = ((CTAS == 2 ? 113 : 227) * 1024 - OFF_RING - 1024 - 512) / TILE, RING = FIT < 8 ? FIT : 8;
   static constexpr int OFF_BAR = OFF_RING + RING * TILE;
   static constexpr int BYTES = OFF_BAR + 256 + 1024;  // with alignment slack
   static_assert(TREE_MAX_REQ * 8 <= OFF_BAR, "the units before each request");
@@ -65,7 +66,7 @@ struct Blocks {
   static __device__ __forceinline__ int tiles(const TreeRequest& r) { return cached(r) + (r.n + KB - 1) / KB; }
 };
 
-// Maps of one array: the first 64 columns of a head, and the second slice.
+// Maps of one array: 64 columns of a head, and the narrow last slice.
 struct Maps {
   CUtensorMap lo, hi;
 };
@@ -80,14 +81,14 @@ __device__ __forceinline__ uint32_t idesc(int m, int n) {
   return std::is_same<T, bf16>::value ? d : d & ~((1u << 7) | (1u << 10));
 }
 
-// Shared-memory descriptor of a slice whose rows are W2 columns (and one swizzle span) wide: groups of 8
+// Shared-memory descriptor of a narrow slice whose rows are W columns (and one swizzle span) wide: groups of 8
 // rows follow each other.  For a K-major operand the rows are its M or N index, for an MN-major one (V) its
 // K index.
-template <int W2>
+template <int W>
 __device__ __forceinline__ uint64_t sdesc_rows(uint32_t saddr) {
-  constexpr uint32_t group = 8 * W2 * 2;
+  constexpr uint32_t group = 8 * W * 2;
   uint64_t d = sdesc_sw128(saddr, group, group) & ~(static_cast<uint64_t>(7) << 61);
-  return d | (static_cast<uint64_t>(W2 == 16 ? 6 : W2 == 32 ? 4 : 2) << 61);  // 32-, 64-, 128-byte swizzle
+  return d | (static_cast<uint64_t>(W == 16 ? 6 : W == 32 ? 4 : 2) << 61);  // 32-, 64-, 128-byte swizzle
 }
 
 // 4-D tiled load (see tma_load_2d).
@@ -156,10 +157,10 @@ __device__ __forceinline__ bool clear_slice(uint8_t* slice, int rows, bool clean
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(THREADS, 2)
+__global__ void __launch_bounds__(THREADS, Cfg<DP>::CTAS)
     tree_attention_tc_kernel(const __grid_constant__ AllMaps maps, const TreeArgs a, int box_shift) {
   using C = Cfg<DP>;
-  constexpr int KB = C::KB, RING = C::RING, W2 = C::W2, PART = tree_part_floats(AQ, DP);
+  constexpr int KB = C::KB, RING = C::RING, FULL = C::FULL, TAIL = C::TAIL, PART = tree_part_floats(AQ, DP);
   using B = Blocks<KB>;
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -185,7 +186,7 @@ __global__ void __launch_bounds__(THREADS, 2)
     fence_mbar_init();
     for (const Maps* m : {&maps.q, &maps.k, &maps.v, &maps.k_new, &maps.v_new}) {
       tma_prefetch_desc(&m->lo);
-      if (W2 > 0) tma_prefetch_desc(&m->hi);
+      if (TAIL > 0) tma_prefetch_desc(&m->hi);
     }
     *sh_abort = 0;
     *sh_odd = 0;
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(THREADS, 2)
   if (warp == 4) {
     fence_proxy_async_smem();  // (the ring was scratch)
     const uint64_t policy = l2_policy_evict_first();
-    const uint32_t q_bytes = a.tile_rows * (128 + W2 * 2);
+    const uint32_t q_bytes = a.tile_rows * C::Q_ROW;
     const int boxes = KB >> box_shift, page_mask = (1 << a.cache.page_shift) - 1;
     TreePlace<B> p = run.at;
     uint32_t t = 0;  // K / V blocks so far
@@ -232,8 +233,9 @@ __global__ void __launch_bounds__(THREADS, 2)
       if (elect_one()) {
         const int head = p.head * a.group, row = p.r.row0 + p.rt * (a.tile_rows / a.group);
         mbar_arrive_expect_tx(q_full, q_bytes);
-        tma_load_3d(sb, &maps.q.lo, 0, head, row, q_full, policy);
-        if (W2 > 0) tma_load_3d(sb + C::Q1, &maps.q.hi, 64, head, row, q_full, policy);
+#pragma unroll
+        for (int c = 0; c < FULL; ++c) tma_load_3d(sb + c * C::Q1, &maps.q.lo, 64 * c, head, row, q_full, policy);
+        if (TAIL > 0) tma_load_3d(sb + FULL * C::Q1, &maps.q.hi, 64 * FULL, head, row, q_full, policy);
       }
       __syncwarp();
       const int* table = a.table + static_cast<size_t>(p.req) * a.max_pages;
@@ -259,16 +261,20 @@ __global__ void __launch_bounds__(THREADS, 2)
               const int id = __shfl_sync(0xffffffffu, ids, b);
               if (elect_one()) {
                 const int token = (kb * KB + (b << box_shift)) & page_mask;
-                tma_load_4d(dst + ((b << box_shift) * 128), &m.lo, 0, p.head, token, id, full, policy);
-                if (W2 > 0) tma_load_4d(dst + C::T1 + ((b << box_shift) * W2 * 2), &m.hi, 64, p.head, token, id, full, policy);
+#pragma unroll
+                for (int c = 0; c < FULL; ++c)
+                  tma_load_4d(dst + c * C::T1 + (b << box_shift) * 128, &m.lo, 64 * c, p.head, token, id, full, policy);
+                if (TAIL > 0)
+                  tma_load_4d(dst + FULL * C::T1 + (b << box_shift) * TAIL * 2, &m.hi, 64 * FULL, p.head, token, id, full, policy);
               }
               __syncwarp();
             }
           } else if (elect_one()) {
             const Maps& m = kv ? maps.v_new : maps.k_new;
             const int row = p.r.row0 + (kb - cached) * KB;
-            tma_load_3d(dst, &m.lo, 0, p.head, row, full, policy);
-            if (W2 > 0) tma_load_3d(dst + C::T1, &m.hi, 64, p.head, row, full, policy);
+#pragma unroll
+            for (int c = 0; c < FULL; ++c) tma_load_3d(dst + c * C::T1, &m.lo, 64 * c, p.head, row, full, policy);
+            if (TAIL > 0) tma_load_3d(dst + FULL * C::T1, &m.hi, 64 * FULL, p.head, row, full, policy);
           }
           __syncwarp();
         }
@@ -295,8 +301,12 @@ __global__ void __launch_bounds__(THREADS, 2)
             const uint32_t kt = sb + C::OFF_RING + slot * C::TILE, id = idesc<T>(AQ, KB);
 #pragma unroll
             for (int c = 0; c < DP / 16; ++c)
-              umma_bf16(tmem, c < 4 ? sdesc_kmajor_sw128(sb + c * 32) : sdesc_rows<W2>(sb + C::Q1 + (c - 4) * 32),
-                        c < 4 ? sdesc_kmajor_sw128(kt + c * 32) : sdesc_rows<W2>(kt + C::T1 + (c - 4) * 32), id, c > 0);
+              umma_bf16(tmem,
+                        c < 4 * FULL ? sdesc_kmajor_sw128(sb + c / 4 * C::Q1 + c % 4 * 32)
+                                     : sdesc_rows<TAIL>(sb + FULL * C::Q1 + (c - 4 * FULL) * 32),
+                        c < 4 * FULL ? sdesc_kmajor_sw128(kt + c / 4 * C::T1 + c % 4 * 32)
+                                     : sdesc_rows<TAIL>(kt + FULL * C::T1 + (c - 4 * FULL) * 32),
+                        id, c > 0);
             umma_commit(t_empty + 8 * slot);
             umma_commit(s_full);
             if (i == blocks - 1) umma_commit(q_empty);
@@ -311,12 +321,17 @@ __global__ void __launch_bounds__(THREADS, 2)
           tc_fence_after();
           if (elect_one()) {
             const uint32_t vt = sb + C::OFF_RING + slot * C::TILE;
-            const uint32_t id0 = idesc<T>(AQ, 64) | (1u << 16), id1 = idesc<T>(AQ, W2 > 0 ? W2 : 16) | (1u << 16);  // (V: MN-major)
+            const uint32_t id0 = idesc<T>(AQ, 64) | (1u << 16), id1 = idesc<T>(AQ, TAIL > 0 ? TAIL : 16) | (1u << 16);  // (V: MN-major)
 #pragma unroll
             for (int c = 0; c < KB / 16; ++c) {
               const uint32_t acc = (i > 1 || c > 0) ? 1u : 0u;
-              umma_bf16_ts(tmem + C::TM_O, tmem + C::TM_P + c * 8, sdesc_sw128(vt + c * 2048, 1024, 1024), id0, acc);
-              if (W2 > 0) umma_bf16_ts(tmem + C::TM_O + 64, tmem + C::TM_P + c * 8, sdesc_rows<W2>(vt + C::T1 + c * 32 * W2), id1, acc);
+#pragma unroll
+              for (int f = 0; f < FULL; ++f)
+                umma_bf16_ts(tmem + C::TM_O + 64 * f, tmem + C::TM_P + c * 8, sdesc_sw128(vt + f * C::T1 + c * 2048, 1024, 1024),
+                             id0, acc);
+              if (TAIL > 0)
+                umma_bf16_ts(tmem + C::TM_O + 64 * FULL, tmem + C::TM_P + c * 8, sdesc_rows<TAIL>(vt + FULL * C::T1 + c * 32 * TAIL),
+                             id1, acc);
             }
             umma_commit(t_empty + 8 * slot);
             umma_commit(o_done);
@@ -355,8 +370,10 @@ __global__ void __launch_bounds__(THREADS, 2)
           const uint32_t t = 2 * j + 1, slot = t % RING;
           if (!(ok = __all_sync(0xffffffffu, wait(t_full + 8 * slot, (t / RING) & 1)))) break;
           uint8_t* v = sm + C::OFF_RING + slot * C::TILE;
-          bool odd = clear_slice<T, KB, 128>(v, keys, kb >= cached, tid);
-          if (W2 > 0) odd |= clear_slice<T, KB, (W2 > 0 ? W2 * 2 : 16)>(v + C::T1, keys, kb >= cached, tid);
+          bool odd = false;
+#pragma unroll
+          for (int c = 0; c < FULL; ++c) odd |= clear_slice<T, KB, 128>(v + c * C::T1, keys, kb >= cached, tid);
+          if (TAIL > 0) odd |= clear_slice<T, KB, (TAIL > 0 ? TAIL * 2 : 16)>(v + FULL * C::T1, keys, kb >= cached, tid);
           if (odd) *sh_odd = n;
           fence_proxy_async_smem();
         }
@@ -506,7 +523,7 @@ PFN_cuTensorMapEncodeTiled_v12000 encoder() {
 }
 
 // Maps of an array of `rank` dimensions, the first a head's values; box: of the others.
-bool make_maps(Maps* m, int dtype, int w2, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
+bool make_maps(Maps* m, int dtype, int tail, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
                const cuuint32_t* box) {
   const auto enc = encoder();
   if (!enc) return false;
@@ -521,7 +538,7 @@ bool make_maps(Maps* m, int dtype, int w2, const void* base, int rank, const cuu
   };
   if (!make(&m->lo, 64)) return false;
   m->hi = m->lo;
-  return w2 == 0 || make(&m->hi, w2);
+  return tail == 0 || make(&m->hi, tail);
 }
 
 template <typename T, int DP>
@@ -535,14 +552,14 @@ cudaError_t launch(const TreeArgs& a, int dtype, int ctas, cudaStream_t s) {
   const auto fresh = [&](Maps* map, const void* base, cuuint64_t heads, long long stride, cuuint32_t box_heads, cuuint32_t box_rows) {
     const cuuint64_t dims[3] = {dim, heads, rows}, strides[2] = {dim * 2, static_cast<cuuint64_t>(stride) * 2};
     const cuuint32_t b[2] = {box_heads, box_rows};
-    return make_maps(map, dtype, C::W2, base, 3, dims, strides, b);
+    return make_maps(map, dtype, C::TAIL, base, 3, dims, strides, b);
   };
   const auto pages = [&](Maps* map, const void* base) {
     const cuuint64_t dims[4] = {dim, kv, static_cast<cuuint64_t>(page), static_cast<cuuint64_t>(a.cache.n_pages)};
     const cuuint64_t strides[3] = {static_cast<cuuint64_t>(a.cache.head_stride) * 2, static_cast<cuuint64_t>(a.cache.token_stride) * 2,
                                    static_cast<cuuint64_t>(a.cache.page_stride) * 2};
     const cuuint32_t b[3] = {1, static_cast<cuuint32_t>(box), 1};
-    return make_maps(map, dtype, C::W2, base, 4, dims, strides, b);
+    return make_maps(map, dtype, C::TAIL, base, 4, dims, strides, b);
   };
   if (!fresh(&m.q, a.q, a.heads, a.q_stride, a.group, a.tile_rows / a.group) || !pages(&m.k, a.k_cache) || !pages(&m.v, a.v_cache) ||
       !fresh(&m.k_new, a.k_new, kv, a.k_new_stride, 1, C::KB) || !fresh(&m.v_new, a.v_new, kv, a.v_new_stride, 1, C::KB))
@@ -557,7 +574,10 @@ cudaError_t launch(const TreeArgs& a, int dtype, int ctas, cudaStream_t s) {
 cudaError_t launch_tree_attention_tc(const TreeArgs& a, int dtype, int dp, int ctas, cudaStream_t s) {
   const auto width = [&](auto type) {
     using T = decltype(type);
-    return dp == 64 ? launch<T, 64>(a, dtype, ctas, s) : dp == 80 ? launch<T, 80>(a, dtype, ctas, s) : launch<T, 128>(a, dtype, ctas, s);
+    return dp == 64    ? launch<T, 64>(a, dtype, ctas, s)
+           : dp == 80  ? launch<T, 80>(a, dtype, ctas, s)
+           : dp == 128 ? launch<T, 128>(a, dtype, ctas, s)
+                       : launch<T, 256>(a, dtype, ctas, s);
   };
   return dtype == IVIT_BF16 ? width(bf16{}) : width(half{});
 }

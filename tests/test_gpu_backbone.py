@@ -374,7 +374,12 @@ ATTENTION = [  # cached, new, heads, kv, dim, page, type, order
     ([191, 192, 500], [128, 33, 97], 5, 1, 80, 128, "float16", "head"), ([700], [256], 2, 2, 64, 64, "bfloat16", "token"),
     ([0, 0, 127, 128, 129], [140, 3, 128, 129, 70], 2, 2, 64, 16, "float16", "token"),
     ([0, 64, 200], [75, 64, 1], 7, 1, 128, 16, "bfloat16", "token"), ([500], [65], 6, 2, 112, 256, "bfloat16", "head"),
-    # what tcgen05 does not take (small pages, wide heads): tiles of 16, 32 and 64 rows
+    # ... of heads above 128, whose last slices may be empty
+    ([63, 64, 65, 500], [40, 1, 64, 20], 5, 1, 136, 16, "bfloat16", "token"), ([200, 0], [130, 17], 2, 2, 192, 32, "float16", "head"),
+    ([300, 128, 1], [129, 256, 9], 4, 2, 256, 8, "bfloat16", "token"), ([900], [20], 32, 2, 256, 512, "bfloat16", "head"),
+    # what tcgen05 does not take (small pages): tiles of 16, 32, 64 and 128 rows
+    ([90, 65], [30, 2], 1, 1, 256, 4, "bfloat16", "token"), ([90, 65], [60, 2], 1, 1, 256, 2, "float16", "head"),
+    ([129], [100], 1, 1, 200, 4, "bfloat16", "token"),
     ([64, 128], [16, 7], 1, 1, 80, 4, "bfloat16", "token"), ([70, 200], [20, 9], 2, 2, 64, 4, "bfloat16", "token"),
     ([70, 0, 130], [50, 3, 1], 1, 1, 128, 2, "float16", "token"), ([66], [12], 8, 4, 96, 4, "bfloat16", "token"),
     ([300, 40], [40, 17], 1, 1, 96, 1, "float16", "head"), ([90, 65], [30, 2], 1, 1, 256, 16, "bfloat16", "token"),
@@ -391,7 +396,7 @@ def test_tree_attention(pkg, lengths, new, heads, kv, dim, page, dtype, order, m
 
 
 @pytest.mark.parametrize("dim,most_new,n", [(64, 2, 700), (72, 2, 700), (40, 2, 700), (96, 2, 500), (256, 2, 300), (72, 20, 200),
-                                            (96, 70, 40)])
+                                            (96, 70, 40), (256, 20, 150)])
 def test_many_short_requests(pkg, dim, most_new, n):
     # every CTA goes through several tiles of rows
     r = np.random.default_rng(2)
@@ -412,7 +417,7 @@ def test_rows_that_see_nothing(pkg):
 
 
 @pytest.mark.parametrize("new,page,dim", [(4, 16, 64), (20, 16, 64), (100, 16, 64), (4, 4, 64), (10, 4, 64), (20, 4, 64), (100, 4, 64),
-                                          (4, 16, 256), (30, 16, 256), (60, 8, 128), (90, 8, 80)])
+                                          (4, 16, 256), (30, 16, 256), (60, 8, 128), (90, 8, 80), (30, 4, 256), (70, 8, 192)])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 def test_what_a_row_does_not_see_does_not_reach_it(pkg, new, page, dim, bad):
     import torch
