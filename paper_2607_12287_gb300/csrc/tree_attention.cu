@@ -767,10 +767,8 @@ Plan plan(const ivit_attention_config& c, const ivit_cache_layout& l) {
   const int group = c.heads / l.kv_heads;
   const int rows = static_cast<int>(std::min<long long>(128, static_cast<long long>(c.max_new) * group));  // that share a key head
   const int dp = l.head_dim <= 64 ? 64 : l.head_dim <= 80 ? 80 : l.head_dim <= 96 ? 96 : l.head_dim <= 128 ? 128 : 256;
-  if (rows > TC_ROWS && group <= 128 && l.page_size >= 8 && l.head_stride > 0 && l.token_stride > 0 && l.page_stride > 0) {
-    const int wide = dp == 96 ? 128 : dp;
-    return {true, wide, 0, tree_tc_rows(group), wide <= 128 ? 2 : 1, tree_part_floats(128, wide)};
-  }
+  if (rows > TC_ROWS && group <= 128 && l.page_size >= 8 && l.head_stride > 0 && l.token_stride > 0 && l.page_stride > 0)
+    return {true, dp, 0, tree_tc_rows(group), dp <= 128 ? 2 : 1, tree_part_floats(128, dp)};
   // the smallest tile that holds the rows
   const auto groups = [&](auto d) {
     constexpr int DP = decltype(d)::value;
@@ -811,11 +809,9 @@ cudaError_t launch(const Plan& p, const TreeArgs& a, int dtype, int ctas, cudaSt
     return launch_ex(tree_join_kernel<T, DP, decltype(m)::value, decltype(tc)::value>, dim3(x, y), dim3(256), 0, s, 1, a, ctas, search);
   };
   cudaError_t e;
-  if constexpr (DP != 96) {
-    if (p.tc) {
-      e = launch_tree_attention_tc(a, dtype, DP, ctas, s);
-      return e != cudaSuccess ? e : join(std::integral_constant<int, 128>{}, std::true_type{});
-    }
+  if (p.tc) {
+    e = launch_tree_attention_tc(a, dtype, DP, ctas, s);
+    return e != cudaSuccess ? e : join(std::integral_constant<int, 128>{}, std::true_type{});
   }
   e = p.rw == 1   ? (a.cache.page_shift >= 4 ? launch_rows<T, DP, 1, true>(a, ctas, s) : launch_rows<T, DP, 1>(a, ctas, s))
       : p.rw == 2 ? launch_rows<T, DP, 2>(a, ctas, s)

@@ -36,7 +36,7 @@ struct TreeArgs {
 // and sum of each row.
 __host__ __device__ constexpr int tree_part_floats(int m, int dp) { return m * (dp + 2); }
 
-// The tcgen05 kernel: dp 64, 80, 128 or 256, pages of 8 tokens and more, groups of up to 128 heads; tiles of
+// The tcgen05 kernel: dp 64, 80, 96, 128 or 256, pages of 8 tokens and more, groups of up to 128 heads; tiles of
 // tree_tc_rows(group) rows, two CTAs per SM (of dp 256 one).
 inline int tree_tc_rows(int group) { return 128 / group * group; }
 cudaError_t launch_tree_attention_tc(const TreeArgs& a, int dtype, int dp, int ctas, cudaStream_t s);

@@ -3,7 +3,7 @@
 // walks the request's keys in blocks of KB: first the cached tokens, then the new rows, each with a last block
 // that may be partly empty.  The blocks of the call are cut into equal runs, two CTAs per SM, as in
 // tree_attention.cu; while one CTA's warps take exponentials the other's MMAs run.  (Heads above 128: one CTA,
-// for O takes 256 columns of tensor memory and two blocks of K and V take 128 KB.)  KB is 96 for heads up to 80,
+// for O takes 256 columns of tensor memory and two blocks of K and V take 128 KB.)  KB is 96 for heads up to 96,
 // else 64: S, P and O of a block fit in 256 columns of tensor memory and a row of S in registers (heads of 64,
 // eight requests of up to 256 rows over up to 4096 tokens, 16 heads: 40 us, 42 at KB = 64, 50 at 128, which spills).
 //
@@ -11,7 +11,8 @@
 //   4      TMA: Q tile (a box of heads x new rows, which is the tile's order of rows), then K and V blocks
 //          through a ring.  A cached block is fetched page by page (or in boxes of the largest power of two
 //          that divides KB, for larger pages), a block of new rows in one box.  64 columns of a head form a
-//          slice with 128-byte swizzle, 16 that are left (heads up to 80) one with 32-byte swizzle.
+//          slice with 128-byte swizzle, 16 or 32 that are left (heads up to 80, up to 96) one with 32- or 64-byte
+//          swizzle (heads of 96, eight requests of up to 256 rows over up to 4096 tokens, 16 heads: 53 us, as 128 60).
 //   5      MMA: S = Q K^T of block i + 1 is issued before O += P V of block i; P is read from tensor memory,
 //          V is the B operand in MN-major form.
 //   0 - 3  softmax, thread = row = tensor-memory lane: S into registers, masked where the block holds keys
@@ -43,7 +44,7 @@ constexpr int THREADS = 192;
 
 template <int DP>
 struct Cfg {
-  static constexpr int KB = DP <= 80 ? 96 : 64;
+  static constexpr int KB = DP <= 96 ? 96 : 64;
   static constexpr int CTAS = DP <= 128 ? 2 : 1;                // of an SM
   static constexpr int FULL = DP / 64, TAIL = DP % 64;          // slices of 64 columns, and columns of a narrow last one
   static constexpr int Q1 = AQ * 128, T1 = KB * 128;            // bytes of a full slice of Q, of a K or V block
@@ -88,7 +89,7 @@ template <int W>
 __device__ __forceinline__ uint64_t sdesc_rows(uint32_t saddr) {
   constexpr uint32_t group = 8 * W * 2;
   uint64_t d = sdesc_sw128(saddr, group, group) & ~(static_cast<uint64_t>(7) << 61);
-  return d | (static_cast<uint64_t>(W == 16 ? 6 : W == 32 ? 4 : 2) << 61);  // 32-, 64-, 128-byte swizzle
+  return d | (static_cast<uint64_t>(W == 16 ? 6 : 4) << 61);  // 32-, 64-byte swizzle
 }
 
 // 4-D tiled load (see tma_load_2d).
@@ -576,6 +577,7 @@ cudaError_t launch_tree_attention_tc(const TreeArgs& a, int dtype, int dp, int c
     using T = decltype(type);
     return dp == 64    ? launch<T, 64>(a, dtype, ctas, s)
            : dp == 80  ? launch<T, 80>(a, dtype, ctas, s)
+           : dp == 96  ? launch<T, 96>(a, dtype, ctas, s)
            : dp == 128 ? launch<T, 128>(a, dtype, ctas, s)
                        : launch<T, 256>(a, dtype, ctas, s);
   };

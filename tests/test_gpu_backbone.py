@@ -374,6 +374,7 @@ ATTENTION = [  # cached, new, heads, kv, dim, page, type, order
     ([191, 192, 500], [128, 33, 97], 5, 1, 80, 128, "float16", "head"), ([700], [256], 2, 2, 64, 64, "bfloat16", "token"),
     ([0, 0, 127, 128, 129], [140, 3, 128, 129, 70], 2, 2, 64, 16, "float16", "token"),
     ([0, 64, 200], [75, 64, 1], 7, 1, 128, 16, "bfloat16", "token"), ([500], [65], 6, 2, 112, 256, "bfloat16", "head"),
+    ([300, 96], [50, 129], 2, 2, 88, 16, "bfloat16", "head"),
     # ... of heads above 128, whose last slices may be empty
     ([63, 64, 65, 500], [40, 1, 64, 20], 5, 1, 136, 16, "bfloat16", "token"), ([200, 0], [130, 17], 2, 2, 192, 32, "float16", "head"),
     ([300, 128, 1], [129, 256, 9], 4, 2, 256, 8, "bfloat16", "token"), ([900], [20], 32, 2, 256, 512, "bfloat16", "head"),
@@ -417,7 +418,7 @@ def test_rows_that_see_nothing(pkg):
 
 
 @pytest.mark.parametrize("new,page,dim", [(4, 16, 64), (20, 16, 64), (100, 16, 64), (4, 4, 64), (10, 4, 64), (20, 4, 64), (100, 4, 64),
-                                          (4, 16, 256), (30, 16, 256), (60, 8, 128), (90, 8, 80), (30, 4, 256), (70, 8, 192)])
+                                          (4, 16, 256), (30, 16, 256), (60, 8, 128), (90, 8, 80), (30, 4, 256), (70, 8, 192), (50, 16, 96)])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 def test_what_a_row_does_not_see_does_not_reach_it(pkg, new, page, dim, bad):
     import torch
