@@ -374,7 +374,9 @@ __device__ __forceinline__ void backward_heads(const RopeArgs& p, const Lane<L>&
         dot = fma_f32x2(tu[e], wu[e], dot);
         dot = fma_f32x2(tv[e], wv[e], dot);
       }
-      const float r = rsqrtf(fmaf(ln.sum(ss.x + ss.y), p.per_dim, p.eps));
+      const float square = ln.sum(ss.x + ss.y);  // (all lanes take part)
+      // lanes without a row add nothing to dw: with eps = 0 their zeros times 1 / sqrt(0) would be NaN
+      const float r = on ? rsqrtf(fmaf(square, p.per_dim, p.eps)) : 0.f;
       const float m = -r * r * r * ln.sum(dot.x + dot.y) * p.per_dim;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {

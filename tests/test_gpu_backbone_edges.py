@@ -1,0 +1,47 @@
+"""The language backbone's operators at the edges of what their arguments may be.
+
+Error bounds as in test_gpu_backbone.py."""
+import numpy as np
+import pytest
+
+from tests import backbone_ref as ref
+from tests.test_gpu_backbone import close_rotation, dev, host, i32, rope_case
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def pkg():
+    import paper_2607_12287_gb300 as p
+    p.load()
+    return p
+
+
+# --------------------------------------------------------------------- rotation
+
+@pytest.mark.parametrize("rows,heads,kv,dim,rot,inter,weights,dtype", [
+    (1, 4, 2, 128, 128, False, "qk", "bfloat16"), (3, 8, 2, 128, 64, True, "qk", "float16"), (5, 6, 2, 64, 64, False, "qk", "bfloat16"),
+    (5, 3, 3, 72, 72, False, "q", "bfloat16"), (7, 2, 1, 40, 40, True, "k", "float16"), (1, 2, 2, 8, 0, False, "qk", "float16"),
+    (4, 2, 1, 256, 256, False, "qk", "bfloat16"), (4001, 8, 2, 96, 96, False, "qk", "bfloat16"),
+])
+def test_gradients_without_eps(pkg, rows, heads, kv, dim, rot, inter, weights, dtype):
+    # eps = 0 and row counts that leave lanes of the last warp without a row
+    import torch
+    r = np.random.default_rng(rows + dim)
+    c = rope_case(r, rows, heads, kv, dim, rot, 1, dtype, weights)
+    cfg = pkg.make_rope_config(heads, kv, dim, rot, 1, inter, 0.0, dtype)
+    g = [dev(r.standard_normal((rows, m, dim)).astype(np.float32), dtype) for m in (heads, kv)]
+    d = [torch.full_like(t, float("nan")) for t in g]
+    dw = [torch.full((dim,), float("nan"), device="cuda") if x in weights else None for x in "qk"]
+    ws = torch.full((pkg.ivit_qk_norm_rope_backward_workspace(cfg),), 255, dtype=torch.uint8, device="cuda")
+    freq, axis = (dev(c["freq"]), i32(c["axis"])) if rot else (None, None)
+    pkg.ivit_qk_norm_rope_backward(cfg, *g, c["q"], c["k"], *c["w"], i32(c["pos"]), freq, axis, *d, *dw, ws)
+    for x, w, gx, dx, dwx, name in zip((c["q"], c["k"]), c["w"], g, d, dw, "qk"):
+        xs, gs = host(x), host(gx)
+        want, want_w = ref.rope_backward(gs, xs, None if w is None else host(w), c["pos"], c["freq"], c["axis"], rot, inter, 0.0)
+        rms = np.sqrt((xs ** 2).mean(-1, keepdims=True)) if w is not None else 1.0
+        close_rotation(dx, want, np.maximum(np.abs(gs), 2 * np.abs(gs) / rms), dtype, "d" + name)
+        if w is not None:
+            y = ref.rope(gs, None, -c["pos"], c["freq"], c["axis"], rot, inter, 0)
+            size = np.abs(y * xs / rms).sum((0, 1))
+            assert (np.abs(host(dwx) - want_w) <= 2.0 ** -16 * size + 1e-6).all(), name
