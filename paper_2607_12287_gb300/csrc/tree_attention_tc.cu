@@ -171,7 +171,9 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP>::CTAS)
                  o_free = bar + 48, t_full = bar + 56, t_empty = t_full + 8 * RING;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(sm + C::OFF_BAR + 56 + 16 * RING);
   volatile int* sh_abort = reinterpret_cast<volatile int*>(tslot + 1);
-  volatile int* sh_odd = reinterpret_cast<volatile int*>(tslot + 2);  // last tile of rows that met a value that is not finite
+  // Last tile of rows, of the even ones and of the odd ones, that met a value that is not finite.  A warp may be in tile n + 1
+  // while another still reads what tile n met; in n + 2 it is not, for the products of n + 1 wait for all four warps.
+  volatile int* sh_odd = reinterpret_cast<volatile int*>(tslot + 2);
   if (tid == 0) {
     mbar_init(q_full, 1);
     mbar_init(q_empty, 1);
@@ -190,7 +192,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP>::CTAS)
       if (TAIL > 0) tma_prefetch_desc(&m->hi);
     }
     *sh_abort = 0;
-    *sh_odd = 0;
+    sh_odd[0] = sh_odd[1] = 0;
   }
   if (warp == 5) {
     tmem_alloc(smem_u32(tslot), C::TM_COLS);
@@ -375,7 +377,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP>::CTAS)
 #pragma unroll
           for (int c = 0; c < FULL; ++c) odd |= clear_slice<T, KB, 128>(v + c * C::T1, keys, kb >= cached, tid);
           if (TAIL > 0) odd |= clear_slice<T, KB, (TAIL > 0 ? TAIL * 2 : 16)>(v + FULL * C::T1, keys, kb >= cached, tid);
-          if (odd) *sh_odd = n;
+          if (odd) sh_odd[n & 1] = n;
           fence_proxy_async_smem();
         }
         if (!(ok = __all_sync(0xffffffffu, wait(s_full, j & 1)))) break;
@@ -452,7 +454,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP>::CTAS)
       const bool whole = blocks == p.nkt;
       if (wrow) {
         const float sum = (l[0].x + l[0].y) + (l[1].x + l[1].y), inv = sum == 0.f ? 0.f : 1.f / sum;
-        const bool odd = *sh_odd == n;
+        const bool odd = sh_odd[n & 1] == n;
         const int h = p.head * a.group + x - node * a.group;
         const long long orow = p.r.row0 + node;
         T* dst = static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * a.cache.dim;

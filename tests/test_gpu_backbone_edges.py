@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 from tests import backbone_ref as ref
-from tests.test_gpu_backbone import close_rotation, dev, host, i32, rope_case
+from tests.test_gpu_backbone import attention_case, close_rotation, dev, host, i32, rope_case, run_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +45,31 @@ def test_gradients_without_eps(pkg, rows, heads, kv, dim, rot, inter, weights, d
             y = ref.rope(gs, None, -c["pos"], c["freq"], c["axis"], rot, inter, 0)
             size = np.abs(y * xs / rms).sum((0, 1))
             assert (np.abs(host(dwx) - want_w) <= 2.0 ** -16 * size + 1e-6).all(), name
+
+
+# -------------------------------------------------------------------- attention
+
+@pytest.mark.parametrize("heads,kv,dim,most_new,n,dtype,mask", [
+    (2, 2, 64, 90, 500, "bfloat16", "causal"), (4, 2, 80, 45, 400, "float16", "causal"), (2, 2, 128, 60, 400, "bfloat16", "causal"),
+    (2, 1, 256, 30, 400, "float16", "causal"), (2, 2, 72, 250, 100, "bfloat16", "all"), (4, 4, 96, 40, 400, "float16", "causal"),
+])
+def test_values_that_are_not_finite_in_every_tile(pkg, heads, kv, dim, most_new, n, dtype, mask):
+    # prompts over empty caches: a CTA goes through several tiles of rows, some with warps of padding rows alone, and
+    # each tile's first keys hold infinities and NaN that some of its rows see
+    r = np.random.default_rng(dim)
+    new = r.integers(max(1, most_new // 2), most_new + 1, n)
+    c = attention_case(r, [0] * n, new, heads, kv, dim, 8, dtype)
+    first, last = i32(c["cu"][:-1]).long(), i32(c["cu"][1:] - 1).long()
+    c["v"][first, :, 3] = float("inf")
+    c["v"][(first + last) // 2, 0, dim - 1] = float("-inf")
+    c["v"][last, kv - 1, 7] = float("nan")
+    out, _ = run_attention(pkg, c, mask, lse=False, check=False, max_new=most_new)
+    sees = {"causal": lambda i, m: np.tril(np.ones((m, m), bool)), "all": lambda i, m: np.ones((m, m), bool)}[mask]
+    with np.errstate(invalid="ignore"):
+        want, _, size = ref.attention(host(c["q"]), host(c["k"]), host(c["v"]), host(c["kc"]), host(c["vc"]), c["table"],
+                                      c["lengths"], c["cu"], sees, dim ** -0.5)
+    got, finite = host(out), np.isfinite(want)
+    np.testing.assert_array_equal(got[~finite], want[~finite])
+    u = ref.UNIT[dtype]
+    bound = u * np.abs(want) + (u + 2.0 ** -14) * size + 2.0 ** -25
+    assert (np.abs(got[finite] - want[finite]) <= bound[finite]).all()
