@@ -21,9 +21,9 @@
 // eight warps that share the keys, the 64 keys too for 32 rows; probabilities are rounded once from 64 rows on.
 // Sums use the fp32 values everywhere.
 //
-// Bound: the cache's bytes for few rows per key head (32 requests of up to 16384 tokens, 32 + 8 heads of 128, 168 us:
-// 6600 GB/s; 64 of up to 8192, 16 + 4 heads of 64, 49.5 us: 5500 GB/s), the chain of dependent reads of a start
-// for short ones (one request of 1041 tokens 7.7 us), mma.sync's rate for many rows.
+// Bound: the cache's bytes for few rows per key head (32 requests of up to 16384 tokens, 32 + 8 heads of 128, 171 us:
+// 6470 GB/s; 64 of up to 8192, 16 + 4 heads of 64, 52 us: 5260 GB/s), the chain of dependent reads of a start
+// for short ones (one request of 1041 tokens 7.5 us), mma.sync's rate for many rows.
 #include <algorithm>
 #include <type_traits>
 
@@ -71,15 +71,10 @@ __device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr)
                : "memory");
 }
 
-// 16 bytes to shared memory, or zeros (nothing is read) if not `ok`.  HINT: with an L2 policy.  Keys and values pass
-// through L2 once: asked to leave it first, they do not push out the parts of the runs, nor the kernels' own instructions.
-template <bool HINT>
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool ok, uint64_t policy) {
-  if (HINT)
-    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0), "l"(policy)
-                 : "memory");
-  else
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+// 16 bytes to shared memory, or zeros (nothing is read) if not `ok`.  Without an L2 policy: a build with one on these
+// copies faulted at heads of 256, and reading showed no cause that would spare the others (it was up to 8 % faster).
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -102,7 +97,6 @@ struct Cfg {
   static constexpr bool QSMEM = DP > 128;                                    // queries in shared memory, not registers
   static constexpr int STAGES = ALONE ? (DP <= 128 ? 3 : 1) : DP > 128 ? 2 : 3;
   static constexpr int TERMS = RW < 4 ? 2 : 1;
-  static constexpr bool HINT = ALONE && DP <= 128;                           // (64 requests, heads of 64: 70 -> 64 us)
   // a copy of a tile (of the warp's keys if it is alone): CP lanes for the pieces of a row, RP rows at a time
   static constexpr int CP = DP <= 64 ? 8 : DP <= 128 ? 16 : 32, RP = (ALONE ? 32 : THREADS) / CP, COPIES = (ALONE ? WK : TK) / RP;
   static constexpr int MEET = DP + 4;                                        // floats of a row where the warps meet
@@ -189,7 +183,6 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
       for (int x = 0; x < IDS; ++x) ids[x] = key + x * RP < load.r.len ? table[(key + x * RP) >> a.cache.page_shift] : -1;
     }
   };
-  const uint64_t policy = C::HINT ? l2_policy_evict_first() : 0;
   const auto copy = [&](int stage) {
     if (cp >= pieces) return;
     const uint32_t ks = sb + stage * 2 * C::TILE, vs = ks + C::TILE;
@@ -208,8 +201,8 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
 #pragma unroll
       for (int x = 0; x < COPIES; ++x) {
         if (!ONE_PAGE && x > 0) off = cached(x, ok);
-        copy16<C::HINT>(ks + place(x), kc + off, ok, policy);
-        copy16<C::HINT>(vs + place(x), vc + off, ok, policy);
+        copy16(ks + place(x), kc + off, ok);
+        copy16(vs + place(x), vc + off, ok);
         if (ONE_PAGE) off += step;
       }
       return;
@@ -231,8 +224,8 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
           v = static_cast<const T*>(a.v_new) + row * a.v_new_stride + col;
         }
       }
-      copy16<C::HINT>(ks + place(x), k, ok, policy);
-      copy16<C::HINT>(vs + place(x), v, ok, policy);
+      copy16(ks + place(x), k, ok);
+      copy16(vs + place(x), v, ok);
     }
   };
 
