@@ -288,7 +288,7 @@ typedef struct ivit_plan_config {
  * The new held lengths are base + new.
  * status_dev [1]: 0, or why the step was refused -- 1 too few free pages, 2 a request has
  * more pages than the table, 4 more rows than max_rows, 8 a negative length or an invalid
- * ring.  A refused step takes and returns no page, ring_out = ring_in, and every row is
+ * ring (one whose free pages and those that are returned are more than n_pages, too).  A refused step takes and returns no page, ring_out = ring_in, and every row is
  * marked as past the step's (cu_rows 0). */
 int ivit_step_plan(const ivit_plan_config* cfg, const int32_t* held_dev, const int32_t* base_dev,
                    const int32_t* new_dev, const int32_t* parent_dev, int32_t* ring_dev,

@@ -99,8 +99,8 @@ __global__ void __launch_bounds__(THREADS) step_plan_kernel(const PlanArgs a) {
     why |= 8;
   } else if (static_cast<unsigned>(sum[1]) > count) {
     why |= 1;
-  } else if (count - sum[1] + sum[2] > places) {
-    why |= 8;
+  } else if (count + sum[2] > places) {  // (a page that is both free and held: returned ids would land on places that are
+    why |= 8;                            // being read)
   }
   // every thread's reasons, in every thread
   int all_why = 0;

@@ -73,3 +73,25 @@ def test_values_that_are_not_finite_in_every_tile(pkg, heads, kv, dim, most_new,
     u = ref.UNIT[dtype]
     bound = u * np.abs(want) + (u + 2.0 ** -14) * size + 2.0 ** -25
     assert (np.abs(got[finite] - want[finite]) <= bound[finite]).all()
+
+
+# ------------------------------------------------------------------------- plan
+
+@pytest.mark.parametrize("free,status", [(2, 0), (3, 8), (4, 8)])
+def test_plan_refuses_pages_that_are_free_and_held(pkg, free, status):
+    # one request takes two pages, another returns two: with three free ones of four a page is on both sides, and the
+    # returned ids would go where the taken ones are read
+    import torch
+    ring, table = torch.tensor([3, 0, 0, 2]), torch.tensor([[-1, -1, -1], [0, 1, -1]])
+    cfg = pkg.make_plan_config(2, 32, 3, 16, 4)
+    out = lambda n: torch.full((n,), -77, dtype=torch.int32, device="cuda")
+    ring_dev, table_dev, cu, slots, ring_out, why = ring.int().cuda(), table.int().cuda(), out(3), out(32), out(2), out(1)
+    pkg.ivit_step_plan(cfg, i32([0, 32]), i32([0, 0]), i32([32, 0]), None, ring_dev, i32([3, free]), table_dev, cu, None, slots,
+                       None, None, ring_out, why)
+    assert int(why) == status
+    if status:
+        assert torch.equal(ring_dev.cpu(), ring.int()) and torch.equal(table_dev.cpu(), table.int())
+        assert ring_out.tolist() == [3, free] and cu.tolist() == [0, 0, 0] and slots.tolist() == [-1] * 32
+    else:
+        assert table_dev[0].tolist() == [2, 3, -1] and ring_dev.tolist() == [3, 0, 1, 2] and ring_out.tolist() == [1, 2]
+        assert cu.tolist() == [0, 32, 32] and slots.tolist() == list(range(32, 48)) + list(range(48, 64))
