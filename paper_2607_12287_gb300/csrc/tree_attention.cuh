@@ -48,9 +48,10 @@ struct TreeRequest {
 
 __device__ __forceinline__ TreeRequest tree_request(const TreeArgs& a, int i) {
   TreeRequest r;
-  const int lo = a.cu[i], hi = a.cu[i + 1], most = a.max_pages << a.cache.page_shift;
-  r.row0 = min(max(lo, 0), a.n_rows);
-  r.n = min(max(min(hi, a.n_rows) - r.row0, 0), a.max_new);
+  const int most = a.max_pages << a.cache.page_shift;
+  const auto bounded = [&](int row) { return min(max(row, 0), a.n_rows); };  // (each by itself: their difference fits)
+  r.row0 = bounded(a.cu[i]);
+  r.n = min(max(bounded(a.cu[i + 1]) - r.row0, 0), a.max_new);
   r.len = min(max(a.len[i], 0), most);
   return r;
 }

@@ -75,6 +75,24 @@ def test_values_that_are_not_finite_in_every_tile(pkg, heads, kv, dim, most_new,
     assert (np.abs(got[finite] - want[finite]) <= bound[finite]).all()
 
 
+@pytest.mark.parametrize("heads", [4, 16])  # (mma.sync, tcgen05)
+def test_row_offsets_out_of_range(pkg, heads):
+    # a request whose offsets are no range of rows has none; rows of no request are left as they are
+    import torch
+    c = attention_case(np.random.default_rng(heads), [40, 30], [5, 7], heads, 2, 64, 16, "bfloat16")
+    want, want_lse = run_attention(pkg, dict(c, cu=np.array([0, 5, 5])), "causal", check=False, max_new=7)
+    assert bool(torch.isfinite(want[:5]).all()) and bool(torch.isnan(want[5:]).all())
+    far = 2 ** 31
+    for cu in ([0, 5, -far], [0, 5, -1], [0, 5, 3], [-far, 5, -7], [-1, 5, -far]):
+        out, lse = run_attention(pkg, dict(c, cu=np.array(cu)), "causal", check=False, max_new=7)
+        for a, b in ((out, want), (lse, want_lse)):
+            assert torch.equal(a[:5], b[:5]) and bool(torch.isnan(a[5:]).all()), cu
+    # beyond the last row: up to it
+    all_rows, _ = run_attention(pkg, c, "causal", max_new=7)
+    out, _ = run_attention(pkg, dict(c, cu=np.array([0, 5, far - 1])), "causal", check=False, max_new=7)
+    assert torch.equal(out, all_rows)
+
+
 # ------------------------------------------------------------------------- plan
 
 @pytest.mark.parametrize("free,status", [(2, 0), (3, 8), (4, 8)])
