@@ -117,7 +117,8 @@ template <int L>
 __device__ __forceinline__ void angles(const RopeArgs& p, const Lane<L>& ln, int row, float2 (&c)[2], float2 (&s)[2]) {
   float c4[4] = {1.f, 1.f, 1.f, 1.f}, s4[4] = {0.f, 0.f, 0.f, 0.f};
   if (ln.rotated) {
-    int at[4] = {p.pos[row], 0, 0, 0};
+    const int first = p.pos[row];
+    int at[4] = {first, first, first, first};  // (axes that there are none of count as the first)
 #pragma unroll
     for (int x = 1; x < 4; ++x)
       if (x < p.n_axes) at[x] = p.pos[x * p.pos_stride + row];

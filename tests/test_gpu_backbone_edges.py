@@ -47,6 +47,26 @@ def test_gradients_without_eps(pkg, rows, heads, kv, dim, rot, inter, weights, d
             assert (np.abs(host(dwx) - want_w) <= 2.0 ** -16 * size + 1e-6).all(), name
 
 
+@pytest.mark.parametrize("axes", [1, 2, 3, 4])
+def test_axes_that_are_none_count_as_the_first(pkg, axes):
+    import torch
+    r = np.random.default_rng(axes)
+    rows, heads, kv, dim = 9, 4, 2, 64
+    c = rope_case(r, rows, heads, kv, dim, dim, axes, "float16", "")
+    cfg = pkg.make_rope_config(heads, kv, dim, dim, axes, False, 1e-6, "float16")
+    odd = r.choice([-2 ** 31, -1, 0, 1, 2, 3, 4, 5, 100, 2 ** 31 - 1], dim // 2)
+    odd[:4] = [2, 3, 1, -1]
+    results = []
+    for axis in (odd, np.where((odd >= 0) & (odd < axes), odd, 0)):
+        args = (i32(c["pos"]), dev(c["freq"]), i32(axis))
+        out, back = ([torch.empty((rows, m, dim), dtype=torch.float16, device="cuda") for m in (heads, kv)] for _ in range(2))
+        pkg.ivit_qk_norm_rope(cfg, c["q"], c["k"], None, None, None, *args, *out)
+        pkg.ivit_qk_norm_rope_backward(cfg, c["q"], c["k"], c["q"], c["k"], None, None, *args, *back)
+        results.append(out + back)
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
 # -------------------------------------------------------------------- attention
 
 @pytest.mark.parametrize("heads,kv,dim,most_new,n,dtype,mask", [
