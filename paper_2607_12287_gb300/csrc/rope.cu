@@ -341,7 +341,8 @@ __device__ __forceinline__ void backward_heads(const RopeArgs& p, const Lane<L>&
   uint2 ga[N], gb[N], xa[N], xb[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    ga[i] = gb[i] = xa[i] = xb[i] = make_uint2(0, 0);
+    ga[i] = gb[i] = xb[i] = make_uint2(0, 0);
+    xa[i] = make_uint2(0x3c003c00u, 0);  // (without a row: positive, so that with eps = 0 nothing is 0 times 1 / sqrt(0))
     if (on) {
       ga[i] = load4(g + i * step + ln.a);
       gb[i] = load4(g + i * step + ln.b);
@@ -375,9 +376,7 @@ __device__ __forceinline__ void backward_heads(const RopeArgs& p, const Lane<L>&
         dot = fma_f32x2(tu[e], wu[e], dot);
         dot = fma_f32x2(tv[e], wv[e], dot);
       }
-      const float square = ln.sum(ss.x + ss.y);  // (all lanes take part)
-      // lanes without a row add nothing to dw: with eps = 0 their zeros times 1 / sqrt(0) would be NaN
-      const float r = on ? rsqrtf(fmaf(square, p.per_dim, p.eps)) : 0.f;
+      const float r = rsqrtf(fmaf(ln.sum(ss.x + ss.y), p.per_dim, p.eps));
       const float m = -r * r * r * ln.sum(dot.x + dot.y) * p.per_dim;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
