@@ -117,8 +117,7 @@ template <int L>
 __device__ __forceinline__ void angles(const RopeArgs& p, const Lane<L>& ln, int row, float2 (&c)[2], float2 (&s)[2]) {
   float c4[4] = {1.f, 1.f, 1.f, 1.f}, s4[4] = {0.f, 0.f, 0.f, 0.f};
   if (ln.rotated) {
-    const int first = p.pos[row];
-    int at[4] = {first, first, first, first};  // (axes that there are none of count as the first)
+    int at[4] = {p.pos[row], 0, 0, 0};
 #pragma unroll
     for (int x = 1; x < 4; ++x)
       if (x < p.n_axes) at[x] = p.pos[x * p.pos_stride + row];
@@ -128,6 +127,7 @@ __device__ __forceinline__ void angles(const RopeArgs& p, const Lane<L>& ln, int
     for (int i = 0; i < 4; ++i) {
       f[i] = p.freq[4 * ln.l + i];
       ax[i] = p.n_axes > 1 ? p.axis[4 * ln.l + i] : 0;
+      if (ax[i] >= p.n_axes) ax[i] = 0;  // (negative ones choose axis 0 below)
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
