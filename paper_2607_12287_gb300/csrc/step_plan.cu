@@ -210,9 +210,9 @@ extern "C" int ivit_step_plan(const ivit_plan_config* cfg, const int32_t* held_d
                       cfg->max_rows, cfg->max_pages, shift, cfg->n_pages, cfg->mask_words};
   const int want = max((cfg->max_rows + THREADS - 1) / THREADS, (cfg->n_req + WARPS - 1) / WARPS);
   const size_t smem = sizeof(int) * (3 * static_cast<size_t>(cfg->n_req) + 1);
-  cudaError_t e = smem <= 48000 ? cudaSuccess
-                                : cudaFuncSetAttribute(step_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                       static_cast<int>(smem));
+  // (the limit is set to the largest call's, never lower: another thread may be about to launch with it)
+  constexpr int most = sizeof(int) * (3 * MAX_REQ + 1);
+  cudaError_t e = smem <= 48000 ? cudaSuccess : allow_smem<step_plan_kernel>(most);
   if (e == cudaSuccess)
     e = launch_ex(step_plan_kernel, dim3(max(1, min(want, sms))), dim3(THREADS), smem,
                                   static_cast<cudaStream_t>(stream), 1, a);

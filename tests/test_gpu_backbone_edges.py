@@ -133,3 +133,34 @@ def test_plan_refuses_pages_that_are_free_and_held(pkg, free, status):
     else:
         assert table_dev[0].tolist() == [2, 3, -1] and ring_dev.tolist() == [3, 0, 1, 2] and ring_out.tolist() == [1, 2]
         assert cu.tolist() == [0, 32, 32] and slots.tolist() == list(range(32, 48)) + list(range(48, 64))
+
+def test_plans_of_many_requests_from_two_threads(pkg):
+    # calls that need more shared memory than is allowed by default, of different sizes, at the same time
+    import threading
+
+    import torch
+    failed = []
+
+    def plans(n):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                cfg = pkg.make_plan_config(n, n, 1, 16, n)
+                zeros = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")
+                ring, table, status = torch.arange(n, dtype=torch.int32, device="cuda"), zeros(n, 1), zeros(1)
+                held, new, ring_in, cu, slots, ring_out = zeros(n), zeros(n) + 1, i32([0, n]), zeros(n + 1), zeros(n), zeros(2)
+                stream.synchronize()
+                for _ in range(3000):
+                    pkg.ivit_step_plan(cfg, held, held, new, None, ring, ring_in, table, cu, None, slots, None, None, ring_out,
+                                       status)
+                stream.synchronize()
+                assert int(status) == 0 and int(cu[n]) == n
+        except Exception as e:  # noqa: BLE001 (a thread's exception is the test's)
+            failed.append(repr(e))
+
+    threads = [threading.Thread(target=plans, args=(n,)) for n in (4000, 4096)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
