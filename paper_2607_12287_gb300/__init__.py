@@ -575,7 +575,9 @@ def ivit_kv_write(cache: IvitCacheLayout, k, v, rows, slots, k_cache, v_cache, s
     if csh[1:] != cache.shape or cst[1:] != cache.strides or vcsh != csh or vcst != cst or csh[0] < layers:
         raise ValueError(f"k_cache, v_cache: shapes {tuple(csh)} and {tuple(vcsh)} are not {layers} caches of the layout, "
                          f"{cache.shape}, with strides {cache.strides}")
-    n = rows.numel() if hasattr(rows, "numel") else 0
+    if rows is None or isinstance(rows, (int, np.ndarray)):
+        raise TypeError("rows: a CUDA tensor is required")
+    n = rows.numel()
     args = (C.addressof(cache), layers, n, n_src, k.data_ptr(), v.data_ptr(), st[1] if n_src > 1 else kv * dim,
             st[0] if layers > 1 else 0, _i32(rows, "rows", n), _i32(slots, "slots", n),
             k_cache.data_ptr(), v_cache.data_ptr(), cst[0] if layers > 1 else 0, _stream(stream))

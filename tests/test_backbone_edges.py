@@ -3,6 +3,12 @@ import glob
 import os
 import re
 
+import numpy as np
+import pytest
+
+import paper_2607_12287_gb300 as pkg
+from tests.test_backbone_checks import bf, ints
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
@@ -12,3 +18,12 @@ def test_asynchronous_copies_take_no_l2_policy():
     assert sources
     for path in sources:
         assert not re.search(r"cp\.async\.c[ag]\.[a-z.:0-9_]*cache_hint", open(path).read(), re.I), path
+
+
+@pytest.mark.parametrize("rows", [None, 0x10000, np.zeros(4, np.int32)])
+def test_write_needs_its_rows(monkeypatch, rows):
+    # how many rows there are is known from this tensor alone
+    monkeypatch.setattr(pkg, "load", lambda *a: pytest.fail("library reached"))
+    caches = bf(3, 4, 16, 2, 64)
+    with pytest.raises(TypeError, match="rows"):
+        pkg.ivit_kv_write(pkg.make_cache_layout(caches[0]), bf(3, 6, 2, 64), bf(3, 6, 2, 64), rows, ints(4), caches, caches)
