@@ -297,7 +297,7 @@ int ivit_step_plan(const ivit_plan_config* cfg, const int32_t* held_dev, const i
                    int32_t* status_dev, void* stream);
 
 /* Norm and rotation of heads of head_dim values (a multiple of 8, up to 256), the first
- * rot_dim (a multiple of 8) of which are rotated; heads and kv_heads up to 256. */
+ * rot_dim (a multiple of 8) of which are rotated; heads and kv_heads up to 256, up to 2^30 rows. */
 typedef struct ivit_rope_config {
   int32_t heads, kv_heads, head_dim, rot_dim;
   int32_t n_axes;        /* axes of a position (1: text; 3: time, height, width), up to 4 */

@@ -28,6 +28,7 @@ namespace {
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int FWD_CTAS = 3, BWD_CTAS = 2;  // per SM
 constexpr int BWD_CTAS_MAX = 1024;  // CTAs of the backward pass: partial weight gradients
+constexpr int MAX_ROWS = 1 << 30;   // (a warp's index, one to a row at most, is an int)
 
 struct RopeArgs {
   const void *q, *k, *v, *q_weight, *k_weight;
@@ -493,7 +494,7 @@ bool valid(const ivit_rope_config& c) {
 }
 
 const char* kShape = "need heads and kv_heads 1..256, head_dim a multiple of 8 up to 256, rot_dim a multiple of 8 up to "
-                     "it, 1..4 axes, interleaved 0 or 1, dtype IVIT_BF16 or IVIT_FP16, eps >= 0";
+                     "it, 1..4 axes, interleaved 0 or 1, dtype IVIT_BF16 or IVIT_FP16, eps >= 0, up to 2^30 rows";
 
 // Warps that share a set of rows: as many as it takes to give each of the chip's warp slots (`ctas` CTAs per
 // SM) work, up to the row's heads.
@@ -553,7 +554,7 @@ extern "C" int ivit_qk_norm_rope(const ivit_rope_config* cfg, int32_t n_rows, co
                                  const int32_t* slot_dev, void* stream) {
   using namespace ivit;
   if (!cfg || n_rows < 0) return fail(IVIT_ERR_ARG, "ivit_qk_norm_rope: null configuration or a negative row count");
-  if (!valid(*cfg)) return fail(IVIT_ERR_SHAPE, kShape);
+  if (!valid(*cfg) || n_rows > MAX_ROWS) return fail(IVIT_ERR_SHAPE, kShape);
   if (cache && (!valid_cache(*cache) || cache->kv_heads != cfg->kv_heads || cache->head_dim != cfg->head_dim ||
                 cache->dtype != cfg->dtype))
     return fail(IVIT_ERR_SHAPE, "ivit_qk_norm_rope: cache layout not supported, or of other heads or type than the rows");
@@ -618,7 +619,7 @@ extern "C" int ivit_qk_norm_rope_backward(const ivit_rope_config* cfg, int32_t n
   using namespace ivit;
   if (!cfg || n_rows < 0)
     return fail(IVIT_ERR_ARG, "ivit_qk_norm_rope_backward: null configuration or a negative row count");
-  if (!valid(*cfg)) return fail(IVIT_ERR_SHAPE, kShape);
+  if (!valid(*cfg) || n_rows > MAX_ROWS) return fail(IVIT_ERR_SHAPE, kShape);
   if ((dq_weight_dev && !q_weight_dev) || (dk_weight_dev && !k_weight_dev))
     return fail(IVIT_ERR_ARG, "ivit_qk_norm_rope_backward: a weight's gradient without the weight");
   const bool weights = dq_weight_dev || dk_weight_dev;
