@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 from tests import backbone_ref as ref
-from tests.test_gpu_backbone import attention_case, close_rotation, dev, host, i32, rope_case, run_attention
+from tests.test_gpu_backbone import attention_case, close_rotation, dev, host, i32, rope_case, run_attention, trees
 
 pytestmark = pytest.mark.gpu
 
@@ -111,6 +111,58 @@ def test_row_offsets_out_of_range(pkg, heads):
     all_rows, _ = run_attention(pkg, c, "causal", max_new=7)
     out, _ = run_attention(pkg, dict(c, cu=np.array([0, 5, far - 1])), "causal", check=False, max_new=7)
     assert torch.equal(out, all_rows)
+
+
+@pytest.mark.parametrize("heads,kv,dim,length,new,page,dtype", [
+    (4, 1, 64, 160, 4, 16, "bfloat16"), (4, 1, 64, 160, 4, 16, "float16"), (16, 16, 128, 64, 2, 16, "bfloat16"),
+    (8, 2, 72, 3000, 2, 16, "bfloat16"), (8, 2, 96, 3000, 4, 8, "float16"), (4, 2, 256, 700, 8, 32, "bfloat16"),
+    (6, 1, 256, 700, 2, 4, "float16"), (8, 2, 64, 200, 8, 4, "bfloat16"), (8, 2, 80, 3000, 6, 4, "float16"),
+    (16, 1, 128, 130, 2, 1, "bfloat16"), (4, 2, 256, 1000, 16, 2, "bfloat16"),  # (17 to 32 rows on small pages: tiles of 32)
+])
+def test_probabilities_keep_both_terms(pkg, heads, kv, dim, length, new, page, dtype):
+    # Up to 16 rows per key head (32 on small pages) probabilities enter the product with V as two 16-bit terms.  Keys of
+    # two kinds take turns, with scores q0 and q0 - q1 and values c and -c, all exact: the output nearly vanishes and with
+    # it its own rounding, while an error of the second kind's probability adds up over all keys.  Bound, with w = sum p |v| /
+    # sum p: u |o| for the output's rounding, u^2 w for the second term's, 2^-17 w for fp32 (the exponent, of at most
+    # 16, to 2^-20; exp2 and the sums).
+    import torch
+    r = np.random.default_rng(dim + new)
+    c = attention_case(r, [length], [new], heads, kv, dim, page, dtype)
+    values = r.choice([-1.5, -1.0, -0.75, 0.75, 1.0, 1.5], (kv, dim))
+
+    def fill(k, v, at, t):
+        kind = (t % 2)[:, None]
+        keys = np.zeros((len(t), kv, dim), np.float32)
+        keys[..., 0], keys[..., 1] = 1, -kind
+        k[at], v[at] = dev(keys, dtype), dev((values * (1 - 2 * kind[..., None])).astype(np.float32), dtype)
+
+    t = np.arange(length)
+    fill(c["kc"], c["vc"], (i32(c["table"][0][t // page]).long(), i32(t % page).long()), t)
+    fill(c["k"], c["v"], slice(0, new), np.arange(new))
+    q = np.zeros((new, heads, dim), np.float32)
+    q[..., 0], q[..., 1] = r.uniform(-2, 2, (new, heads)), r.uniform(0.01, 0.06, (new, heads))
+    c["q"] = dev(q, dtype)
+    out, _ = run_attention(pkg, c, "all", scale=1.0, check=False)
+    p = np.exp(-host(c["q"])[..., 1:2])
+    v = np.repeat(values, heads // kv, 0)[None]
+    u = ref.UNIT[dtype]
+    want, size = v * (1 - p) / (1 + p), np.abs(v) + 0 * p
+    bound = u * np.abs(want) + (u * u + 2.0 ** -17) * size
+    # (one term would not do, for most rows)
+    one = torch.from_numpy(p).to(c["q"].dtype).double().numpy()
+    assert ((np.abs(v * (1 - one) / (1 + p) - want) > bound).any(-1)).mean() > 0.5
+    assert (np.abs(host(out) - want) <= bound).all()
+
+
+@pytest.mark.parametrize("heads,kv,dim,lengths,new,page,dtype", [
+    (129, 1, 64, [70, 3], [1, 2], 16, "bfloat16"), (256, 1, 72, [100], [3], 16, "float16"), (200, 1, 128, [0, 65], [2, 1], 8, "bfloat16"),
+    (130, 1, 256, [40], [1], 32, "float16"),
+])
+@pytest.mark.parametrize("mask", ["causal", "all", "tree"])
+def test_groups_above_128_heads(pkg, heads, kv, dim, lengths, new, page, dtype, mask):
+    r = np.random.default_rng(heads)
+    c = attention_case(r, lengths, new, heads, kv, dim, page, dtype)
+    run_attention(pkg, c, mask, trees(r, new) if mask == "tree" else None)
 
 
 # ------------------------------------------------------------------------- plan
