@@ -349,7 +349,7 @@ int ivit_qk_norm_rope_backward(const ivit_rope_config* cfg, int32_t n_rows, cons
 #define IVIT_MASK_TREE 2       /* a row sees the rows whose bits are set in its mask */
 
 /* Limits: n_req up to 4096, heads up to 256 and a multiple of the cache's kv_heads, max_new up
- * to 65536, max_pages * page_size < 2^31, mask_words up to 32768. */
+ * to 65536, max_pages * page_size < 2^31 - 2^20, mask_words up to 32768. */
 typedef struct ivit_attention_config {
   int32_t n_req;
   int32_t heads;         /* query heads; head h reads key / value head h * kv_heads / heads */
@@ -367,7 +367,8 @@ typedef struct ivit_attention_config {
  * (not read from the cache, so that drafts need no slots before they are accepted).  A row that
  * sees nothing gets o = 0, lse = -inf; keys whose scores are -inf take no part; what a row does
  * not see does not reach it, NaN and infinities included.  Sums and the softmax are fp32;
- * probabilities enter the product with V as 16-bit values.
+ * probabilities enter the product with V as sums of two 16-bit values up to 16 rows (new rows x heads of the
+ * group) per key head, 32 on pages of fewer than 8 tokens, and as one 16-bit value above.
  * table_dev int32 [n_req][max_pages]; len_dev int32 [n_req] (more than the table holds counts as
  * that much, pages outside the cache read as zeros); cu_rows_dev int32 [n_req + 1];
  * mask_dev uint32 [n_rows][mask_words] for IVIT_MASK_TREE, else NULL; out [n_rows][heads]

@@ -18,12 +18,15 @@
 // as two 16-bit terms (16 bits and more of their fp32 value), which is free beside the cache's bytes.
 // Tiles of 32 to 128 rows are for what the tcgen05 kernel (tree_attention_tc.cu) does not take: pages of fewer
 // than 8 tokens, groups of more than 128 heads.  Row groups of 16 are split over four or
-// eight warps that share the keys, the 64 keys too for 32 rows; probabilities are rounded once from 64 rows on.
-// Sums use the fp32 values everywhere.
+// eight warps that share the keys, the 64 keys too for 32 rows; probabilities are rounded once from 64 rows on, where
+// the second term's products would not be free.  Sums use the fp32 values everywhere.
 //
 // Bound: the cache's bytes for few rows per key head (32 requests of up to 16384 tokens, 32 + 8 heads of 128, 171 us:
 // 6470 GB/s; 64 of up to 8192, 16 + 4 heads of 64, 52 us: 5260 GB/s), the chain of dependent reads of a start
-// for short ones (one request of 1041 tokens 7.5 us), mma.sync's rate for many rows.
+// for short ones (one request of 1041 tokens 7.5 us), mma.sync's rate for many rows (16 trees of up to 31 drafts over up to
+// 8192 tokens, 32 + 8 heads of 128, pages of 4 tokens 150 us; of 32, on tcgen05, 62).  Heads of 256 have one stage of the
+// ring, and with eight warps on an SM the cache's bytes still bound a decoding step (32 requests of up to 16384 tokens,
+// 16 + 4 heads, 171 us: 6470 GB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -836,7 +839,8 @@ extern "C" int ivit_tree_attention(const ivit_attention_config* cfg, const ivit_
   if (!valid(*cfg, *cache))
     return fail(IVIT_ERR_SHAPE,
                 "ivit_tree_attention: need 1..4096 requests, heads up to 256 and a multiple of the cache's, head_dim a "
-                "multiple of 8 up to 256, max_new 1..65536, a mask mode (trees with 1..32768 mask words), scale > 0 and a "
+                "multiple of 8 up to 256, max_pages * page_size below 2^31 - 2^20, max_new 1..65536, a mask mode (trees "
+                "with 1..32768 mask words), scale > 0 and a "
                 "supported cache layout");
   if (n_rows == 0) return IVIT_OK;
   if (!q_dev || !k_new_dev || !v_new_dev || !k_cache_dev || !v_cache_dev || !table_dev || !len_dev || !cu_rows_dev ||
