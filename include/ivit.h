@@ -398,6 +398,97 @@ int ivit_kv_write(const ivit_cache_layout* cache, int32_t n_layers, int32_t n, i
                   const int32_t* slot_dev, void* k_cache_dev, void* v_cache_dev, int64_t cache_layer_stride,
                   void* stream);
 
+/* ---- a cache of 8 bits
+ * Half the bytes of a decoding step: keys and values as e4m3 codes, with one fp32 scale for each block
+ * of `block` consecutive tokens of a page (tokens 0 .. block - 1, block .. 2 block - 1, ...) and head.  Code c of a
+ * block with scale s stands for c * s.  Element d of head h of token t of page p is at p * page_stride +
+ * t * token_stride + h * head_stride + d of an array of codes, the scale of that token's block at
+ * ((p * (page_size / block) + t / block) * kv_heads + h) of an array of scales; keys and values have
+ * arrays of their own of the same layout.  Supported: as for ivit_cache_layout, and block a power of two up to
+ * page_size; codes' arrays 8-byte aligned, scales' 4-byte.  16-byte aligned arrays with strides and a head_dim that
+ * are multiples of 16 take wider copies. */
+typedef struct ivit_quantised_layout {
+  int32_t n_pages, page_size, kv_heads, head_dim;
+  int32_t dtype;         /* IVIT_BF16 or IVIT_FP16: the type of rows (not of the cache) */
+  int32_t block;         /* tokens that share a scale */
+  int64_t page_stride, token_stride, head_stride;  /* in bytes (= elements), multiples of 8 */
+} ivit_quantised_layout;
+
+/* ivit_kv_write for a cache of 8 bits: row src_row_dev[i] of k and v ([n_layers][n_src][kv_heads][head_dim], row and
+ * layer strides in elements, multiples of 8) into slot slot_dev[i] of every layer's cache, for i < n; entries whose row is outside
+ * [0, n_src) or whose slot is outside the cache are skipped, slots of a call are distinct, and those of one block lie
+ * next to each other in the list (skipped ones may be between), as those of ivit_step_plan do.
+ * Of a block that is written, tokens before the last written one stay, if they are not written themselves, and what lies
+ * behind it is of no meaning from then on (a block whose first token is written with the rest behind it starts afresh, so
+ * that a page's next owner finds no old scale).  The new scale is the smallest power of two from 2^-60 to 2^60 by which
+ * the finite new values are at most 448, and not below the old scale where tokens stay; those are rounded again
+ * if the scale grew (a power of two: exact but for codes that leave the normal range).  Codes are rounded to nearest even;
+ * values that are not finite become NaN, finite ones beyond 448 * 2^60 the largest code.  A repeated call changes nothing.
+ * Layer l's codes begin cache_layer_stride * l bytes in (a multiple of 8), its scales scale_layer_stride * l elements in. */
+int ivit_kv_quantise(const ivit_quantised_layout* cache, int32_t n_layers, int32_t n, int32_t n_src, const void* k_dev,
+                     const void* v_dev, int64_t row_stride, int64_t layer_stride, const int32_t* src_row_dev,
+                     const int32_t* slot_dev, void* k_cache_dev, void* v_cache_dev, int64_t cache_layer_stride,
+                     float* k_scale_dev, float* v_scale_dev, int64_t scale_layer_stride, void* stream);
+
+/* Cached tokens back as rows: slot slot_dev[i] of every layer into row i of k and v ([n_layers][n][kv_heads][head_dim],
+ * strides as above), code * scale rounded once to the rows' type, for i < n.  Rows whose slot is outside the cache
+ * are left as they are. */
+int ivit_kv_dequantise(const ivit_quantised_layout* cache, int32_t n_layers, int32_t n, const int32_t* slot_dev,
+                       const void* k_cache_dev, const void* v_cache_dev, int64_t cache_layer_stride,
+                       const float* k_scale_dev, const float* v_scale_dev, int64_t scale_layer_stride, void* k_dev,
+                       void* v_dev, int64_t row_stride, int64_t layer_stride, void* stream);
+
+/* ivit_tree_attention over a cache of 8 bits: the operation, arguments, limits and workspace rules are those given
+ * there, with cached keys code * k_scale and values code * v_scale; new rows (q, k_new, v_new, out) are of the layout's
+ * 16-bit type.  Scales other than ivit_kv_quantise's have to be positive and within 2^-60 .. 2^60 (one that is not positive counts as
+ * none: 0 for keys, 2^-100 for values).  Codes enter the products as they are, exactly, as 16-bit values; a block's scale
+ * of keys multiplies their scores and one of values their probabilities, in fp32.  Probabilities enter the product
+ * with V as sums of two 16-bit values up to 16 rows (new rows x heads of the group) per key head and as one above. */
+size_t ivit_tree_attention_quantised_workspace(const ivit_attention_config* cfg, const ivit_quantised_layout* cache);
+int ivit_tree_attention_quantised(const ivit_attention_config* cfg, const ivit_quantised_layout* cache, int32_t n_rows,
+                                  const void* q_dev, int64_t q_stride, const void* k_new_dev, int64_t k_new_stride,
+                                  const void* v_new_dev, int64_t v_new_stride, const void* k_cache_dev,
+                                  const void* v_cache_dev, const float* k_scale_dev, const float* v_scale_dev,
+                                  const int32_t* table_dev, const int32_t* len_dev, const int32_t* cu_rows_dev,
+                                  const uint32_t* mask_dev, void* out_dev, int64_t out_stride, float* lse_dev,
+                                  void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Limits: n_req up to 65536, vocab up to 2^24, max_new up to 1024. */
+#define IVIT_FP32 2
+typedef struct ivit_verify_config {
+  int32_t n_req;
+  int32_t vocab;
+  int32_t max_new;       /* most rows of a request (further ones are not looked at: never accepted) */
+  int32_t dtype;         /* of the logits: IVIT_BF16, IVIT_FP16 or IVIT_FP32 */
+} ivit_verify_config;
+
+/* Verification of drafted tokens against the target's probabilities, from given random numbers: tokens that are accepted
+ * and the one that follows them are distributed as if the target had been sampled token by token.
+ * Row r of a step is a token, token_dev[r], and the target's logits after it, logits_dev [n_rows][vocab]; rows of a
+ * request lie back to back (cu_rows_dev [n_req + 1]), its first is the known token and is always accepted, the others
+ * are drafts.  parent_dev [n_rows] says which row a draft hangs on, as in ivit_step_plan (NULL: a run); a draft that hangs on none is
+ * never accepted.  draft_prob_dev fp32 [n_rows][vocab]: row r has the probabilities q from which the drafts that hang on row
+ * r were drawn, independently of each other; NULL: drafts were not drawn (q is 1 at the draft's token).
+ * temperature_dev fp32 [n_req]: the target is p = softmax(logits / temperature); 0 or less (or NaN), or NULL for
+ * all requests: the first of the likeliest tokens has probability 1.
+ * From the first row on, with w = p and W = 1: of the drafts that hang on the last accepted row, in their order, draft x in
+ * row r is accepted if uniform_dev[r] * W * q(x) < w(x), and its row is the last accepted one then (w = p, W = 1);
+ * else w loses what was tried, w = max(w - W q, 0) (without q: w(x) = 0), and W = sum(w).  When no draft is left, next_dev[i] is the
+ * token with the largest w / noise among positive ones, the first of equals, where noise_dev fp32 [n_req][vocab] has exponential random numbers
+ * (those that are not positive take no part).  If no w is left then w = p; if no token has a probability (no logit above
+ * -inf; NaN counts as -inf) the next token is -1.  A token outside [0, vocab) is never accepted and changes nothing.
+ * uniform_dev fp32 [n_rows], of [0, 1); it and noise_dev may be NULL if temperature_dev is.
+ * Out: accepted_dev [n_req] the number of accepted rows (0 for a request without rows, whose next token is -1), next_dev [n_req],
+ * and path_dev [n_rows]: at cu_rows[i] + j the j-th accepted row of request i, -1 past them, so that path_dev and
+ * ivit_step_plan's slots are what ivit_kv_write and ivit_kv_quantise take; entries of no request are left as they are.
+ * Row strides in elements, at least vocab (16-byte aligned rows take wider loads).  All arithmetic is fp32; sums are made in an
+ * order that depends on the sizes alone. */
+int ivit_tree_verify(const ivit_verify_config* cfg, int32_t n_rows, const void* logits_dev, int64_t logits_stride,
+                     const float* draft_prob_dev, int64_t draft_prob_stride, const int32_t* token_dev,
+                     const int32_t* parent_dev, const int32_t* cu_rows_dev, const float* temperature_dev,
+                     const float* uniform_dev, const float* noise_dev, int64_t noise_stride, int32_t* path_dev,
+                     int32_t* accepted_dev, int32_t* next_dev, void* stream);
+
 /* Message of the last failure on `h` (or of the last failed create if h is NULL). */
 const char* ivit_last_error(const ivit_handle* h);
 

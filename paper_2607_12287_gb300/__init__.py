@@ -31,11 +31,13 @@ EXPORTED = [
     "ivit_timeline_read", "ivit_device_status", "ivit_last_launch_count", "ivit_destroy",
     "ivit_last_error", "ivit_select_noalloc", "ivit_action_combine", "ivit_step_plan",
     "ivit_qk_norm_rope", "ivit_qk_norm_rope_backward_workspace", "ivit_qk_norm_rope_backward",
-    "ivit_tree_attention_workspace", "ivit_tree_attention", "ivit_kv_write",
+    "ivit_tree_attention_workspace", "ivit_tree_attention", "ivit_kv_write", "ivit_kv_quantise", "ivit_kv_dequantise",
+    "ivit_tree_attention_quantised_workspace", "ivit_tree_attention_quantised", "ivit_tree_verify",
 ]
 IVIT_NOALLOC_MAX_TOKENS = 65536
 IVIT_BF16 = 0
 IVIT_FP16 = 1
+IVIT_FP32 = 2
 
 
 class IvitConfig(C.Structure):
@@ -70,6 +72,19 @@ class IvitRopeConfig(C.Structure):
 class IvitAttentionConfig(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_req", "heads", "max_pages", "max_new", "mask_mode", "mask_words")]
     _fields_.append(("scale", C.c_float))
+
+
+class IvitQuantisedLayout(C.Structure):
+    """Layout of a paged key (or value) cache of 8 bits of one layer; build it with ``make_quantised_layout``."""
+    _fields_ = [
+        ("n_pages", C.c_int32), ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("dtype", C.c_int32), ("block", C.c_int32), ("page_stride", C.c_int64), ("token_stride", C.c_int64),
+        ("head_stride", C.c_int64),
+    ]
+
+
+class IvitVerifyConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_req", "vocab", "max_new", "dtype")]
 
 
 class IvitError(RuntimeError):
@@ -123,6 +138,13 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     L.ivit_tree_attention_workspace.argtypes = [P, P]
     L.ivit_tree_attention.argtypes = [P, P, I32, P, I64, P, I64, P, I64, P, P, P, P, P, P, P, I64, P, P, C.c_size_t, P]
     L.ivit_kv_write.argtypes = [P, I32, I32, I32, P, P, I64, I64, P, P, P, P, I64, P]
+    L.ivit_kv_quantise.argtypes = [P, I32, I32, I32, P, P, I64, I64, P, P, P, P, I64, P, P, I64, P]
+    L.ivit_kv_dequantise.argtypes = [P, I32, I32, P, P, P, I64, P, P, I64, P, P, I64, I64, P]
+    L.ivit_tree_attention_quantised_workspace.restype = C.c_size_t
+    L.ivit_tree_attention_quantised_workspace.argtypes = [P, P]
+    L.ivit_tree_attention_quantised.argtypes = [P, P, I32, P, I64, P, I64, P, I64, P, P, P, P, P, P, P, P, P, I64, P, P,
+                                                C.c_size_t, P]
+    L.ivit_tree_verify.argtypes = [P, I32, P, I64, P, I64, P, P, P, P, P, P, I64, P, P, P, P]
     _lib = L
     return L
 
@@ -148,7 +170,7 @@ def _tensor_type():
     t = _dtypes.get("tensor")
     if t is None:
         import torch
-        for name in ("uint8", "int32", "float32", "bfloat16", "float16"):
+        for name in ("uint8", "int32", "float32", "bfloat16", "float16", "float8_e4m3fn"):
             _dtypes[name] = getattr(torch, name)
         _dtypes[IVIT_BF16], _dtypes[IVIT_FP16] = torch.bfloat16, torch.float16  # (by the library's codes, too)
         _Int32 = torch.int32
@@ -582,6 +604,196 @@ def ivit_kv_write(cache: IvitCacheLayout, k, v, rows, slots, k_cache, v_cache, s
             st[0] if layers > 1 else 0, _i32(rows, "rows", n), _i32(slots, "slots", n),
             k_cache.data_ptr(), v_cache.data_ptr(), cst[0] if layers > 1 else 0, _stream(stream))
     _check(load().ivit_kv_write(*args), None)
+
+
+# a cache of 8 bits, and the verification of drafts
+
+_VERIFY_DTYPES = {**_DTYPES, "float32": IVIT_FP32}
+
+
+def make_quantised_layout(cache, block: int, dtype="bfloat16") -> IvitQuantisedLayout:
+    """Layout of a paged cache of 8 bits given as a float8_e4m3fn tensor [pages, page_size, kv_heads, head_dim] (any strides with
+    contiguous heads); ``block``: tokens that share a scale, ``dtype``: of the rows that are written and read.  Scales are
+    a float32 tensor [pages, page_size // block, kv_heads]."""
+    if len(cache.shape) != 4:
+        raise ValueError(f"cache: shape {tuple(cache.shape)}, expected [pages, page_size, kv_heads, head_dim]")
+    if str(cache.dtype) != "torch.float8_e4m3fn":
+        raise TypeError(f"cache: dtype {cache.dtype}, expected torch.float8_e4m3fn")
+    st = cache.stride()
+    if st[3] != 1:
+        raise ValueError("cache: the values of a head are not contiguous")
+    lay = IvitQuantisedLayout(*cache.shape, _dtype_code(dtype), block, st[0], st[1], st[2])
+    lay.shape, lay.strides = tuple(cache.shape), tuple(st)
+    lay.scales = (cache.shape[0], cache.shape[1] // max(block, 1), cache.shape[2])
+    return lay
+
+
+def make_verify_config(n_req: int, vocab: int, max_new: int, dtype="bfloat16") -> IvitVerifyConfig:
+    """``dtype``: of the logits (bfloat16, float16 or float32)."""
+    name = str(dtype).replace("torch.", "")
+    if name not in _VERIFY_DTYPES:
+        raise TypeError(f"dtype {dtype}: bfloat16, float16 or float32 is required")
+    return IvitVerifyConfig(n_req, vocab, max_new, _VERIFY_DTYPES[name])
+
+
+def _device_of(t, name: str) -> None:
+    """Rejects a tensor of another device than the current one, on which the library launches."""
+    if type(t) is _Tensor and _current and t.get_device() != _current[1]():
+        raise ValueError(f"{name}: tensor on {t.device}, the current device is cuda:{_current[1]()}")
+
+
+def _float8(t, name: str):
+    """The tensor, if it is a device tensor of e4m3 codes."""
+    if t is None or isinstance(t, (int, np.ndarray)):
+        raise TypeError(f"{name}: a CUDA tensor is required")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name}: tensor on {t.device}; a CUDA tensor is required")
+    if str(t.dtype) != "torch.float8_e4m3fn":
+        raise TypeError(f"{name}: dtype {t.dtype}, expected torch.float8_e4m3fn")
+    _device_of(t, name)
+    return t
+
+
+def _codes(t, name: str, layout: IvitQuantisedLayout) -> int:
+    """The pointer of a cache of 8 bits of this layout; rejects any other tensor."""
+    if (type(t) is _Tensor and t.is_cuda and t.dtype is _dtypes["float8_e4m3fn"] and t.shape == layout.shape
+            and t.stride() == layout.strides):
+        return t.data_ptr()
+    _float8(t, name)
+    if tuple(t.shape) != layout.shape or tuple(t.stride()) != layout.strides:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} and strides {t.stride()} are not the layout's, {layout.shape} and "
+                         f"{layout.strides}")
+    return t.data_ptr()
+
+
+def _scales(t, name: str, layout: IvitQuantisedLayout) -> int:
+    """The pointer of the scales [pages, blocks, kv_heads] of such a cache."""
+    if t is None or isinstance(t, (int, np.ndarray)):
+        raise TypeError(f"{name}: a CUDA tensor is required")
+    n_pages, blocks, heads = layout.scales
+    return _arg(t, name, "float32", n_pages * blocks * heads)
+
+
+def _quantised_layers(cache: IvitQuantisedLayout, layers: int, k_cache, v_cache, k_scale, v_scale) -> tuple:
+    """Pointers and layer strides of the caches [layers, pages, page_size, kv_heads, head_dim] and their scales [layers, pages,
+    blocks, kv_heads]."""
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        _float8(t, name)
+        if len(t.shape) != 5 or t.shape[0] < layers or tuple(t.shape[1:]) != cache.shape or tuple(t.stride()[1:]) != cache.strides:
+            raise ValueError(f"{name}: shape {tuple(t.shape)} is not {layers} caches of the layout, {cache.shape}, with strides "
+                             f"{cache.strides}")
+    for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+        if t is None or isinstance(t, (int, np.ndarray)):
+            raise TypeError(f"{name}: a CUDA tensor is required")
+        if len(t.shape) != 4 or t.shape[0] < layers or tuple(t.shape[1:]) != cache.scales:
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [{layers}, {', '.join(map(str, cache.scales))}]")
+        _arg(t, name, "float32", 0)
+        _device_of(t, name)
+    cst = k_cache.stride()[0] if layers > 1 else 0
+    if layers > 1 and v_cache.stride()[0] != cst:
+        raise ValueError("k_cache, v_cache: the strides differ")
+    n_pages, blocks, heads = cache.scales
+    return k_cache.data_ptr(), v_cache.data_ptr(), cst, k_scale.data_ptr(), v_scale.data_ptr(), n_pages * blocks * heads
+
+
+def _layer_rows(k, v, cache: IvitQuantisedLayout) -> tuple:
+    """Layers, rows, and row and layer stride of k and v [layers, rows, kv_heads, head_dim]."""
+    kv, dim = cache.kv_heads, cache.head_dim
+    (sh, st), (vsh, vst) = _layers(k, "k", cache.dtype), _layers(v, "v", cache.dtype)
+    if len(sh) != 4 or sh[2] != kv or sh[3] != dim or sh != vsh:
+        raise ValueError(f"k, v: shapes {tuple(sh)} and {tuple(vsh)}, expected [layers, rows, {kv}, {dim}]")
+    if st[3] != 1 or (st[2] != dim and kv > 1) or st != vst:
+        raise ValueError("k, v: the heads of a row are not contiguous, or the strides differ")
+    _device_of(k, "k")
+    _device_of(v, "v")
+    return sh[0], sh[1], st[1] if sh[1] > 1 else kv * dim, st[0] if sh[0] > 1 else 0
+
+
+def ivit_kv_quantise(cache: IvitQuantisedLayout, k, v, rows, slots, k_cache, v_cache, k_scale, v_scale, stream=None) -> None:
+    """Rows ``rows`` (int32, -1: none) of k and v [layers, rows, kv_heads, head_dim] into the ``slots`` of the caches of 8 bits
+    [layers, pages, page_size, kv_heads, head_dim] of all layers and their scales [layers, pages, blocks, kv_heads]."""
+    layers, n_src, row, layer = _layer_rows(k, v, cache)
+    kc, vc, cst, ks, vs, sst = _quantised_layers(cache, layers, k_cache, v_cache, k_scale, v_scale)
+    if rows is None or isinstance(rows, (int, np.ndarray)):
+        raise TypeError("rows: a CUDA tensor is required")
+    n, run = rows.numel(), _stream(stream)
+    args = (C.addressof(cache), layers, n, n_src, k.data_ptr(), v.data_ptr(), row, layer, _i32(rows, "rows", n),
+            _i32(slots, "slots", n), kc, vc, cst, ks, vs, sst, run)
+    _check(load().ivit_kv_quantise(*args), None)
+
+
+def ivit_kv_dequantise(cache: IvitQuantisedLayout, slots, k_cache, v_cache, k_scale, v_scale, k, v, stream=None) -> None:
+    """The cached tokens in ``slots`` (int32, -1: none) of all layers into the rows of k and v [layers, rows, kv_heads,
+    head_dim], one for each slot."""
+    layers, n, row, layer = _layer_rows(k, v, cache)
+    kc, vc, cst, ks, vs, sst = _quantised_layers(cache, layers, k_cache, v_cache, k_scale, v_scale)
+    if slots is None or isinstance(slots, (int, np.ndarray)):
+        raise TypeError("slots: a CUDA tensor is required")
+    run = _stream(stream)
+    args = (C.addressof(cache), layers, n, _i32(slots, "slots", n), kc, vc, cst, ks, vs, sst, k.data_ptr(), v.data_ptr(), row,
+            layer, run)
+    _check(load().ivit_kv_dequantise(*args), None)
+
+
+def ivit_tree_attention_quantised_workspace(cfg: IvitAttentionConfig, cache: IvitQuantisedLayout) -> int:
+    """Bytes of the workspace of ``ivit_tree_attention_quantised`` (0: the arguments are invalid)."""
+    return int(load().ivit_tree_attention_quantised_workspace(C.addressof(cfg), C.addressof(cache)))
+
+
+def ivit_tree_attention_quantised(cfg: IvitAttentionConfig, cache: IvitQuantisedLayout, q, k_new, v_new, k_cache, v_cache, k_scale,
+                                  v_scale, table, lengths, cu_rows, mask, out, lse=None, workspace=None, stream=None) -> None:
+    """``ivit_tree_attention`` over a cache of 8 bits: ``k_scale``, ``v_scale`` fp32 [pages, blocks, kv_heads], the rest as there."""
+    n, dt, dim, heads, req = _row_count(q, "q"), cache.dtype, cache.head_dim, cfg.heads, cfg.n_req
+    q_shape, k_shape = (n, heads, dim), (n, cache.kv_heads, dim)
+    if cfg.mask_mode != IVIT_MASK_TREE:
+        mask = None
+    _device_of(q, "q")
+    args = (C.addressof(cfg), C.addressof(cache), n, *_rows(q, "q", dt, q_shape), *_rows(k_new, "k_new", dt, k_shape),
+            *_rows(v_new, "v_new", dt, k_shape), _codes(k_cache, "k_cache", cache), _codes(v_cache, "v_cache", cache),
+            _scales(k_scale, "k_scale", cache), _scales(v_scale, "v_scale", cache),
+            _i32(table, "table", req * cfg.max_pages), _i32(lengths, "lengths", req),
+            _i32(cu_rows, "cu_rows", req + 1), _i32(mask, "mask", n * cfg.mask_words),
+            *_rows(out, "out", dt, q_shape), _arg(lse, "lse", "float32", n * heads),
+            *_workspace(workspace), _stream(stream))
+    _check(load().ivit_tree_attention_quantised(*args), None)
+
+
+def _table(t, name: str, dtype_name: str, rows: int, width: int) -> tuple:
+    """Pointer and row stride of a tensor [rows, width] whose rows are contiguous; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if isinstance(t, (int, np.ndarray)):
+        raise TypeError(f"{name}: a CUDA tensor is required")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name}: tensor on {t.device}; a CUDA tensor is required")
+    if str(t.dtype) != "torch." + dtype_name:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected torch.{dtype_name}")
+    sh, st = t.shape, t.stride()
+    if len(sh) != 2 or sh[0] < rows or sh[1] != width or (st[1] != 1 and width > 1):
+        raise ValueError(f"{name}: shape {tuple(sh)} and strides {tuple(st)}, expected [{rows}, {width}] with contiguous rows")
+    _device_of(t, name)
+    return t.data_ptr(), st[0] if sh[0] > 1 else width
+
+
+def ivit_tree_verify(cfg: IvitVerifyConfig, logits, draft_probs, tokens, parent, cu_rows, temperature, uniform, noise, path,
+                     accepted, next_token, stream=None) -> None:
+    """Which drafts of every request are right, and the token that follows them, from the target's ``logits`` [rows, vocab] after
+    each row, the drafter's probabilities fp32 [rows, vocab] (or None), ``tokens``, ``parent`` (or None) int32 [rows],
+    ``temperature`` fp32 [n_req] (or None: the likeliest token), ``uniform`` fp32 [rows] and exponential ``noise`` fp32
+    [n_req, vocab]: the accepted rows go to ``path`` int32 [rows], their number and the next token to ``accepted`` and ``next_token`` int32
+    [n_req]."""
+    if logits is None or isinstance(logits, (int, np.ndarray)) or len(logits.shape) != 2:
+        raise ValueError("logits: a CUDA tensor [rows, vocab] is required")
+    n, req, vocab = logits.shape[0], cfg.n_req, cfg.vocab
+    name = {IVIT_BF16: "bfloat16", IVIT_FP16: "float16", IVIT_FP32: "float32"}.get(cfg.dtype)
+    if name is None:
+        raise TypeError("the configuration's dtype: bfloat16, float16 or float32 is required")
+    args = (C.addressof(cfg), n, *_table(logits, "logits", name, n, vocab),
+            *_table(draft_probs, "draft_probs", "float32", n, vocab), _i32(tokens, "tokens", n), _i32(parent, "parent", n),
+            _i32(cu_rows, "cu_rows", req + 1), _arg(temperature, "temperature", "float32", req),
+            _arg(uniform, "uniform", "float32", n), *_table(noise, "noise", "float32", req, vocab), _i32(path, "path", n),
+            _i32(accepted, "accepted", req), _i32(next_token, "next_token", req), _stream(stream))
+    _check(load().ivit_tree_verify(*args), None)
 
 
 # ------------------------------------------------------------ convenience

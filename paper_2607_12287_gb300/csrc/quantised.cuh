@@ -1,0 +1,50 @@
+// What the kernels of the 8-bit cache share: e4m3 codes, the layout and its check.
+#pragma once
+
+#include "backbone.cuh"
+
+namespace ivit {
+
+// Two codes (the low 16 bits) as fp16 values, which hold every e4m3 value exactly, and four of a word.
+__device__ __forceinline__ uint32_t codes_to_half2(uint16_t c) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(c));
+  return r;
+}
+__device__ __forceinline__ void codes_to_half4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  lo = codes_to_half2(static_cast<uint16_t>(w));
+  hi = codes_to_half2(static_cast<uint16_t>(w >> 16));
+}
+// Codes of two fp32 values, rounded to nearest even (beyond 448: 448; NaN stays NaN).
+__device__ __forceinline__ uint32_t to_codes2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// A paged cache of 8 bits of one layer (ivit_quantised_layout).
+struct QuantisedCache {
+  int n_pages, page_shift, block_shift, heads, dim;
+  long long page_stride, token_stride, head_stride;  // bytes
+
+  __device__ __forceinline__ bool holds(int slot) const { return slot >= 0 && (slot >> page_shift) < n_pages; }
+  __device__ __forceinline__ long long token(int slot) const {  // byte of head 0 of a slot
+    return (slot >> page_shift) * page_stride + (slot & ((1 << page_shift) - 1)) * token_stride;
+  }
+  // (blocks of a page follow each other, so a slot's block is slot >> block_shift)
+  __device__ __forceinline__ long long scale(int slot, int head) const {
+    return static_cast<long long>(slot >> block_shift) * heads + head;
+  }
+};
+
+inline bool valid_quantised(const ivit_quantised_layout& c) {
+  const ivit_cache_layout l = {c.n_pages, c.page_size, c.kv_heads, c.head_dim, c.dtype, 0, c.page_stride, c.token_stride, c.head_stride};
+  return valid_cache(l) && page_shift(c.block) >= 0 && c.block <= c.page_size;
+}
+
+inline QuantisedCache quantised(const ivit_quantised_layout& c) {
+  return {c.n_pages, page_shift(c.page_size), page_shift(c.block), c.kv_heads, c.head_dim, c.page_stride, c.token_stride,
+          c.head_stride};
+}
+
+}  // namespace ivit

@@ -30,7 +30,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "tree_attention.cuh"
+#include "tree_join.cuh"
 
 namespace ivit {
 namespace {
@@ -47,43 +47,6 @@ struct Keys64 {
   static constexpr int LEAST = 1;
   static __device__ __forceinline__ int tiles(const TreeRequest& r) { return (r.len + r.n + TK - 1) / TK; }
 };
-
-template <typename T>
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
-template <>
-__device__ __forceinline__ void mma<bf16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  mma_bf16_16816(d, a[0], a[1], a[2], a[3], b0, b1);
-}
-template <>
-__device__ __forceinline__ void mma<half>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr)
-               : "memory");
-}
-__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr)
-               : "memory");
-}
-
-// 16 bytes to shared memory, or zeros (nothing is read) if not `ok`.  Without an L2 policy: a build with one on these
-// copies faulted at heads of 256, and reading showed no cause that would spare the others (it was up to 8 % faster).
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool ok) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
 
 template <int DP, int RW>
 struct Cfg {
@@ -605,146 +568,8 @@ __global__ void __launch_bounds__(Cfg<DP, RW>::THREADS, Cfg<DP, RW>::CTAS) tree_
   }
 }
 
-// Joins the parts of a tile of rows that several runs have, in the order of their keys.  Blocks (i, y) take the
-// tile that CTA i's run begins or, where the call has few tiles (`search`), look for the i-th of them among the
-// runs' notes.  A thread has 4 columns of a row, an element of the parts.  Up to FEW parts, it reads four parts
-// at a time; more parts are shared by the warps of a block, 32 elements at a time, which meet in shared memory.
-// TC: the parts are the tcgen05 kernel's.
-template <typename T, int DP, int M, bool TC>
-__global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a, int ctas, bool search) {
-  constexpr int PART = tree_part_floats(M, DP), WARPS = 8, FEW = 16, NOTES = 4;
-  static_assert(NOTES * 256 >= 4 * TREE_MAX_SMS, "the notes of all CTAs");
-  __shared__ float2 ml_of[WARPS][32];
-  __shared__ float4 o_of[WARPS][32];
-  __shared__ int found[NOTES][WARPS], which;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if (tid == 0) which = -1;
-  pdl_wait();
-  // (Dependents start when the blocks end: launched earlier, the next call's CTAs that find no room beside these
-  // begin their equal shares late; 64 requests with heads of 64 took 65 us instead of 49.)
-  int c = blockIdx.x;
-  if (search) {
-    bool has[NOTES];
-    unsigned mine[NOTES];
-#pragma unroll
-    for (int k = 0; k < NOTES; ++k) has[k] = 256 * k + tid < ctas && a.joins[2 * (256 * k + tid)].x >= 0;
-#pragma unroll
-    for (int k = 0; k < NOTES; ++k) {
-      mine[k] = __ballot_sync(0xffffffffu, has[k]);
-      if (lane == 0) found[k][warp] = __popc(mine[k]);
-    }
-    __syncthreads();
-    int before = 0;
-#pragma unroll
-    for (int k = 0; k < NOTES; ++k) {
-      int rank = before + __popc(mine[k] & ((1u << lane) - 1));
-#pragma unroll
-      for (int w = 0; w < WARPS; ++w) {
-        if (w < warp) rank += found[k][w];
-        before += found[k][w];
-      }
-      if (has[k] && rank == static_cast<int>(blockIdx.x)) which = 256 * k + tid;
-    }
-    __syncthreads();
-    c = which;
-    if (c < 0) return;
-  }
-  const int4 note = a.joins[2 * c], rest = a.joins[2 * c + 1];
-  if (note.x < 0) return;
-  const int head = note.x, x0 = note.y, row0 = note.z, n = note.w >> 1, rows = rest.x;
-  // the tile's parts: CTA c's second or first, then the first ones of the head's CTAs behind it
-  const float* parts = a.parts + static_cast<size_t>(2 * c) * PART;
-  const auto part = [&](int i) { return parts + static_cast<size_t>(2 * i * a.cache.heads + (i == 0 ? note.w & 1 : 0)) * PART; };
-  const int elements = TC ? (rows + 7) / 8 * (2 * DP) : rows * (DP / 4);
-  const auto place = [&](int e, int& row, int& col) {  // columns 4 col .. 4 col + 3 of a row; whether it is one of the tile's
-    const int g = e / (TC ? 2 * DP : DP / 4), w = e - g * (TC ? 2 * DP : DP / 4);
-    row = TC ? 8 * g + (w & 7) : g;
-    col = TC ? w >> 3 : w;
-    return e < elements && row < rows;
-  };
-  // element e of parts i, i + step, i + 2 step, i + 3 step, into (m, l, o)
-  const auto add4 = [&](int i, int step, int e, int row, float& m, float& l, float4& o) {
-    float2 ml[4];
-    float4 x[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      ml[k] = make_float2(-INFINITY, 0.f);
-      x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (i + k * step < n) {
-        const float* p = part(i + k * step);
-        ml[k] = *reinterpret_cast<const float2*>(p + M * DP + 2 * row);
-        x[k] = reinterpret_cast<const float4*>(p)[e];
-      }
-    }
-    const float top = fmaxf(fmaxf(m, fmaxf(ml[0].x, ml[1].x)), fmaxf(ml[2].x, ml[3].x)), ref = top == -INFINITY ? 0.f : top;
-    const float f = ex2((m - ref) * a.scale_log2);
-    m = top;
-    l *= f;
-    o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (i + k * step < n) {
-        const float g = ex2((ml[k].x - ref) * a.scale_log2);
-        l += ml[k].y * g;
-        o = make_float4(o.x + x[k].x * g, o.y + x[k].y * g, o.z + x[k].z * g, o.w + x[k].w * g);
-      }
-  };
-  const auto write = [&](int row, int col, float m, float l, const float4& o) {
-    const int x = x0 + row, node = x / a.group, h = head * a.group + x - node * a.group;
-    const long long orow = row0 + node;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (4 * col < a.cache.dim)
-      *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * a.cache.dim + 4 * col) =
-          make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
-    if (a.lse && col == 0) a.lse[orow * a.heads + h] = (m * a.scale_log2 + (log2f(l) - TREE_SHIFT)) * 0.6931471805599453f;
-  };
-
-  if (n <= FEW) {
-    for (int e = blockIdx.y * 256 + tid; e < elements; e += gridDim.y * 256) {
-      int row, col;
-      if (!place(e, row, col)) continue;
-      float m = -INFINITY, l = 0.f;
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i = 0; i < n; i += 4) add4(i, 1, e, row, m, l, o);
-      write(row, col, m, l, o);
-    }
-    return;
-  }
-  for (int first = blockIdx.y * 32; first < elements; first += gridDim.y * 32) {
-    int row, col;
-    const bool has = place(first + lane, row, col);
-    float m = -INFINITY, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (has)
-      for (int i = warp; i < n; i += 4 * WARPS) add4(i, WARPS, first + lane, row, m, l, o);
-    ml_of[warp][lane] = make_float2(m, l);
-    o_of[warp][lane] = o;
-    __syncthreads();
-    if (warp == 0 && has) {
-#pragma unroll
-      for (int w = 1; w < WARPS; ++w) m = fmaxf(m, ml_of[w][lane].x);
-      const float ref = m == -INFINITY ? 0.f : m;
-      l = 0.f;
-      o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < WARPS; ++w) {
-        const float2 ml = ml_of[w][lane];
-        const float4 x = o_of[w][lane];
-        const float g = ex2((ml.x - ref) * a.scale_log2);
-        l += ml.y * g;
-        o = make_float4(o.x + x.x * g, o.y + x.y * g, o.z + x.z * g, o.w + x.w * g);
-      }
-      write(row, col, m, l, o);
-    }
-    __syncthreads();  // the sums are read before the next ones
-  }
-}
-
 bool valid(const ivit_attention_config& c, const ivit_cache_layout& l) {
-  return valid_cache(l) && c.n_req >= 1 && c.n_req <= TREE_MAX_REQ && c.heads >= 1 && c.heads <= 256 && c.heads % l.kv_heads == 0 &&
-         c.max_pages >= 1 && static_cast<long long>(c.max_pages) * l.page_size < (1LL << 31) - (1 << 20) && c.max_new >= 1 &&
-         c.max_new <= 65536 && c.mask_mode >= IVIT_MASK_CAUSAL && c.mask_mode <= IVIT_MASK_TREE && c.mask_words >= 0 &&
-         c.mask_words <= 32768 && (c.mask_mode != IVIT_MASK_TREE || c.mask_words > 0) && c.scale > 0.f && c.scale < 1e30f;
+  return valid_cache(l) && valid_attention(c, l.kv_heads, l.page_size);
 }
 
 // Which kernel, and its sizes: tiles of 16 * rw rows of mma.sync, or with tc the tcgen05 kernel's of up to 128.
@@ -794,15 +619,7 @@ cudaError_t launch_rows(const TreeArgs& a, int ctas, cudaStream_t s) {
 template <typename T, int DP>
 cudaError_t launch(const Plan& p, const TreeArgs& a, int dtype, int ctas, cudaStream_t s) {
   const auto join = [&](auto m, auto tc) {
-    // at most one joined tile per run and tile of rows; a thread for 4 columns of a row, up to some 16 blocks per SM
-    const long long most = static_cast<long long>(a.max_new) * a.group;  // rows that share a key head
-    const long long tiles = static_cast<long long>(a.n_req) * a.cache.heads * ((most + a.tile_rows - 1) / a.tile_rows);
-    const bool search = 4 * tiles < ctas;
-    const int x = search ? static_cast<int>(tiles) : ctas, rows = static_cast<int>(std::min<long long>(a.tile_rows, most));
-    const int elements = p.tc ? (rows + 7) / 8 * 2 * DP : rows * (DP / 4);
-    const int blocks = ctas > 8 * x ? (elements + 31) / 32 : (elements + 255) / 256;  // (many parts: 32 elements each)
-    const int y = std::max(1, std::min(blocks, 8 * ctas / x));
-    return launch_ex(tree_join_kernel<T, DP, decltype(m)::value, decltype(tc)::value>, dim3(x, y), dim3(256), 0, s, 1, a, ctas, search);
+    return launch_tree_join<T, DP, decltype(m)::value, decltype(tc)::value>(a, ctas, s);
   };
   cudaError_t e;
   if (p.tc) {

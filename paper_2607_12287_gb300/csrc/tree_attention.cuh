@@ -32,6 +32,50 @@ struct TreeArgs {
   float scale_log2;                 // scale * log2(e)
 };
 
+template <typename T>
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma<bf16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  mma_bf16_16816(d, a[0], a[1], a[2], a[3], b0, b1);
+}
+template <>
+__device__ __forceinline__ void mma<half>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+
+// 16 bytes to shared memory, or zeros (nothing is read) if not `ok`.  Without an L2 policy: a build with one on these
+// copies faulted at heads of 256, and reading showed no cause that would spare the others (it was up to 8 % faster).
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+inline bool valid_attention(const ivit_attention_config& c, int kv_heads, int page_size) {
+  return c.n_req >= 1 && c.n_req <= TREE_MAX_REQ && c.heads >= 1 && c.heads <= 256 && c.heads % kv_heads == 0 &&
+         c.max_pages >= 1 && static_cast<long long>(c.max_pages) * page_size < (1LL << 31) - (1 << 20) && c.max_new >= 1 &&
+         c.max_new <= 65536 && c.mask_mode >= IVIT_MASK_CAUSAL && c.mask_mode <= IVIT_MASK_TREE && c.mask_words >= 0 &&
+         c.mask_words <= 32768 && (c.mask_mode != IVIT_MASK_TREE || c.mask_words > 0) && c.scale > 0.f && c.scale < 1e30f;
+}
+
 // Floats of a part in the workspace: output [m][dp] (of the tcgen05 kernel [m / 8][dp / 4][8][4]), then running maximum
 // and sum of each row.
 __host__ __device__ constexpr int tree_part_floats(int m, int dp) { return m * (dp + 2); }

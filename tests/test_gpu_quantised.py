@@ -1,0 +1,751 @@
+"""GPU parity of the 8-bit cache's operators and of the verification of drafts against their 64-bit restatement.
+
+Writes are equal, code by code and scale by scale (powers of two make every step but the last rounding exact).  Reads: one
+rounding, u |x| with u half a unit in the last place (2^-8 bf16, 2^-11 fp16; 2^-25 below fp16's normal range).  Attention,
+per value: u |o| for the rounding, u sum p |v| / sum p for probabilities of 16 bits, and 2^-14 of the same for fp32 scores
+(|s| < 2^6, each a sum of at most 256 products) in the exponent; lse 2^-14.  Verification: equal, where no decision is nearer than
+2^-16 to its border (fp32 sums of up to 2^17 exponentials, in trees, and products of a few roundings; exponentials of
+arguments up to 2^6).
+"""
+import numpy as np
+import pytest
+
+from tests import backbone_ref, quantised_ref as ref
+from tests.test_gpu_backbone import dev, host, i32, trees
+
+pytestmark = pytest.mark.gpu
+
+UNIT = backbone_ref.UNIT
+
+
+@pytest.fixture(scope="module")
+def pkg():
+    import paper_2607_12287_gb300 as p
+    p.load()
+    return p
+
+
+def codes_on_gpu(codes, order="token"):
+    """uint8 codes [..., page, heads, dim] as a float8 tensor, whose heads lie in front of the tokens in memory if order is "head"."""
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(codes)).cuda()
+    if order == "head":
+        t = t.transpose(-3, -2).contiguous().transpose(-3, -2)
+    return t.view(torch.float8_e4m3fn)
+
+
+def codes_of(t):
+    import torch
+    return t.view(torch.uint8).cpu().numpy()
+
+
+def random_cache(r, lead, page, kv, dim, block, spread=(-9, -4)):
+    """Codes and scales as writing leaves them."""
+    codes = ref.encode(np.clip(r.standard_normal((*lead, page, kv, dim)) * 90, -448, 448))
+    return codes, 2.0 ** r.integers(spread[0], spread[1], (*lead, page // block, kv)).astype(np.float32)
+
+
+# ---------------------------------------------------------------- writing, reading
+
+WRITES = [  # layers, requests' (cached, new) tokens, heads, dim, page, block, type, order
+    (1, [(0, 1)], 1, 8, 1, 1, "bfloat16", "token"), (27, [(5, 1), (16, 1), (31, 1)], 4, 64, 16, 16, "bfloat16", "token"),
+    (2, [(0, 70), (3, 13), (40, 25)], 2, 72, 8, 4, "float16", "head"), (3, [(7, 100)], 3, 256, 64, 32, "bfloat16", "token"),
+    (2, [(1, 3), (2, 1), (3, 5), (15, 2)], 8, 128, 16, 8, "float16", "token"), (1, [(600, 1300)], 2, 40, 1024, 1024, "bfloat16", "token"),
+    (2, [(0, 33)], 5, 104, 32, 1, "bfloat16", "head"), (1, [(9, 200), (100, 300)], 1, 16, 128, 128, "float16", "token"),
+    (6, [(3 * i, 1 + i % 6) for i in range(60)], 8, 80, 32, 16, "bfloat16", "token"),
+]
+
+
+def write_case(r, layers, requests, kv, dim, page, block, dtype, order):
+    slots, used, pages = [], 0, sum(-(-(b + n) // page) for b, n in requests) + 2
+    ids = r.permutation(pages)
+    for b, n in requests:
+        t = np.arange(b, b + n)
+        slots.append(ids[used + t // page] * page + t % page)
+        used += -(-(b + n) // page)
+    slots = np.concatenate(slots)
+    n = len(slots)
+    drafts = n + 4
+    src = dev(r.standard_normal((layers, drafts, 2 * kv * dim)).astype(np.float32)
+              * 2.0 ** r.integers(-6, 7, (layers, drafts, 1)).astype(np.float32), dtype)
+    k, v = src[..., :kv * dim].unflatten(2, (kv, dim)), src[..., kv * dim:].unflatten(2, (kv, dim))
+    rows = r.permutation(drafts)[:n]
+    caches = [random_cache(r, (layers, pages), page, kv, dim, block) for _ in range(2)]
+    return k, v, rows, slots, caches
+
+
+def check_write(pkg, k, v, rows, slots, caches, block, dtype, order, repeat=2):
+    import torch
+    layers, pages, page = caches[0][0].shape[:3]
+    kc, vc = (codes_on_gpu(c, order) for c, _ in caches)
+    ks, vs = (dev(s) for _, s in caches)
+    lay = pkg.make_quantised_layout(kc[0], block, dtype)
+    ok = (rows >= 0) & (rows < k.shape[1])
+    want = []
+    for x, (c, s) in zip((k, v), caches):
+        c, s, x = c.copy(), s.copy(), host(x)
+        for layer in range(layers):
+            ref.quantise(c[layer], s[layer], [x[layer, i] if o else None for i, o in zip(rows, ok)], slots, block)
+        want.append((c, s))
+    for _ in range(repeat):
+        pkg.ivit_kv_quantise(lay, k, v, i32(rows), i32(slots), kc, vc, ks, vs)
+        for (c, s), got_c, got_s in zip(want, (kc, vc), (ks, vs)):
+            assert np.array_equal(host(got_s), s, equal_nan=True)  # (NaN: blocks that were not written)
+            assert np.array_equal(codes_of(got_c), c)
+    return kc, vc, ks, vs, lay
+
+
+@pytest.mark.parametrize("layers,requests,kv,dim,page,block,dtype,order", WRITES)
+def test_kv_quantise(pkg, layers, requests, kv, dim, page, block, dtype, order):
+    r = np.random.default_rng(dim + len(requests))
+    k, v, rows, slots, caches = write_case(r, layers, requests, kv, dim, page, block, dtype, order)
+    if len(rows) > 6:  # entries that are skipped
+        rows[1], slots[3], rows[4] = -1, -1, k.shape[1]
+        slots[-1] = caches[0][0].shape[1] * page
+    check_write(pkg, k, v, rows, slots, caches, block, dtype, order)
+
+
+def test_a_block_grows_token_by_token(pkg):
+    # every call adds a token to the block: its scale follows the largest so far, the codes are rounded again
+    import torch
+    r = np.random.default_rng(1)
+    page = block = 16
+    codes, scale = (np.full((1, 3, page, 2, 64), 0x55, np.uint8), np.full((1, 3, 1, 2), 2.0 ** 30, np.float32))
+    kc, vc, ks, vs = codes_on_gpu(codes), codes_on_gpu(codes), dev(scale), dev(scale)
+    want = [(codes.copy(), scale.copy()), (codes.copy(), scale.copy())]
+    lay = pkg.make_quantised_layout(kc[0], block)
+    for t in range(2 * page):
+        slot = (2 * page if t < page else 0) + t % page
+        x = dev((r.standard_normal((2, 1, 1, 2, 64)) * 2.0 ** r.integers(-20, 20)).astype(np.float32), "bfloat16")
+        pkg.ivit_kv_quantise(lay, x[0], x[1], i32([0]), i32([slot]), kc, vc, ks, vs)
+        for part, (c, s) in zip(host(x), want):
+            ref.quantise(c[0], s[0], [part[0, 0]], [slot], block)
+        for (c, s), got_c, got_s in zip(want, (kc, vc), (ks, vs)):
+            assert np.array_equal(host(got_s), s) and np.array_equal(codes_of(got_c), c), t
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_values_at_the_ends(pkg, dtype):
+    # zeros, the smallest and largest values, values next to a scale's border, and such that are not finite
+    import torch
+    tiny, huge = (2.0 ** -133, 3.3e38) if dtype == "bfloat16" else (2.0 ** -24, 65504.0)
+    rows = np.zeros((1, 9, 2, 16))
+    rows[0, 1] = tiny
+    rows[0, 2, 0, 3] = huge
+    rows[0, 3, 1, :4] = [448, 449, -448, 2.0 ** -9]
+    rows[0, 4, 0, :4] = [450, 1, 2.0 ** -5, -0.0]
+    rows[0, 5, 0, :4] = [np.inf, 1, -np.inf, np.nan]
+    rows[0, 6] = np.nan
+    rows[0, 7, 1] = np.linspace(-448, 448, 16)
+    rows[0, 8, 0] = 2.0 ** np.arange(-10, 6)
+    k = dev(rows.astype(np.float32), dtype)
+    caches = [(np.zeros((1, 4, 4, 2, 16), np.uint8), np.full((1, 4, 4, 2), np.nan, np.float32)) for _ in range(2)]
+    check_write(pkg, k, k, np.arange(9), np.arange(9), caches, 1, dtype, "token")
+    # blocks whose old scale is of no use
+    for bad in (np.nan, 0.0, np.inf, -1.0):
+        caches = [(np.full((1, 1, 4, 2, 16), 0x22, np.uint8), np.full((1, 1, 1, 2), bad, np.float32)) for _ in range(2)]
+        check_write(pkg, k, k, np.array([8]), np.array([2]), caches, 4, dtype, "token")
+
+
+def test_old_scales_that_are_no_powers_of_two(pkg):
+    r = np.random.default_rng(3)
+    caches = [(ref.encode(r.standard_normal((1, 2, 8, 2, 32)) * 90), (1.37 * 2.0 ** r.integers(-9, -5, (1, 2, 1, 2))).astype(np.float32))
+              for _ in range(2)]
+    k = dev((r.standard_normal((1, 2, 2, 32)) * 0.05).astype(np.float32), "float16")
+    check_write(pkg, k, k, np.array([0, 1]), np.array([5, 14]), caches, 8, "float16", "token")
+
+
+@pytest.mark.parametrize("layers,n,kv,dim,page,block,dtype,order", [
+    (1, 1, 1, 8, 1, 1, "bfloat16", "token"), (27, 5, 4, 64, 16, 16, "bfloat16", "token"), (3, 70, 2, 72, 8, 2, "float16", "head"),
+    (2, 333, 8, 256, 64, 32, "bfloat16", "head"), (1, 40, 3, 104, 128, 128, "float16", "token"),
+])
+def test_kv_dequantise(pkg, layers, n, kv, dim, page, block, dtype, order):
+    import torch
+    r = np.random.default_rng(n)
+    pages = -(-n // page) + 2
+    caches = [random_cache(r, (layers, pages), page, kv, dim, block, (-20, 7)) for _ in range(2)]
+    caches[0][0][0, 0, 0, 0, 0] = 0x7f
+    slots = r.permutation(pages * page)[:n]
+    slots[0] = 0
+    if n > 4:
+        slots[1], slots[2] = -1, pages * page
+    ok = (slots >= 0) & (slots < pages * page)
+    kc, vc = (codes_on_gpu(c, order) for c, _ in caches)
+    # rows of a wider array
+    out = torch.full((layers, n, 2, kv, dim), 3.0, dtype=getattr(torch, dtype), device="cuda")
+    k, v = out[:, :, 0], out[:, :, 1]
+    pkg.ivit_kv_dequantise(pkg.make_quantised_layout(kc[0], block, dtype), i32(slots), kc, vc, *(dev(s) for _, s in caches), k, v)
+    for got, (c, s) in zip((k, v), caches):
+        got = host(got)
+        assert (got[:, ~ok] == 3).all()
+        for layer in range(layers):
+            want = ref.decode(c[layer], s[layer], block).reshape(pages * page, kv, dim)[slots[ok]]
+            nan = np.isnan(want)
+            assert np.array_equal(np.isnan(got[layer, ok]), nan)
+            assert (np.abs(got[layer, ok] - want)[~nan] <= UNIT[dtype] * np.abs(want)[~nan] + 2.0 ** -25 * (dtype == "float16")).all()
+
+
+# ------------------------------------------------------------------------ attention
+
+def attention_case(r, lengths, new, heads, kv, dim, page, block, dtype, order="token", spread=(-9, -5)):
+    n, rows = len(lengths), int(np.sum(new))
+    need = [-(-int(x) // page) for x in lengths]
+    pages = sum(need) + 3
+    ids, used = r.permutation(pages), 0
+    table = np.full((n, max(need + [0]) + 2), -1, np.int64)
+    for i, m in enumerate(need):
+        table[i, :m] = ids[used:used + m]
+        used += m
+    caches = [random_cache(r, (pages,), page, kv, dim, block, spread) for _ in range(2)]
+    # (what lies in the pages past a request's tokens must not matter, nor the scales of blocks that hold none)
+    for i, m in enumerate(lengths):
+        if m % page:
+            for c, s in caches:
+                c[table[i, m // page], m % page:] = 0x7f
+                s[table[i, m // page], -(-(m % page) // block):] = np.nan
+    qkv = dev(r.standard_normal((rows, (heads + 2 * kv) * dim)).astype(np.float32), dtype)
+    part = lambda lo, m: qkv[:, lo * dim:(lo + m) * dim].unflatten(1, (m, dim))
+    return dict(q=part(0, heads), k=part(heads, kv), v=part(heads + kv, kv), caches=caches, table=table, block=block, order=order,
+                lengths=np.asarray(lengths), cu=np.concatenate([[0], np.cumsum(new)]).astype(np.int64), dtype=dtype)
+
+
+def call(pkg, c, mask, packed=None, words=0, scale=None, max_new=None, fill=float("nan")):
+    """The call's arguments on the GPU: configuration, layout, and what follows."""
+    import torch
+    rows, heads, dim = c["q"].shape
+    most = int(np.diff(c["cu"]).max()) if max_new is None else max_new
+    kc, vc = (codes_on_gpu(codes, c["order"]) for codes, _ in c["caches"])
+    lay = pkg.make_quantised_layout(kc, c["block"], c["dtype"])
+    cfg = pkg.make_attention_config(len(c["cu"]) - 1, heads, c["table"].shape[1], most, mask, words, dim ** -0.5 if scale is None else scale)
+    out = torch.full((rows, heads, dim), fill, dtype=c["q"].dtype, device="cuda")
+    lse = torch.full((rows, heads), fill, device="cuda")
+    ws = torch.full((pkg.ivit_tree_attention_quantised_workspace(cfg, lay),), 255, dtype=torch.uint8, device="cuda")
+    return [cfg, lay, c["q"], c["k"], c["v"], kc, vc, *(dev(s) for _, s in c["caches"]), i32(c["table"]), i32(c["lengths"]),
+            i32(c["cu"]), packed, out, lse, ws]
+
+
+def run_attention(pkg, c, mask, vis=None, check=True, scale=None, max_new=None, mask_words=None):
+    import torch
+    new = np.diff(c["cu"])
+    words = (int(new.max()) + 31) // 32 if mask_words is None else mask_words
+    packed = dev(np.concatenate([backbone_ref.words(vis[i], words) for i in range(len(new))])) if mask == "tree" else None
+    args = call(pkg, c, mask, packed, words if mask == "tree" else 0, scale, max_new)
+    pkg.ivit_tree_attention_quantised(*args)
+    out, lse, ws = args[-3:]
+    assert int(ws[:4].view(torch.int32)) == 0  # no wait of the kernel expired
+    if not check:
+        return out, lse
+    sees = {"causal": lambda i, n: np.tril(np.ones((n, n), bool)), "all": lambda i, n: np.ones((n, n), bool),
+            "tree": lambda i, n: vis[i]}[mask]
+    kc, vc = (ref.decode(codes, s, c["block"]) for codes, s in c["caches"])
+    want, want_lse, size = backbone_ref.attention(host(c["q"]), host(c["k"]), host(c["v"]), kc, vc, c["table"], c["lengths"], c["cu"],
+                                                  sees, args[0].scale)
+    u = UNIT[c["dtype"]]
+    bound = u * np.abs(want) + (u + 2.0 ** -14) * size + 2.0 ** -25
+    err = np.abs(host(out) - want)
+    assert (err <= bound).all(), f"{np.nanmax(err / bound)} of the bound, {np.isnan(host(out)).sum()} NaN"
+    got, none = host(lse), np.isneginf(want_lse)
+    assert np.array_equal(np.isneginf(got), none)
+    assert (np.abs(got[~none] - want_lse[~none]) <= 2.0 ** -14).all()
+    return out, lse
+
+
+ATTENTION = [  # cached, new, heads, kv, dim, page, block, type, order
+    ([0], [1], 4, 4, 64, 16, 16, "bfloat16", "token"), ([1], [1], 8, 2, 64, 16, 4, "float16", "token"),
+    ([63], [1], 1, 1, 64, 8, 8, "bfloat16", "token"), ([64], [1], 16, 4, 128, 16, 16, "bfloat16", "head"),
+    ([130, 0, 65, 700], [1, 3, 0, 9], 8, 2, 72, 16, 8, "bfloat16", "token"),
+    ([5, 64, 127, 128, 129], [2, 1, 64, 63, 65], 4, 2, 80, 1, 1, "float16", "head"),
+    ([1500], [31], 8, 1, 128, 64, 32, "float16", "token"), ([40, 900, 33], [12, 1, 40], 14, 2, 96, 32, 32, "bfloat16", "token"),
+    ([100, 300], [17, 5], 5, 1, 256, 128, 64, "float16", "head"), ([257], [3], 2, 2, 256, 16, 2, "bfloat16", "token"),
+    ([90, 10], [70, 130], 3, 3, 40, 16, 16, "bfloat16", "token"), ([2000, 3, 777], [4, 4, 4], 8, 8, 8, 1024, 1024, "float16", "token"),
+    ([33], [7], 32, 1, 200, 4, 2, "bfloat16", "head"), ([31, 500], [1, 1], 6, 3, 104, 2, 1, "float16", "token"),
+    # many rows per key head, groups that do not divide a tile
+    ([300, 95, 96, 97, 0], [65, 96, 20, 1, 130], 8, 4, 72, 8, 8, "bfloat16", "token"),
+    ([191, 192, 500], [128, 33, 97], 5, 1, 80, 128, 16, "float16", "head"), ([700], [256], 2, 2, 64, 64, 64, "bfloat16", "token"),
+    ([0, 0, 127, 128, 129], [140, 3, 128, 129, 70], 2, 2, 64, 16, 1, "float16", "token"),
+    ([0, 64, 200], [75, 64, 1], 7, 1, 128, 16, 16, "bfloat16", "token"), ([500], [65], 6, 2, 112, 256, 128, "bfloat16", "head"),
+    ([300, 96], [50, 129], 2, 2, 88, 16, 8, "bfloat16", "head"), ([63, 64, 65, 500], [40, 1, 64, 20], 5, 1, 136, 16, 16, "bfloat16", "token"),
+    ([200, 0], [130, 17], 2, 2, 192, 32, 16, "float16", "head"), ([300, 128, 1], [129, 256, 9], 4, 2, 256, 8, 4, "bfloat16", "token"),
+    ([900], [20], 32, 2, 256, 512, 32, "bfloat16", "head"), ([129], [100], 1, 1, 200, 4, 4, "bfloat16", "token"),
+    ([70, 0, 130], [50, 3, 1], 1, 1, 128, 2, 2, "float16", "token"), ([300, 40], [40, 17], 1, 1, 96, 1, 1, "float16", "head"),
+    ([200, 10], [2, 1], 150, 1, 64, 16, 16, "bfloat16", "token"),
+]
+
+
+@pytest.mark.parametrize("lengths,new,heads,kv,dim,page,block,dtype,order", ATTENTION)
+@pytest.mark.parametrize("mask", ["causal", "all", "tree"])
+def test_tree_attention_quantised(pkg, lengths, new, heads, kv, dim, page, block, dtype, order, mask):
+    r = np.random.default_rng(sum(lengths) + sum(new) + dim)
+    c = attention_case(r, lengths, new, heads, kv, dim, page, block, dtype, order)
+    run_attention(pkg, c, mask, trees(r, new) if mask == "tree" else None)
+
+
+@pytest.mark.parametrize("dim,most_new,n", [(64, 2, 700), (72, 2, 700), (40, 2, 700), (96, 2, 500), (256, 2, 300), (72, 20, 200),
+                                            (96, 70, 40), (256, 20, 150)])
+def test_many_short_requests(pkg, dim, most_new, n):
+    # every CTA goes through several tiles of rows
+    r = np.random.default_rng(2)
+    c = attention_case(r, r.integers(0, 90, n), r.integers(0, most_new + 1, n), 6, 3, dim, 8, 4, "bfloat16")
+    run_attention(pkg, c, "causal")
+
+
+@pytest.mark.parametrize("new", [2, 40])
+def test_scales_far_apart(pkg, new):
+    # blocks of values from 2^-50 to 2^20, in an order that makes the running maximum grow and others vanish; keys a little
+    r = np.random.default_rng(5)
+    c = attention_case(r, [600], [new], 4, 2, 64, 16, 4, "bfloat16")
+    (kc, ks), (vc, vs) = c["caches"]
+    vs[:] = 2.0 ** r.integers(-50, 21, vs.shape).astype(np.float32)
+    run_attention(pkg, c, "causal")
+    vs[:] = 2.0 ** -60                 # alone, and beside new rows of ordinary size
+    run_attention(pkg, c, "causal")
+    vs[:] = 1.7 * 2.0 ** r.integers(-9, -5, vs.shape).astype(np.float32)  # not ivit_kv_quantise's
+    ks[:] = 1.3 * 2.0 ** r.integers(-9, -5, ks.shape).astype(np.float32)
+    run_attention(pkg, c, "causal")
+
+
+@pytest.mark.parametrize("new", [1, 30])
+def test_queries_of_every_size(pkg, new):
+    # bf16 queries beyond fp16's range, and tiny ones
+    r = np.random.default_rng(8)
+    for power in (-60, -30, 20, 60):
+        c = attention_case(r, [300], [new], 4, 2, 72, 16, 16, "bfloat16")
+        c["q"] = (c["q"].float() * 2.0 ** power).bfloat16()
+        c["k"] = (c["k"].float() * 0).bfloat16()  # (the new rows' scores stay small)
+        run_attention(pkg, c, "causal", scale=0.1 * 2.0 ** -power)
+    c = attention_case(r, [100], [new], 4, 2, 64, 16, 16, "bfloat16")
+    c["q"] = c["q"] * 0
+    run_attention(pkg, c, "all")
+
+
+def test_rows_that_see_nothing(pkg):
+    r = np.random.default_rng(4)
+    new = [5, 40, 3]
+    vis = [np.zeros((n, n), bool) for n in new]
+    vis[1][7, 3] = vis[1][39, 0] = vis[1][39, 39] = True
+    for lengths in ([0, 0, 0], [0, 0, 90]):
+        c = attention_case(r, lengths, new, 4, 2, 64, 16, 8, "bfloat16")
+        out, lse = run_attention(pkg, c, "tree", vis)
+        assert float(out[:5].abs().max()) == 0 and float(lse[:5].max()) == -np.inf
+
+
+@pytest.mark.parametrize("new,page,dim", [(4, 16, 64), (20, 16, 64), (100, 16, 64), (4, 4, 64), (20, 4, 72), (100, 4, 64), (4, 16, 256),
+                                          (30, 16, 256), (60, 8, 128), (90, 8, 80), (70, 8, 192), (50, 16, 96)])
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_what_a_row_does_not_see_does_not_reach_it(pkg, new, page, dim, dtype, bad):
+    import torch
+    r = np.random.default_rng(new)
+    c = attention_case(r, [70], [new], 4, 2, dim, page, page, dtype)
+    vis = [np.tril(np.ones((new, new), bool))]
+    vis[0][:, 2] = False
+    vis[0][new - 1, 2] = True          # only the last row sees draft 2
+    clean, clean_lse = run_attention(pkg, c, "tree", vis)
+    c["v"][2, 1, 5] = bad              # one value of one head
+    out, lse = run_attention(pkg, c, "tree", vis, check=False)
+    assert torch.equal(lse, clean_lse)
+    others = torch.ones(new, 4, dim, dtype=torch.bool)
+    others[new - 1, 2:, 5] = False     # (query heads 2 and 3 read key head 1)
+    assert torch.equal(out.cpu()[others], clean.cpu()[others])
+    hit = out[new - 1, 2:, 5].float().cpu().numpy()
+    assert np.isnan(hit).all() if np.isnan(bad) else np.array_equal(hit, [bad, bad])
+    # a key that no other row sees
+    c["v"][2, 1, 5] = 0.5
+    c["k"][2] = bad
+    out, lse = run_attention(pkg, c, "tree", vis, check=False)
+    assert torch.equal(out[:new - 1], clean[:new - 1]) and torch.equal(lse[:new - 1], clean_lse[:new - 1])
+
+
+def test_cached_codes_that_are_no_numbers(pkg):
+    # a value that could not be kept (NaN) reaches its column of every row that sees it, and no other head or request
+    r = np.random.default_rng(9)
+    for new in (1, 33):
+        c = attention_case(r, [80, 50], [new, new], 4, 2, 64, 16, 8, "bfloat16")
+        c["caches"][1][0][c["table"][0, 2], 3, 1, 7] = 0x7f
+        out, lse = run_attention(pkg, c, "causal", check=False)
+        bad = np.isnan(host(out))
+        assert bad[:new, 2:, 7].all() and bad.sum() == 2 * new and np.isfinite(host(lse)).all()
+
+
+def test_pages_outside_the_cache_read_as_zeros(pkg):
+    r = np.random.default_rng(12)
+    for new in (2, 50):
+        for page in (4, 16):
+            c = attention_case(r, [100], [new], 4, 2, 64, page, page, "bfloat16")
+            c["table"][0, 1] = -1
+            c["table"][0, 3] = 1 << 30
+            out, lse = run_attention(pkg, c, "causal", check=False)
+            zero = dict(c, caches=[(codes.copy(), s.copy()) for codes, s in c["caches"]])
+            table = c["table"].copy()
+            free = [p for p in range(zero["caches"][0][0].shape[0]) if p not in table][0]
+            for codes, s in zero["caches"]:  # (a page of zeros, which no request has, in the place of both)
+                codes[free], s[free] = 0, 1
+            table[0, 1] = table[0, 3] = free
+            zero["table"] = table
+            want, want_lse = run_attention(pkg, zero, "causal")
+            assert (np.abs(host(out) - host(want)) <= 2.0 ** -7 * np.abs(host(want)) + 2.0 ** -12).all()
+            assert (np.abs(host(lse) - host(want_lse)) <= 2.0 ** -13).all()
+
+
+def test_large_scores_and_growing_maximum(pkg):
+    # scores up to a few hundred that grow along the keys: the running maximum moves in every tile
+    r = np.random.default_rng(6)
+    c = attention_case(r, [1000, 640], [2, 33], 4, 1, 64, 16, 8, "float16", spread=(-7, -6))
+    codes, scale = c["caches"][0]
+    q = host(c["q"])[0, 0]
+    t = np.arange(1000)
+    codes[c["table"][0][t // 16], t % 16, 0] = ref.encode(q * np.linspace(0.3, 120.0, 1000)[:, None])
+    run_attention(pkg, c, "causal", scale=0.125)
+
+
+@pytest.mark.parametrize("group", [1, 8])
+def test_offsets_past_32_bits(pkg, group):
+    # pages at the far end of a cache of more than 2^32 codes
+    import torch
+    page, kv, dim, block = 16, 8, 128, 8
+    pages = (1 << 32) // (page * kv * dim) + 64
+    r = np.random.default_rng(7)
+    if torch.cuda.mem_get_info()[0] < 3 * pages * page * kv * dim:
+        pytest.skip("needs 13 GB of device memory")
+    c = attention_case(r, [300], [3], 8 * group, 8, dim, page, block, "bfloat16")
+    want, want_lse = run_attention(pkg, c, "causal")
+    args = call(pkg, c, "causal")
+    big = torch.empty((pages, page, kv, dim), dtype=torch.uint8, device="cuda")
+    scales = [torch.empty((pages, page // block, kv), device="cuda") for _ in range(2)]
+    n = c["caches"][0][0].shape[0]
+    far = (pages - 1 - np.arange(n)).astype(np.int64)  # keys in the last pages, values of the same pages 2 n lower
+    fi = torch.from_numpy(far).cuda()
+    big[fi], big[fi - 2 * n] = args[5].view(torch.uint8), args[6].view(torch.uint8)
+    # (the array of keys begins 2 n pages into the one of values; a table entry is a page of both)
+    ids = np.where(c["table"] >= 0, far[np.maximum(c["table"], 0)] - 2 * n, -1)
+    f8 = big.view(torch.float8_e4m3fn)
+    keys, values = f8[2 * n:], f8[:pages - 2 * n]
+    lay = pkg.make_quantised_layout(keys, block, "bfloat16")
+    ks, vs = (s[:pages - 2 * n].contiguous() for s in scales)
+    ks[fi - 2 * n], vs[fi - 2 * n] = args[7], args[8]
+    args[1], args[5], args[6], args[7], args[8], args[9] = lay, keys, values, ks, vs, i32(ids)
+    pkg.ivit_tree_attention_quantised(*args)
+    assert torch.equal(args[-3], want) and torch.equal(args[-2], want_lse)
+    # and a write and a read there
+    src = torch.randn((1, 2, kv, dim), device="cuda").to(torch.bfloat16)
+    lay = pkg.make_quantised_layout(f8, block, "bfloat16")
+    slots = i32([pages * page - 1, pages * page - 16])
+    for s in scales:
+        s[-1] = 2.0 ** -9
+    pkg.ivit_kv_quantise(lay, src, src, i32([1, 0]), slots, f8[None], f8[None], scales[0][None], scales[1][None])
+    back = torch.zeros_like(src)
+    pkg.ivit_kv_dequantise(lay, slots, f8[None], f8[None], scales[0][None], scales[1][None], back, back.clone())
+    # (half a step of e4m3, and below 2^-6 of the scale 2^-10)
+    assert ((back.float() - src[:, [1, 0]].float()).abs() <= 2.0 ** -4 * src[:, [1, 0]].float().abs() + 2.0 ** -16).all()
+
+
+def test_rows_of_no_request_stay(pkg):
+    import torch
+    r = np.random.default_rng(13)
+    for new in (2, 40):
+        c = attention_case(r, [30, 70], [new, new + 1], 4, 2, 64, 16, 16, "bfloat16")
+        want, want_lse = run_attention(pkg, c, "causal")
+        pad = lambda t: torch.cat([t, t[:3] * float("nan")])
+        padded = dict(c, q=pad(c["q"]), k=pad(c["k"]), v=pad(c["v"]))
+        args = call(pkg, padded, "causal", fill=7.0)
+        pkg.ivit_tree_attention_quantised(*args)
+        n = want.shape[0]
+        assert torch.equal(args[-3][:n], want) and torch.equal(args[-2][:n], want_lse)
+        assert (args[-3][n:] == 7).all() and (args[-2][n:] == 7).all()
+
+
+def test_on_another_stream_and_in_a_graph(pkg):
+    import torch
+    r = np.random.default_rng(10)
+    for new in ([1, 6], [40, 3]):
+        c = attention_case(r, [500, 20], new, 8, 2, 64, 16, 16, "bfloat16")
+        want, want_lse = run_attention(pkg, c, "causal")
+        args = call(pkg, c, "causal")
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            pkg.ivit_tree_attention_quantised(*args)
+        side.synchronize()
+        assert torch.equal(args[-3], want) and torch.equal(args[-2], want_lse)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            pkg.ivit_tree_attention_quantised(*args)
+        for _ in range(3):
+            args[-3].zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(args[-3], want) and torch.equal(args[-2], want_lse)
+
+
+# --------------------------------------------------------------------- verification
+
+def verify_case(r, new, vocab, tree, probs, dtype, temperature, peaked=3.0):
+    n, rows = len(new), int(np.sum(new))
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int64)
+    idx = np.concatenate([np.arange(m) for m in new] + [np.zeros(0, np.int64)]).astype(np.int64)
+    parent = idx - 1 - (np.floor(r.random(rows) * np.minimum(idx, 4)).astype(np.int64) if tree else 0)
+    parent[idx == 0] = -1
+    logits = dev((peaked * r.standard_normal((rows, vocab))).astype(np.float32), dtype)
+    z = host(logits) + 0.5 * r.standard_normal((rows, vocab))
+    p = np.exp(z - z.max(1, keepdims=True)) if rows else z
+    p = (p / p.sum(1, keepdims=True)).astype(np.float32) if rows else z.astype(np.float32)
+    tokens = np.zeros(rows, np.int64)
+    for i in range(rows):
+        if parent[i] >= 0:
+            a = i - idx[i] + parent[i]
+            tokens[i] = (p[a] / r.exponential(size=vocab)).argmax() if probs or r.random() < 0.3 else z[a].argmax()
+    t = None if temperature is None else np.broadcast_to(np.float32(temperature), (n,)).copy()
+    return dict(logits=logits, probs=p if probs else None, tokens=tokens, parent=parent if tree else None, cu=cu, temperature=t,
+                uniform=r.random(rows).astype(np.float32), noise=r.exponential(size=(n, vocab)).astype(np.float32), dtype=dtype)
+
+
+def run_verify(pkg, c, max_new=None, fill=77, check=True, least=0.95):
+    import torch
+    n, vocab, rows = len(c["cu"]) - 1, c["logits"].shape[1], c["logits"].shape[0]
+    most = max(1, int(np.diff(c["cu"]).max())) if max_new is None else max_new
+    opt = lambda a: None if a is None else a if torch.is_tensor(a) else dev(a)
+    path, accepted, after = (torch.full((m,), fill, dtype=torch.int32, device="cuda") for m in (rows, n, n))
+    cfg = pkg.make_verify_config(n, vocab, most, c["dtype"])
+    none = c["temperature"] is None
+    pkg.ivit_tree_verify(cfg, c["logits"], opt(c["probs"]), i32(c["tokens"]), None if c["parent"] is None else i32(c["parent"]),
+                         i32(c["cu"]), opt(c["temperature"]), None if none else opt(c["uniform"]), None if none else opt(c["noise"]),
+                         path, accepted, after)
+    got = [host(x).astype(np.int64) for x in (path, accepted, after)]
+    if check:
+        probs = None if c["probs"] is None else host(opt(c["probs"]))
+        noise = None if c["noise"] is None else host(opt(c["noise"]))
+        *want, margin = ref.verify(host(c["logits"]), probs, c["tokens"], c["parent"], c["cu"], c["temperature"], c["uniform"], noise, most)
+        sure = margin > 2.0 ** -16
+        assert sure.mean() >= least
+        for i in np.nonzero(sure)[0]:
+            lo, hi = c["cu"][i], c["cu"][i + 1]
+            assert np.array_equal(got[0][lo:hi], want[0][lo:hi]) and got[1][i] == want[1][i] and got[2][i] == want[2][i], i
+        assert (got[0][c["cu"][-1]:] == fill).all()
+    return got
+
+
+@pytest.mark.parametrize("new,vocab,tree,probs,dtype", [
+    ([1], 1, False, False, "float32"), ([5], 1000, False, False, "bfloat16"), ([4, 0, 7, 1], 33, True, True, "float16"),
+    ([16] * 20, 5001, True, True, "float32"), ([8] * 30, 777, True, False, "bfloat16"), ([40, 3, 100], 130, True, True, "bfloat16"),
+    ([3] * 400, 300, False, True, "float16"), ([6, 6], 70001, False, True, "bfloat16"), ([5] * 8, 32768, True, False, "bfloat16"),
+    ([12] * 40, 2048, True, True, "float32"), ([2] * 700, 64, False, True, "bfloat16"), ([6], 131072, True, True, "float16"),
+    ([4] * 3, 262144, True, True, "float32"),
+])
+@pytest.mark.parametrize("temperature", [None, 0.7, 1.0, "mixed"])
+def test_tree_verify(pkg, new, vocab, tree, probs, dtype, temperature):
+    r = np.random.default_rng(vocab + len(new))
+    t = np.where(r.random(len(new)) < 0.4, 0.0, r.uniform(0.3, 2.0, len(new))) if temperature == "mixed" else temperature
+    c = verify_case(r, new, vocab, tree, probs, dtype, t)
+    got = run_verify(pkg, c)
+    if vocab > 1:
+        # (drafts near the target: some are accepted)
+        assert got[1].max() > 1 or len(new) < 4
+    again = run_verify(pkg, c, check=False)
+    assert all(np.array_equal(a, b) for a, b in zip(got, again))
+
+
+def test_drafts_that_hang_on_one_row_in_many(pkg):
+    # 200 candidates behind the first row, none likely, some of them twice, some outside the vocabulary
+    r = np.random.default_rng(21)
+    for probs in (False, True):
+        c = verify_case(r, [201] * 6, 500, True, probs, "float32", 1.0, peaked=0.5)
+        c["parent"] = np.tile(np.concatenate([[-1], np.zeros(200, np.int64)]), 6)
+        c["tokens"] = r.integers(-2, 503, 6 * 201)
+        run_verify(pkg, c, least=0.8)
+
+
+def test_more_rows_than_are_looked_at(pkg):
+    r = np.random.default_rng(22)
+    c = verify_case(r, [9, 30, 2], 400, True, True, "bfloat16", 0.9)
+    run_verify(pkg, c, max_new=6)
+
+
+def test_logits_that_are_not_finite(pkg):
+    import torch
+    r = np.random.default_rng(23)
+    for temperature in (None, 1.0):
+        c = verify_case(r, [1, 3, 3, 2, 2], 300, False, False, "float32", temperature)
+        c["logits"][0] = -np.inf                # no token has a probability
+        c["logits"][1, :200] = -np.inf          # some have none
+        c["logits"][4, ::2] = float("nan")
+        c["logits"][7, 11] = c["logits"][7, 200] = np.inf  # two have it all
+        c["tokens"][8] = 11
+        got = run_verify(pkg, c)
+        assert got[2][0] == -1
+
+
+def test_ties_and_noise_that_takes_no_part(pkg):
+    import torch
+    r = np.random.default_rng(24)
+    c = verify_case(r, [1, 1], 5000, False, False, "bfloat16", None)
+    c["logits"][:] = 0.5
+    c["logits"][0, 77] = c["logits"][0, 4000] = 2.0
+    assert np.array_equal(run_verify(pkg, c)[2], [77, 0])
+    c["temperature"] = np.ones(2, np.float32)
+    c["noise"][:] = 1.0
+    assert np.array_equal(run_verify(pkg, c, check=False)[2], [77, 0])
+    c["noise"][0, :100] = 0.0
+    c["noise"][1, :10] = -1.0
+    c["noise"][1, 10] = np.nan
+    assert np.array_equal(run_verify(pkg, c, check=False)[2], [4000, 11])
+
+
+def test_nothing_left_to_draw(pkg):
+    # probabilities of the drafter that leave nothing of the target's: the next token is the target's
+    r = np.random.default_rng(25)
+    c = verify_case(r, [2, 2], 50, False, True, "float32", 1.0)
+    c["probs"][:] = 1.0
+    c["uniform"][:] = 0.999
+    got = run_verify(pkg, c)
+    assert np.array_equal(got[1], [1, 1]) and (got[2] >= 0).all()
+
+
+def test_rows_with_strides_and_any_alignment(pkg):
+    import torch
+    r = np.random.default_rng(26)
+    c = verify_case(r, [5] * 10, 1000, True, True, "bfloat16", 0.8)
+    want = run_verify(pkg, c)
+    for pad, first in ((8, 0), (1, 0), (7, 3), (24, 8)):
+        def wide(a):
+            a = dev(a) if not torch.is_tensor(a) else a
+            x = torch.full((a.shape[0], a.shape[1] + pad), float("nan"), dtype=a.dtype, device="cuda")
+            x = torch.nn.functional.pad(x, (first, 0), value=float("nan"))[:, first:first + a.shape[1]]
+            x.copy_(a)
+            return x
+        got = run_verify(pkg, dict(c, logits=wide(c["logits"]), probs=wide(c["probs"]), noise=wide(c["noise"])))
+        assert all(np.array_equal(a, b) for a, b in zip(got, want))
+
+
+def test_accepted_tokens_are_distributed_as_the_target(pkg):
+    # 2^15 requests with a draft each, drawn from the drafter's probabilities: the first token after the known one follows p
+    import torch
+    r = np.random.default_rng(27)
+    n, vocab = 1 << 15, 12
+    logits = r.standard_normal((1, vocab)).astype(np.float32)
+    z = r.standard_normal(vocab)
+    q = (np.exp(z) / np.exp(z).sum()).astype(np.float32)
+    p = np.exp(logits[0].astype(np.float64))
+    p /= p.sum()
+    for two in (False, True):
+        m = 3 if two else 2
+        drafts = r.choice(vocab, (n, m - 1), p=q / q.sum(dtype=np.float64))
+        tokens = np.concatenate([np.zeros((n, 1), np.int64), drafts], 1).reshape(-1)
+        parent = np.tile([-1] + [0] * (m - 1), n)
+        c = dict(logits=dev(np.repeat(logits, n * m, 0)), probs=dev(np.repeat(q[None], n * m, 0)), tokens=tokens, parent=parent,
+                 cu=np.arange(0, n * m + 1, m), temperature=np.ones(n, np.float32), uniform=r.random(n * m).astype(np.float32),
+                 noise=r.exponential(size=(n, vocab)).astype(np.float32), dtype="float32")
+        path, accepted, after = run_verify(pkg, c, check=False)
+        first = np.where(accepted > 1, tokens[np.maximum(path.reshape(n, m)[:, 1], 0)], after)
+        count = np.bincount(first, minlength=vocab)
+        # a count is within 6 standard deviations of n p (chance of any outside: 12 * 2 * 1e-9)
+        assert (np.abs(count - n * p) <= 6 * np.sqrt(n * p * (1 - p))).all()
+        assert (accepted > 1).mean() > 0.3
+
+
+# ---------------------------------------------------------------------- together
+
+@pytest.mark.parametrize("dtype,block", [("bfloat16", 16), ("float16", 4)])
+def test_a_decoding_loop(pkg, dtype, block):
+    """Plan, attention over the 8-bit cache, verification, and the write of the accepted rows, step by step and in a captured
+    graph on another stream: the cache holds what writing the accepted rows one after another would have left."""
+    import torch
+    r = np.random.default_rng(31)
+    n, page, pages, cols, heads, kv, dim, layers, vocab, most = 5, 16, 64, 12, 4, 2, 64, 2, 200, 6
+    kind = getattr(torch, dtype)
+    empty = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")
+    kc, vc = (torch.zeros((layers, pages, page, kv, dim), dtype=torch.float8_e4m3fn, device="cuda") for _ in range(2))
+    ks, vs = (torch.zeros((layers, pages, page // block, kv), device="cuda") for _ in range(2))
+    lay = pkg.make_quantised_layout(kc[0], block, dtype)
+    table, ring, ring_in = empty(n, cols) - 1, torch.randperm(pages).int().cuda(), i32([0, pages])
+    held, base, new = empty(n), empty(n), i32([most] * n)
+    rows = n * most
+    parent = i32(np.tile([-1, 0, 0, 1, 1, 2], n))
+    cu, slots, pos, mask, ring_out, status = empty(n + 1), empty(rows), empty(rows), empty(rows, 1), empty(2), empty(1)
+    plan = pkg.make_plan_config(n, rows, cols, page, pages, 1)
+    cfg = pkg.make_attention_config(n, heads, cols, most, "tree", 1, dim ** -0.5)
+    vcfg = pkg.make_verify_config(n, vocab, most, dtype)
+    ws = torch.empty(pkg.ivit_tree_attention_quantised_workspace(cfg, lay), dtype=torch.uint8, device="cuda")
+    q, k, v = (torch.zeros((layers, rows, h, dim), dtype=kind, device="cuda") for h in (heads, kv, kv))
+    out = torch.zeros((layers, rows, heads, dim), dtype=kind, device="cuda")
+    logits, probs = torch.zeros((rows, vocab), dtype=kind, device="cuda"), torch.zeros((rows, vocab), device="cuda")
+    tokens, path, accepted, after = empty(rows), empty(rows), empty(n), empty(n)
+    temperature, uniform, noise = torch.full((n,), 0.9, device="cuda"), torch.zeros(rows, device="cuda"), torch.zeros((n, vocab), device="cuda")
+
+    def step():
+        pkg.ivit_step_plan(plan, held, base, new, parent, ring, ring_in, table, cu, None, slots, pos, mask, ring_out, status)
+        for layer in range(layers):
+            pkg.ivit_tree_attention_quantised(cfg, lay, q[layer], k[layer], v[layer], kc[layer], vc[layer], ks[layer], vs[layer], table,
+                                              base, cu, mask, out[layer], None, ws)
+        pkg.ivit_tree_verify(vcfg, logits, probs, tokens, parent, cu, temperature, uniform, noise, path, accepted, after)
+        pkg.ivit_kv_quantise(lay, k, v, path, slots, kc, vc, ks, vs)
+
+    want = {}  # (layer, request, which) -> codes and scales of its tokens in a cache of its own, page after page
+    graph, side = None, torch.cuda.Stream()
+    lengths = np.zeros(n, np.int64)
+    for t in range(12):
+        for x in (q, k, v):
+            x.copy_(torch.from_numpy(r.standard_normal(tuple(x.shape)) * 2.0 ** r.integers(-3, 4)))
+        c = verify_case(r, [most] * n, vocab, True, True, dtype, 0.9)
+        c["parent"] = host(parent).astype(np.int64)
+        for i in range(n):
+            for j in range(1, most):
+                a = i * most + c["parent"][i * most + j]
+                c["tokens"][i * most + j] = (c["probs"][a] / r.exponential(size=vocab)).argmax()
+        logits.copy_(c["logits"])
+        for x, y in ((probs, c["probs"]), (uniform, c["uniform"]), (noise, c["noise"]), (tokens, c["tokens"])):
+            x.copy_(torch.from_numpy(y))
+        torch.cuda.synchronize()
+        if t < 4:
+            step()
+        elif t < 8:
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                step()
+            torch.cuda.current_stream().wait_stream(side)
+        else:
+            if graph is None:
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph):
+                    step()
+            graph.replay()
+        torch.cuda.synchronize()
+        assert int(status) == 0 and int(ws[:4].view(torch.int32)) == 0
+        # the attention over what the reference's caches hold
+        *found, margin = ref.verify(host(logits), c["probs"], c["tokens"], c["parent"], c["cu"], np.full(n, 0.9, np.float32),
+                                    c["uniform"], host(noise), most)
+        assert margin.min() > 2.0 ** -16
+        assert np.array_equal(host(path), found[0]) and np.array_equal(host(accepted), found[1]) and np.array_equal(host(after), found[2])
+        vis = backbone_ref.ancestors([int(p) for p in c["parent"][:most]])
+        for layer in range(layers):
+            mine = []
+            for which in range(2):
+                pair = want.setdefault((layer, which), (np.zeros((n * cols, page, kv, dim), np.uint8),
+                                                        np.zeros((n * cols, page // block, kv), np.float32)))
+                mine.append(ref.decode(*pair, block))
+            o, _, size = backbone_ref.attention(host(q[layer]), host(k[layer]), host(v[layer]), *mine, np.arange(n * cols).reshape(n, cols),
+                                                lengths, c["cu"], lambda i, m: vis, dim ** -0.5)
+            bound = UNIT[dtype] * np.abs(o) + (UNIT[dtype] + 2.0 ** -14) * size + 2.0 ** -25
+            assert (np.abs(host(out[layer]) - o) <= bound).all()
+        # the accepted rows into the reference's caches, request after request
+        for layer in range(layers):
+            for which, x in ((0, k), (1, v)):
+                codes, scale = want[layer, which]
+                for i in range(n):
+                    rows_i = found[0][i * most:i * most + found[1][i]]
+                    at = i * cols * page + lengths[i] + np.arange(len(rows_i))
+                    ref.quantise(codes, scale, list(host(x[layer])[rows_i]), at, block)
+        lengths += found[1]
+        held.copy_(base + most)
+        base.copy_(torch.from_numpy(lengths))
+        ring_in.copy_(ring_out)
+        pages_of = host(table).astype(np.int64)
+        for layer in range(layers):
+            for which, (codes, scale) in enumerate(((kc, ks), (vc, vs))):
+                for i in range(n):
+                    for j in range(-(-int(lengths[i]) // page)):
+                        m = min(page, int(lengths[i]) - j * page)
+                        wc, wscale = want[layer, which]
+                        assert np.array_equal(codes_of(codes[layer, pages_of[i, j]])[:m], wc[i * cols + j, :m])
+                        b = -(-m // block)
+                        assert np.array_equal(host(scale[layer, pages_of[i, j]])[:b], wscale[i * cols + j, :b])
+    assert lengths.min() > 12
