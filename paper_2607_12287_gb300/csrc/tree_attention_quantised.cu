@@ -49,7 +49,7 @@ struct Cfg {
   static constexpr bool PADDED = DP == 80 || DP == 96;
   static constexpr int ROW = DP == 96 ? 112 : DP;             // bytes of a row of codes: odd numbers of 16-byte pieces if padded
   static constexpr int PIECES = DP / 16, TILE = TK * ROW;
-  static constexpr int CTAS = DP <= 64 ? 4 : DP <= 128 ? 3 : 2;  // per SM
+  static constexpr int CTAS = DP <= 64 ? 4 : DP <= 96 ? 3 : 2;  // per SM
   static constexpr int STAGES = DP <= 128 ? 4 : 2;
   // a copy of a warp's keys: CP lanes for the pieces of a row, RP rows at a time
   static constexpr int CP = DP <= 64 ? 4 : DP <= 128 ? 8 : 16, RP = 32 / CP, COPIES = WK / RP;
@@ -193,164 +193,30 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP>::CTAS) tree_attention_quantis
   const auto value = [&](int s) {
     return s < 4 * C::FULL ? 64 * (s >> 2) + 16 * t + 4 * (s & 3) : 64 * C::FULL + (C::TAIL == 32 ? 8 * t + 4 * (s & 1) : 4 * t);
   };
-  uint32_t q[STEPS][4];
-  float o[DP / 8][4], m[2], l[2], factor[2];
-  int node[2];               // new row of the lane's rows g, g + 8 (-1: none)
-  const T* from[2];          // their queries
-  bool two = true;           // the tile has rows past its first 8
-  bool begun = true;         // of the tile's keys the run has seen the first
-
-  for (int u = 0; u < units; ++u) {
-    const int stage = u % STAGES;
-    if (u == 0 || at.kt == 0) {  // a new tile of rows
-      begun = at.kt == 0;
-      two = at.rt * M + 8 < at.r.n * a.group;
+  int u = 0;  // units done
+#pragma unroll 1
+  while (u < units) {
+    // A segment: consecutive key tiles [at.kt, at.kt + tiles) of one tile of rows, cached ones in front.
+    const int tiles = min(at.nkt - at.kt, units - u), cached = QuantisedKeys::cached(at.r), n_old = max(0, min(tiles, cached - at.kt));
+    const bool two = at.rt * M + 8 < at.r.n * a.group;  // the tile has rows past its first 8
+    float o[DP / 8][4], m[2], l[2];
+    int node[2];               // new row of the lane's rows g, g + 8 (-1: none)
+    const T* from[2];          // their queries
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int x = at.rt * M + g + 8 * r, n = x / a.group;
-        node[r] = n < at.r.n ? n : -1;
-        from[r] = static_cast<const T*>(a.q) + (at.r.row0 + n) * a.q_stride +
-                  static_cast<long long>(at.head * a.group + x - n * a.group) * dim;
-        m[r] = -INFINITY;
-        l[r] = 0.f;
-        factor[r] = a.score_log2;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-          const int d = value(s);
-          const uint2 w = node[r] >= 0 && d < dim ? *reinterpret_cast<const uint2*>(from[r] + d) : make_uint2(0, 0);
-          q[s][r] = w.x;
-          q[s][r + 2] = w.y;
-        }
-        if (BF16) {
-          float size = 0.f;
-#pragma unroll
-          for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-            for (int e = r; e < 4; e += 2) {
-              const float2 y = unpack2<T>(q[s][e]);
-              const float y0 = fabsf(y.x), y1 = fabsf(y.y);
-              size = fmaxf(size, fmaxf(y0 < INFINITY ? y0 : 0.f, y1 < INFINITY ? y1 : 0.f));
-            }
-          size = fmaxf(size, __shfl_xor_sync(ALL, size, 1));
-          size = fmaxf(size, __shfl_xor_sync(ALL, size, 2));
-          const int e2 = max(static_cast<int>(__float_as_uint(size) >> 23) - 127, -100) - 14;  // (-114 .. 113)
-          const float up = __int_as_float((127 - e2) << 23);
-          factor[r] *= __int_as_float((127 + e2) << 23);
-#pragma unroll
-          for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-            for (int e = r; e < 4; e += 2) {
-              const float2 y = unpack2<T>(q[s][e]);
-              q[s][e] = pack2<half>(y.x * up, y.y * up);
-            }
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < DP / 8; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
+    for (int r = 0; r < 2; ++r) {
+      const int x = at.rt * M + g + 8 * r, n = x / a.group;
+      node[r] = n < at.r.n ? n : -1;
+      from[r] = static_cast<const T*>(a.q) + (at.r.row0 + n) * a.q_stride + static_cast<long long>(at.head * a.group + x - n * a.group) * dim;
+      m[r] = -INFINITY;
+      l[r] = 0.f;
     }
-    copies_wait<STAGES - 2>();
-    __syncwarp();  // the lanes' copies have landed, and the stage of the tile before is free
-    fill((u + STAGES - 1) % STAGES);
+#pragma unroll
+    for (int j = 0; j < DP / 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
 
-    const int cached = QuantisedKeys::cached(at.r);
-    const bool fresh = at.kt >= cached;
-    const int k0 = (fresh ? at.kt - cached : at.kt) * TK + warp * WK;  // first key of the warp's: cached token or new row
-    const int keys = (fresh ? at.r.n : at.r.len) - k0;
-    if (keys > 0) {
-      float s[2][4], lv[2][2], iv[2][2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[j][e] = 0.f;
-      const uint8_t* kt = sm + stage * 2 * C::TILE;
-      if (!fresh) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int row = warp * WK + 8 * j + g;
-#pragma unroll
-          for (int c = 0; c < C::FULL; ++c) {
-            const uint4 w = *reinterpret_cast<const uint4*>(kt + piece<DP, false>(row, 4 * c + t));
-            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t b0, b1;
-              codes_to_half4(ww[i], b0, b1);
-              mma<half>(s[j], q[4 * c + i], b0, b1);
-            }
-          }
-          if (C::TAIL == 32) {
-            const uint2 w = *reinterpret_cast<const uint2*>(kt + piece<DP, false>(row, 4 * C::FULL + (t >> 1)) + 8 * (t & 1));
-            uint32_t b0, b1;
-            codes_to_half4(w.x, b0, b1);
-            mma<half>(s[j], q[STEPS - 2], b0, b1);
-            codes_to_half4(w.y, b0, b1);
-            mma<half>(s[j], q[STEPS - 1], b0, b1);
-          }
-          if (C::TAIL == 16) {
-            uint32_t b0, b1;
-            codes_to_half4(*reinterpret_cast<const uint32_t*>(kt + piece<DP, false>(row, 4 * C::FULL) + 4 * t), b0, b1);
-            mma<half>(s[j], q[STEPS - 1], b0, b1);
-          }
-        }
-        const float* scales = reinterpret_cast<const float*>(sm + C::OFF_SCALES) + 2 * stage * TK + warp * WK + 2 * t;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float2 kf = *reinterpret_cast<const float2*>(scales + 8 * j), vf = *reinterpret_cast<const float2*>(scales + TK + 8 * j);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float x = e ? vf.y : vf.x, f = e ? kf.y : kf.x;
-            const int b = __float_as_int(x);
-            const bool power = !(b & 0x7fffff);
-            lv[j][e] = power ? static_cast<float>((b >> 23) - 127) : __log2f(x);
-            iv[j][e] = power ? __int_as_float(0x7f000000 - b) : __fdividef(1.f, x);
-            if (b < 0x00800000 || b >= 0x7f000000) {  // none (or out of range): the values are as good as 0
-              lv[j][e] = -100.f;
-              iv[j][e] = __int_as_float((100 + 127) << 23);
-            }
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-              s[j][2 * r + e] = 8 * j + 2 * t + e < keys ? fmaf(s[j][2 * r + e], f * factor[r], lv[j][e]) : -INFINITY;
-          }
-        }
-      } else {
-        // Scores of new rows, in their own type.
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
-          const int d = value(st);
-          uint32_t qt[4];
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            if (BF16) {
-              const uint2 w = node[r] >= 0 && d < dim ? *reinterpret_cast<const uint2*>(from[r] + d) : make_uint2(0, 0);
-              qt[r] = w.x;
-              qt[r + 2] = w.y;
-            } else {
-              qt[r] = q[st][r];
-              qt[r + 2] = q[st][r + 2];
-            }
-          }
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const T* k = static_cast<const T*>(a.k_new) + static_cast<long long>(at.r.row0 + k0 + 8 * j + g) * a.k_new_stride + at.head * dim + d;
-            const uint2 w = 8 * j + g < keys && d < dim ? *reinterpret_cast<const uint2*>(k) : make_uint2(0, 0);
-            mma<T>(s[j], qt, w.x, w.y);
-          }
-        }
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const uint64_t bits = node[r] >= 0 ? seen(a, at.r, node[r], k0 - warp * WK) >> (warp * WK) : 0;
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              s[j][2 * r + e] = bits >> (8 * j + 2 * t + e) & 1 ? s[j][2 * r + e] * a.score_log2 : -INFINITY;
-              iv[j][e] = 1.f;
-            }
-        }
-      }
-      // probabilities against the reference maximum, and their sum
+    // Scores s (log2 units, -inf where a key is not seen) to probabilities against the reference maximum, added to l times iv.
+    const auto probabilities = [&](float (&s)[2][4], const float (&iv)[2][2]) {
       float mx[2];
       bool grow = false;
 #pragma unroll
@@ -387,24 +253,126 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP>::CTAS) tree_attention_quantis
             l[r] = fmaf(s[j][2 * r + e], iv[j][e], l[r]);
           }
       }
-      // two 16-bit terms of each
-      const auto terms = [&](auto type, uint32_t (&p)[2][4]) {
-        using P = decltype(type);
+    };
+    // two 16-bit terms of each
+    const auto terms = [&](auto type, const float (&s)[2][4], uint32_t (&p)[2][4]) {
+      using P = decltype(type);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if ((e & 1) && !two) {
-            p[0][e] = p[1][e] = 0u;
-            continue;
-          }
-          const float x = s[e >> 1][2 * (e & 1)], y = s[e >> 1][2 * (e & 1) + 1];
-          p[0][e] = pack2<P>(x, y);
-          const float2 h = unpack2<P>(p[0][e]);
-          p[1][e] = pack2<P>(x - h.x, y - h.y);
+      for (int e = 0; e < 4; ++e) {
+        if ((e & 1) && !two) {
+          p[0][e] = p[1][e] = 0u;
+          continue;
         }
-      };
-      uint32_t p[2][4];
-      if (!fresh) {
-        terms(half{}, p);
+        const float x = s[e >> 1][2 * (e & 1)], y = s[e >> 1][2 * (e & 1) + 1];
+        p[0][e] = pack2<P>(x, y);
+        const float2 h = unpack2<P>(p[0][e]);
+        p[1][e] = pack2<P>(x - h.x, y - h.y);
+      }
+    };
+    const auto step = [&] {  // the next unit's copies have landed, and those of a later one begin
+      copies_wait<STAGES - 2>();
+      __syncwarp();  // the lanes' copies have landed, and the stage of the tile before is free
+      fill((u + STAGES - 1) % STAGES);
+    };
+
+    if (n_old > 0) {
+      uint32_t q[STEPS][4];
+      float factor[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        factor[r] = a.score_log2;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+          const int d = value(s);
+          const uint2 w = node[r] >= 0 && d < dim ? *reinterpret_cast<const uint2*>(from[r] + d) : make_uint2(0, 0);
+          q[s][r] = w.x;
+          q[s][r + 2] = w.y;
+        }
+        if (BF16) {
+          float size = 0.f;
+#pragma unroll
+          for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int e = r; e < 4; e += 2) {
+              const float2 y = unpack2<T>(q[s][e]);
+              const float y0 = fabsf(y.x), y1 = fabsf(y.y);
+              size = fmaxf(size, fmaxf(y0 < INFINITY ? y0 : 0.f, y1 < INFINITY ? y1 : 0.f));
+            }
+          size = fmaxf(size, __shfl_xor_sync(ALL, size, 1));
+          size = fmaxf(size, __shfl_xor_sync(ALL, size, 2));
+          const int e2 = max(static_cast<int>(__float_as_uint(size) >> 23) - 127, -100) - 14;  // (-114 .. 113)
+          const float up = __int_as_float((127 - e2) << 23);
+          factor[r] *= __int_as_float((127 + e2) << 23);
+#pragma unroll
+          for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int e = r; e < 4; e += 2) {
+              const float2 y = unpack2<T>(q[s][e]);
+              q[s][e] = pack2<half>(y.x * up, y.y * up);
+            }
+        }
+      }
+#pragma unroll 1
+      for (int kt = at.kt; kt < at.kt + n_old; ++kt, ++u) {
+        const int stage = u % STAGES;
+        step();
+        const int keys = at.r.len - kt * TK - warp * WK;  // cached tokens from the warp's first on
+        if (keys <= 0) continue;
+        float s[2][4], lv[2][2], iv[2][2];
+        const uint8_t* kt8 = sm + stage * 2 * C::TILE;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[j][e] = 0.f;
+          const int row = warp * WK + 8 * j + g;
+#pragma unroll
+          for (int c = 0; c < C::FULL; ++c) {
+            const uint4 w = *reinterpret_cast<const uint4*>(kt8 + piece<DP, false>(row, 4 * c + t));
+            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t b0, b1;
+              codes_to_half4(ww[i], b0, b1);
+              mma<half>(s[j], q[4 * c + i], b0, b1);
+            }
+          }
+          if constexpr (C::TAIL == 32) {
+            const uint2 w = *reinterpret_cast<const uint2*>(kt8 + piece<DP, false>(row, 4 * C::FULL + (t >> 1)) + 8 * (t & 1));
+            uint32_t b0, b1;
+            codes_to_half4(w.x, b0, b1);
+            mma<half>(s[j], q[STEPS - 2], b0, b1);
+            codes_to_half4(w.y, b0, b1);
+            mma<half>(s[j], q[STEPS - 1], b0, b1);
+          }
+          if constexpr (C::TAIL == 16) {
+            uint32_t b0, b1;
+            codes_to_half4(*reinterpret_cast<const uint32_t*>(kt8 + piece<DP, false>(row, 4 * C::FULL) + 4 * t), b0, b1);
+            mma<half>(s[j], q[STEPS - 1], b0, b1);
+          }
+        }
+        const float* scales = reinterpret_cast<const float*>(sm + C::OFF_SCALES) + 2 * stage * TK + warp * WK + 2 * t;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float2 kf = *reinterpret_cast<const float2*>(scales + 8 * j), vf = *reinterpret_cast<const float2*>(scales + TK + 8 * j);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float x = e ? vf.y : vf.x, f = e ? kf.y : kf.x;
+            const int b = __float_as_int(x);
+            const bool power = !(b & 0x7fffff);
+            lv[j][e] = power ? static_cast<float>((b >> 23) - 127) : __log2f(x);
+            iv[j][e] = power ? __int_as_float(0x7f000000 - b) : __fdividef(1.f, x);
+            if (b < 0x00800000 || b >= 0x7f000000) {  // none (or out of range): the values are as good as 0
+              lv[j][e] = -100.f;
+              iv[j][e] = __int_as_float((100 + 127) << 23);
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+              s[j][2 * r + e] = 8 * j + 2 * t + e < keys ? fmaf(s[j][2 * r + e], f * factor[r], lv[j][e]) : -INFINITY;
+          }
+        }
+        probabilities(s, iv);
+        uint32_t p[2][4];
+        terms(half{}, s, p);
 #pragma unroll
         for (int c = 0; c < C::PIECES; c += 2) {
           const int mine = c + 1 < C::PIECES ? c + (lane >> 4) : c;
@@ -425,128 +393,164 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP>::CTAS) tree_attention_quantis
             }
           }
         }
-      } else {
-        terms(T{}, p);
-        bool odd = false;
+      }
+    }
+
+    // New rows, in their own type.
+#pragma unroll 1
+    for (int nt = at.kt + n_old - cached; nt < at.kt + tiles - cached; ++nt, ++u) {
+      step();
+      const int k0 = nt * TK + warp * WK, keys = at.r.n - k0;  // first new row of the warp's
+      if (keys <= 0) continue;
+      float s[2][4] = {};
+      const float iv[2][2] = {{1.f, 1.f}, {1.f, 1.f}};
 #pragma unroll
-        for (int c = 0; c < C::PIECES; ++c) {
-          const int d = 16 * c + 2 * g;
-          uint32_t w[4];  // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+      for (int st = 0; st < STEPS; ++st) {
+        const int d = value(st);
+        uint32_t qt[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int key = 2 * t + (i & 1) + 8 * (i >> 1);
-            const T* v = static_cast<const T*>(a.v_new) + static_cast<long long>(at.r.row0 + k0 + key) * a.v_new_stride + at.head * dim + d;
-            w[i] = key < keys && d < dim ? *reinterpret_cast<const uint32_t*>(v) : 0u;
-            // Values that are not finite would reach rows that do not see them (0 * NaN): left out here, added below.
-            const bool lo = odd16<T>(w[i]), hi = odd16<T>(w[i] >> 16);
-            if (lo) w[i] &= 0xffff0000u;
-            if (hi) w[i] &= 0x0000ffffu;
-            odd |= lo || hi;
-          }
-          const uint32_t x0 = __byte_perm(w[0], w[1], 0x5410), x1 = __byte_perm(w[0], w[1], 0x7632);
-          const uint32_t y0 = __byte_perm(w[2], w[3], 0x5410), y1 = __byte_perm(w[2], w[3], 0x7632);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            mma<T>(o[2 * c], p[i], x0, y0);
-            mma<T>(o[2 * c + 1], p[i], x1, y1);
-          }
+        for (int r = 0; r < 2; ++r) {
+          const uint2 w = node[r] >= 0 && d < dim ? *reinterpret_cast<const uint2*>(from[r] + d) : make_uint2(0, 0);
+          qt[r] = w.x;
+          qt[r + 2] = w.y;
         }
-        if (__any_sync(ALL, odd)) {
-          for (int k = 0; k < min(keys, WK); ++k) {
-            const T* v = static_cast<const T*>(a.v_new) + static_cast<long long>(at.r.row0 + k0 + k) * a.v_new_stride + at.head * dim + 4 * t;
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
-              if (node[r] >= 0 && seen(a, at.r, node[r], k0 - warp * WK) >> (warp * WK + k) & 1) {
+        for (int j = 0; j < 2; ++j) {
+          const T* k = static_cast<const T*>(a.k_new) + static_cast<long long>(at.r.row0 + k0 + 8 * j + g) * a.k_new_stride + at.head * dim + d;
+          const uint2 w = 8 * j + g < keys && d < dim ? *reinterpret_cast<const uint2*>(k) : make_uint2(0, 0);
+          mma<T>(s[j], qt, w.x, w.y);
+        }
+      }
 #pragma unroll
-                for (int c = 0; c < C::PIECES; ++c)
-                  if (16 * c + 4 * t < dim) {
-                    const uint2 w = *reinterpret_cast<const uint2*>(v + 16 * c);
-                    const float2 x = unpack2<T>(w.x), y = unpack2<T>(w.y);
-                    if (!isfinite(x.x)) o[2 * c][2 * r] += x.x;
-                    if (!isfinite(x.y)) o[2 * c + 1][2 * r] += x.y;
-                    if (!isfinite(y.x)) o[2 * c][2 * r + 1] += y.x;
-                    if (!isfinite(y.y)) o[2 * c + 1][2 * r + 1] += y.y;
-                  }
-              }
-          }
+      for (int r = 0; r < 2; ++r) {
+        const uint64_t bits = node[r] >= 0 ? seen(a, at.r, node[r], nt * TK) >> (warp * WK) : 0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            s[j][2 * r + e] = bits >> (8 * j + 2 * t + e) & 1 ? s[j][2 * r + e] * a.score_log2 : -INFINITY;
+      }
+      probabilities(s, iv);
+      uint32_t p[2][4];
+      terms(T{}, s, p);
+      bool odd = false;
+#pragma unroll
+      for (int c = 0; c < C::PIECES; ++c) {
+        const int d = 16 * c + 2 * g;
+        uint32_t w[4];  // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = 2 * t + (i & 1) + 8 * (i >> 1);
+          const T* v = static_cast<const T*>(a.v_new) + static_cast<long long>(at.r.row0 + k0 + key) * a.v_new_stride + at.head * dim + d;
+          w[i] = key < keys && d < dim ? *reinterpret_cast<const uint32_t*>(v) : 0u;
+          // Values that are not finite would reach rows that do not see them (0 * NaN): left out here, added below.
+          const bool lo = odd16<T>(w[i]), hi = odd16<T>(w[i] >> 16);
+          if (lo) w[i] &= 0xffff0000u;
+          if (hi) w[i] &= 0x0000ffffu;
+          odd |= lo || hi;
+        }
+        const uint32_t x0 = __byte_perm(w[0], w[1], 0x5410), x1 = __byte_perm(w[0], w[1], 0x7632);
+        const uint32_t y0 = __byte_perm(w[2], w[3], 0x5410), y1 = __byte_perm(w[2], w[3], 0x7632);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          mma<T>(o[2 * c], p[i], x0, y0);
+          mma<T>(o[2 * c + 1], p[i], x1, y1);
+        }
+      }
+      if (__any_sync(ALL, odd)) {
+#pragma unroll 1
+        for (int k = 0; k < min(keys, WK); ++k) {
+          const T* v = static_cast<const T*>(a.v_new) + static_cast<long long>(at.r.row0 + k0 + k) * a.v_new_stride + at.head * dim + 4 * t;
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            if (node[r] >= 0 && seen(a, at.r, node[r], nt * TK) >> (warp * WK + k) & 1) {
+#pragma unroll
+              for (int c = 0; c < C::PIECES; ++c)
+                if (16 * c + 4 * t < dim) {
+                  const uint2 w = *reinterpret_cast<const uint2*>(v + 16 * c);
+                  const float2 x = unpack2<T>(w.x), y = unpack2<T>(w.y);
+                  if (!isfinite(x.x)) o[2 * c][2 * r] += x.x;
+                  if (!isfinite(x.y)) o[2 * c + 1][2 * r] += x.y;
+                  if (!isfinite(y.x)) o[2 * c][2 * r + 1] += y.x;
+                  if (!isfinite(y.y)) o[2 * c + 1][2 * r + 1] += y.y;
+                }
+            }
         }
       }
     }
 
-    if (at.kt == at.nkt - 1 || u == units - 1) {  // the run has no more keys of this tile of rows
-      // The warps meet: every output against the largest maximum, added up in the order of the warps.
-      float2* ml = reinterpret_cast<float2*>(sm + C::OFF_ML);
-      float* meet = reinterpret_cast<float*>(sm + C::OFF_MEET);
+    // The warps meet: every output against the largest maximum, added up in the order of the warps.
+    float2* ml = reinterpret_cast<float2*>(sm + C::OFF_ML);
+    float* meet = reinterpret_cast<float*>(sm + C::OFF_MEET);
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        l[r] += __shfl_xor_sync(ALL, l[r], 1);
-        l[r] += __shfl_xor_sync(ALL, l[r], 2);
-        if (t == 0) ml[warp * M + g + 8 * r] = make_float2(m[r], l[r]);
-      }
-      __syncthreads();
-      float f[2];
+    for (int r = 0; r < 2; ++r) {
+      l[r] += __shfl_xor_sync(ALL, l[r], 1);
+      l[r] += __shfl_xor_sync(ALL, l[r], 2);
+      if (t == 0) ml[warp * M + g + 8 * r] = make_float2(m[r], l[r]);
+    }
+    __syncthreads();
+    float f[2];
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        float top = -INFINITY;
+    for (int r = 0; r < 2; ++r) {
+      float top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) top = fmaxf(top, ml[w * M + g + 8 * r].x);
-        f[r] = ex2(m[r] - (top == -INFINITY ? 0.f : top));
-      }
+      for (int w = 0; w < WARPS; ++w) top = fmaxf(top, ml[w * M + g + 8 * r].x);
+      f[r] = ex2(m[r] - (top == -INFINITY ? 0.f : top));
+    }
 #pragma unroll 1
-      for (int w = 0; w < WARPS; ++w) {
-        if (warp == w) {
+    for (int w = 0; w < WARPS; ++w) {
+      if (warp == w) {
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            if (r == 1 && !two) break;
+        for (int r = 0; r < 2; ++r) {
+          if (r == 1 && !two) break;
 #pragma unroll
-            for (int c = 0; c < C::PIECES; ++c) {
-              float4* dst = reinterpret_cast<float4*>(meet + (g + 8 * r) * DP + 16 * c + 4 * t);
-              float4 y = make_float4(o[2 * c][2 * r] * f[r], o[2 * c + 1][2 * r] * f[r], o[2 * c][2 * r + 1] * f[r],
-                                     o[2 * c + 1][2 * r + 1] * f[r]);
-              if (w > 0) {
-                const float4 x = *dst;
-                y = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
-              }
-              *dst = y;
+          for (int c = 0; c < C::PIECES; ++c) {
+            float4* dst = reinterpret_cast<float4*>(meet + (g + 8 * r) * DP + 16 * c + 4 * t);
+            float4 y = make_float4(o[2 * c][2 * r] * f[r], o[2 * c + 1][2 * r] * f[r], o[2 * c][2 * r + 1] * f[r],
+                                   o[2 * c + 1][2 * r + 1] * f[r]);
+            if (w > 0) {
+              const float4 x = *dst;
+              y = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
             }
+            *dst = y;
           }
         }
-        __syncthreads();
       }
-      const bool whole = begun && at.kt == at.nkt - 1;
-      // a part: the first of the run, or the one it ends with
-      float* part = a.parts + static_cast<size_t>(2 * blockIdx.x + (u - at.kt > 0 && begun ? 1 : 0)) * C::PART;
-      const int rows = min(M, at.r.n * a.group - at.rt * M);
-#pragma unroll 1
-      for (int e = tid; e < rows * (DP / 4); e += THREADS) {
-        const int row = e / (DP / 4), col = e - row * (DP / 4);
-        const float4 y = *reinterpret_cast<const float4*>(meet + row * DP + 4 * col);
-        float top = -INFINITY, sum = 0.f;
-        float2 of[WARPS];
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-          of[w] = ml[w * M + row];
-          top = fmaxf(top, of[w].x);
-        }
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) sum += of[w].y * ex2(of[w].x - (top == -INFINITY ? 0.f : top));
-        if (whole) {
-          const int x = at.rt * M + row, nd = x / a.group, h = at.head * a.group + x - nd * a.group;
-          const long long orow = at.r.row0 + nd;
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          if (4 * col < dim)
-            *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * dim + 4 * col) =
-                make_uint2(pack2<T>(y.x * inv, y.y * inv), pack2<T>(y.z * inv, y.w * inv));
-          if (a.lse && col == 0) a.lse[orow * a.heads + h] = (top + (log2f(sum) - TREE_SHIFT)) * 0.6931471805599453f;
-        } else {
-          reinterpret_cast<float4*>(part + row * DP)[col] = y;
-          if (col == 0) *reinterpret_cast<float2*>(part + M * DP + 2 * row) = make_float2(top, sum);
-        }
-      }
-      __syncthreads();  // the place of the meeting is free
-      if (!whole && begun && tid == 0) run.note_join(a, at, run.lo + u - at.kt);
+      __syncthreads();
     }
-    at.next(a);
+    const bool whole = tiles == at.nkt;
+    // a part: the first of the run, or the one it ends with
+    float* part = a.parts + static_cast<size_t>(2 * blockIdx.x + (u > tiles ? 1 : 0)) * C::PART;
+    const int rows = min(M, at.r.n * a.group - at.rt * M);
+#pragma unroll 1
+    for (int e = tid; e < rows * (DP / 4); e += THREADS) {
+      const int row = e / (DP / 4), col = e - row * (DP / 4);
+      const float4 y = *reinterpret_cast<const float4*>(meet + row * DP + 4 * col);
+      float top = -INFINITY, sum = 0.f;
+      float2 of[WARPS];
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        of[w] = ml[w * M + row];
+        top = fmaxf(top, of[w].x);
+      }
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) sum += of[w].y * ex2(of[w].x - (top == -INFINITY ? 0.f : top));
+      if (whole) {
+        const int x = at.rt * M + row, nd = x / a.group, h = at.head * a.group + x - nd * a.group;
+        const long long orow = at.r.row0 + nd;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (4 * col < dim)
+          *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * dim + 4 * col) =
+              make_uint2(pack2<T>(y.x * inv, y.y * inv), pack2<T>(y.z * inv, y.w * inv));
+        if (a.lse && col == 0) a.lse[orow * a.heads + h] = (top + (log2f(sum) - TREE_SHIFT)) * 0.6931471805599453f;
+      } else {
+        reinterpret_cast<float4*>(part + row * DP)[col] = y;
+        if (col == 0) *reinterpret_cast<float2*>(part + M * DP + 2 * row) = make_float2(top, sum);
+      }
+    }
+    __syncthreads();  // the place of the meeting is free
+    if (!whole && at.kt == 0 && tid == 0) run.note_join(a, at, run.lo + u - tiles);
+    at.next_rows(a);
   }
 }
 
