@@ -5,15 +5,11 @@
 
 namespace ivit {
 
-// Two codes (the low 16 bits) as fp16 values, which hold every e4m3 value exactly, and four of a word.
-__device__ __forceinline__ uint32_t codes_to_half2(uint16_t c) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(c));
-  return r;
-}
+// Four codes of a word as fp16 values, which hold every e4m3 value exactly.
 __device__ __forceinline__ void codes_to_half4(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  lo = codes_to_half2(static_cast<uint16_t>(w));
-  hi = codes_to_half2(static_cast<uint16_t>(w >> 16));
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(w));
 }
 // Codes of two fp32 values, rounded to nearest even (beyond 448: 448; NaN stays NaN).
 __device__ __forceinline__ uint32_t to_codes2(float lo, float hi) {
