@@ -2,17 +2,12 @@
 //
 //   o = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q.k_j - m),  k_j = a_j s_j,  v_j = b_j t_j  for cached keys
 //
-// with e4m3 codes a_j, b_j and the scales s_j, t_j of their blocks.  Codes of keys are operands of the products as they are
-// (mma.sync of e4m3, 2.4 times fp16's rate, and no conversions on the way); queries are split into terms of e4m3, 4 bits each,
-//
-//   q 2^-e = q1 + q2 / 16 (+ q3 / 256),  so S = S1 + S2 / 16 (+ S3 / 256)
-//
-// 2 of them exact for bf16, 3 for fp16, but for values 2^-13 of the row's largest and less, which are off by up to 2^-21 of it.  Codes of
-// values become fp16 (exact): probabilities as terms of e4m3 would be off by a share of the largest one, and a key with much
-// weight and small values would drown the others.  s_j multiplies the score, t_j the probability: p'_j = 2^(y_j - m),
-// y_j = s_j (q.a_j) c + log2 t_j, which stays within fp16 whatever the blocks' scales are, for m is the running maximum of
-// y; the sum has p'_j / t_j.  p' is rounded to fp16 for bf16 rows, 2^-12 of each and an eighth of what their own rounding is, and has
-// two terms for fp16 rows.
+// with e4m3 codes a_j, b_j and the scales s_j, t_j of their blocks.  The codes enter the products as fp16 values (exact; mma.sync of
+// e4m3 itself is no option: it takes 37 cycles of a quarter SM for 16 x 8 x 32, two of fp16 16 and the conversions): s_j multiplies
+// the score, t_j the probability, p'_j = 2^(y_j - m), y_j = s_j (q.a_j) c + log2 t_j, which stays within fp16 whatever the
+// blocks' scales are, for m is the running maximum of y; the sum has p'_j / t_j.  Queries in bf16 enter as fp16 times a power of two
+// that puts a row's largest value at 2^14 (exact but for values 2^-28 of it and less).  p' is rounded to fp16 for bf16 rows,
+// 2^-12 of each and an eighth of what their own rounding is, and has two terms for fp16 rows.
 //
 // The work is cut as in tree_attention.cu, whose run, part and join it shares: tiles of 8 or 16 rows (new row x head of the
 // group), 128 keys at a time, first the cached tokens, then the new rows; 32 keys of a tile belong to each of the four warps, which
@@ -66,7 +61,7 @@ struct Cfg {
   static constexpr int STAGES = DP <= 80 || DP > 128 || (DP <= 96 && CTAS == 2) ? 3 : 2;
   // a copy of a warp's keys: CP lanes for the pieces of a row, RP rows at a time
   static constexpr int CP = DP <= 64 ? 4 : DP <= 128 ? 8 : 16, RP = 32 / CP, COPIES = WK / RP;
-  static constexpr int FULL = DP / 64, TAIL = DP % 64, STEPS = 2 * FULL + (TAIL > 0);  // of the product: of 32 values (or 16 that are left)
+  static constexpr int FULL = DP / 64, TAIL = DP % 64, STEPS = DP / 16;  // of the product, of 16 values
   static constexpr int MEET = DP + 4;                          // floats of a row where the warps meet
   static constexpr int OFF_SCALES = STAGES * 2 * TILE;         // [stage][K, V][key]
   static constexpr int OFF_MEET = OFF_SCALES + STAGES * 2 * TK * 4;  // [row][MEET] fp32
@@ -95,31 +90,6 @@ __device__ __forceinline__ uint32_t seen(const TreeArgs& a, const TreeRequest& r
   return w < a.mask_words ? bits & a.mask[static_cast<size_t>(r.row0 + node) * a.mask_words + w] : 0u;
 }
 
-// Products of e4m3 codes, 16 x 32 times 32 x 8.
-__device__ __forceinline__ void mma_e4m3(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// N e4m3 terms of two fp16 values (in 16 bits), x = t0 + t1 / 16 + t2 / 256.
-template <int N>
-__device__ __forceinline__ void split2(uint32_t x, uint32_t (&t)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    uint32_t back;
-    uint16_t c;
-    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(c) : "r"(x));
-    t[i] = c;
-    if (i + 1 < N) {
-      asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(c));
-      const __half2 rest = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&back));
-      const __half2 next = __hmul2(rest, __float2half2_rn(16.f));
-      x = *reinterpret_cast<const uint32_t*>(&next);
-    }
-  }
-}
-
 // An 8 x 8 matrix of 16-bit values, of which lane 4 i + j has values 2 j and 2 j + 1 of row i, turned over.
 __device__ __forceinline__ uint32_t transposed8x8(uint32_t x) {
   uint32_t y;
@@ -140,7 +110,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
   constexpr unsigned ALL = 0xffffffffu;
   constexpr int M = C::M, STAGES = C::STAGES, COPIES = C::COPIES, RP = C::RP;
   constexpr bool BF16 = std::is_same<T, bf16>::value;
-  constexpr int QT = BF16 ? 2 : 3, PT = BF16 ? 1 : 2;  // terms of queries and of probabilities
+  constexpr int PT = BF16 ? 1 : 2;  // terms of probabilities
   extern __shared__ __align__(128) uint8_t sm[];
   const uint32_t sb = smem_u32(sm);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -253,10 +223,9 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
 #pragma unroll 1
   for (int s = 0; s < STAGES - 1; ++s) fill(s);
 
-  // First of the values of a head that the lane has in a step of the product with K: eight of cached keys (four in a last step
-  // of 16 values), four of new rows'.
+  // First of the four values of a head that the lane has in a step of the product with cached keys.
   const auto value = [&](int s) {
-    return s < 2 * C::FULL ? 64 * (s >> 1) + 16 * t + 8 * (s & 1) : 64 * C::FULL + (C::TAIL == 32 ? 8 * t : 4 * t);
+    return s < 4 * C::FULL ? 64 * (s >> 2) + 16 * t + 4 * (s & 3) : 64 * C::FULL + (C::TAIL == 32 ? 8 * t + 4 * (s & 1) : 4 * t);
   };
   // Rows of the tile are columns of the products: S^T = K q^T with 16 keys (of the lane: g and g + 8, twice) times 8 rows (2 t and 2 t + 1),
   // O^T = V^T P^T with 16 values of a head (2 g and 2 g + 1) times 8 rows.
@@ -353,52 +322,40 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
     };
 
     if (n_old > 0) {
-      uint32_t q[NR][C::STEPS][QT][2];
+      uint32_t q[NR][C::STEPS][2];
       float factor[NR][2];  // of rows 2 t, 2 t + 1
 #pragma unroll
       for (int h = 0; h < NR; ++h) {
         const T* from = query(8 * h + g);
-        uint4 raw[C::STEPS];
-        float size = 0.f;
+        float size = 0.f, mine = a.score_log2;
 #pragma unroll
         for (int s = 0; s < C::STEPS; ++s) {
           const int d = value(s);
-          raw[s] = make_uint4(0, 0, 0, 0);
-          if (8 * h + g < rows && d < dim) {
-            if (C::TAIL == 16 && s == C::STEPS - 1) {
-              const uint2 w = *reinterpret_cast<const uint2*>(from + d);
-              raw[s].x = w.x, raw[s].y = w.y;
-            } else {
-              raw[s] = *reinterpret_cast<const uint4*>(from + d);
-            }
-          }
-          const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 y = unpack2<T>(w[i]);
-            const float y0 = fabsf(y.x), y1 = fabsf(y.y);
-            size = fmaxf(size, fmaxf(y0 < INFINITY ? y0 : 0.f, y1 < INFINITY ? y1 : 0.f));
-          }
+          const uint2 w = 8 * h + g < rows && d < dim ? *reinterpret_cast<const uint2*>(from + d) : make_uint2(0, 0);
+          q[h][s][0] = w.x;
+          q[h][s][1] = w.y;
         }
-        size = fmaxf(size, __shfl_xor_sync(ALL, size, 1));
-        size = fmaxf(size, __shfl_xor_sync(ALL, size, 2));
-        // the largest value becomes 2^7 .. 2^8; what is not finite, NaN (e4m3 has no infinities)
-        const int e2 = max(static_cast<int>(__float_as_uint(size) >> 23) - 127, -100) - 7;  // (-107 .. 120)
-        const float up = __int_as_float((127 - e2) << 23), mine = a.score_log2 * __int_as_float((127 + e2) << 23);
+        if (BF16) {
 #pragma unroll
-        for (int s = 0; s < C::STEPS; ++s) {
-          const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
-          uint32_t part[4][QT];
+          for (int s = 0; s < C::STEPS; ++s)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 y = unpack2<T>(w[i]);
-            const auto scaled = [&](float v) { return fabsf(v) < INFINITY ? v * up : __uint_as_float(0x7fffffffu); };
-            split2<QT>(pack2<half>(scaled(y.x), scaled(y.y)), part[i]);
-          }
+            for (int e = 0; e < 2; ++e) {
+              const float2 y = unpack2<T>(q[h][s][e]);
+              const float y0 = fabsf(y.x), y1 = fabsf(y.y);
+              size = fmaxf(size, fmaxf(y0 < INFINITY ? y0 : 0.f, y1 < INFINITY ? y1 : 0.f));
+            }
+          size = fmaxf(size, __shfl_xor_sync(ALL, size, 1));
+          size = fmaxf(size, __shfl_xor_sync(ALL, size, 2));
+          const int e2 = max(static_cast<int>(__float_as_uint(size) >> 23) - 127, -100) - 14;  // (-114 .. 113)
+          const float up = __int_as_float((127 - e2) << 23);
+          mine *= __int_as_float((127 + e2) << 23);
 #pragma unroll
-          for (int x = 0; x < QT; ++x)
+          for (int s = 0; s < C::STEPS; ++s)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) q[h][s][x][e] = part[2 * e][x] | part[2 * e + 1][x] << 16;
+            for (int e = 0; e < 2; ++e) {
+              const float2 y = unpack2<T>(q[h][s][e]);
+              q[h][s][e] = pack2<half>(y.x * up, y.y * up);
+            }
         }
         factor[h][0] = __shfl_sync(ALL, mine, 8 * t);  // (row r is that of lanes 4 r ..)
         factor[h][1] = __shfl_sync(ALL, mine, 8 * t + 4);
@@ -414,36 +371,37 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
         float s[2][NR][4], iv[2][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {  // 16 keys
-          float sum[NR][QT][4];
+          float sum[2][NR][4];  // two, for shorter chains
 #pragma unroll
           for (int h = 0; h < NR; ++h)
 #pragma unroll
-            for (int x = 0; x < QT; ++x)
+            for (int e = 0; e < 4; ++e) sum[0][h][e] = sum[1][h][e] = 0.f;
+          const auto product = [&](int st, uint32_t x, uint32_t y) {  // step st, four codes of keys g and g + 8
+            uint32_t k4[4];
+            codes_to_half4(x, k4[0], k4[2]);
+            codes_to_half4(y, k4[1], k4[3]);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) sum[h][x][e] = 0.f;
-          const auto product = [&](int st, uint32_t x0, uint32_t y0, uint32_t x1, uint32_t y1) {  // step st, codes of keys g (x) and g + 8 (y)
-            const uint32_t k4[4] = {x0, y0, x1, y1};
-#pragma unroll
-            for (int h = 0; h < NR; ++h)
-#pragma unroll
-              for (int x = 0; x < QT; ++x) mma_e4m3(sum[h][x], k4, q[h][st][x][0], q[h][st][x][1]);
+            for (int h = 0; h < NR; ++h) mma<half>(sum[st & 1][h], k4, q[h][st][0], q[h][st][1]);
           };
           const int row = warp * WK + 16 * i + g;
 #pragma unroll
           for (int c = 0; c < C::FULL; ++c) {
             const uint4 x = *reinterpret_cast<const uint4*>(k_tile + piece<DP, false>(row, 4 * c + t));
             const uint4 y = *reinterpret_cast<const uint4*>(k_tile + piece<DP, false>(row + 8, 4 * c + t));
-            product(2 * c, x.x, y.x, x.y, y.y);
-            product(2 * c + 1, x.z, y.z, x.w, y.w);
+            product(4 * c, x.x, y.x);
+            product(4 * c + 1, x.y, y.y);
+            product(4 * c + 2, x.z, y.z);
+            product(4 * c + 3, x.w, y.w);
           }
           if constexpr (C::TAIL == 32) {
             const uint2 x = *reinterpret_cast<const uint2*>(k_tile + piece<DP, false>(row, 4 * C::FULL + (t >> 1)) + 8 * (t & 1));
             const uint2 y = *reinterpret_cast<const uint2*>(k_tile + piece<DP, false>(row + 8, 4 * C::FULL + (t >> 1)) + 8 * (t & 1));
-            product(C::STEPS - 1, x.x, y.x, x.y, y.y);
+            product(C::STEPS - 2, x.x, y.x);
+            product(C::STEPS - 1, x.y, y.y);
           }
           if constexpr (C::TAIL == 16)
             product(C::STEPS - 1, *reinterpret_cast<const uint32_t*>(k_tile + piece<DP, false>(row, 4 * C::FULL) + 4 * t),
-                    *reinterpret_cast<const uint32_t*>(k_tile + piece<DP, false>(row + 8, 4 * C::FULL) + 4 * t), 0u, 0u);
+                    *reinterpret_cast<const uint32_t*>(k_tile + piece<DP, false>(row + 8, 4 * C::FULL) + 4 * t));
           // Scales of keys g, g + 8: of keys, log2 and inverse of values (one that is none, or out of range: the values are as good as 0).
           float kf[2], lv[2];
 #pragma unroll
@@ -464,10 +422,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
           for (int h = 0; h < NR; ++h)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              float y = sum[h][QT - 1][e];
-#pragma unroll
-              for (int x = QT - 2; x >= 0; --x) y = fmaf(y, 1.f / 16, sum[h][x][e]);
-              s[i][h][e] = fmaf(y, kf[e >> 1] * factor[h][e & 1], lv[e >> 1]);
+              s[i][h][e] = fmaf(sum[0][h][e] + sum[1][h][e], kf[e >> 1] * factor[h][e & 1], lv[e >> 1]);
             }
         }
         if (keys < WK) {
