@@ -17,7 +17,8 @@ OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT_DIR, "libivit.so")
 SOURCES = ["gemm.cu", "gemm_pair.cu", "ops.cu", "attention.cu", "attention_rows.cu", "persistent.cu", "stream.cu", "engine.cu", "noalloc.cu",
            "action.cu", "step_plan.cu", "rope.cu", "tree_attention.cu", "tree_attention_tc.cu", "kv_write.cu",
-           "kv_quantise.cu", "tree_attention_quantised.cu", "tree_attention_quantised_fp16.cu", "tree_verify.cu"]
+           "kv_quantise.cu", "tree_attention_quantised.cu", "tree_attention_quantised_fp16.cu", "tree_attention_quantised_tc.cu",
+           "tree_verify.cu"]
 HEADERS = ["ptx.cuh", "internal.h", "select.cuh", "attention.cuh", "gelu.cuh", "backbone.cuh", "tree_attention.cuh", "tree_join.cuh", "quantised.cuh",
            "tree_attention_quantised.cuh"]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")

@@ -14,17 +14,24 @@ bool valid(const ivit_attention_config& c, const ivit_quantised_layout& l) {
   return valid_quantised(l) && valid_attention(c, l.kv_heads, l.page_size);
 }
 
+// More rows per key head than this take the tcgen05 kernel, where a group has at most 128 heads.
+constexpr int TC_ROWS = 16;
+
+// Tiles of 8 nr rows, or with tc the tcgen05 kernel's.
 struct Plan {
-  int dp, nr, ctas_per_sm, part_floats;
+  bool tc;
+  int dp, nr, tile_rows, ctas_per_sm, part_floats;
 };
 
 Plan plan(const ivit_attention_config& c, const ivit_quantised_layout& l) {
-  const long long rows = static_cast<long long>(c.max_new) * (c.heads / l.kv_heads);  // that share a key head
+  const int group = c.heads / l.kv_heads;
+  const long long rows = static_cast<long long>(c.max_new) * group;  // that share a key head
   const auto of = [&](auto d) {
     constexpr int DP = decltype(d)::value;
+    if (rows > TC_ROWS && group <= 128) return Plan{true, DP, 0, tree_tc_rows(group), DP <= 128 ? 2 : 1, tree_part_floats(128, DP)};
     if constexpr (DP <= MOST_DP)
-      if (rows > 8) return Plan{DP, 2, Cfg<DP, 2>::CTAS, Cfg<DP, 2>::PART};
-    return Plan{DP, 1, Cfg<DP, 1>::CTAS, Cfg<DP, 1>::PART};
+      if (rows > 8) return Plan{false, DP, 2, 16, Cfg<DP, 2>::CTAS, Cfg<DP, 2>::PART};
+    return Plan{false, DP, 1, 8, Cfg<DP, 1>::CTAS, Cfg<DP, 1>::PART};
   };
   return l.head_dim <= 64    ? of(std::integral_constant<int, 64>{})
          : l.head_dim <= 80  ? of(std::integral_constant<int, 80>{})
@@ -112,11 +119,12 @@ extern "C" int ivit_tree_attention_quantised(const ivit_attention_config* cfg, c
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // whole runs of all key heads, at least one (more CTAs than fit at a time wait for a place, not for each other)
   const int ctas = std::max(1, p.ctas_per_sm * std::min(TREE_MAX_SMS, sms) / cache->kv_heads) * cache->kv_heads;
-  a.tile_rows = 8 * p.nr;
+  a.tile_rows = p.tile_rows;
   a.err = static_cast<int*>(workspace_dev);
   a.joins = static_cast<int4*>(workspace_dev) + 1;
   a.parts = reinterpret_cast<float*>(a.joins + 2 * p.ctas_per_sm * TREE_MAX_SMS);
-  const cudaError_t e = cache->dtype == IVIT_BF16 ? launch_tree_attention_quantised_bf16(a, p.dp, p.nr, ctas, s)
-                                                  : launch_tree_attention_quantised_fp16(a, p.dp, p.nr, ctas, s);
+  const cudaError_t e = p.tc                        ? launch_tree_attention_quantised_tc(a, cache->dtype, p.dp, ctas, s)
+                        : cache->dtype == IVIT_BF16 ? launch_tree_attention_quantised_bf16(a, p.dp, p.nr, ctas, s)
+                                                    : launch_tree_attention_quantised_fp16(a, p.dp, p.nr, ctas, s);
   return e == cudaSuccess ? IVIT_OK : fail_cuda(e);
 }

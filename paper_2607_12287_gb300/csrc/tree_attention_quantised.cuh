@@ -665,4 +665,8 @@ cudaError_t launch(const QuantisedArgs& a, int dp, int nr, int ctas, cudaStream_
 cudaError_t launch_tree_attention_quantised_bf16(const QuantisedArgs& a, int dp, int nr, int ctas, cudaStream_t s);
 cudaError_t launch_tree_attention_quantised_fp16(const QuantisedArgs& a, int dp, int nr, int ctas, cudaStream_t s);
 
+// The form for many rows per key head (tree_attention_quantised_tc.cu), for groups of up to 128 heads: tiles of tree_tc_rows(group)
+// rows, two CTAs per SM (of dp 256 one).
+cudaError_t launch_tree_attention_quantised_tc(const QuantisedArgs& a, int dtype, int dp, int ctas, cudaStream_t s);
+
 }  // namespace ivit

@@ -233,13 +233,17 @@ def run_attention(pkg, c, mask, vis=None, check=True, scale=None, max_new=None, 
     pkg.ivit_tree_attention_quantised(*args)
     out, lse, ws = args[-3:]
     assert int(ws[:4].view(torch.int32)) == 0  # no wait of the kernel expired
-    if not check:
-        return out, lse
+    if check:
+        check_attention(c, out, lse, mask, vis, args[0].scale)
+    return out, lse
+
+
+def check_attention(c, out, lse, mask, vis, scale):
     sees = {"causal": lambda i, n: np.tril(np.ones((n, n), bool)), "all": lambda i, n: np.ones((n, n), bool),
             "tree": lambda i, n: vis[i]}[mask]
     kc, vc = (ref.decode(codes, s, c["block"]) for codes, s in c["caches"])
     want, want_lse, size = backbone_ref.attention(host(c["q"]), host(c["k"]), host(c["v"]), kc, vc, c["table"], c["lengths"], c["cu"],
-                                                  sees, args[0].scale)
+                                                  sees, scale)
     u = UNIT[c["dtype"]]
     bound = u * np.abs(want) + (u + 2.0 ** -14) * size + 2.0 ** -25
     err = np.abs(host(out) - want)
@@ -247,7 +251,6 @@ def run_attention(pkg, c, mask, vis=None, check=True, scale=None, max_new=None, 
     got, none = host(lse), np.isneginf(want_lse)
     assert np.array_equal(np.isneginf(got), none)
     assert (np.abs(got[~none] - want_lse[~none]) <= 2.0 ** -14).all()
-    return out, lse
 
 
 ATTENTION = [  # cached, new, heads, kv, dim, page, block, type, order
@@ -382,9 +385,10 @@ def test_pages_outside_the_cache_read_as_zeros(pkg):
                 codes[free], s[free] = 0, 1
             table[0, 1] = table[0, 3] = free
             zero["table"] = table
-            want, want_lse = run_attention(pkg, zero, "causal")
-            assert (np.abs(host(out) - host(want)) <= 2.0 ** -7 * np.abs(host(want)) + 2.0 ** -12).all()
-            assert (np.abs(host(lse) - host(want_lse)) <= 2.0 ** -13).all()
+            # (each against the definition: two results may be twice its bound apart, for their probabilities are rounded
+            # against other maxima)
+            check_attention(zero, out, lse, "causal", None, 64 ** -0.5)
+            run_attention(pkg, zero, "causal")
 
 
 def test_large_scores_and_growing_maximum(pkg):
