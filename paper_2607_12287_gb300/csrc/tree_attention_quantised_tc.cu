@@ -5,8 +5,8 @@
 // Warps of a CTA:
 //   0 - 3  softmax, thread = row = tensor-memory lane, as there; scores of cached keys are scaled and shifted by their blocks' scales.
 //   4      MMA: S = Q K^T of block i + 1 is issued before O += P V of block i.
-//   5, 6   K and V blocks through the ring: cached tokens' codes are read from global memory, a block of K or V ahead of the
-//          conversion, become 16-bit values of the rows' type (exact) and go where TMA would have put them, and their scales beside
+//   5 - 7  K and V blocks through the ring: cached tokens' codes come by asynchronous copies, some blocks ahead, each thread's to a place of
+//          its own, become 16-bit values of the rows' type (exact) and go where TMA would have put them, and their scales beside
 //          them; blocks of new rows come by TMA, as does the tile of Q.
 #include <cudaTypedefs.h>
 
@@ -18,9 +18,10 @@ namespace ivit {
 namespace {
 
 constexpr int AQ = 128;                // rows of a tile (MMA M)
-constexpr int TC_THREADS = 224;
+constexpr int FILL = 96;               // threads of the warps that fill the ring
+constexpr int TC_THREADS = 160 + FILL;
 constexpr int KB = 64;                 // keys of a block
-constexpr int SCALES = 8;              // blocks whose scales are kept: more than the ring and the softmax are apart
+constexpr int SCALES = 4;              // blocks whose scales are kept: V blocks in the ring, and one
 
 template <int DP>
 struct TcCfg {
@@ -31,15 +32,18 @@ struct TcCfg {
   static constexpr int T_BYTES = KB * Q_ROW, TILE = (T_BYTES + 1023) / 1024 * 1024;
   static constexpr int TM_O = KB, TM_P = KB + DP, TM_COLS = 512 / CTAS;  // S at column 0
   static_assert(TM_P + KB / 2 <= TM_COLS, "tensor memory of one CTA");
-  static constexpr int OFF_RING = AQ * Q_ROW, EXTRA = SCALES * 3 * KB * 4 + 1024 + 512;
-  static constexpr int FIT = ((CTAS == 2 ? 113 : 227) * 1024 - OFF_RING - EXTRA) / TILE, RING = FIT < 8 ? FIT : 8;
-  static constexpr int OFF_SCALES = OFF_RING + RING * TILE;     // [block % SCALES][of keys, log2 and inverse of values][KB]
+  static constexpr int PIECES = DP / 16, PASSES = (KB * PIECES + FILL - 1) / FILL;  // 16 codes each, of a row and of a thread
+  static constexpr int RAW = PASSES * FILL * 16;                // bytes of codes of a block
+  static constexpr int RING = DP <= 64 ? 6 : DP <= 96 ? 4 : 3, AHEAD = DP <= 96 ? 4 : 3;
+  static constexpr int OFF_RING = AQ * Q_ROW;
+  static constexpr int OFF_RAW = OFF_RING + RING * TILE;        // [block % AHEAD][pass][thread]
+  static constexpr int OFF_RAW_SCALES = OFF_RAW + AHEAD * RAW;  // [block % AHEAD][of keys, of values][KB]
+  static constexpr int OFF_SCALES = OFF_RAW_SCALES + AHEAD * 2 * KB * 4;  // [block % SCALES][of keys, log2 and inverse of values][KB]
   static constexpr int OFF_BAR = OFF_SCALES + SCALES * 3 * KB * 4;
   static constexpr int BYTES = OFF_BAR + 256 + 1024;  // with alignment slack
-  // codes of a block: CP lanes for the pieces of a row, RP rows at a time by 64 threads
-  static constexpr int CP = DP <= 64 ? 4 : DP <= 128 ? 8 : 16, RP = 64 / CP, LOADS = KB / RP;
-  static_assert(TREE_MAX_REQ * 8 <= OFF_SCALES, "the units before each request");
-  static_assert(RING >= 4 && RING / 2 + 2 < SCALES, "K and V of two blocks");
+  static_assert(TREE_MAX_REQ * 8 <= OFF_RAW, "the units before each request");
+  static_assert(CTAS * (BYTES + 1024 + 64) <= 228 * 1024, "shared memory of an SM");
+  static_assert(RING >= 3 && (RING + 1) / 2 + 1 <= SCALES, "V blocks in the ring, and the one that is multiplied");
 };
 
 struct TcBlocks {
@@ -180,7 +184,7 @@ __global__ void __launch_bounds__(TC_THREADS, TcCfg<DP>::CTAS)
     mbar_init(o_done, 1);
     mbar_init(o_free, 4);
     for (int i = 0; i < RING; ++i) {
-      mbar_init(t_full + 8 * i, 2);  // (a warp that fills has done its part)
+      mbar_init(t_full + 8 * i, FILL / 32);  // (a warp that fills has done its part)
       mbar_init(t_empty + 8 * i, 1);
     }
     fence_mbar_init();
@@ -225,12 +229,79 @@ __global__ void __launch_bounds__(TC_THREADS, TcCfg<DP>::CTAS)
     const uint64_t policy = l2_policy_evict_first();
     const uint32_t q_bytes = a.tile_rows * C::Q_ROW;
     const int tid2 = tid - 160, page_mask = (1 << a.cache.page_shift) - 1, dim = a.cache.dim;
-    const int cp = tid2 % C::CP, r0 = tid2 / C::CP;  // the thread's piece of a row, and its first row of a block
-    const bool piece = 16 * cp < dim, second = 16 * cp + 8 < dim;
+    // The place and the pages of the next cached block to be copied; its codes and scales.
+    TreePlace<B> next = run.at;
+    unsigned long long next_u = 0;
+    int next_kb = next.kt, next_end = 0, ids[C::PASSES], scale_id = -1;
+    const long long head = next.head * a.cache.head_stride;
+    const auto bounds = [&] {  // the next segment that has cached blocks, from `next` on
+      while (next_u < units) {
+        const int blocks = static_cast<int>(min(static_cast<unsigned long long>(next.nkt - next.kt), units - next_u));
+        next_end = min(next.kt + blocks, B::cached(next.r));
+        next_kb = next.kt;
+        if (next_kb < next_end) return;
+        next_u += blocks;
+        next.next_rows(a);
+      }
+    };
+    const auto look_up = [&] {
+      if (next_u >= units) return;
+      const int* table = a.table + static_cast<size_t>(next.req) * a.max_pages;
+      const auto page = [&](int row) {
+        const int key = next_kb * KB + row, id = row < KB && key < next.r.len ? table[key >> a.cache.page_shift] : -1;
+        return static_cast<unsigned>(id) < static_cast<unsigned>(a.cache.n_pages) ? id : -1;
+      };
+#pragma unroll
+      for (int x = 0; x < C::PASSES; ++x) ids[x] = page((tid2 + x * FILL) / C::PIECES);
+      scale_id = page(tid2);
+    };
+    uint32_t copied = 0;  // K and V blocks, in turn
+    const auto copy = [&] {
+      if (next_u < units) {
+        const bool values = copied & 1;
+        const uint32_t raw = sb + C::OFF_RAW + copied % C::AHEAD * C::RAW + tid2 * 16;
+        const uint8_t* from = static_cast<const uint8_t*>(values ? a.v_cache : a.k_cache) + head;
+#pragma unroll
+        for (int x = 0; x < C::PASSES; ++x) {
+          const int e = tid2 + x * FILL, row = e / C::PIECES, d = 16 * (e - row * C::PIECES);
+          const bool ok = ids[x] >= 0 && d < dim;
+          const uint8_t* src = ok ? from + ids[x] * a.cache.page_stride + ((next_kb * KB + row) & page_mask) * a.cache.token_stride + d : from;
+          const uint32_t to = raw + x * FILL * 16;
+          if (a.wide) {
+            copy16(to, src, ok);
+          } else {
+            copy8(to, src, ok);
+            const bool second = ok && d + 8 < dim;
+            copy8(to + 8, second ? src + 8 : src, second);
+          }
+        }
+        if (values) {
+          if (tid2 < KB) {
+            const bool ok = scale_id >= 0;
+            const long long at =
+                ok ? static_cast<long long>(((scale_id << a.cache.page_shift) + ((next_kb * KB + tid2) & page_mask)) >> a.block_shift) * a.cache.heads + next.head : 0;
+            const uint32_t to = sb + C::OFF_RAW_SCALES + (copied % C::AHEAD * 2 * KB + tid2) * 4;
+            copy4(to, a.k_scale + at, ok);
+            copy4(to + KB * 4, a.v_scale + at, ok);
+          }
+          if (++next_kb == next_end) {
+            next_u += static_cast<int>(min(static_cast<unsigned long long>(next.nkt - next.kt), units - next_u));
+            next.next_rows(a);
+            bounds();
+          }
+          look_up();
+        }
+      }
+      ++copied;
+      copies_commit();
+    };
+    bounds();
+    look_up();
+#pragma unroll 1
+    for (int x = 0; x < C::AHEAD; ++x) copy();
+
     TreePlace<B> p = run.at;
-    const uint8_t* const from[2] = {static_cast<const uint8_t*>(a.k_cache) + p.head * a.cache.head_stride + 16 * cp,
-                                    static_cast<const uint8_t*>(a.v_cache) + p.head * a.cache.head_stride + 16 * cp};
-    uint32_t t = 0;  // K / V blocks so far
+    uint32_t t = 0, converted = 0;  // K / V blocks so far, and cached ones
     for (uint32_t n = 0; u < units; ++n) {
       const int blocks = segment(p), cached = B::cached(p.r);
       if (!__all_sync(0xffffffffu, wait(q_empty, (n & 1) ^ 1))) break;
@@ -242,44 +313,6 @@ __global__ void __launch_bounds__(TC_THREADS, TcCfg<DP>::CTAS)
         if (TAIL > 0) tma_load_3d(sb + FULL * C::Q1, &maps.q.hi, 64 * FULL, head, row, q_full, policy);
       }
       __syncwarp();
-      const int* table = a.table + static_cast<size_t>(p.req) * a.max_pages;
-      // Pages of the thread's rows of a cached block, and of its key's scales (-1: none); codes of a K or V block; scales.
-      int ids[C::LOADS], scale_id = -1;
-      uint4 codes[C::LOADS];
-      float k_scale = 0.f, v_scale = 0.f;
-      const auto look_up = [&](int kb) {
-        const auto page = [&](int key) {
-          const int id = kb < cached && key < p.r.len ? table[key >> a.cache.page_shift] : -1;
-          return static_cast<unsigned>(id) < static_cast<unsigned>(a.cache.n_pages) ? id : -1;
-        };
-#pragma unroll
-        for (int x = 0; x < C::LOADS; ++x) ids[x] = page(kb * KB + r0 + x * C::RP);
-        scale_id = page(kb * KB + tid2);
-      };
-      const auto load = [&](int kb, int kv) {
-#pragma unroll
-        for (int x = 0; x < C::LOADS; ++x) {
-          codes[x] = make_uint4(0, 0, 0, 0);
-          if (ids[x] < 0 || !piece) continue;
-          const uint8_t* src = from[kv] + ids[x] * a.cache.page_stride + ((kb * KB + r0 + x * C::RP) & page_mask) * a.cache.token_stride;
-          if (a.wide) {
-            codes[x] = *reinterpret_cast<const uint4*>(src);
-          } else {
-            const uint2 lo = *reinterpret_cast<const uint2*>(src), hi = second ? *reinterpret_cast<const uint2*>(src + 8) : make_uint2(0, 0);
-            codes[x] = make_uint4(lo.x, lo.y, hi.x, hi.y);
-          }
-        }
-        if (kv == 0) {
-          k_scale = v_scale = 0.f;
-          if (scale_id >= 0) {
-            const long long at = static_cast<long long>(((scale_id << a.cache.page_shift) + ((kb * KB + tid2) & page_mask)) >> a.block_shift) * a.cache.heads + p.head;
-            k_scale = a.k_scale[at];
-            v_scale = a.v_scale[at];
-          }
-        }
-      };
-      look_up(p.kt);
-      if (p.kt < cached) load(p.kt, 0);
       bool ok = true;
       for (int i = 0; i < blocks && ok; ++i) {
         const int kb = p.kt + i;
@@ -289,35 +322,32 @@ __global__ void __launch_bounds__(TC_THREADS, TcCfg<DP>::CTAS)
           if (!ok) break;
           const uint32_t dst = sb + C::OFF_RING + slot * C::TILE, full = t_full + 8 * slot;
           if (kb < cached) {
-            uint8_t* tile = sm + C::OFF_RING + slot * C::TILE;
-            if (kv == 1) {  // (beside the values: their slot stays full until the block's probabilities have been multiplied)
+            copies_wait<C::AHEAD - 1>();  // (this thread's, of this block)
+            const int stage = converted++ % C::AHEAD;
+            if (kv == 1 && tid2 < KB) {  // (beside the values: their slot stays full until the block's probabilities have been multiplied)
+              const float* raw = reinterpret_cast<const float*>(sm + C::OFF_RAW_SCALES) + stage * 2 * KB + tid2;
               float* scales = reinterpret_cast<float*>(sm + C::OFF_SCALES) + (t / 2 % SCALES) * 3 * KB + tid2;
+              const float v_scale = raw[KB];
               const int b = __float_as_int(v_scale);
               const bool power = !(b & 0x7fffff), none = b < 0x00800000 || b >= 0x7f000000;
-              scales[0] = k_scale * a.score_log2;
+              scales[0] = raw[0] * a.score_log2;
               scales[KB] = none ? -100.f : power ? static_cast<float>((b >> 23) - 127) : __log2f(v_scale);
               scales[2 * KB] = none ? __int_as_float((100 + 127) << 23) : power ? __int_as_float(0x7f000000 - b) : __fdividef(1.f, v_scale);
             }
-            if (16 * cp < DP) {
-#pragma unroll
-              for (int x = 0; x < C::LOADS; ++x) {
-                const int row = r0 + x * C::RP;
-                uint4 lo, hi;
-                values16<T>(codes[x], lo, hi);
-                *reinterpret_cast<uint4*>(tile + chunk_at<DP>(row, 2 * cp)) = lo;
-                *reinterpret_cast<uint4*>(tile + chunk_at<DP>(row, 2 * cp + 1)) = hi;
-              }
+            uint8_t* tile = sm + C::OFF_RING + slot * C::TILE;
+#pragma unroll 2
+            for (int x = 0; x < C::PASSES; ++x) {
+              const int e = tid2 + x * FILL, row = e / C::PIECES, c = e - row * C::PIECES;
+              if (C::PASSES * FILL > KB * C::PIECES && row >= KB) break;
+              uint4 lo, hi;
+              values16<T>(*reinterpret_cast<const uint4*>(sm + C::OFF_RAW + stage * C::RAW + e * 16), lo, hi);
+              *reinterpret_cast<uint4*>(tile + chunk_at<DP>(row, 2 * c)) = lo;
+              *reinterpret_cast<uint4*>(tile + chunk_at<DP>(row, 2 * c + 1)) = hi;
             }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(full);
-            // the next block's loads, which arrive while its place is being freed
-            if (kv == 0) {
-              load(kb, 1);
-            } else if (kb + 1 < cached && i + 1 < blocks) {
-              look_up(kb + 1);
-              load(kb + 1, 0);
-            }
+            copy();
           } else if (elect_one()) {
             if (warp == 5) {
               mbar_arrive_expect_tx(full, C::T_BYTES);
