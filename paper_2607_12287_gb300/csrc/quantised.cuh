@@ -18,6 +18,14 @@ __device__ __forceinline__ uint32_t to_codes2(float lo, float hi) {
   return r;
 }
 
+// 8 and 4 bytes to shared memory (see copy16).
+__device__ __forceinline__ void copy8(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(ok ? 8 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(ok ? 4 : 0) : "memory");
+}
+
 // A paged cache of 8 bits of one layer (ivit_quantised_layout).
 struct QuantisedCache {
   int n_pages, page_shift, block_shift, heads, dim;

@@ -41,13 +41,6 @@ struct QuantisedKeys {
   static __device__ __forceinline__ int tiles(const TreeRequest& r) { return cached(r) + (r.n + TK - 1) / TK; }
 };
 
-__device__ __forceinline__ void copy8(uint32_t dst, const void* src, bool ok) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(ok ? 8 : 0) : "memory");
-}
-__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool ok) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(ok ? 4 : 0) : "memory");
-}
-
 constexpr int MOST_DP = 128;  // of tiles of 16 rows, whose outputs and queries take 7 / 8 DP registers
 
 // Heads of up to DP values, tiles of 8 NR rows.
