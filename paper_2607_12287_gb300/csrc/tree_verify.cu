@@ -132,6 +132,7 @@ __global__ void __launch_bounds__(THREADS) tree_verify_kernel(const VerifyArgs a
   // Calls f(v, step) for the thread's tokens v, v + step, ..., U at a time.
   constexpr int STEP = VEC ? 1 : 32;
   const auto tokens = [&](auto f) {
+#pragma unroll 2
     for (int base = v0 + warp * 32 * U; base < v1; base += THREADS * U) f(base + (VEC ? lane * U : lane));
   };
   const auto logits_of = [&](int row) { return static_cast<const L*>(a.logits) + row * a.logits_stride; };
@@ -187,72 +188,65 @@ __global__ void __launch_bounds__(THREADS) tree_verify_kernel(const VerifyArgs a
     n_tried = 0;
   };
 
-  int j = 1;  // the next row to look at
-  while (true) {
-    enter();
-    bool moved = false;
-    while (!moved) {
-      // the next row that hangs on `at`
-      int found = n;
-      if (!a.parent) {
-        if (j == at + 1 && j < n) found = j;
+  // The next row from j on that hangs on row `on`, n if there is none.
+  const auto next_draft = [&](int j, int on) {
+    if (!a.parent) return j == on + 1 && j < n ? j : n;
+    for (; j < n; j += 32) {
+      const unsigned bits = __ballot_sync(ALL, j + lane < n && a.parent[row0 + j + lane] == on);
+      if (bits) return j + __ffs(bits) - 1;
+    }
+    return n;
+  };
+  enter();
+  int found = next_draft(1, 0);
+  while (found < n) {
+    const int row = row0 + found, x = a.token[row];
+    bool ok = false, tested = x >= 0 && x < a.vocab;
+    if (!tested) {
+    } else if (greedy) {
+      ok = x == best;
+    } else {
+      const float e = weight(static_cast<float>(logits_of(row0 + at)[x]), top);
+      if (a.prob) {
+        const float q = a.prob[(row0 + at) * a.prob_stride + x];
+        ok = a.uniform[row] * total * q < fmaxf(e - taken * q, 0.f);
       } else {
-        for (; j < n; j += 32) {
-          const bool hit = j + lane < n && a.parent[row0 + j + lane] == at;
-          const unsigned bits = __ballot_sync(ALL, hit);
-          if (bits) {
-            found = j + __ffs(bits) - 1;
-            break;
-          }
+        bool again = false;
+        for (int i = 0; i < n_tried; ++i) again |= tried[i] == x;
+        ok = !again && a.uniform[row] * total < e;
+        if (!ok && !again) {
+          total = fmaxf(total - e, 0.f);
+          __syncthreads();  // (everyone has looked at the list)
+          if (tid == 0) tried[n_tried] = x;
+          ++n_tried;
+          __syncthreads();
         }
-      }
-      if (found >= n) break;
-      j = found + 1;
-      const int row = row0 + found, x = a.token[row];
-      if (x < 0 || x >= a.vocab) continue;
-      bool ok;
-      if (greedy) {
-        ok = x == best;
-      } else {
-        const float e = weight(static_cast<float>(logits_of(row0 + at)[x]), top);
-        if (a.prob) {
-          const float q = a.prob[(row0 + at) * a.prob_stride + x];
-          ok = a.uniform[row] * total * q < fmaxf(e - taken * q, 0.f);
-        } else {
-          bool again = false;
-          for (int i = 0; i < n_tried; ++i) again |= tried[i] == x;
-          ok = !again && a.uniform[row] * total < e;
-          if (!ok && !again) {
-            total = fmaxf(total - e, 0.f);
-            __syncthreads();  // (everyone has looked at the list)
-            if (tid == 0) tried[n_tried] = x;
-            ++n_tried;
-            __syncthreads();
-          }
-        }
-      }
-      if (ok) {
-        if (rank == 0 && tid == 0) a.path[row0 + accepted] = row;
-        ++accepted;
-        at = found;
-        moved = true;
-      } else if (!greedy && a.prob) {
-        taken += total;
-        const L* l_row = logits_of(row0 + at);
-        const float* q_row = a.prob + (row0 + at) * a.prob_stride;
-        float sum = 0.f, none = 0.f;
-        tokens([&](int v) {
-          float l[U], q[U];
-          load8<L, VEC>(l_row, v, v1, -INFINITY, l);
-          load8<float, VEC>(q_row, v, v1, 0.f, q);
-#pragma unroll
-          for (int i = 0; i < U; ++i) sum += fmaxf(weight(l[i], top) - taken * q[i], 0.f);
-        });
-        everywhere(sum, none, add);
-        total = sum;
       }
     }
-    if (!moved) break;
+    if (ok) {
+      if (rank == 0 && tid == 0) a.path[row0 + accepted] = row;
+      ++accepted;
+      at = found;
+      enter();
+      found = next_draft(at + 1, at);
+      continue;
+    }
+    found = next_draft(found + 1, at);
+    if (!tested || greedy || !a.prob) continue;
+    taken += total;
+    if (found >= n) break;  // (nothing is tried against what is left)
+    const L* l_row = logits_of(row0 + at);
+    const float* q_row = a.prob + (row0 + at) * a.prob_stride;
+    float sum = 0.f, none = 0.f;
+    tokens([&](int v) {
+      float l[U], q[U];
+      load8<L, VEC>(l_row, v, v1, -INFINITY, l);
+      load8<float, VEC>(q_row, v, v1, 0.f, q);
+#pragma unroll
+      for (int i = 0; i < U; ++i) sum += fmaxf(weight(l[i], top) - taken * q[i], 0.f);
+    });
+    everywhere(sum, none, add);
+    total = sum;
   }
 
   if (!greedy) {
