@@ -255,23 +255,32 @@ __global__ void __launch_bounds__(TC_THREADS, TcCfg<DP>::CTAS)
       for (int x = 0; x < C::PASSES; ++x) ids[x] = page((tid2 + x * FILL) / C::PIECES);
       scale_id = page(tid2);
     };
+    // The thread's pieces: from where in a page (-1: no piece of a head), and to where in a K or V block.
+    long long from_at[C::PASSES];
+    int to_at[C::PASSES];
+#pragma unroll
+    for (int x = 0; x < C::PASSES; ++x) {
+      const int e = tid2 + x * FILL, row = e / C::PIECES, c = e - row * C::PIECES;
+      from_at[x] = row < KB && 16 * c < dim ? (row & page_mask) * a.cache.token_stride + 16 * c : -1;
+      to_at[x] = row < KB ? chunk_at<DP>(row, 2 * c) : -1;
+    }
     uint32_t copied = 0;  // K and V blocks, in turn
     const auto copy = [&] {
       if (next_u < units) {
         const bool values = copied & 1;
         const uint32_t raw = sb + C::OFF_RAW + copied % C::AHEAD * C::RAW + tid2 * 16;
-        const uint8_t* from = static_cast<const uint8_t*>(values ? a.v_cache : a.k_cache) + head;
+        const uint8_t* const cache = static_cast<const uint8_t*>(values ? a.v_cache : a.k_cache) + head;
+        const uint8_t* const from = cache + (next_kb * KB & page_mask) * a.cache.token_stride;  // (a page above 64 tokens has whole blocks)
 #pragma unroll
         for (int x = 0; x < C::PASSES; ++x) {
-          const int e = tid2 + x * FILL, row = e / C::PIECES, d = 16 * (e - row * C::PIECES);
-          const bool ok = ids[x] >= 0 && d < dim;
-          const uint8_t* src = ok ? from + ids[x] * a.cache.page_stride + ((next_kb * KB + row) & page_mask) * a.cache.token_stride + d : from;
+          const bool ok = ids[x] >= 0 && from_at[x] >= 0;
+          const uint8_t* src = ok ? from + from_at[x] + ids[x] * a.cache.page_stride : cache;
           const uint32_t to = raw + x * FILL * 16;
           if (a.wide) {
             copy16(to, src, ok);
           } else {
             copy8(to, src, ok);
-            const bool second = ok && d + 8 < dim;
+            const bool second = ok && 16 * ((tid2 + x * FILL) % C::PIECES) + 8 < dim;
             copy8(to + 8, second ? src + 8 : src, second);
           }
         }
@@ -335,14 +344,14 @@ __global__ void __launch_bounds__(TC_THREADS, TcCfg<DP>::CTAS)
               scales[2 * KB] = none ? __int_as_float((100 + 127) << 23) : power ? __int_as_float(0x7f000000 - b) : __fdividef(1.f, v_scale);
             }
             uint8_t* tile = sm + C::OFF_RING + slot * C::TILE;
-#pragma unroll 2
+            const uint8_t* raw = sm + C::OFF_RAW + stage * C::RAW + tid2 * 16;
+#pragma unroll
             for (int x = 0; x < C::PASSES; ++x) {
-              const int e = tid2 + x * FILL, row = e / C::PIECES, c = e - row * C::PIECES;
-              if (C::PASSES * FILL > KB * C::PIECES && row >= KB) break;
+              if (C::PASSES * FILL > KB * C::PIECES && x == C::PASSES - 1 && to_at[x] < 0) break;
               uint4 lo, hi;
-              values16<T>(*reinterpret_cast<const uint4*>(sm + C::OFF_RAW + stage * C::RAW + e * 16), lo, hi);
-              *reinterpret_cast<uint4*>(tile + chunk_at<DP>(row, 2 * c)) = lo;
-              *reinterpret_cast<uint4*>(tile + chunk_at<DP>(row, 2 * c + 1)) = hi;
+              values16<T>(*reinterpret_cast<const uint4*>(raw + x * FILL * 16), lo, hi);
+              *reinterpret_cast<uint4*>(tile + to_at[x]) = lo;
+              *reinterpret_cast<uint4*>(tile + (to_at[x] ^ 16)) = hi;  // (the swizzles leave a pair of chunks beside each other)
             }
             fence_proxy_async_smem();
             __syncwarp();
