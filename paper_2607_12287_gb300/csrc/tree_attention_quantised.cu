@@ -14,8 +14,10 @@ bool valid(const ivit_attention_config& c, const ivit_quantised_layout& l) {
   return valid_quantised(l) && valid_attention(c, l.kv_heads, l.page_size);
 }
 
-// More rows per key head than this take the tcgen05 kernel, where a group has at most 128 heads.
-constexpr int TC_ROWS = 16;
+// More rows per key head than this take the tcgen05 kernel, where a group has at most 128 heads.  Both sides, 16 requests of up to
+// 8192 tokens, us: 32 rows of heads of 64 65 (tcgen05) and 43, of 128 112 and 72, of 256 233 and 258; 40 rows of 64 68 and 50, of 96
+// 80 and 84, of 128 114 and 90; 48 rows of 128 99 and 103 (fp16); 20 rows of 256 232 and 186.
+constexpr int tc_rows(int dp) { return dp <= 128 ? 40 : 24; }
 
 // Tiles of 8 nr rows, or with tc the tcgen05 kernel's.
 struct Plan {
@@ -28,7 +30,7 @@ Plan plan(const ivit_attention_config& c, const ivit_quantised_layout& l) {
   const long long rows = static_cast<long long>(c.max_new) * group;  // that share a key head
   const auto of = [&](auto d) {
     constexpr int DP = decltype(d)::value;
-    if (rows > TC_ROWS && group <= 128) return Plan{true, DP, 0, tree_tc_rows(group), DP <= 128 ? 2 : 1, tree_part_floats(128, DP)};
+    if (rows > tc_rows(DP) && group <= 128) return Plan{true, DP, 0, tree_tc_rows(group), DP <= 128 ? 2 : 1, tree_part_floats(128, DP)};
     if constexpr (DP <= MOST_DP)
       if (rows > 8) return Plan{false, DP, 2, 16, Cfg<DP, 2>::CTAS, Cfg<DP, 2>::PART};
     return Plan{false, DP, 1, 8, Cfg<DP, 1>::CTAS, Cfg<DP, 1>::PART};

@@ -180,16 +180,17 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
         }
       }
     };
-    if (ONE_BLOCK && key0 + TK <= load.r.len) {  // nearly all
+    if (ONE_BLOCK && a.wide && key0 + TK <= load.r.len) {  // nearly all
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const bool ok = inside(ids[half]);
         const long long step = ok ? RP * a.cache.token_stride : 0;
-        long long off = ok ? ids[half] * a.cache.page_stride + ((key0 + r0 + 16 * half) & page_mask) * a.cache.token_stride : 0;
+        const long long off = ok ? ids[half] * a.cache.page_stride + ((key0 + r0 + 16 * half) & page_mask) * a.cache.token_stride : 0;
+        const uint8_t *k = k_from + off, *v = v_from + off;
 #pragma unroll
-        for (int x = 0; x < COPIES / 2; ++x) {
-          both(half * (COPIES / 2) + x, off, ok);
-          off += step;
+        for (int x = half * (COPIES / 2); x < (half + 1) * (COPIES / 2); ++x, k += step, v += step) {
+          copy16(tile + k_to + x * RP * C::ROW, k, ok);
+          copy16(tile + v_place(x), v, ok);
         }
       }
       return;
