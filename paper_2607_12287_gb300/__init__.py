@@ -677,23 +677,32 @@ def _scales(t, name: str, layout: IvitQuantisedLayout) -> int:
 def _quantised_layers(cache: IvitQuantisedLayout, layers: int, k_cache, v_cache, k_scale, v_scale) -> tuple:
     """Pointers and layer strides of the caches [layers, pages, page_size, kv_heads, head_dim] and their scales [layers, pages,
     blocks, kv_heads]."""
-    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        _float8(t, name)
-        if len(t.shape) != 5 or t.shape[0] < layers or tuple(t.shape[1:]) != cache.shape or tuple(t.stride()[1:]) != cache.strides:
-            raise ValueError(f"{name}: shape {tuple(t.shape)} is not {layers} caches of the layout, {cache.shape}, with strides "
-                             f"{cache.strides}")
-    for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-        if t is None or isinstance(t, (int, np.ndarray)):
-            raise TypeError(f"{name}: a CUDA tensor is required")
-        if len(t.shape) != 4 or t.shape[0] < layers or tuple(t.shape[1:]) != cache.scales:
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [{layers}, {', '.join(map(str, cache.scales))}]")
-        _arg(t, name, "float32", 0)
-        _device_of(t, name)
-    cst = k_cache.stride()[0] if layers > 1 else 0
-    if layers > 1 and v_cache.stride()[0] != cst:
-        raise ValueError("k_cache, v_cache: the strides differ")
-    n_pages, blocks, heads = cache.scales
-    return k_cache.data_ptr(), v_cache.data_ptr(), cst, k_scale.data_ptr(), v_scale.data_ptr(), n_pages * blocks * heads
+    f8, f32, strides = _dtypes.get("float8_e4m3fn"), _dtypes.get("float32"), k_cache.stride() if type(k_cache) is _Tensor else None
+    # the common case: the checks below without formatting names
+    if not (type(k_cache) is type(v_cache) is type(k_scale) is type(v_scale) is _Tensor and k_cache.dtype is v_cache.dtype is f8
+            and k_scale.dtype is v_scale.dtype is f32 and k_cache.is_cuda and v_cache.is_cuda and k_scale.is_cuda and v_scale.is_cuda
+            and k_cache.shape == v_cache.shape and k_cache.shape[1:] == cache.shape and strides[1:] == cache.strides
+            and v_cache.stride() == strides and k_scale.shape == v_scale.shape and k_scale.shape[1:] == cache.scales
+            and len(k_cache.shape) == 5 and len(k_scale.shape) == 4 and k_cache.shape[0] >= layers and k_scale.shape[0] >= layers
+            and k_scale.is_contiguous() and v_scale.is_contiguous() and _current
+            and k_cache.get_device() == v_cache.get_device() == k_scale.get_device() == v_scale.get_device() == _current[1]()):
+        for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+            _float8(t, name)
+            if len(t.shape) != 5 or t.shape[0] < layers or tuple(t.shape[1:]) != cache.shape or tuple(t.stride()[1:]) != cache.strides:
+                raise ValueError(f"{name}: shape {tuple(t.shape)} is not {layers} caches of the layout, {cache.shape}, with strides "
+                                 f"{cache.strides}")
+        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t is None or isinstance(t, (int, np.ndarray)):
+                raise TypeError(f"{name}: a CUDA tensor is required")
+            if len(t.shape) != 4 or t.shape[0] < layers or tuple(t.shape[1:]) != cache.scales:
+                raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [{layers}, {', '.join(map(str, cache.scales))}]")
+            _arg(t, name, "float32", 0)
+            _device_of(t, name)
+        strides = k_cache.stride()
+        if layers > 1 and v_cache.stride()[0] != strides[0]:
+            raise ValueError("k_cache, v_cache: the strides differ")
+    return (k_cache.data_ptr(), v_cache.data_ptr(), strides[0] if layers > 1 else 0, k_scale.data_ptr(), v_scale.data_ptr(),
+            cache.scales[0] * cache.scales[1] * cache.scales[2])
 
 
 def _layer_rows(k, v, cache: IvitQuantisedLayout) -> tuple:
@@ -762,6 +771,10 @@ def _table(t, name: str, dtype_name: str, rows: int, width: int) -> tuple:
     """Pointer and row stride of a tensor [rows, width] whose rows are contiguous; (None, 0) for None."""
     if t is None:
         return None, 0
+    if type(t) is _Tensor and t.is_cuda and t.dtype is _dtypes[dtype_name] and t.dim() == 2:
+        sh, st = t.shape, t.stride()  # the common case: the checks below without formatting names
+        if sh[0] >= rows > 1 and sh[1] == width and st[1] == 1 and _current and t.get_device() == _current[1]():
+            return t.data_ptr(), st[0]
     if isinstance(t, (int, np.ndarray)):
         raise TypeError(f"{name}: a CUDA tensor is required")
     if t.device.type != "cuda":
