@@ -106,8 +106,9 @@ extern "C" int ivit_tree_attention_quantised(const ivit_attention_config* cfg, c
   const QuantisedCache c = quantised(*cache);
   a.cache = {c.n_pages, c.page_shift, c.heads, c.dim, c.page_stride, c.token_stride, c.head_stride};
   a.block_shift = c.block_shift;
-  a.wide = all_aligned({k_cache_dev, v_cache_dev}, 16) && c.dim % 16 == 0 && c.page_stride % 16 == 0 && c.token_stride % 16 == 0 &&
-           c.head_stride % 16 == 0;
+  const bool lines = all_aligned({k_cache_dev, v_cache_dev}, 16) && (c.page_stride | c.token_stride) % 16 == 0;
+  a.window = !p.tc && lines && (c.dim == 72 || c.dim == 88);
+  a.wide = a.window || (lines && c.dim % 16 == 0 && c.head_stride % 16 == 0);
   a.n_req = cfg->n_req;
   a.n_rows = n_rows;
   a.heads = cfg->heads;

@@ -29,6 +29,7 @@ struct QuantisedArgs : TreeArgs {    // scale_log2 is 1: running maxima are thos
   float score_log2;                  // scale * log2(e)
   int block_shift;
   bool wide;                         // copies of 16 bytes
+  bool window;                       // ... of heads of 72 or 88: of the 16-byte pieces that a head lies in
 };
 
 namespace {
@@ -116,11 +117,14 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
   if (!run.find<THREADS>(a, reinterpret_cast<unsigned long long*>(sm))) return;
   TreePlace<QuantisedKeys> load = run.at, at = run.at;
   const int units = static_cast<int>(run.hi - run.lo);
+  // Where a head begins in a row of codes: heads of 72 or 88 bytes lie 0 or 8 bytes behind a 16-byte boundary, and stay so (8-byte
+  // copies took 310 us instead of 227 for 32 requests of up to 16384 tokens, 16 heads of 72).
+  const int shift = C::PADDED && a.window ? load.head * a.cache.head_stride & 15 : 0;
   if (dim < DP) {
-    // bytes past a head's are zero for good: no copy touches them
-    const int words = (DP - dim) / 8;
-    for (int x = tid; x < STAGES * 2 * TK * words; x += THREADS) {
-      const int row = x / words, d = dim + 8 * (x - row * words), key = row & (TK - 1), tile = row / TK;
+    // bytes beside a head's are zero for good: no copy touches them
+    for (int x = tid; x < STAGES * 2 * TK * (DP / 8); x += THREADS) {
+      const int row = x / (DP / 8), d = 8 * (x - row * (DP / 8)), key = row & (TK - 1), tile = row / TK;
+      if (d >= shift && d < shift + dim) continue;
       *reinterpret_cast<uint2*>(sm + tile * C::TILE + (tile & 1 ? piece<DP, true>(key, d >> 4) : piece<DP, false>(key, d >> 4)) + (d & 8)) =
           make_uint2(0, 0);
     }
@@ -128,11 +132,12 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
 
   // A copy's part of this thread: piece cp of the rows r0, r0 + RP, ... of the warp's.
   const int cp = lane % C::CP, r0 = warp * WK + lane / C::CP, page_mask = (1 << a.cache.page_shift) - 1;
-  const bool copies = 16 * cp < dim, second = 16 * cp + 8 < dim;  // (the piece, and its second half, are the head's)
+  const bool first = 16 * cp >= shift, second = 16 * cp + 8 < shift + dim;  // (halves of the piece that are the head's)
+  const bool copies = 16 * cp < shift + dim;
   const uint32_t k_to = sb + piece<DP, false>(r0, cp), v_to = piece<DP, true>(r0, cp);
   const auto v_place = [&](int x) { return sb + C::TILE + (C::PADDED || DP == 64 ? v_to : v_to ^ ((x * RP & 7) << 4)) + x * RP * C::ROW; };
-  const uint8_t* const k_from = static_cast<const uint8_t*>(a.k_cache) + load.head * a.cache.head_stride + 16 * cp;
-  const uint8_t* const v_from = static_cast<const uint8_t*>(a.v_cache) + load.head * a.cache.head_stride + 16 * cp;
+  const uint8_t* const k_from = static_cast<const uint8_t*>(a.k_cache) + load.head * a.cache.head_stride - shift + 16 * cp;
+  const uint8_t* const v_from = static_cast<const uint8_t*>(a.v_cache) + load.head * a.cache.head_stride - shift + 16 * cp;
   // Scales: lane l's are those of the warp's key l (of common ones, keys 0 and 16).
   const uint32_t scale_to = sb + C::OFF_SCALES + (warp * WK + lane) * 4;
   // The pages of the tile at `load`, of those rows (of the two halves), and of the lane's scale; kept a tile ahead of the copies.
@@ -166,18 +171,14 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
     }
     if (!copies) return;
     const uint32_t tile = 2 * stage * C::TILE;
-    const auto both = [&](int x, long long off, bool ok) {
-      const uint32_t kd = tile + k_to + x * RP * C::ROW, vd = tile + v_place(x);
-      if (a.wide) {
-        copy16(kd, k_from + off, ok);
-        copy16(vd, v_from + off, ok);
+    const auto one = [&](uint32_t to, const uint8_t* from, bool ok) {
+      if (a.wide && first && second) {
+        copy16(to, from, ok);
+      } else if (a.wide) {
+        copy8(to + (first ? 0 : 8), from + (first ? 0 : 8), ok);
       } else {
-        copy8(kd, k_from + off, ok);
-        copy8(vd, v_from + off, ok);
-        if (second) {
-          copy8(kd + 8, k_from + off + 8, ok);
-          copy8(vd + 8, v_from + off + 8, ok);
-        }
+        copy8(to, from, ok);
+        if (second) copy8(to + 8, from + 8, ok);
       }
     };
     if (ONE_BLOCK && a.wide && key0 + TK <= load.r.len) {  // nearly all
@@ -189,8 +190,13 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
         const uint8_t *k = k_from + off, *v = v_from + off;
 #pragma unroll
         for (int x = half * (COPIES / 2); x < (half + 1) * (COPIES / 2); ++x, k += step, v += step) {
-          copy16(tile + k_to + x * RP * C::ROW, k, ok);
-          copy16(tile + v_place(x), v, ok);
+          if constexpr (C::PADDED) {
+            one(tile + k_to + x * RP * C::ROW, k, ok);
+            one(tile + v_place(x), v, ok);
+          } else {
+            copy16(tile + k_to + x * RP * C::ROW, k, ok);
+            copy16(tile + v_place(x), v, ok);
+          }
         }
       }
       return;
@@ -199,7 +205,9 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
     for (int x = 0; x < COPIES; ++x) {
       const int key = key0 + r0 + x * RP, id = ids[ONE_BLOCK ? 2 * x / COPIES : x];
       const bool ok = key < load.r.len && inside(id);
-      both(x, ok ? id * a.cache.page_stride + (key & page_mask) * a.cache.token_stride : 0, ok);
+      const long long off = ok ? id * a.cache.page_stride + (key & page_mask) * a.cache.token_stride : 0;
+      one(tile + k_to + x * RP * C::ROW, k_from + off, ok);
+      one(tile + v_place(x), v_from + off, ok);
     }
   };
 
@@ -324,8 +332,8 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
         float size = 0.f, mine = a.score_log2;
 #pragma unroll
         for (int s = 0; s < C::STEPS; ++s) {
-          const int d = value(s);
-          const uint2 w = 8 * h + g < rows && d < dim ? *reinterpret_cast<const uint2*>(from + d) : make_uint2(0, 0);
+          const int d = value(s) - shift;
+          const uint2 w = 8 * h + g < rows && d >= 0 && d < dim ? *reinterpret_cast<const uint2*>(from + d) : make_uint2(0, 0);
           q[h][s][0] = w.x;
           q[h][s][1] = w.y;
         }
@@ -502,12 +510,12 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
         bool odd = false;
 #pragma unroll
         for (int c = 0; c < C::PIECES; ++c) {
-          const int d = 16 * c + 2 * g;
+          const int d = 16 * c + 2 * g - shift;
           uint32_t w[4];  // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int key = 2 * t + (i & 1) + 8 * (i >> 1);
-            w[i] = key < keys && d < dim ? *reinterpret_cast<const uint32_t*>(v_new + key * a.v_new_stride + d) : 0u;
+            w[i] = key < keys && d >= 0 && d < dim ? *reinterpret_cast<const uint32_t*>(v_new + key * a.v_new_stride + d) : 0u;
             // Values that are not finite would reach rows that do not see them (0 * NaN): left out here, added below.
             const bool lo = odd16<T>(w[i]), hi = odd16<T>(w[i] >> 16);
             if (lo) w[i] &= 0xffff0000u;
@@ -533,8 +541,8 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
                 if (row >= rows || !(seen(a, at.r, node_of(row), k0 & ~31) >> ((k0 & 16) + k) & 1)) continue;
 #pragma unroll
                 for (int c = 0; c < C::PIECES; ++c)
-                  if (16 * c + 2 * g < dim) {
-                    const float2 x = unpack2<T>(*reinterpret_cast<const uint32_t*>(v_new + k * a.v_new_stride + 16 * c + 2 * g));
+                  if (const int d = 16 * c + 2 * g - shift; d >= 0 && d < dim) {
+                    const float2 x = unpack2<T>(*reinterpret_cast<const uint32_t*>(v_new + k * a.v_new_stride + d));
                     if (!isfinite(x.x)) o[h][c][r] += x.x;
                     if (!isfinite(x.y)) o[h][c][2 + r] += x.y;
                   }
@@ -596,8 +604,9 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
     float* part = a.parts + static_cast<size_t>(2 * blockIdx.x + (u > tiles ? 1 : 0)) * C::PART;
 #pragma unroll 1
     for (int e = tid; e < rows * (DP / 4); e += THREADS) {
-      const int row = e / (DP / 4), col = e - row * (DP / 4);
-      const float4 y = *reinterpret_cast<const float4*>(meet + row * C::MEET + 4 * col);
+      const int row = e / (DP / 4), col = e - row * (DP / 4);  // (columns of the output)
+      if (4 * col >= dim) continue;
+      const float4 y = *reinterpret_cast<const float4*>(meet + row * C::MEET + 4 * col + shift);
       float top = -INFINITY, sum = 0.f;
       float2 of[WARPS];
 #pragma unroll
@@ -611,9 +620,8 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
         const int x = at.rt * M + row, nd = x / a.group, h = at.head * a.group + x - nd * a.group;
         const long long orow = at.r.row0 + nd;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        if (4 * col < dim)
-          *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * dim + 4 * col) =
-              make_uint2(pack2<T>(y.x * inv, y.y * inv), pack2<T>(y.z * inv, y.w * inv));
+        *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + orow * a.out_stride + static_cast<long long>(h) * dim + 4 * col) =
+            make_uint2(pack2<T>(y.x * inv, y.y * inv), pack2<T>(y.z * inv, y.w * inv));
         if (a.lse && col == 0) a.lse[orow * a.heads + h] = (top + (log2f(sum) - TREE_SHIFT)) * 0.6931471805599453f;
       } else {
         reinterpret_cast<float4*>(part + row * DP)[col] = y;
