@@ -13,6 +13,12 @@ example shows is how the operators work together:
     ivit_kv_write        keys and values of the accepted drafts of all layers into their slots
 
 With greedy verification the trees give the same tokens as decoding one at a time, in fewer passes.
+
+``sample`` does the same over a cache of 8 bits, with drafts that are drawn from a drafter's probabilities:
+
+    ivit_tree_attention_quantised  the new rows over the cached tokens' codes and over each other
+    ivit_tree_verify               which drafts are right, and the next token, from given random numbers
+    ivit_kv_quantise               the accepted rows of all layers into their slots, in 8 bits
 """
 from __future__ import annotations
 
@@ -72,12 +78,19 @@ class Backbone:
         self.held, self.ring_at = self.length + new, ring_at
         return cu, slots, pos, mask if words else None
 
+    def workspace(self, cfg):
+        return ivit.ivit_tree_attention_workspace(cfg, self.layout)
+
+    def attend(self, layer, cfg, q, k, v, cu, mask, out, ws):
+        ivit.ivit_tree_attention(cfg, self.layout, q, k, v, self.k_cache[layer], self.v_cache[layer], self.table,
+                                 _i32(self.length), cu, mask, out, None, ws)
+
     def forward(self, x, cu, positions, mask_mode, mask, slots=None):
         """Logits of new rows x, and their keys and values per layer; into the cache at once if they have ``slots``."""
         self.passes += 1
         n = x.shape[0]
         cfg = ivit.make_attention_config(1, self.heads, TABLE, n, mask_mode, 0 if mask is None else mask.shape[1], self.hd ** -0.5)
-        ws = torch.empty(ivit.ivit_tree_attention_workspace(cfg, self.layout), dtype=torch.uint8, device="cuda")
+        ws = torch.empty(self.workspace(cfg), dtype=torch.uint8, device="cuda")
         keys, values = [], []
         for layer in range(self.layers):
             qkv = torch.nn.functional.rms_norm(x.float(), x.shape[-1:]).bfloat16() @ self.w_qkv[layer].T
@@ -86,8 +99,7 @@ class Backbone:
             ivit.ivit_qk_norm_rope(self.rope, q, k, v if put else None, self.norm, self.norm, positions, self.freq, self.axis, q, k,
                                    *put)  # (in place, in the projection's output)
             out = torch.empty((n, self.heads, self.hd), dtype=torch.bfloat16, device="cuda")
-            ivit.ivit_tree_attention(cfg, self.layout, q, k, v, self.k_cache[layer], self.v_cache[layer], self.table,
-                                     _i32(self.length), cu, mask, out, None, ws)
+            self.attend(layer, cfg, q, k, v, cu, mask, out, ws)
             x = x + out.flatten(1) @ self.w_o[layer].T
             keys.append(k)
             values.append(v)
@@ -119,6 +131,52 @@ class Backbone:
         ivit.ivit_kv_write(self.layout, k, v, _i32(*path), slots, self.k_cache, self.v_cache)
         self.length += len(path)
         return said
+
+
+class QuantisedBackbone(Backbone):
+    """The same over a cache of 8 bits, with a scale for each ``block`` tokens of a page and key head."""
+
+    def __init__(self, *args, block=8, **kw):
+        super().__init__(*args, **kw)
+        shape = self.k_cache.shape
+        self.k_cache, self.v_cache = (torch.zeros(shape, dtype=torch.float8_e4m3fn, device="cuda") for _ in range(2))
+        self.k_scale, self.v_scale = (torch.zeros((*shape[:2], PAGE // block, self.kv), device="cuda") for _ in range(2))
+        self.layout = ivit.make_quantised_layout(self.k_cache[0], block)
+
+    def workspace(self, cfg):
+        return ivit.ivit_tree_attention_quantised_workspace(cfg, self.layout)
+
+    def attend(self, layer, cfg, q, k, v, cu, mask, out, ws):
+        ivit.ivit_tree_attention_quantised(cfg, self.layout, q, k, v, self.k_cache[layer], self.v_cache[layer], self.k_scale[layer],
+                                           self.v_scale[layer], self.table, _i32(self.length), cu, mask, out, None, ws)
+
+    def write(self, k, v, rows, slots):
+        ivit.ivit_kv_quantise(self.layout, k, v, rows, slots, self.k_cache, self.v_cache, self.k_scale, self.v_scale)
+
+    def forward(self, x, cu, positions, mask_mode, mask, slots=None):
+        logits, k, v = super().forward(x, cu, positions, mask_mode, mask)
+        if slots is not None:  # a prompt's rows, all of them
+            self.write(k, v, torch.arange(x.shape[0], dtype=torch.int32, device="cuda"), slots)
+        return logits, k, v
+
+    def sampled_step(self, tokens, parents, probs, temperature, generator):
+        """One pass over a tree of drafts, of which those behind a node were drawn from its row of ``probs``: the tokens that
+        follow the root, distributed as if the backbone had been sampled token by token."""
+        n = len(tokens)
+        parents = _i32(*parents)
+        cu, slots, positions, mask = self.plan(n, parents)
+        logits, k, v = self.forward(self.embed[tokens.long()], cu, positions, "tree", mask)
+        vocab = logits.shape[1]
+        uniform = torch.rand(n, generator=generator, device="cuda")
+        noise = torch.empty((1, vocab), device="cuda").exponential_(generator=generator)
+        path, accepted, after = (torch.empty(m, dtype=torch.int32, device="cuda") for m in (n, 1, 1))
+        cfg = ivit.make_verify_config(1, vocab, n, "float32")
+        ivit.ivit_tree_verify(cfg, logits, probs, tokens, parents, cu, torch.full((1,), temperature, device="cuda"), uniform, noise,
+                              path, accepted, after)
+        self.write(k, v, path, slots)  # (rows that were not accepted are -1 there)
+        count = int(accepted)
+        self.length += count
+        return tokens[path[1:count].long()].tolist() + [int(after)]
 
 
 def encode(seed=0):
@@ -156,8 +214,29 @@ def decode(count=40, seed=0, drafts=4, right=0.8):
     return said[:count], found[:count], one.passes, tree.passes
 
 
+def sample(count=40, seed=0, drafts=3, temperature=0.7):
+    """``count`` tokens over a cache of 8 bits, by trees of two candidates behind each of ``drafts`` nodes that a drafter, which knows
+    the last token alone, draws from its probabilities: the tokens, and the passes that they took."""
+    tokens, h, w = encode(seed)
+    b = QuantisedBackbone(tokens.shape[1], seed)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    bigram = torch.softmax(b.embed.float() @ b.w_out.T / temperature, 1)
+    said = [b.prompt(tokens, h, w)]
+    while len(said) < count:
+        nodes, parents = [said[-1]], [-1]
+        for node in range(drafts):  # (breadth first: two behind the root, two behind the first of them, ...)
+            nodes += torch.multinomial(bigram[nodes[node]], 2, replacement=True, generator=g).tolist()
+            parents += [node, node]
+        ids = _i32(*nodes)
+        said += b.sampled_step(ids, parents, bigram[ids.long()].contiguous(), temperature, g)
+    return said[:count], b.passes
+
+
 if __name__ == "__main__":
     said, found, passes_one, passes_tree = decode()
     print("one at a time:", said)
     print("by trees:     ", found)
     print(f"{'the same' if said == found else 'DIFFERENT'}; {passes_one} passes against {passes_tree}")
+    said, passes = sample()
+    print("sampled, 8-bit cache:", said)
+    print(f"{passes} passes")

@@ -418,6 +418,7 @@ typedef struct ivit_quantised_layout {
  * layer strides in elements, multiples of 8) into slot slot_dev[i] of every layer's cache, for i < n; entries whose row is outside
  * [0, n_src) or whose slot is outside the cache are skipped, slots of a call are distinct, and those of one block lie
  * next to each other in the list (skipped ones may be between), as those of ivit_step_plan do.
+ * At most 2^20 entries and 4096 layers.
  * Of a block that is written, tokens before the last written one stay, if they are not written themselves, and what lies
  * behind it is of no meaning from then on (a block whose first token is written with the rest behind it starts afresh, so
  * that a page's next owner finds no old scale).  The new scale is the smallest power of two from 2^-60 to 2^60 by which
@@ -440,10 +441,12 @@ int ivit_kv_dequantise(const ivit_quantised_layout* cache, int32_t n_layers, int
 
 /* ivit_tree_attention over a cache of 8 bits: the operation, arguments, limits and workspace rules are those given
  * there, with cached keys code * k_scale and values code * v_scale; new rows (q, k_new, v_new, out) are of the layout's
- * 16-bit type.  Scales other than ivit_kv_quantise's have to be positive and within 2^-60 .. 2^60 (one that is not positive counts as
- * none: 0 for keys, 2^-100 for values).  Codes enter the products as they are, exactly, as 16-bit values; a block's scale
- * of keys multiplies their scores and one of values their probabilities, in fp32.  Probabilities enter the product
- * with V as sums of two 16-bit values up to 16 rows (new rows x heads of the group) per key head and as one above. */
+ * 16-bit type.  Scales other than ivit_kv_quantise's have to be positive and within 2^-60 .. 2^60 (one that is not a positive
+ * number counts as 0 for keys and 2^-100 for values).  Codes enter the products as they are, as 16-bit values that hold them exactly; a
+ * block's scale of keys multiplies their scores and one of values their probabilities, in fp32.  Up to 40 rows (new rows x heads of
+ * the group) per key head, 24 for heads above 128, probabilities of cached keys enter the product with V as one fp16 value for bf16
+ * rows and two for fp16 ones, above as one of the rows' type; those of new rows as two of that type or, above, one.
+ * bf16 queries are scaled by powers of two to fp16 up to there (exact but for values 2^-28 of a row's largest and less). */
 size_t ivit_tree_attention_quantised_workspace(const ivit_attention_config* cfg, const ivit_quantised_layout* cache);
 int ivit_tree_attention_quantised(const ivit_attention_config* cfg, const ivit_quantised_layout* cache, int32_t n_rows,
                                   const void* q_dev, int64_t q_stride, const void* k_new_dev, int64_t k_new_stride,

@@ -25,7 +25,7 @@ namespace {
 constexpr int THREADS = 256, WARPS = THREADS / 32;                 // reading
 constexpr int W_THREADS = 128, W_WARPS = W_THREADS / 32;           // writing
 constexpr int MIN_E = -60, MAX_E = 60;
-constexpr int MAX_ROWS = 1 << 30;
+constexpr int MAX_ROWS = 1 << 30, MAX_WRITTEN = 1 << 20, MAX_LAYERS = 4096;
 
 struct QuantiseArgs {
   const void *k, *v;
@@ -448,8 +448,8 @@ extern "C" int ivit_kv_quantise(const ivit_quantised_layout* cache, int32_t n_la
   using namespace ivit;
   if (!cache || n_layers < 0 || n < 0 || n_src < 0)
     return fail(IVIT_ERR_ARG, "ivit_kv_quantise: null cache layout or a negative size");
-  if (!valid_quantised(*cache) || n > MAX_ROWS)
-    return fail(IVIT_ERR_SHAPE, "ivit_kv_quantise: cache layout not supported, or more than 2^30 entries");
+  if (!valid_quantised(*cache) || n > MAX_WRITTEN || n_layers > MAX_LAYERS)
+    return fail(IVIT_ERR_SHAPE, "ivit_kv_quantise: cache layout not supported, more than 2^20 entries or 4096 layers");
   if (row_stride < 0 || layer_stride < 0 || cache_layer_stride < 0 || scale_layer_stride < 0 || row_stride % 8 ||
       layer_stride % 8 || cache_layer_stride % 8)
     return fail(IVIT_ERR_ARG, "ivit_kv_quantise: strides must not be negative, and multiples of 8 (of scales any)");
@@ -467,8 +467,6 @@ extern "C" int ivit_kv_quantise(const ivit_quantised_layout* cache, int32_t n_la
   // A chunk's layers are CTAs of their own up to some waves of them (rows of a layer lie together: with all layers of a chunk to a CTA,
   // 256 requests' drafts took 126 us instead of 99), or several where there are few, each with a unit for every warp.
   const long long chunks = (n + CHUNK - 1) / CHUNK, places = 5LL * sms;
-  if (chunks > 65535 || n_layers > 65535)
-    return fail(IVIT_ERR_SHAPE, "ivit_kv_quantise: more than 2^21 entries or 65535 layers");
   a.layers = static_cast<int>(std::max(1LL, std::min<long long>(n_layers, chunks * n_layers / (16 * places))));
   const int groups = (n_layers + a.layers - 1) / a.layers;
   const long long most = std::min<long long>(n, CHUNK) * 2 * ((cache->kv_heads + 2 * W_WARPS - 1) / (2 * W_WARPS));

@@ -105,6 +105,75 @@ def test_kv_quantise(pkg, layers, requests, kv, dim, page, block, dtype, order):
     check_write(pkg, k, v, rows, slots, caches, block, dtype, order)
 
 
+def test_skipped_entries_between_those_of_a_block(pkg):
+    # runs of skipped entries inside a block's, some longer than what a block's CTA looks at together, and at both ends
+    r = np.random.default_rng(41)
+    for gap in (1, 30, 200, 700):
+        requests = [(3, 9), (40, 20), (64, 33)]
+        k, v, rows, slots, caches = write_case(r, 2, requests, 2, 72, 32, 16, "bfloat16", "token")
+        at = np.sort(r.choice(len(rows) + 1, 6, replace=False))
+        fill = lambda x, with_what: np.insert(x, np.repeat(at, gap), with_what)
+        check_write(pkg, k, v, fill(rows, 0), fill(slots, -1), caches, 16, "bfloat16", "token")
+        check_write(pkg, k, v, fill(rows, -1), fill(slots, -1), caches, 16, "bfloat16", "token", repeat=1)
+    # a list of which nothing counts
+    check_write(pkg, k, v, np.full(50, -1), np.arange(50), caches, 16, "bfloat16", "token", repeat=1)
+    check_write(pkg, k, v, np.zeros(50, np.int64), np.full(50, -7), caches, 16, "bfloat16", "token", repeat=1)
+
+
+def test_writes_and_reads_on_another_stream_and_in_a_graph(pkg):
+    import torch
+    r = np.random.default_rng(42)
+    k, v, rows, slots, caches = write_case(r, 3, [(5, 40), (0, 3)], 4, 64, 16, 8, "float16", "token")
+    kc, vc, ks, vs, lay = check_write(pkg, k, v, rows, slots, caches, 8, "float16", "token", repeat=1)
+    want = [codes_of(kc), codes_of(vc), host(ks), host(vs)]
+    back = [torch.zeros((3, len(slots), 4, 64), dtype=torch.float16, device="cuda") for _ in range(4)]
+    rows, slots = i32(rows), i32(slots)
+    pkg.ivit_kv_dequantise(lay, slots, kc, vc, ks, vs, back[0], back[1])
+    fresh = lambda: [codes_on_gpu(caches[0][0]), codes_on_gpu(caches[1][0]), dev(caches[0][1]), dev(caches[1][1])]
+    one, two, side = fresh(), fresh(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        pkg.ivit_kv_quantise(lay, k, v, rows, slots, *one)
+        pkg.ivit_kv_dequantise(lay, slots, *one, back[2], back[3])
+    side.synchronize()
+    same = lambda c: all(np.array_equal(a, b, equal_nan=True) for a, b in zip([codes_of(c[0]), codes_of(c[1]), host(c[2]), host(c[3])], want))
+    assert same(one) and torch.equal(back[0], back[2]) and torch.equal(back[1], back[3])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pkg.ivit_kv_quantise(lay, k, v, rows, slots, *two)
+        pkg.ivit_kv_dequantise(lay, slots, *two, back[2], back[3])
+    for _ in range(2):
+        for x, y in zip(two, fresh()):
+            x.view(torch.uint8).copy_(y.view(torch.uint8))
+        back[2].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(two) and torch.equal(back[0], back[2])
+
+
+def test_of_nothing(pkg):
+    # no entries, no rows, no layers, requests without rows: nothing is touched
+    import torch
+    codes, scale = np.full((1, 2, 8, 2, 16), 0x33, np.uint8), np.full((1, 2, 2, 2), 0.5, np.float32)
+    kc, vc, ks, vs = codes_on_gpu(codes), codes_on_gpu(codes), dev(scale), dev(scale)
+    lay = pkg.make_quantised_layout(kc[0], 4)
+    k = torch.ones((1, 3, 2, 16), dtype=torch.bfloat16, device="cuda")
+    pkg.ivit_kv_quantise(lay, k, k, i32([]), i32([]), kc, vc, ks, vs)
+    pkg.ivit_kv_quantise(lay, k[:, :0], k[:, :0], i32([0]), i32([0]), kc, vc, ks, vs)
+    pkg.ivit_kv_quantise(lay, k[:0], k[:0], i32([0]), i32([0]), kc, vc, ks, vs)
+    pkg.ivit_kv_dequantise(lay, i32([]), kc, vc, ks, vs, k[:, :0], k[:, :0])
+    assert np.array_equal(codes_of(kc), codes) and np.array_equal(host(ks), scale) and (k == 1).all()
+    cfg = pkg.make_verify_config(3, 10, 4, "float32")
+    path, accepted, after = i32([5]), i32([7, 7, 7]), i32([7, 7, 7])
+    pkg.ivit_tree_verify(cfg, torch.zeros((0, 10), device="cuda"), None, i32([]), None, i32([0, 0, 0, 0]), None, None, None, path, accepted, after)
+    assert accepted.tolist() == [0, 0, 0] and after.tolist() == [-1, -1, -1] and path.tolist() == [5]
+    c = attention_case(np.random.default_rng(1), [20, 30], [0, 2], 2, 2, 64, 8, 8, "bfloat16")
+    c["cu"] = np.zeros(3, np.int64)
+    args = call(pkg, c, "causal", max_new=50, fill=3.0)
+    pkg.ivit_tree_attention_quantised(*args)
+    assert (args[-3] == 3).all() and (args[-2] == 3).all()
+
+
 def test_a_block_grows_token_by_token(pkg):
     # every call adds a token to the block: its scale follows the largest so far, the codes are rounded again
     import torch
@@ -479,6 +548,42 @@ def test_on_another_stream_and_in_a_graph(pkg):
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(args[-3], want) and torch.equal(args[-2], want_lse)
+
+
+def test_bounds_that_are_not_reached_and_lengths_beyond_the_table(pkg):
+    # max_new chooses the kernel: one row of many that were allowed; lengths longer than the table count as its tokens
+    r = np.random.default_rng(14)
+    for dim in (64, 72, 128, 256):
+        c = attention_case(r, [100, 33], [1, 2], 4, 2, dim, 16, 16, "float16")
+        want, want_lse = run_attention(pkg, c, "causal")
+        run_attention(pkg, c, "causal", max_new=60000)
+        c["table"] = c["table"][:, :7]
+        c["lengths"] = np.array([112, 33])
+        for codes, s in c["caches"]:
+            codes[c["table"][0, 6]] = 0x11
+            s[c["table"][0, 6]] = 0.25
+        want, want_lse = run_attention(pkg, c, "causal")
+        c["lengths"] = np.array([5000, 33])
+        got, got_lse = run_attention(pkg, c, "causal", check=False)
+        assert bool((got == want).all()) and bool((got_lse == want_lse).all())
+
+
+def test_two_calls_at_once(pkg):
+    # two streams, a workspace each
+    import torch
+    r = np.random.default_rng(15)
+    cases = [attention_case(r, [900, 400, 10], new, 8, 2, 128, 16, 16, "bfloat16") for new in ([1, 1, 1], [30, 40, 2])]
+    want = [run_attention(pkg, c, "causal") for c in cases]
+    args = [call(pkg, c, "causal") for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for a, s in zip(args, streams):
+            with torch.cuda.stream(s):
+                pkg.ivit_tree_attention_quantised(*a)
+    torch.cuda.synchronize()
+    for a, (out, lse) in zip(args, want):
+        assert torch.equal(a[-3], out) and torch.equal(a[-2], lse)
 
 
 # --------------------------------------------------------------------- verification

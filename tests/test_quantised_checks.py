@@ -66,6 +66,8 @@ def test_write_and_read_pointers_and_strides(lib):
     for f in (quantise, dequantise):
         assert f(lib, None) == f(lib, layout(), layers=-1) == f(lib, layout(), n=-1) == pkg.IVIT_ERR_ARG
         assert f(lib, layout(), n=(1 << 30) + 1) == pkg.IVIT_ERR_SHAPE
+    assert quantise(lib, layout(), n=(1 << 20) + 1) == quantise(lib, layout(), layers=4097) == pkg.IVIT_ERR_SHAPE
+    for f in (quantise, dequantise):
         for change in (dict(k=None), dict(v=None), dict(slot=None), dict(kc=None), dict(vc=None), dict(ks=None), dict(vs=None),
                        dict(k=ODD8), dict(v=ODD8), dict(kc=ODD4), dict(vc=ODD4), dict(ks=ODD), dict(vs=ODD), dict(slot=ODD), dict(rs=4),
                        dict(ls=-8), dict(cs=4), dict(ss=-1)):
