@@ -13,7 +13,14 @@
 // group), 128 keys at a time, first the cached tokens, then the new rows; 32 keys of a tile belong to each of the four warps, which
 // walk on without barriers.  Rows are columns of the products: S^T = K q^T, O^T = V^T P^T.  The order of a head's values
 // in a product is free, so a lane reads 16 consecutive codes of a key in one load; of V, transposed loads give two values of two
-// tokens, of which a byte permutation makes an operand.  New rows are few and stay in their own type, read from global memory.
+// tokens, of which a byte permutation and two conversions make an operand.  New rows are few and stay in their own type, read from
+// global memory, in a loop of their own behind that of the cached keys.
+//
+// Bound: latency and instructions (32 requests of up to 16384 tokens, 32 + 8 heads of 128, 104 us: 5330 GB/s of 128 bytes a
+// key and head; 750 warp instructions to 32 keys, 44 % issue at 12 warps an SM).  Rows as columns halve the products and the outputs'
+// registers of a step of 8 rows (153 -> 135 us); two CTAs an SM with three stages were slower than three with two (124 and 110), heads that
+// lie together in a row read by one CTA gave nothing (one key head and eight are alike).  Others, us: 16 + 4 heads of 64 39, of 256
+// 143, 16 heads of 80 164, of 72 231 (8-byte halves of their pieces), blocks of 8 tokens instead of 16 117.
 #pragma once
 
 #include <algorithm>
