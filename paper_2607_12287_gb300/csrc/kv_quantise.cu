@@ -173,15 +173,19 @@ __global__ void __launch_bounds__(W_THREADS, 5) kv_quantise_kernel(const Quantis
   // Blocks that begin among the chunk's entries: an entry whose nearest one before it that counts is of another block.
   static_assert(CHUNK == 32, "an entry to a lane");
   const int slot0 = slots[lane];
-  bool first = a.cache.holds(slot0);
-  if (first) {
-    for (int e = lane - 1; i0 + e >= 0; --e) {
-      const int s = e >= 0 ? slots[e] : a.slot[i0 + e];
-      if (!a.cache.holds(s)) continue;
-      first = s >> a.cache.block_shift != slot0 >> a.cache.block_shift;
+  const unsigned holding = __ballot_sync(ALL, a.cache.holds(slot0)), holding_before = holding & ((1u << lane) - 1);
+  int before = -1;  // of the chunk's first entry that counts, the nearest slot in front of the chunk
+  if (holding)
+    for (int j = i0 - 32; j > -32; j -= 32) {
+      const int s = j + lane >= 0 ? a.slot[j + lane] : -1;
+      const unsigned good = __ballot_sync(ALL, a.cache.holds(s));
+      if (!good) continue;
+      before = __shfl_sync(ALL, s, 31 - __clz(good));
       break;
     }
-  }
+  const int nearest = __shfl_sync(ALL, slot0, holding_before ? 31 - __clz(holding_before) : 0);
+  const int previous = holding_before ? nearest : before;
+  const bool first = a.cache.holds(slot0) && (previous < 0 || previous >> a.cache.block_shift != slot0 >> a.cache.block_shift);
   const unsigned firsts = __ballot_sync(ALL, first);
   const int n_blocks = __popc(firsts);
   for (int k = warp; k < n_blocks; k += W_WARPS) {  // the k-th of them
@@ -208,8 +212,8 @@ __global__ void __launch_bounds__(W_THREADS, 5) kv_quantise_kernel(const Quantis
       }
       if (limit < 32 || i0 + e + 32 >= a.n) break;
     }
-    const int before = last - 32 * lane;  // places of the lane's that are before the last
-    const unsigned all_before = before >= 32 ? ALL : before > 0 ? (1u << before) - 1 : 0u;
+    const int in_front = last - 32 * lane;  // places of the lane's that are before the last
+    const unsigned all_before = in_front >= 32 ? ALL : in_front > 0 ? (1u << in_front) - 1 : 0u;
     stay[k][lane] = all_before & ~written;
     if (lane == 0) {
       const int fit = last < 0 || end > ENTRIES ? 0 : min(MOST_STAGED / ((end - at) * dim * 2), min(heads, 2 * W_WARPS));
