@@ -441,8 +441,9 @@ int ivit_kv_dequantise(const ivit_quantised_layout* cache, int32_t n_layers, int
 
 /* ivit_tree_attention over a cache of 8 bits: the operation, arguments, limits and workspace rules are those given
  * there, with cached keys code * k_scale and values code * v_scale; new rows (q, k_new, v_new, out) are of the layout's
- * 16-bit type.  Scales other than ivit_kv_quantise's have to be positive and within 2^-60 .. 2^60 (one that is not a positive
- * number counts as 0 for keys and 2^-100 for values).  Codes enter the products as they are, as 16-bit values that hold them exactly; a
+ * 16-bit type.  Scales other than ivit_kv_quantise's have to be within 2^-60 .. 2^60 (one that is not positive and
+ * finite counts as 0 for keys and 2^-80 for values).  Of products of a key's probability and its block's scale of values,
+ * those of 2^-126 of a row's largest and less may be left out of the sums, of 2^-34 and less of the product with V.  Codes enter the products as they are, as 16-bit values that hold them exactly; a
  * block's scale of keys multiplies their scores and one of values their probabilities, in fp32.  Up to 40 rows (new rows x heads of
  * the group) per key head, 24 for heads above 128, probabilities of cached keys enter the product with V as one fp16 value for bf16
  * rows and two for fp16 ones, above as one of the rows' type; those of new rows as two of that type or, above, one.

@@ -104,6 +104,18 @@ __device__ __forceinline__ bool odd16(uint32_t half_word) {  // infinite or not 
   return (half_word & e) == e;
 }
 
+// A block's scale; one that is not positive and finite counts as 0 for keys, and as 2^-80 for values (as good as 0, and the sum of
+// 2^31 probabilities over it stays below 2^127).  Bits of a positive, normal one: 2^23 .. 254 * 2^23 (2^127 counts as none).
+__device__ __forceinline__ float key_scale(float x) {
+  return static_cast<unsigned>(__float_as_int(x)) - 0x00800000u < 0x7e800000u ? x : 0.f;
+}
+__device__ __forceinline__ void value_scale(float x, float& log2_of, float& inverse) {
+  const int b = __float_as_int(x);
+  const bool power = !(b & 0x7fffff), none = b < 0x00800000 || b >= 0x7f000000;
+  log2_of = none ? -80.f : power ? static_cast<float>((b >> 23) - 127) : __log2f(x);
+  inverse = none ? __int_as_float((80 + 127) << 23) : power ? __int_as_float(0x7f000000 - b) : __fdividef(1.f, x);
+}
+
 // ONE_BLOCK: 16 keys of a warp, of whose 32 there are two such halves, have their page and their scales in common.
 template <typename T, int DP, int NR, bool ONE_BLOCK>
 __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_quantised_kernel(const QuantisedArgs a) {
@@ -411,7 +423,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
           if constexpr (C::TAIL == 16)
             product(C::STEPS - 1, *reinterpret_cast<const uint32_t*>(k_tile + piece<DP, false>(row, 4 * C::FULL) + 4 * t),
                     *reinterpret_cast<const uint32_t*>(k_tile + piece<DP, false>(row + 8, 4 * C::FULL) + 4 * t));
-          // Scales of keys g, g + 8: of keys, log2 and inverse of values (one that is none, or out of range: the values are as good as 0).
+          // Scales of keys g, g + 8: of keys, log2 and inverse of values.
           float kf[2], lv[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
@@ -420,12 +432,8 @@ __global__ void __launch_bounds__(THREADS, Cfg<DP, NR>::CTAS) tree_attention_qua
               break;
             }
             const int at_key = 16 * i + (ONE_BLOCK ? 0 : g + 8 * e);
-            kf[e] = scales[at_key];
-            const float x = scales[TK + at_key];
-            const int b = __float_as_int(x);
-            const bool power = !(b & 0x7fffff), none = b < 0x00800000 || b >= 0x7f000000;
-            lv[e] = none ? -100.f : power ? static_cast<float>((b >> 23) - 127) : __log2f(x);
-            iv[i][e] = none ? __int_as_float((100 + 127) << 23) : power ? __int_as_float(0x7f000000 - b) : __fdividef(1.f, x);
+            kf[e] = key_scale(scales[at_key]);
+            value_scale(scales[TK + at_key], lv[e], iv[i][e]);
           }
 #pragma unroll
           for (int h = 0; h < NR; ++h)

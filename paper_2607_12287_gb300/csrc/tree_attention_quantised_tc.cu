@@ -341,12 +341,8 @@ __global__ void __launch_bounds__(TC_THREADS, TcCfg<DP>::CTAS)
             if (kv == 1 && tid2 < KB) {  // (beside the values: their slot stays full until the block's probabilities have been multiplied)
               const float* raw = reinterpret_cast<const float*>(sm + C::OFF_RAW_SCALES) + stage * 2 * KB + tid2;
               float* scales = reinterpret_cast<float*>(sm + C::OFF_SCALES) + (t / 2 % SCALES) * 3 * KB + tid2;
-              const float v_scale = raw[KB];
-              const int b = __float_as_int(v_scale);
-              const bool power = !(b & 0x7fffff), none = b < 0x00800000 || b >= 0x7f000000;
-              scales[0] = raw[0] * a.score_log2;
-              scales[KB] = none ? -100.f : power ? static_cast<float>((b >> 23) - 127) : __log2f(v_scale);
-              scales[2 * KB] = none ? __int_as_float((100 + 127) << 23) : power ? __int_as_float(0x7f000000 - b) : __fdividef(1.f, v_scale);
+              scales[0] = key_scale(raw[0]) * a.score_log2;
+              value_scale(raw[KB], scales[KB], scales[2 * KB]);
             }
             uint8_t* tile = sm + C::OFF_RING + slot * C::TILE;
             const uint8_t* raw = sm + C::OFF_RAW + stage * C::RAW + tid2 * 16;

@@ -439,6 +439,35 @@ def test_cached_codes_that_are_no_numbers(pkg):
         assert bad[:new, 2:, 7].all() and bad.sum() == 2 * new and np.isfinite(host(lse)).all()
 
 
+@pytest.mark.parametrize("block", [4, 16])
+@pytest.mark.parametrize("new", [1, 3, 30])
+def test_scales_that_are_none(pkg, new, block):
+    # scales that are not positive or not finite: such keys count as 0, such values as good as 0 (2^-80 of their codes, below the
+    # bound's 2^-25), beside ordinary ones, and where no others are
+    r = np.random.default_rng(14)
+    for share in (0.3, 1.0):
+        c = attention_case(r, [300, 9], [new, new], 4, 2, 64, 16, block, "bfloat16")
+        none = np.array([0.0, -0.0, -1.0, -2.0 ** -8, 1e-40, np.nan, -np.inf, np.inf], np.float32)
+        scales = [s for _, s in c["caches"]]
+        at = [r.random(s.shape) < share for s in scales]
+        for s, here in zip(scales, at):
+            s[here] = r.choice(none, int(here.sum()))
+        out, lse = run_attention(pkg, c, "causal", check=False)
+        for s, here in zip(scales, at):
+            s[here] = 0
+        check_attention(c, out, lse, "causal", None, 64 ** -0.5)
+
+
+@pytest.mark.parametrize("new", [1, 30])
+def test_long_cache_of_scales_that_are_none(pkg, new):
+    # (the sum of their probabilities, each over its scale, stays finite)
+    r = np.random.default_rng(15)
+    c = attention_case(r, [270000], [new], 2, 1, 64, 16, 16, "bfloat16")
+    for _, s in c["caches"]:
+        s[:] = 0
+    run_attention(pkg, c, "causal")
+
+
 def test_pages_outside_the_cache_read_as_zeros(pkg):
     r = np.random.default_rng(12)
     for new in (2, 50):
