@@ -638,6 +638,8 @@ def make_verify_config(n_req: int, vocab: int, max_new: int, dtype="bfloat16") -
 
 def _device_of(t, name: str) -> None:
     """Rejects a tensor of another device than the current one, on which the library launches."""
+    if not _current:  # (a first call, or calls that all give their stream)
+        _stream(None)
     if type(t) is _Tensor and _current and t.get_device() != _current[1]():
         raise ValueError(f"{name}: tensor on {t.device}, the current device is cuda:{_current[1]()}")
 
@@ -658,6 +660,7 @@ def _codes(t, name: str, layout: IvitQuantisedLayout) -> int:
     """The pointer of a cache of 8 bits of this layout; rejects any other tensor."""
     if (type(t) is _Tensor and t.is_cuda and t.dtype is _dtypes["float8_e4m3fn"] and t.shape == layout.shape
             and t.stride() == layout.strides):
+        _device_of(t, name)
         return t.data_ptr()
     _float8(t, name)
     if tuple(t.shape) != layout.shape or tuple(t.stride()) != layout.strides:
@@ -756,7 +759,6 @@ def ivit_tree_attention_quantised(cfg: IvitAttentionConfig, cache: IvitQuantised
     q_shape, k_shape = (n, heads, dim), (n, cache.kv_heads, dim)
     if cfg.mask_mode != IVIT_MASK_TREE:
         mask = None
-    _device_of(q, "q")
     args = (C.addressof(cfg), C.addressof(cache), n, *_rows(q, "q", dt, q_shape), *_rows(k_new, "k_new", dt, k_shape),
             *_rows(v_new, "v_new", dt, k_shape), _codes(k_cache, "k_cache", cache), _codes(v_cache, "v_cache", cache),
             _scales(k_scale, "k_scale", cache), _scales(v_scale, "v_scale", cache),
@@ -764,6 +766,7 @@ def ivit_tree_attention_quantised(cfg: IvitAttentionConfig, cache: IvitQuantised
             _i32(cu_rows, "cu_rows", req + 1), _i32(mask, "mask", n * cfg.mask_words),
             *_rows(out, "out", dt, q_shape), _arg(lse, "lse", "float32", n * heads),
             *_workspace(workspace), _stream(stream))
+    _device_of(q, "q")
     _check(load().ivit_tree_attention_quantised(*args), None)
 
 

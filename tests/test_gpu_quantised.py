@@ -439,6 +439,28 @@ def test_cached_codes_that_are_no_numbers(pkg):
         assert bad[:new, 2:, 7].all() and bad.sum() == 2 * new and np.isfinite(host(lse)).all()
 
 
+def test_tensors_of_another_device_than_the_current_one(pkg, monkeypatch):
+    # refused before anything is launched, also by calls that give their stream
+    import torch
+    c = attention_case(np.random.default_rng(2), [20], [2], 4, 2, 64, 16, 16, "bfloat16")
+    args = call(pkg, c, "causal")
+    lay, k, kc, vc, ks, vs = args[1], args[3], *args[5:9]
+    layers = [x[None] for x in (kc, vc, ks, vs)]
+    stream = torch.cuda.current_stream()
+    cfg = pkg.make_verify_config(1, 10, 4, "float32")
+    rows, logits = i32([0, 1]), torch.zeros((2, 10), device="cuda")
+    calls = [lambda: pkg.ivit_tree_attention_quantised(*args, stream=stream),
+             lambda: pkg.ivit_kv_quantise(lay, k[None], k[None], rows, rows, *layers, stream=stream),
+             lambda: pkg.ivit_kv_dequantise(lay, rows, *layers, k[None], k[None], stream=stream),
+             lambda: pkg.ivit_tree_verify(cfg, logits, None, rows, None, i32([0, 2]), None, None, None, i32([0, 0]), i32([0]), i32([0]),
+                                          stream=stream)]
+    pkg._stream(None)
+    monkeypatch.setattr(pkg, "_current", [pkg._current[0], lambda: 1])
+    for f in calls:
+        with pytest.raises(ValueError, match="the current device is cuda:1"):
+            f()
+
+
 @pytest.mark.parametrize("block", [4, 16])
 @pytest.mark.parametrize("new", [1, 3, 30])
 def test_scales_that_are_none(pkg, new, block):
