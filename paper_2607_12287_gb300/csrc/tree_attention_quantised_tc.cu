@@ -12,7 +12,7 @@
 // Bound: the chain of a block, 3.3 us for two CTAs an SM (heads of 128), of which 2.2 are the handshakes of S, P and O that
 // tree_attention_tc.cu has too; conversions wait for a place in the ring, which has three at heads of 128 beside the 32 KB of Q.
 // Without conversions and copies 79 us instead of 110 for 16 trees of up to 31 drafts over up to 8192 tokens (32 + 8 heads of 128, fp16; bf16
-// 124), without most of the softmax's work 101.  Eight requests of up to 256 rows over up to 2048 tokens, 16 heads of 72, 59 us.
+// 124), without most of the softmax's work 101.  Eight requests of up to 256 rows over up to 2048 tokens, 16 heads of 72, 58 us.
 #include <cudaTypedefs.h>
 
 #include <type_traits>
@@ -260,13 +260,11 @@ __global__ void __launch_bounds__(TC_THREADS, TcCfg<DP>::CTAS)
       for (int x = 0; x < C::PASSES; ++x) ids[x] = page((tid2 + x * FILL) / C::PIECES);
       scale_id = page(tid2);
     };
-    // The thread's pieces: from where in a page (-1: no piece of a head), and to where in a K or V block.
-    long long from_at[C::PASSES];
+    // To where in a K or V block the thread's pieces go.
     int to_at[C::PASSES];
 #pragma unroll
     for (int x = 0; x < C::PASSES; ++x) {
       const int e = tid2 + x * FILL, row = e / C::PIECES, c = e - row * C::PIECES;
-      from_at[x] = row < KB && 16 * c < dim ? (row & page_mask) * a.cache.token_stride + 16 * c : -1;
       to_at[x] = row < KB ? chunk_at<DP>(row, 2 * c) : -1;
     }
     uint32_t copied = 0;  // K and V blocks, in turn
@@ -278,14 +276,15 @@ __global__ void __launch_bounds__(TC_THREADS, TcCfg<DP>::CTAS)
         const uint8_t* const from = cache + (next_kb * KB & page_mask) * a.cache.token_stride;  // (a page above 64 tokens has whole blocks)
 #pragma unroll
         for (int x = 0; x < C::PASSES; ++x) {
-          const bool ok = ids[x] >= 0 && from_at[x] >= 0;
-          const uint8_t* src = ok ? from + from_at[x] + ids[x] * a.cache.page_stride : cache;
+          const int e = tid2 + x * FILL, row = e / C::PIECES, c = e - row * C::PIECES;  // (places kept for all pieces spilled: 112 instead of 109 us)
+          const bool ok = ids[x] >= 0 && 16 * c < dim;
+          const uint8_t* src = ok ? from + (row & page_mask) * a.cache.token_stride + 16 * c + ids[x] * a.cache.page_stride : cache;
           const uint32_t to = raw + x * FILL * 16;
           if (a.wide) {
             copy16(to, src, ok);
           } else {
             copy8(to, src, ok);
-            const bool second = ok && 16 * ((tid2 + x * FILL) % C::PIECES) + 8 < dim;
+            const bool second = ok && 16 * c + 8 < dim;
             copy8(to + 8, second ? src + 8 : src, second);
           }
         }
