@@ -416,8 +416,8 @@ typedef struct ivit_quantised_layout {
 
 /* ivit_kv_write for a cache of 8 bits: row src_row_dev[i] of k and v ([n_layers][n_src][kv_heads][head_dim], row and
  * layer strides in elements, multiples of 8) into slot slot_dev[i] of every layer's cache, for i < n; entries whose row is outside
- * [0, n_src) or whose slot is outside the cache are skipped, slots of a call are distinct, and those of one block lie
- * next to each other in the list (skipped ones may be between), as those of ivit_step_plan do.
+ * [0, n_src) or whose slot is outside the cache are skipped; slots of the others are distinct, and those of one block lie
+ * next to each other in the list, as those of ivit_step_plan do (skipped ones may be between, whatever slots they have).
  * At most 2^20 entries and 4096 layers.
  * Of a block that is written, tokens before the last written one stay, if they are not written themselves, and what lies
  * behind it is of no meaning from then on (a block whose first token is written with the rest behind it starts afresh, so

@@ -43,6 +43,13 @@ struct QuantiseArgs {
   QuantisedCache cache;
   int n_layers, n, n_src;
   int layers;  // of a CTA
+
+  // Slot and row of entry j if it counts, that is if the cache holds the slot and the row is one of the source's, else -1 and -1.
+  __device__ __forceinline__ int2 entry(int j) const {
+    const bool in = j >= 0 && j < n;
+    const int s = in ? slot[j] : -1, r = in ? row[j] : -1;
+    return cache.holds(s) && static_cast<unsigned>(r) < static_cast<unsigned>(n_src) ? make_int2(s, r) : make_int2(-1, -1);
+  }
 };
 
 __device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
@@ -154,38 +161,38 @@ __global__ void __launch_bounds__(W_THREADS, 5) kv_quantise_kernel(const Quantis
   __shared__ __align__(8) uint64_t arrived[MOST_STAGES];
   __shared__ int rows[ENTRIES];                  // of the entries (-1: skipped)
   __shared__ long long places[ENTRIES];          // their slots' bytes in the cache
-  __shared__ int slots[ENTRIES];
+  __shared__ int slots[ENTRIES];                 // (-1: skipped)
   __shared__ Written blocks[CHUNK];
   __shared__ unsigned stay[CHUNK][WORDS];        // places before the last written one that are not written themselves
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int block = 1 << a.cache.block_shift, dim = a.cache.dim, heads = a.cache.heads;
   const int i0 = blockIdx.y * CHUNK;
   for (int e = tid; e < ENTRIES; e += W_THREADS) {
-    const int slot = i0 + e < a.n ? a.slot[i0 + e] : -1;
-    const int row = a.cache.holds(slot) ? a.row[i0 + e] : -1;
-    slots[e] = slot;
-    rows[e] = static_cast<unsigned>(row) < static_cast<unsigned>(a.n_src) ? row : -1;
-    places[e] = a.cache.holds(slot) ? a.cache.token(slot) : 0;
+    const int2 entry = a.entry(i0 + e);
+    slots[e] = entry.x;
+    rows[e] = entry.y;
+    places[e] = entry.x >= 0 ? a.cache.token(entry.x) : 0;
   }
   if (tid < MOST_STAGES) mbar_init(smem_u32(&arrived[tid]), 1);
   fence_mbar_init();
   __syncthreads();
-  // Blocks that begin among the chunk's entries: an entry whose nearest one before it that counts is of another block.
+  // Blocks that begin among the chunk's entries: an entry whose nearest one before it that counts is of another block.  (Skipped
+  // entries may have any slot: one of another block does not end a block.)
   static_assert(CHUNK == 32, "an entry to a lane");
   const int slot0 = slots[lane];
-  const unsigned holding = __ballot_sync(ALL, a.cache.holds(slot0)), holding_before = holding & ((1u << lane) - 1);
+  const unsigned holding = __ballot_sync(ALL, slot0 >= 0), holding_before = holding & ((1u << lane) - 1);
   int before = -1;  // of the chunk's first entry that counts, the nearest slot in front of the chunk
   if (holding)
     for (int j = i0 - 32; j > -32; j -= 32) {
-      const int s = j + lane >= 0 ? a.slot[j + lane] : -1;
-      const unsigned good = __ballot_sync(ALL, a.cache.holds(s));
+      const int s = a.entry(j + lane).x;
+      const unsigned good = __ballot_sync(ALL, s >= 0);
       if (!good) continue;
       before = __shfl_sync(ALL, s, 31 - __clz(good));
       break;
     }
   const int nearest = __shfl_sync(ALL, slot0, holding_before ? 31 - __clz(holding_before) : 0);
   const int previous = holding_before ? nearest : before;
-  const bool first = a.cache.holds(slot0) && (previous < 0 || previous >> a.cache.block_shift != slot0 >> a.cache.block_shift);
+  const bool first = slot0 >= 0 && (previous < 0 || previous >> a.cache.block_shift != slot0 >> a.cache.block_shift);
   const unsigned firsts = __ballot_sync(ALL, first);
   const int n_blocks = __popc(firsts);
   for (int k = warp; k < n_blocks; k += W_WARPS) {  // the k-th of them
@@ -195,12 +202,11 @@ __global__ void __launch_bounds__(W_THREADS, 5) kv_quantise_kernel(const Quantis
     unsigned written = 0;
     int end = at, last = -1, count = 0;
     for (int e = at;; e += 32) {
-      const int j = i0 + e + lane, s = e + lane < ENTRIES ? slots[e + lane] : j < a.n ? a.slot[j] : -1;
-      const bool holds = a.cache.holds(s), same = holds && s >> a.cache.block_shift == id;
-      const unsigned others = __ballot_sync(ALL, holds && !same);
+      const int s = e + lane < ENTRIES ? slots[e + lane] : a.entry(i0 + e + lane).x;
+      const bool same = s >= 0 && s >> a.cache.block_shift == id;
+      const unsigned others = __ballot_sync(ALL, s >= 0 && !same);
       const int limit = others ? __ffs(others) - 1 : 32;  // entries from here on are not the block's
-      const int r = !same || lane >= limit ? -1 : e + lane < ENTRIES ? rows[e + lane] : a.row[j];
-      unsigned good = __ballot_sync(ALL, static_cast<unsigned>(r) < static_cast<unsigned>(a.n_src));
+      unsigned good = __ballot_sync(ALL, same && lane < limit);
       if (good) end = e + 32 - __clz(good);
       count += __popc(good);
       while (good) {
@@ -216,8 +222,8 @@ __global__ void __launch_bounds__(W_THREADS, 5) kv_quantise_kernel(const Quantis
     const unsigned all_before = in_front >= 32 ? ALL : in_front > 0 ? (1u << in_front) - 1 : 0u;
     stay[k][lane] = all_before & ~written;
     if (lane == 0) {
-      const int fit = last < 0 || end > ENTRIES ? 0 : min(MOST_STAGED / ((end - at) * dim * 2), min(heads, 2 * W_WARPS));
-      blocks[k] = {id, at, end, last, fit, last < 0 ? 0 : (heads + max(fit, 1) - 1) / max(fit, 1), count < end - at};
+      const int fit = end > ENTRIES ? 0 : min(MOST_STAGED / ((end - at) * dim * 2), min(heads, 2 * W_WARPS));
+      blocks[k] = {id, at, end, last, fit, (heads + max(fit, 1) - 1) / max(fit, 1), count < end - at};
     }
   }
   __syncthreads();
@@ -323,10 +329,10 @@ __global__ void __launch_bounds__(W_THREADS, 5) kv_quantise_kernel(const Quantis
             if (rows[u.w.first + e] >= 0) f(*reinterpret_cast<const uint4*>(mine + e * row_bytes), places + u.w.first + e);
         } else {
           for (int e = begin; e < n; e += rows_at_once) {
-            const int j = i0 + u.w.first + e, s = a.slot[j], r = a.row[j];
-            if (!a.cache.holds(s) || static_cast<unsigned>(r) >= static_cast<unsigned>(a.n_src)) continue;
-            const long long place = a.cache.token(s);
-            f(*reinterpret_cast<const uint4*>(from + r * a.row_stride), &place);
+            const int2 entry = a.entry(i0 + u.w.first + e);
+            if (entry.x < 0) continue;
+            const long long place = a.cache.token(entry.x);
+            f(*reinterpret_cast<const uint4*>(from + entry.y * a.row_stride), &place);
           }
         }
       };

@@ -120,6 +120,34 @@ def test_skipped_entries_between_those_of_a_block(pkg):
     check_write(pkg, k, v, np.zeros(50, np.int64), np.full(50, -7), caches, 16, "bfloat16", "token", repeat=1)
 
 
+@pytest.mark.parametrize("gap", [1, 31, 150, 400])
+def test_skipped_entries_with_slots_of_other_blocks(pkg, gap):
+    # entries without a row, whose slots are those of other blocks or are written by entries that count, inside a block's run: next to
+    # each other, across the 32 entries that a CTA begins with, and past the 160 that it looks at together
+    r = np.random.default_rng(43 + gap)
+    for block, page in ((16, 32), (128, 128)):
+        k, v, rows, slots, caches = write_case(r, 2, [(3, 9), (40, 20), (64, 73)], 2, 72, page, block, "bfloat16", "token")
+        n, total = k.shape[1], caches[0][0].shape[1] * page
+        at = np.sort(np.repeat(r.choice(len(rows) + 1, 12, replace=False), gap))
+        none = r.choice([-1, n, n + 5, -(1 << 31), (1 << 31) - 1], len(at))
+        check_write(pkg, k, v, np.insert(rows, at, none), np.insert(slots, at, r.integers(0, total, len(at))), caches, block, "bfloat16", "token")
+
+
+def test_a_skipped_entry_of_another_block_between_two_of_one(pkg):
+    # blocks of 16: entries 0 and 2 are of block 0, entry 1 has no row.  All places of the run are written by it, so the old scale does not
+    # count; with a first place that stays it does.
+    r = np.random.default_rng(44)
+    for first in (0, 1):
+        for lead in (0, 29, 30, 31):  # entries in front, each of a block of its own
+            k, v, _, _, caches = write_case(r, 1, [(0, 16)] * 35, 2, 64, 16, 16, "bfloat16", "token")
+            front = 16 * np.arange(3, 3 + lead)
+            slots = np.concatenate([front, [first, 16, first + 1, 32]])
+            rows = np.concatenate([np.arange(lead), [lead, -1, lead + 1, lead + 2]])
+            for _, s in caches:
+                s[:, 0] = 2.0 ** 20
+            check_write(pkg, k, v, rows, slots, caches, 16, "bfloat16", "token")
+
+
 def test_writes_and_reads_on_another_stream_and_in_a_graph(pkg):
     import torch
     r = np.random.default_rng(42)
