@@ -5,7 +5,8 @@
 // A request's rows are looked at in their order: a row that hangs on the last accepted one is a draft x, accepted if
 // u W q_x < w_x; then it is the last accepted row, c = 0 and the rows that hang on it are tried.  Else c grows by W, for
 // max(max(e - c q, 0) - W q, 0) = max(e - (c + W) q, 0).  Drafts without probabilities (q = 1 at x) leave a list of tokens that
-// were tried: w is 0 there.  In the end the token is the argmax of w_v / noise_v, an exponential race.  Only rows on
+// were tried: w is 0 there.  W loses e_x then, in fp32 with an error of 2^-25 of W, and is summed again over the tokens that are left
+// when it is below half of what the last sum gave or 32 have been taken off: the error stays near a sum's own.  In the end the token is the argmax of w_v / noise_v, an exponential race.  Only rows on
 // the path are read.
 //
 // A cluster of up to 8 CTAs has a request, each CTA a part of the vocabulary; sums and maxima of a CTA meet in
@@ -143,8 +144,20 @@ __global__ void __launch_bounds__(THREADS) tree_verify_kernel(const VerifyArgs a
   // exp((l - top) / T); nothing for -inf and NaN
   const auto weight = [&](float l, float top) { return !(l > -INFINITY) ? 0.f : l == top ? 1.f : ex2((l - top) * per); };
 
-  int at = 0, accepted = 1, n_tried = 0;  // the last accepted row of the request, how many, tokens tried behind it
+  // Bit i: the thread's token v + i STEP was tried without probabilities and not accepted.
+  int n_tried = 0;
+  const auto left_out = [&](int v) {
+    unsigned out = 0;
+    for (int i = 0; i < n_tried; ++i) {
+      const int d = tried[i] - v;
+      if (d >= 0 && d % STEP == 0 && d / STEP < U) out |= 1u << (d / STEP);
+    }
+    return out;
+  };
+
+  int at = 0, accepted = 1;                // the last accepted row of the request, how many
   float top = -INFINITY, total = 0.f, taken = 0.f;  // max l, W, c
+  float summed = 0.f;                      // W as the last sum over all tokens gave it
   int best = -1;                          // greedy: the likeliest token
   const auto enter = [&] {  // of row `at`
     const L* row = logits_of(row0 + at);
@@ -187,7 +200,7 @@ __global__ void __launch_bounds__(THREADS) tree_verify_kernel(const VerifyArgs a
       x = m;
     });
     top = x;
-    total = y;
+    total = summed = y;
     taken = 0.f;
     n_tried = 0;
   };
@@ -205,7 +218,7 @@ __global__ void __launch_bounds__(THREADS) tree_verify_kernel(const VerifyArgs a
   int found = next_draft(1, 0);
   while (found < n) {
     const int row = row0 + found, x = a.token[row];
-    bool ok = false, tested = x >= 0 && x < a.vocab;
+    bool ok = false, tested = x >= 0 && x < a.vocab, less = false;  // (less: W has lost a token)
     if (!tested) {
     } else if (greedy) {
       ok = x == best;
@@ -220,6 +233,7 @@ __global__ void __launch_bounds__(THREADS) tree_verify_kernel(const VerifyArgs a
         ok = !again && a.uniform[row] * total < e;
         if (!ok && !again) {
           total = fmaxf(total - e, 0.f);
+          less = true;
           __syncthreads();  // (everyone has looked at the list)
           if (tid == 0) tried[n_tried] = x;
           ++n_tried;
@@ -236,10 +250,24 @@ __global__ void __launch_bounds__(THREADS) tree_verify_kernel(const VerifyArgs a
       continue;
     }
     found = next_draft(found + 1, at);
-    if (!tested || greedy || !a.prob) continue;
-    taken += total;
+    if (!tested || greedy) continue;
+    if (a.prob) taken += total;
     if (found >= n) break;  // (nothing is tried against what is left)
     const L* l_row = logits_of(row0 + at);
+    if (!a.prob) {
+      if (!less || (total >= 0.5f * summed && n_tried % 32 != 0)) continue;
+      float sum = 0.f, none = 0.f;
+      tokens([&](int v) {
+        float l[U];
+        load8<L, VEC>(l_row, v, v1, -INFINITY, l);
+        const unsigned out = left_out(v);
+#pragma unroll
+        for (int i = 0; i < U; ++i) sum += out >> i & 1 ? 0.f : weight(l[i], top);
+      });
+      everywhere(sum, none, add);
+      total = summed = sum;
+      continue;
+    }
     const float* q_row = a.prob + (row0 + at) * a.prob_stride;
     float sum = 0.f, none = 0.f;
     tokens([&](int v) {
@@ -265,11 +293,7 @@ __global__ void __launch_bounds__(THREADS) tree_verify_kernel(const VerifyArgs a
         load8<L, VEC>(l_row, v, v1, -INFINITY, l);
         load8<float, VEC>(noise, v, v1, 0.f, z);
         if (q_row) load8<float, VEC>(q_row, v, v1, 0.f, q);
-        unsigned out = 0;
-        for (int i = 0; i < n_tried; ++i) {
-          const int d = tried[i] - v;
-          if (d >= 0 && d % STEP == 0 && d / STEP < U) out |= 1u << (d / STEP);
-        }
+        const unsigned out = left_out(v);
 #pragma unroll
         for (int i = 0; i < U; ++i) {
           float w = weight(l[i], top);

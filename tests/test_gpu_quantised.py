@@ -742,6 +742,39 @@ def test_drafts_that_hang_on_one_row_in_many(pkg):
         run_verify(pkg, c, least=0.8)
 
 
+@pytest.mark.parametrize("vocab,dtype", [(64, "bfloat16"), (5001, "float32"), (40000, "float16"), (131072, "float32")])
+def test_what_is_left_after_likely_drafts(pkg, vocab, dtype):
+    # without probabilities, logits 0, -2.25, -4.5, ...: each of the candidates behind the first row has 1 - e^-2.25 = 0.8946 of what the
+    # ones before it leave, so what is left after k is e^(-2.25 k), 2^-52 after 16; one u on either side of the last one's share
+    r = np.random.default_rng(29)
+    share, counts = 1 - np.exp(-2.25), np.arange(1, 17)
+    for near in (share - 0.02, share + 0.02):
+        new, n = counts + 1, len(counts)
+        c = verify_case(r, new, vocab, True, False, dtype, 1.0)
+        order = r.permutation(vocab)[:40]
+        logits = np.full((c["logits"].shape[0], vocab), -np.inf, np.float32)
+        logits[:, order] = -2.25 * np.arange(40, dtype=np.float32)  # (up to -87.75: nine bits at most, eight of the first 17)
+        c["logits"] = dev(logits, dtype)
+        idx = np.concatenate([np.arange(m) for m in new])
+        c["parent"], c["tokens"] = np.where(idx == 0, -1, 0), order[np.maximum(idx - 1, 0)]
+        c["uniform"] = np.where(idx == np.repeat(new - 1, new), near, 0.95).astype(np.float32)
+        _, accepted, _ = run_verify(pkg, c, least=1.0)
+        assert (accepted == (2 if near < share else 1)).all()
+
+
+def test_many_drafts_that_take_a_little_each(pkg):
+    # 1000 candidates of 4096 equal tokens: what is left shrinks by one of them each time, and the last is accepted by its share
+    r = np.random.default_rng(30)
+    for off, want in ((-0.01, 2), (0.01, 1)):
+        c = verify_case(r, [1002], 4096, True, False, "float32", 1.0)
+        c["logits"][:] = 0.0
+        c["parent"] = np.concatenate([[-1], np.zeros(1001, np.int64)])
+        c["tokens"] = r.permutation(4096)[:1002]
+        c["uniform"] = np.full(1002, 0.999, np.float32)
+        c["uniform"][-1] = (1 + off) / (4096 - 1000)
+        assert run_verify(pkg, c, least=1.0)[1][0] == want
+
+
 def test_more_rows_than_are_looked_at(pkg):
     r = np.random.default_rng(22)
     c = verify_case(r, [9, 30, 2], 400, True, True, "bfloat16", 0.9)
