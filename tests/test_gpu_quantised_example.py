@@ -18,6 +18,14 @@ def test_sampling_over_eight_bits(seed, drafts):
     assert drafted_actions.sample(30, seed, drafts) == (said, passes)  # the same seed
 
 
+@pytest.mark.parametrize("seed,drafts", [(0, 3), (1, 6), (2, 1)])
+def test_sampling_takes_fewer_passes_than_tokens(seed, drafts):
+    # the prompt's pass gives the first token; if no draft were accepted, every other token would take a pass of its own
+    import drafted_actions
+    said, passes = drafted_actions.sample(30, seed, drafts)
+    assert passes < 30
+
+
 def test_greedy_steps_over_eight_bits_follow_those_over_sixteen():
     # the first tokens of both: the logits of a prompt, whose rows see each other in 16 bits, are the same; a step's are near
     import drafted_actions as ex
