@@ -636,12 +636,16 @@ def make_verify_config(n_req: int, vocab: int, max_new: int, dtype="bfloat16") -
     return IvitVerifyConfig(n_req, vocab, max_new, _VERIFY_DTYPES[name])
 
 
-def _device_of(t, name: str) -> None:
-    """Rejects a tensor of another device than the current one, on which the library launches."""
+def _all_here(names: str, *tensors) -> None:
+    """Rejects tensors (their names in order, or None) of another device than the current one, on which the library launches."""
     if not _current:  # (a first call, or calls that all give their stream)
         _stream(None)
-    if type(t) is _Tensor and _current and t.get_device() != _current[1]():
-        raise ValueError(f"{name}: tensor on {t.device}, the current device is cuda:{_current[1]()}")
+        if not _current:
+            return
+    here = _current[1]()
+    for i, t in enumerate(tensors):
+        if type(t) is _Tensor and t.get_device() != here:
+            raise ValueError(f"{names.split()[i]}: tensor on {t.device}, the current device is cuda:{here}")
 
 
 def _float8(t, name: str):
@@ -652,7 +656,6 @@ def _float8(t, name: str):
         raise ValueError(f"{name}: tensor on {t.device}; a CUDA tensor is required")
     if str(t.dtype) != "torch.float8_e4m3fn":
         raise TypeError(f"{name}: dtype {t.dtype}, expected torch.float8_e4m3fn")
-    _device_of(t, name)
     return t
 
 
@@ -660,7 +663,6 @@ def _codes(t, name: str, layout: IvitQuantisedLayout) -> int:
     """The pointer of a cache of 8 bits of this layout; rejects any other tensor."""
     if (type(t) is _Tensor and t.is_cuda and t.dtype is _dtypes["float8_e4m3fn"] and t.shape == layout.shape
             and t.stride() == layout.strides):
-        _device_of(t, name)
         return t.data_ptr()
     _float8(t, name)
     if tuple(t.shape) != layout.shape or tuple(t.stride()) != layout.strides:
@@ -687,8 +689,7 @@ def _quantised_layers(cache: IvitQuantisedLayout, layers: int, k_cache, v_cache,
             and k_cache.shape == v_cache.shape and k_cache.shape[1:] == cache.shape and strides[1:] == cache.strides
             and v_cache.stride() == strides and k_scale.shape == v_scale.shape and k_scale.shape[1:] == cache.scales
             and len(k_cache.shape) == 5 and len(k_scale.shape) == 4 and k_cache.shape[0] >= layers and k_scale.shape[0] >= layers
-            and k_scale.is_contiguous() and v_scale.is_contiguous() and _current
-            and k_cache.get_device() == v_cache.get_device() == k_scale.get_device() == v_scale.get_device() == _current[1]()):
+            and k_scale.is_contiguous() and v_scale.is_contiguous()):
         for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
             _float8(t, name)
             if len(t.shape) != 5 or t.shape[0] < layers or tuple(t.shape[1:]) != cache.shape or tuple(t.stride()[1:]) != cache.strides:
@@ -700,7 +701,6 @@ def _quantised_layers(cache: IvitQuantisedLayout, layers: int, k_cache, v_cache,
             if len(t.shape) != 4 or t.shape[0] < layers or tuple(t.shape[1:]) != cache.scales:
                 raise ValueError(f"{name}: shape {tuple(t.shape)}, expected [{layers}, {', '.join(map(str, cache.scales))}]")
             _arg(t, name, "float32", 0)
-            _device_of(t, name)
         strides = k_cache.stride()
         if layers > 1 and v_cache.stride()[0] != strides[0]:
             raise ValueError("k_cache, v_cache: the strides differ")
@@ -716,8 +716,6 @@ def _layer_rows(k, v, cache: IvitQuantisedLayout) -> tuple:
         raise ValueError(f"k, v: shapes {tuple(sh)} and {tuple(vsh)}, expected [layers, rows, {kv}, {dim}]")
     if st[3] != 1 or (st[2] != dim and kv > 1) or st != vst:
         raise ValueError("k, v: the heads of a row are not contiguous, or the strides differ")
-    _device_of(k, "k")
-    _device_of(v, "v")
     return sh[0], sh[1], st[1] if sh[1] > 1 else kv * dim, st[0] if sh[0] > 1 else 0
 
 
@@ -731,6 +729,7 @@ def ivit_kv_quantise(cache: IvitQuantisedLayout, k, v, rows, slots, k_cache, v_c
     n, run = rows.numel(), _stream(stream)
     args = (C.addressof(cache), layers, n, n_src, k.data_ptr(), v.data_ptr(), row, layer, _i32(rows, "rows", n),
             _i32(slots, "slots", n), kc, vc, cst, ks, vs, sst, run)
+    _all_here("k v rows slots k_cache v_cache k_scale v_scale", k, v, rows, slots, k_cache, v_cache, k_scale, v_scale)
     _check(load().ivit_kv_quantise(*args), None)
 
 
@@ -744,6 +743,7 @@ def ivit_kv_dequantise(cache: IvitQuantisedLayout, slots, k_cache, v_cache, k_sc
     run = _stream(stream)
     args = (C.addressof(cache), layers, n, _i32(slots, "slots", n), kc, vc, cst, ks, vs, sst, k.data_ptr(), v.data_ptr(), row,
             layer, run)
+    _all_here("k v slots k_cache v_cache k_scale v_scale", k, v, slots, k_cache, v_cache, k_scale, v_scale)
     _check(load().ivit_kv_dequantise(*args), None)
 
 
@@ -766,7 +766,8 @@ def ivit_tree_attention_quantised(cfg: IvitAttentionConfig, cache: IvitQuantised
             _i32(cu_rows, "cu_rows", req + 1), _i32(mask, "mask", n * cfg.mask_words),
             *_rows(out, "out", dt, q_shape), _arg(lse, "lse", "float32", n * heads),
             *_workspace(workspace), _stream(stream))
-    _device_of(q, "q")
+    _all_here("q k_new v_new k_cache v_cache k_scale v_scale table lengths cu_rows mask out lse workspace", q, k_new, v_new, k_cache,
+              v_cache, k_scale, v_scale, table, lengths, cu_rows, mask, out, lse, workspace)
     _check(load().ivit_tree_attention_quantised(*args), None)
 
 
@@ -776,7 +777,7 @@ def _table(t, name: str, dtype_name: str, rows: int, width: int) -> tuple:
         return None, 0
     if type(t) is _Tensor and t.is_cuda and t.dtype is _dtypes[dtype_name] and t.dim() == 2:
         sh, st = t.shape, t.stride()  # the common case: the checks below without formatting names
-        if sh[0] >= rows > 1 and sh[1] == width and st[1] == 1 and _current and t.get_device() == _current[1]():
+        if sh[0] >= rows > 1 and sh[1] == width and st[1] == 1:
             return t.data_ptr(), st[0]
     if isinstance(t, (int, np.ndarray)):
         raise TypeError(f"{name}: a CUDA tensor is required")
@@ -787,7 +788,6 @@ def _table(t, name: str, dtype_name: str, rows: int, width: int) -> tuple:
     sh, st = t.shape, t.stride()
     if len(sh) != 2 or sh[0] < rows or sh[1] != width or (st[1] != 1 and width > 1):
         raise ValueError(f"{name}: shape {tuple(sh)} and strides {tuple(st)}, expected [{rows}, {width}] with contiguous rows")
-    _device_of(t, name)
     return t.data_ptr(), st[0] if sh[0] > 1 else width
 
 
@@ -809,6 +809,8 @@ def ivit_tree_verify(cfg: IvitVerifyConfig, logits, draft_probs, tokens, parent,
             _i32(cu_rows, "cu_rows", req + 1), _arg(temperature, "temperature", "float32", req),
             _arg(uniform, "uniform", "float32", n), *_table(noise, "noise", "float32", req, vocab), _i32(path, "path", n),
             _i32(accepted, "accepted", req), _i32(next_token, "next_token", req), _stream(stream))
+    _all_here("logits draft_probs tokens parent cu_rows temperature uniform noise path accepted next_token", logits, draft_probs, tokens,
+              parent, cu_rows, temperature, uniform, noise, path, accepted, next_token)
     _check(load().ivit_tree_verify(*args), None)
 
 

@@ -201,6 +201,50 @@ def test_binding_rejects_tensors_it_would_misread(monkeypatch):
             pkg.ivit_tree_verify(vcfg, **{**good, **change})
 
 
+class On(Fake):
+    """A tensor of a given device."""
+    is_cuda = True
+
+    def __init__(self, t, device):
+        super().__init__(t.shape, t.dtype, t.stride())
+        self.device = torch.device("cuda", device)
+
+    def get_device(self):
+        return self.device.index
+
+
+@pytest.mark.parametrize("given", [True, False])
+def test_binding_rejects_any_tensor_of_another_device(monkeypatch, given):
+    # each tensor of each call by itself, whether the call gives its stream or not
+    reached = []
+    pkg._tensor_type()
+    monkeypatch.setattr(pkg, "load", lambda *a: reached.append(1) or pytest.fail("library reached"))
+    monkeypatch.setattr(pkg, "_Tensor", On)
+    monkeypatch.setitem(pkg._dtypes, "tensor", On)
+    monkeypatch.setattr(pkg, "_current", [lambda device: 0, lambda: 1])
+    stream = 0 if given else None
+    lay, one = pkg.make_quantised_layout(f8(4, 16, 2, 64), 8), f8(4, 16, 2, 64)
+    caches, scales = f8(3, 4, 16, 2, 64), f32(3, 4, 2, 2)
+    layers = dict(k=bf(3, 6, 2, 64), v=bf(3, 6, 2, 64), slots=ints(6), k_cache=caches, v_cache=caches, k_scale=scales, v_scale=scales)
+    acfg, vcfg = pkg.make_attention_config(2, 8, 3, 4, "tree", 1, 0.125), pkg.make_verify_config(2, 100, 4)
+    calls = [(lambda **t: pkg.ivit_kv_quantise(lay, stream=stream, **t), dict(layers, rows=ints(6))),
+             (lambda **t: pkg.ivit_kv_dequantise(lay, stream=stream, **t), layers),
+             (lambda **t: pkg.ivit_tree_attention_quantised(acfg, lay, stream=stream, **t),
+              dict(q=bf(5, 8, 64), k_new=bf(5, 2, 64), v_new=bf(5, 2, 64), k_cache=one, v_cache=one, k_scale=f32(4, 2, 2),
+                   v_scale=f32(4, 2, 2), table=ints(2, 3), lengths=ints(2), cu_rows=ints(3), mask=ints(5, 1), out=bf(5, 8, 64),
+                   lse=f32(5, 8), workspace=Fake((1 << 28,), torch.uint8))),
+             (lambda **t: pkg.ivit_tree_verify(vcfg, stream=stream, **t),
+              dict(logits=bf(5, 100), draft_probs=f32(5, 100), tokens=ints(5), parent=ints(5), cu_rows=ints(3), temperature=f32(2),
+                   uniform=f32(5), noise=f32(2, 100), path=ints(5), accepted=ints(2), next_token=ints(2)))]
+    for f, tensors in calls:
+        for name in tensors:
+            with pytest.raises(ValueError, match=f"^{name}: tensor on cuda:0, the current device is cuda:1"):
+                f(**{k: On(t, 0 if k == name else 1) for k, t in tensors.items()})
+        with pytest.raises(pytest.fail.Exception):  # (all of the current one)
+            f(**{k: On(t, 1) for k, t in tensors.items()})
+    assert len(reached) == len(calls)
+
+
 def test_restated_codes_are_the_formats():
     codes = np.arange(256, dtype=np.uint8)
     assert np.array_equal(ref.VALUES, torch.from_numpy(codes).view(torch.float8_e4m3fn).double().numpy(), equal_nan=True)
