@@ -21,6 +21,7 @@
 // 512 bytes), six CTAs an SM with less room 250 and 102, kept tokens' codes by bulk copies beside the rows 238 and 194, all layers of a chunk
 // to a CTA 427 and 126.  Reading: HBM (4099 rows of 32 layers of 8 heads of 128 137 us, 5870 GB/s).
 #include <algorithm>
+#include <climits>
 #include <type_traits>
 
 #include "quantised.cuh"
@@ -159,6 +160,9 @@ __global__ void __launch_bounds__(W_THREADS, 5) kv_quantise_kernel(const Quantis
   constexpr unsigned ALL = 0xffffffffu;
   __shared__ __align__(128) uint8_t staged[STAGED];
   __shared__ __align__(8) uint64_t arrived[MOST_STAGES];
+  // First unit a wait for whose rows has expired: from it on rows are read from where they lie, as those of blocks that do not fit
+  // are, and nothing is copied any more.
+  __shared__ int late_from;
   __shared__ int rows[ENTRIES];                  // of the entries (-1: skipped)
   __shared__ long long places[ENTRIES];          // their slots' bytes in the cache
   __shared__ int slots[ENTRIES];                 // (-1: skipped)
@@ -174,6 +178,7 @@ __global__ void __launch_bounds__(W_THREADS, 5) kv_quantise_kernel(const Quantis
     places[e] = entry.x >= 0 ? a.cache.token(entry.x) : 0;
   }
   if (tid < MOST_STAGES) mbar_init(smem_u32(&arrived[tid]), 1);
+  if (tid == 0) late_from = INT_MAX;
   fence_mbar_init();
   __syncthreads();
   // Blocks that begin among the chunk's entries: an entry whose nearest one before it that counts is of another block.  (Skipped
@@ -290,14 +295,17 @@ __global__ void __launch_bounds__(W_THREADS, 5) kv_quantise_kernel(const Quantis
   if (warp == 0)
     for (int i = 0; i < stages - 1; ++i) copy(blockIdx.x + i * gridDim.x, i);
   ahead = stages - 1;
+  bool late = false;  // (the same in all threads)
 #pragma unroll 1
   for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const Unit u = unit_of(unit);
     // the unit's rows are here, and all warps are done with the one before
-    if (!mbar_wait(smem_u32(&arrived[stage]), phase)) return;  // (cannot be: only this CTA's copies)
+    if (!late && !mbar_wait(smem_u32(&arrived[stage]), phase)) atomicMin(&late_from, unit);
     __syncthreads();
-    if (warp == 0) copy(unit + (stages - 1) * gridDim.x, ahead);
+    late = *static_cast<volatile int*>(&late_from) <= unit;  // (one that a thread ahead of this one sets is a later unit)
+    if (warp == 0 && !late) copy(unit + (stages - 1) * gridDim.x, ahead);
     ahead = ahead == stages - 1 ? 0 : ahead + 1;
+    const bool here = u.w.heads > 0 && !late;  // in shared memory
 
     const int n = u.w.end - u.w.first, n_heads = u.n_heads, row_bytes = n_heads * dim * 2;
     const uint8_t* held = staged + stage * unit_bytes;
@@ -318,13 +326,13 @@ __global__ void __launch_bounds__(W_THREADS, 5) kv_quantise_kernel(const Quantis
       const uint8_t* const mine = held + h * dim * 2 + my_piece * 16;
       const T* const from = sources + h * dim;
       // Calls f(piece, its place in the cache) for the lane's pieces: of rows in shared memory one after another, of such between which
-      // some are skipped, or of a block that does not fit there.
+      // some are skipped, or of a block that is not there.
       const auto each = [&](auto f) {
-        if (u.w.heads > 0 && !u.w.gaps) {
+        if (here && !u.w.gaps) {
           const long long* place = places + u.w.first;
 #pragma unroll 4
           for (int e = begin; e < n; e += rows_at_once) f(*reinterpret_cast<const uint4*>(mine + e * row_bytes), place + e);
-        } else if (u.w.heads > 0) {
+        } else if (here) {
           for (int e = begin; e < n; e += rows_at_once)
             if (rows[u.w.first + e] >= 0) f(*reinterpret_cast<const uint4*>(mine + e * row_bytes), places + u.w.first + e);
         } else {
@@ -394,6 +402,10 @@ __global__ void __launch_bounds__(W_THREADS, 5) kv_quantise_kernel(const Quantis
       phase ^= 1;
     }
   }
+  // copies that are on their way end (or get as long again) before the shared memory may be another CTA's
+  if (late)
+    for (int unit = late_from, i = (unit - blockIdx.x) / gridDim.x, last = i + stages - 1; i < last && unit < units; ++i, unit += gridDim.x)
+      mbar_wait(smem_u32(&arrived[i % stages]), i / stages & 1);
 }
 
 struct DequantiseArgs {

@@ -148,6 +148,31 @@ def test_a_skipped_entry_of_another_block_between_two_of_one(pkg):
             check_write(pkg, k, v, rows, slots, caches, 16, "bfloat16", "token")
 
 
+def test_a_wait_that_expires_loses_nothing(pkg, tmp_path, monkeypatch):
+    """Writes whose waits for their copies give up in some CTAs (quantise_probe.cu): the rows are read from where they lie."""
+    import ctypes as C
+    import subprocess
+    from paper_2607_12287_gb300 import build as b
+    so = str(tmp_path / "probe.so")
+    subprocess.run([b.NVCC, *b.ARCH, *b.FLAGS, "-shared", f"{b.ROOT}/tests/quantise_probe.cu", b.LIB, "-Xlinker",
+                    "-rpath=" + b.OUT_DIR, "-o", so], check=True)
+    probe = C.CDLL(so)
+    probe.ivit_kv_quantise.argtypes = pkg.load().ivit_kv_quantise.argtypes
+    monkeypatch.setattr(pkg, "load", lambda *a: probe)
+    counts = [0, 0, 0]
+    for requests, layers, kv, dim, page, block, dtype in (
+            ([(3 * i, 1 + i % 6) for i in range(60)], 6, 8, 80, 32, 16, "bfloat16"), ([(5, 700), (0, 333)], 27, 16, 72, 32, 32, "float16"),
+            ([(9, 200), (100, 300)], 3, 2, 128, 128, 128, "bfloat16"), ([(1, 3), (2, 1)], 1, 3, 64, 16, 8, "float16")):
+        for expire in (0, 1, 2):
+            assert probe.probe_expire(expire) == 0
+            r = np.random.default_rng(dim)
+            k, v, rows, slots, caches = write_case(r, layers, requests, kv, dim, page, block, dtype, "token")
+            rows[2], slots[3] = -1, -1
+            check_write(pkg, k, v, rows, slots, caches, block, dtype, "token")
+            counts[expire] += probe.probe_expired() - sum(counts)
+    assert counts[0] == 0 and min(counts[1:]) > 100
+
+
 def test_writes_and_reads_on_another_stream_and_in_a_graph(pkg):
     import torch
     r = np.random.default_rng(42)
