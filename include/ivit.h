@@ -447,7 +447,8 @@ int ivit_kv_dequantise(const ivit_quantised_layout* cache, int32_t n_layers, int
  * block's scale of keys multiplies their scores and one of values their probabilities, in fp32.  Up to 40 rows (new rows x heads of
  * the group) per key head, 24 for heads above 128, probabilities of cached keys enter the product with V as one fp16 value for bf16
  * rows and two for fp16 ones, above as one of the rows' type; those of new rows as two of that type or, above, one.
- * bf16 queries are scaled by powers of two to fp16 up to there (exact but for values 2^-28 of a row's largest and less). */
+ * bf16 queries are scaled by powers of two to fp16 up to there (exact but for values 2^-28 of a row's largest and less).
+ * Above 40 rows per key head (24 for heads above 128) it saves the cache's room, not time: ivit_tree_attention is faster there. */
 size_t ivit_tree_attention_quantised_workspace(const ivit_attention_config* cfg, const ivit_quantised_layout* cache);
 int ivit_tree_attention_quantised(const ivit_attention_config* cfg, const ivit_quantised_layout* cache, int32_t n_rows,
                                   const void* q_dev, int64_t q_stride, const void* k_new_dev, int64_t k_new_stride,
@@ -485,8 +486,10 @@ typedef struct ivit_verify_config {
  * Out: accepted_dev [n_req] the number of accepted rows (0 for a request without rows, whose next token is -1), next_dev [n_req],
  * and path_dev [n_rows]: at cu_rows[i] + j the j-th accepted row of request i, -1 past them, so that path_dev and
  * ivit_step_plan's slots are what ivit_kv_write and ivit_kv_quantise take; entries of no request are left as they are.
- * Row strides in elements, at least vocab (16-byte aligned rows take wider loads).  All arithmetic is fp32; sums are made in an
- * order that depends on the sizes alone. */
+ * Row strides in elements, at least vocab (16-byte aligned rows take wider loads).  All arithmetic is fp32 (W without q: what is left
+ * of the last sum over all tokens, made again when half of it or 32 drafts are gone); sums are made in an order that depends on the
+ * sizes, on whether all rows are 16-byte aligned, and on the device's number of SMs, so that equal calls give equal results, and the
+ * same values at another alignment may decide otherwise where a draft is within the sums' rounding of its border. */
 int ivit_tree_verify(const ivit_verify_config* cfg, int32_t n_rows, const void* logits_dev, int64_t logits_stride,
                      const float* draft_prob_dev, int64_t draft_prob_stride, const int32_t* token_dev,
                      const int32_t* parent_dev, const int32_t* cu_rows_dev, const float* temperature_dev,

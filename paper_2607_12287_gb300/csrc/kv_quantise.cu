@@ -14,9 +14,10 @@
 // rows at a time, once for the maximum and once for the rounding.
 // Reading: a warp has a unit of (layer, entry) as in kv_write.cu.
 //
-// Bound, writing: instructions.  4608 rows of 27 layers of 16 heads of 72 211 us (4110 GB/s read and written), of 128 288 us
-// (5330); blocks of a few rows, half of which round earlier tokens again, cost some 340 warp instructions a head whatever they hold
-// (896 rows of 32 layers of 8 heads of 128 in 280 blocks 124 us, 1770 GB/s).  What was tried: a warp to a block and head with
+// What writing spends its time on is instructions (no limit of the machine is reached): 4608 rows of 27 layers of 16 heads of 72 213 us
+// (4050 GB/s read and written), of 128 355 us (4330); blocks of a few rows, half of which round earlier tokens again, cost some 340 warp
+// instructions a head whatever they hold (896 rows of 32 layers of 8 heads of 128 in 280 blocks 126 us, 1730 GB/s).  The look at
+// whether a wait has expired is some 2 us of these.  What was tried: a warp to a block and head with
 // its rows in registers 535 us and 191 (119 registers, latency), in shared memory by 16-byte copies 291 and 99 (144 instructions to
 // 512 bytes), six CTAs an SM with less room 250 and 102, kept tokens' codes by bulk copies beside the rows 238 and 194, all layers of a chunk
 // to a CTA 427 and 126.  Reading: HBM (4099 rows of 32 layers of 8 heads of 128 137 us, 5870 GB/s).

@@ -107,6 +107,10 @@ extern "C" int ivit_tree_attention_quantised(const ivit_attention_config* cfg, c
   a.cache = {c.n_pages, c.page_shift, c.heads, c.dim, c.page_stride, c.token_stride, c.head_stride};
   a.block_shift = c.block_shift;
   const bool lines = all_aligned({k_cache_dev, v_cache_dev}, 16) && (c.page_stride | c.token_stride) % 16 == 0;
+  // Windows are built for 72 and 88 alone, in tiles of their own width.  Other heads of 8 more than a multiple of 16 are copied by 8
+  // bytes, which costs (32 requests of up to 16384 tokens, 32 + 8 heads, us): 40 113 (of 48 70), 56 131 (of 64 63), 104 185 (of 112 104),
+  // 120 189 (of 128 106), 136 581 (of 144 245), 248 631 (of 256 260).  The tcgen05 form converts on the way and copies 72 in halves too
+  // (views of 256 rows 59 us, of 80 56).
   a.window = !p.tc && lines && (c.dim == 72 || c.dim == 88);
   a.wide = a.window || (lines && c.dim % 16 == 0 && c.head_stride % 16 == 0);
   a.n_req = cfg->n_req;

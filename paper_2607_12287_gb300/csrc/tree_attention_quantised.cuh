@@ -16,11 +16,12 @@
 // tokens, of which a byte permutation and two conversions make an operand.  New rows are few and stay in their own type, read from
 // global memory, in a loop of their own behind that of the cached keys.
 //
-// Bound: latency and instructions (32 requests of up to 16384 tokens, 32 + 8 heads of 128, 104 us: 5330 GB/s of 128 bytes a
+// Bound: latency and instructions (32 requests of up to 16384 tokens, 32 + 8 heads of 128, 106 us: 5240 GB/s of 128 bytes a
 // key and head; 750 warp instructions to 32 keys, 44 % issue at 12 warps an SM).  Rows as columns halve the products and the outputs'
 // registers of a step of 8 rows (153 -> 135 us); two CTAs an SM with three stages were slower than three with two (124 and 110), heads that
 // lie together in a row read by one CTA gave nothing (one key head and eight are alike).  Others, us: 16 + 4 heads of 64 39, of 256
-// 143, 16 heads of 80 164, of 72 231 (8-byte halves of their pieces), blocks of 8 tokens instead of 16 117.
+// 144, 16 heads of 80 172, of 72 228 (8-byte halves of their pieces), blocks of 8 tokens instead of 16 117; their floors at the
+// copy rate are 20.5, 82, 102 and 92: narrow heads have nearly the same instructions to 32 keys, heads of 256 one CTA of four warps an SM.
 #pragma once
 
 #include <algorithm>

@@ -9,8 +9,9 @@
 //          its own, become 16-bit values of the rows' type (exact) and go where TMA would have put them, and their scales beside
 //          them; blocks of new rows come by TMA, as does the tile of Q.
 //
-// Bound: the chain of a block, 3.3 us for two CTAs an SM (heads of 128), of which 2.2 are the handshakes of S, P and O that
-// tree_attention_tc.cu has too; conversions wait for a place in the ring, which has three at heads of 128 beside the 32 KB of Q.
+// Where the time goes: into the chain of a block, 3.3 us for two CTAs an SM (heads of 128), of which 2.2 are the handshakes of S, P and O
+// that tree_attention_tc.cu has too; it is no limit of the machine, and the 16-bit cache's kernel, which converts nothing, takes 62 us for
+// the trees below and 34 for the views; conversions wait for a place in the ring, which has three at heads of 128 beside the 32 KB of Q.
 // Without conversions and copies 79 us instead of 110 for 16 trees of up to 31 drafts over up to 8192 tokens (32 + 8 heads of 128, fp16; bf16
 // 124), without most of the softmax's work 101.  Eight requests of up to 256 rows over up to 2048 tokens, 16 heads of 72, 58 us.
 #include <cudaTypedefs.h>

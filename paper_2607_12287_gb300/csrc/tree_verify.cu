@@ -12,8 +12,9 @@
 // A cluster of up to 8 CTAs has a request, each CTA a part of the vocabulary; sums and maxima of a CTA meet in
 // shared memory, those of a cluster through distributed shared memory, all in fixed order, and every thread walks
 // through the rows alike.  A request's rows are walked one after another, so a pass over a row (or over a row and its drafter's
-// probabilities after a draft that was not right) is what a step costs: 500 requests of up to 4 rows of 50001 logits in 32 bits 47 us
-// (of 50000, with 16-byte loads, 42: HBM), 64 trees of up to 16 rows of 131072 logits with probabilities 86 us (without 33), one
+// probabilities after a draft that was not right) is what a step costs, and the requests with most passes end last: 500 requests of
+// up to 4 rows of 50001 logits in 32 bits 47 us (3380 GB/s of the 794 rows that are visited; of 50000, with 16-byte loads, 42), a CTA each
+// on 304 places; 304 of them, one wave of one to four rows one after another, 30.  64 trees of up to 16 rows of 131072 logits with probabilities 86 us (without 33), one
 // run of five rows of 32768 8.9 us.  256 threads instead of 512 took 126 us for the trees; twice the CTAs to a request 83, but 41 instead of
 // 33 without probabilities; four loads in flight at one CTA an SM 103.
 #include <algorithm>
