@@ -642,9 +642,9 @@ def _all_here(names: str, *tensors) -> None:
         _stream(None)
         if not _current:
             return
-    here = _current[1]()
+    here, kind = _current[1](), _tensor_type()
     for i, t in enumerate(tensors):
-        if type(t) is _Tensor and t.get_device() != here:
+        if isinstance(t, kind) and t.get_device() != here:
             raise ValueError(f"{names.split()[i]}: tensor on {t.device}, the current device is cuda:{here}")
 
 

@@ -213,8 +213,12 @@ class On(Fake):
         return self.device.index
 
 
-@pytest.mark.parametrize("given", [True, False])
-def test_binding_rejects_any_tensor_of_another_device(monkeypatch, given):
+class Kind(On):
+    """One of a type of its own, as parameters are."""
+
+
+@pytest.mark.parametrize("given,kind", [(True, On), (False, On), (True, Kind)])
+def test_binding_rejects_any_tensor_of_another_device(monkeypatch, given, kind):
     # each tensor of each call by itself, whether the call gives its stream or not
     reached = []
     pkg._tensor_type()
@@ -239,9 +243,9 @@ def test_binding_rejects_any_tensor_of_another_device(monkeypatch, given):
     for f, tensors in calls:
         for name in tensors:
             with pytest.raises(ValueError, match=f"^{name}: tensor on cuda:0, the current device is cuda:1"):
-                f(**{k: On(t, 0 if k == name else 1) for k, t in tensors.items()})
+                f(**{k: kind(t, 0 if k == name else 1) for k, t in tensors.items()})
         with pytest.raises(pytest.fail.Exception):  # (all of the current one)
-            f(**{k: On(t, 1) for k, t in tensors.items()})
+            f(**{k: kind(t, 1) for k, t in tensors.items()})
     assert len(reached) == len(calls)
 
 
